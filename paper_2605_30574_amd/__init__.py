@@ -4,7 +4,8 @@ The hot path of the splice intervention in "Probing the Prompt KV Cache:
 Where It Becomes Dispensable": single-query GQA decode attention over a
 prompt cache whose span slots are read, per sweep cell (L, W), from a donor
 cache.  The work runs in hand-written HIP kernels behind the C ABI declared
-in include/splice_attn.h; ``splice`` is its ctypes binding.
+in include/splice_attn.h; ``splice`` is its ctypes binding.  ``tree`` binds
+include/splice_tree.h: several candidate tokens per cell judged in one pass.
 """
 from .splice import (EXPORTS, LIB_PATH, SPLICE_BF16, SPLICE_DONOR_BUFFER, SPLICE_DONOR_ZERO,
                      SPLICE_EHIP, SPLICE_EINVAL, SPLICE_ESHAPE, SPLICE_EUNSUPPORTED,
@@ -17,5 +18,9 @@ from .splice import (EXPORTS, LIB_PATH, SPLICE_BF16, SPLICE_DONOR_BUFFER, SPLICE
                      splice_kv_build, splice_status_str, splice_visible_len, splice_workspace_handovers,
                      splice_workspace_init,
                      status_name)
+from .tree import (SPLICE_KV_BF16, SPLICE_KV_E4M3, SPLICE_MAX_NODES, SPLICE_MAX_TOP, SPLICE_ROPE_HALF,
+                   SPLICE_ROPE_INTERLEAVED, SpliceRope, SpliceTree, TokenScores, make_rope, make_tree, rope_frequencies,
+                   splice_token_scores, splice_token_scores_workspace_bytes, splice_tree_append, splice_tree_attn,
+                   splice_tree_attn_workspace_bytes, splice_tree_keep, splice_tree_read, token_scores, tree_layout)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

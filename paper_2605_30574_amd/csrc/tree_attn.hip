@@ -1,0 +1,108 @@
+// tree_attn.hip -- host side of splice_tree_attn (splice_tree.h): checks, plan,
+// launch.  The kernels are in tree_attn.hpp, one unit per head_dim.
+
+#include "tree_attn.hpp"
+
+using splice_dev::TreeArgs;
+
+extern "C" {
+
+int64_t splice_tree_attn_workspace_bytes(const splice_shape *shape, const splice_call *call, const splice_tree *tree) {
+    int32_t rc = splice::validate_tree_shape(shape, tree);
+    if (rc != SPLICE_OK) return rc;
+    if (!call) return SPLICE_EINVAL;
+    splice_call checked = *call;
+    checked.step = 0;
+    rc = splice::validate_call(*shape, &checked);
+    if (rc != SPLICE_OK) return rc;
+    // any steps: every number of active cells, over as many keys as there may be
+    const int64_t keys = (int64_t)shape->prompt_len + shape->gen_capacity;
+    size_t bytes = 0;
+    for (int n = 1; n <= shape->n_cells; ++n) {
+        const size_t b = splice::tree_plan(*shape, checked, tree->n_nodes, n, keys).bytes;
+        bytes = b > bytes ? b : bytes;
+    }
+    return (int64_t)bytes;
+}
+
+int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, const splice_tree *tree,
+                         const int32_t *cell_LW, const int32_t *cell_step, const int32_t *depth,
+                         const uint64_t *visible, const void *q, const void *clean_k, const void *clean_v,
+                         const void *donor_k, const void *donor_v, const void *gen_k, const void *gen_v,
+                         const uint8_t *gen_k_exp, const uint8_t *gen_v_exp, void *out, float *lse, void *workspace,
+                         size_t workspace_bytes, void *stream) {
+    int32_t rc = splice::validate_tree(shape, tree, cell_step);
+    if (rc != SPLICE_OK) return rc;
+    const splice_shape &sh = *shape;
+    if (!call) return SPLICE_EINVAL;
+    splice_call checked = *call;
+    checked.step = 0;   // every node takes its own step
+    rc = splice::validate_call(sh, &checked);
+    if (rc != SPLICE_OK) return rc;
+    rc = splice::validate_cells(sh, cell_LW);
+    if (rc != SPLICE_OK) return rc;
+    if (sh.n_cells == 0) return SPLICE_OK;
+    const bool zero = sh.donor_kind == SPLICE_DONOR_ZERO, has_prompt = sh.prompt_len > 0;
+    const bool f8 = tree->kv_format == SPLICE_KV_E4M3;
+    if (!depth || !visible || !q || !gen_k || !gen_v || !out || !lse) return SPLICE_EINVAL;
+    if (has_prompt && (!clean_k || !clean_v)) return SPLICE_EINVAL;
+    if (zero ? (donor_k || donor_v) : (has_prompt && (!donor_k || !donor_v))) return SPLICE_EINVAL;
+    if (f8 ? (!gen_k_exp || !gen_v_exp) : (gen_k_exp || gen_v_exp)) return SPLICE_EINVAL;
+    const void *ptrs[] = {q, clean_k, clean_v, donor_k, donor_v, gen_k, gen_v, out};
+    for (const void *p : ptrs)
+        if (!splice::aligned(p, 16)) return SPLICE_EINVAL;
+    if (!splice::aligned(depth, 4) || !splice::aligned(visible, 8) || !splice::aligned(lse, 4)) return SPLICE_EINVAL;
+
+    const int T = tree->n_nodes;
+    TreeArgs a;
+    const int n = splice::active_cells(sh, cell_step, a.cells);
+    if (n == 0) return SPLICE_OK;
+    int64_t keys = 0;
+    for (int i = 0; i < n; ++i) {
+        const int64_t k = splice::tree_keys(sh, checked, T, a.cells.step[i]);
+        keys = k > keys ? k : keys;
+        const int c = a.cells.cell[i];
+        const int64_t ahead = (int64_t)cell_LW[2 * c + 1] - a.cells.step[i];   // depth of the onset
+        const bool never = call->layer < cell_LW[2 * c] || ahead > SPLICE_MAX_NODES;
+        a.onset[i] = (uint8_t)(never ? SPLICE_MAX_NODES : (ahead > 0 ? ahead : 0));
+    }
+    const splice::TreePlan p = splice::tree_plan(sh, checked, T, n, keys);
+    if ((int64_t)sh.n_kv_heads * n * p.row_tiles * p.n_split > INT32_MAX ||
+        (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30)
+        return SPLICE_EUNSUPPORTED;
+    if (p.bytes > 0 && (!workspace || !splice::aligned(workspace, 256) || workspace_bytes < p.bytes)) return SPLICE_EWORKSPACE;
+    a.q = (const char *)q;
+    a.ck = (const char *)clean_k;
+    a.cv = (const char *)clean_v;
+    a.dk = (const char *)donor_k;
+    a.dv = (const char *)donor_v;
+    a.gk = (const char *)gen_k;
+    a.gv = (const char *)gen_v;
+    a.gke = gen_k_exp;
+    a.gve = gen_v_exp;
+    a.depth = depth;
+    a.visible = visible;
+    a.out = (__bf16 *)out;
+    a.lse = lse;
+    a.part = (float *)workspace;
+    a.T = T;
+    a.G = splice::group_of(sh);
+    a.Hkv = sh.n_kv_heads;
+    a.Tp = sh.prompt_len;
+    a.cap = sh.gen_capacity;
+    a.span_lo = sh.span_lo;
+    a.span_hi = sh.span_hi;
+    a.window = call->window;
+    a.zero_donor = zero ? 1 : 0;
+    a.n_active = n;
+    a.row_tiles = p.row_tiles;
+    a.n_split = p.n_split;
+    a.qk_scale = call->scale * splice_dev::kLog2e;
+    hipStream_t st = (hipStream_t)stream;
+    const bool ok = sh.head_dim == 64    ? splice_dev::launch_tree_d64(a, p, tree->kv_format, st)
+                    : sh.head_dim == 128 ? splice_dev::launch_tree_d128(a, p, tree->kv_format, st)
+                                         : splice_dev::launch_tree_d256(a, p, tree->kv_format, st);
+    return ok ? SPLICE_OK : SPLICE_EHIP;
+}
+
+}  // extern "C"

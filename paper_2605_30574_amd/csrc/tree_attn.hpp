@@ -1,0 +1,517 @@
+// tree_attn.hpp -- attention of a tree of drafted nodes per cell over the
+// cell's spliced prompt, its generated rows and the tree's own rows
+// (splice_tree_attn).
+//
+// The queries of a (cell, KV head) are its T * G (node, head) rows.  A work
+// group takes 32 RW of them (RW waves of 32 rows; the other 4 / RW waves of a
+// row take other keys) and walks a list of keys in tiles that it stages in LDS
+// for all its waves, two tiles deep: the next tile's loads are in flight in
+// registers while one is computed.  Per wave and 32 keys
+//   S^T = K Q^T   v_mfma_f32_32x32x16_bf16, A = K from LDS, B = Q^T held in
+//                 registers: lane (half h, r) gets row r's scores of the keys
+//                 8 b + 4 h + i, so a row's statistics take one exchange
+//                 between the halves;
+//   softmax       running maximum with lazy rescaling, sums in fp32;
+//   O^T += V^T P  A = V^T by transposing LDS reads, in the order of keys in
+//                 which P lies in the lanes; P rounded to bf16 (weights of at
+//                 most 2^kSlack with relative errors of 2^-9 that average
+//                 out; their sum is not rounded).
+// Keys are listed in segments (prompt before, in and behind the span, each
+// span form that the tile's rows need, the generated rows with the tree's
+// behind them); only tiles that some row does not see wholly are masked.
+#pragma once
+
+#include <atomic>
+
+#include "kv_format.hpp"
+#include "tree_plan.hpp"
+#include "wave_mfma.hpp"
+
+namespace splice_dev {
+
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) i16x4_t lds_tr_t;
+
+struct TreeArgs {
+    const char *q, *ck, *cv, *dk, *dv, *gk, *gv;
+    const uint8_t *gke, *gve;
+    const int32_t *depth;
+    const uint64_t *visible;
+    __bf16 *out;
+    float *lse;
+    float *part;   // [split][active cell][node][q head][D], then [..][2] (m, l)
+    int T, G, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, n_split;
+    float qk_scale;   // scale * log2(e)
+    splice::TreeCells cells;
+    uint8_t onset[SPLICE_MAX_CELLS];   // depth from which an active cell's nodes are spliced (64: none)
+};
+
+template <int D, int RW>
+struct TreeTile {
+    static constexpr int KW = 4 / RW;                          // waves over keys
+    static constexpr int KB = splice::tree_key_blocks(D, RW);  // 32-key blocks of a wave
+    static constexpr int TK = splice::tree_tile_keys(D, RW);   // keys of a tile
+    static constexpr int ROW = 2 * D;                          // bytes of a staged row
+    static constexpr int CPR = D / 8;                          // 16-byte chunks of a row
+    static constexpr int TILE = TK * ROW;                      // bytes of a K (or V) tile
+    static constexpr int LDS = 4 * TILE;                       // two buffers of K and V
+    static constexpr int NL = TK * CPR / 256;                  // chunks a thread loads of a K (or V) tile
+    static constexpr int NL8 = NL / 2;                         // ... of 8-bit rows
+    static constexpr int ND = D / 32;                          // 32-wide d blocks of the output
+    static_assert(RW * KW == 4 && NL8 >= 1 && (KW == 1 || KW * 32 * RW * D * 4 <= LDS), "");
+};
+
+// Chunk-slot swizzles (XOR on the 16-byte chunk index) of key r: the 16 rows
+// that a quarter-wave reads of K, and the four rows that a 16-lane group reads
+// 32 bytes each of V, fall into different banks.
+template <int D>
+__device__ __forceinline__ int tree_swz_k(int r) { return D == 64 ? (r >> 1) & 7 : r & 15; }
+template <int D>
+__device__ __forceinline__ int tree_swz_v(int r) { return D == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; }
+
+// Bits [b, e) of a word, for any b and e.
+__device__ __forceinline__ uint64_t bits(int b, int e) {
+    b = max(b, 0);
+    e = min(e, 64);
+    if (e <= b) return 0;
+    return (e - b == 64 ? ~0ull : (1ull << (e - b)) - 1) << b;
+}
+__device__ __forceinline__ uint64_t shifted(uint64_t x, int by) {   // left, or right when by < 0
+    if (by >= 64 || by <= -64) return 0;
+    return by >= 0 ? x << by : x >> -by;
+}
+
+// Which words of two bf16 values hold an infinity or NaN.
+__device__ __forceinline__ bool has_non_finite(u32x4_t w) {
+    bool bad = false;
+    static_for<0, 4>([&](auto i) {
+        bad |= (w[(int)i] & 0x7f80u) == 0x7f80u || (w[(int)i] & 0x7f800000u) == 0x7f800000u;
+    });
+    return bad;
+}
+
+// The words with every infinity and NaN replaced by 0, and 1.0 where a value
+// is +inf or NaN (above) or -inf or NaN (under).
+__device__ __forceinline__ void split_non_finite(u32x4_t &w, u32x4_t &above, u32x4_t &under) {
+    static_for<0, 4>([&](auto i) {
+        uint32_t fin = 0, up = 0, down = 0;
+        static_for<0, 2>([&](auto h) {
+            const uint32_t x = (w[(int)i] >> (16 * h)) & 0xffffu;
+            const bool bad = (x & 0x7f80u) == 0x7f80u, nan = bad && (x & 0x7fu);
+            fin |= (bad ? 0u : x) << (16 * h);
+            up |= (bad && (nan || !(x >> 15)) ? 0x3f80u : 0u) << (16 * h);
+            down |= (bad && (nan || (x >> 15)) ? 0x3f80u : 0u) << (16 * h);
+        });
+        w[(int)i] = fin;
+        above[(int)i] = up;
+        under[(int)i] = down;
+    });
+}
+
+template <int D, int RW, bool F8>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs a) {
+    using X = TreeTile<D, RW>;
+    constexpr int KW = X::KW, KB = X::KB, TK = X::TK, ND = X::ND, NST = D / 16;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int s_bad[2];
+    __shared__ float s_ml[KW > 1 ? KW : 1][32 * RW][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 31, h = lane >> 5, rw = wave % RW, kw = wave / RW;
+
+    // ---- which rows: KV heads run fastest, so that with eight (or a multiple) an XCD keeps to its own
+    const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, n_items = a.n_active * a.row_tiles;
+    const int split = rest / n_items, item = rest % n_items, ci = item / a.row_tiles, rt = item % a.row_tiles;
+    const int c = a.cells.cell[ci], step = a.cells.step[ci], onset = a.onset[ci], rows = a.T * a.G;
+    const int row0 = 32 * RW * rt, row = row0 + 32 * rw + r;
+    const int64_t node0 = (int64_t)c * a.T;
+    int d_node = lane < a.T ? a.depth[node0 + lane] : -1;   // lane u: node u's depth
+    d_node = min(d_node, a.T - 1);
+    const uint64_t alive = __ballot(d_node >= 0);
+    const uint64_t mine = bits(row0 / a.G, min(row0 + 32 * RW - 1, rows - 1) / a.G + 1) & alive;   // the work group's nodes
+    if (mine == 0) return;
+    const int node = min(row / a.G, a.T - 1), depth = __shfl(d_node, node), p0 = a.Tp + step;
+    const bool valid = row < rows && depth >= 0;
+    const bool spliced = depth >= onset;
+    const int low = a.window > 0 ? p0 + max(depth, 0) - a.window + 1 : 0;   // first position the row sees
+    uint64_t word = valid ? a.visible[node0 + node] & alive : 0;
+    if (a.window > 0 && a.window < a.T) {
+        for (int u = 0; u < a.T; ++u)
+            if (depth - __shfl(d_node, u) >= a.window) word &= ~(1ull << u);
+    }
+    // of the work group's nodes: the least and the largest depth, and whether spliced and unspliced ones are there
+    const bool in = (mine >> lane) & 1;
+    int d_min = in ? d_node : SPLICE_MAX_NODES, d_max = in ? d_node : 0;
+    for (int o = 32; o > 0; o >>= 1) {
+        d_min = min(d_min, __shfl_xor(d_min, o));
+        d_max = max(d_max, __shfl_xor(d_max, o));
+    }
+    d_min = __builtin_amdgcn_readfirstlane(d_min);
+    d_max = __builtin_amdgcn_readfirstlane(d_max);
+    const bool any_clean = d_min < onset, any_donor = d_max >= onset;
+    const int low_all = a.window > 0 ? max(p0 + d_min - a.window + 1, 0) : 0;   // some row sees from here on,
+    const int low_max = a.window > 0 ? p0 + d_max - a.window + 1 : 0;           // every row from here on
+
+    // ---- the list of keys
+    KeyListN<5> L;
+    list_init(L);
+    const size_t head_p = (size_t)g * a.Tp * X::ROW;
+    const int grow = F8 ? D : X::ROW;   // bytes of a generated row
+    const int64_t pair = (int64_t)c * a.Hkv + g;
+    const int b0 = min(low_all, a.Tp), sa = min(max(a.span_lo, b0), a.Tp), sb = max(a.span_hi, sa);
+    const int g0 = min(max(low_all - a.Tp, 0), step);
+    {
+        const char *ck = a.ck + head_p, *cv = a.cv + head_p;
+        auto prompt = [&](const char *k, const char *v, int b, int e, int cols) {
+            list_add<TK>(L, k + (size_t)b * X::ROW, v + (size_t)b * X::ROW, e - b, cols, b);
+        };
+        if (!any_donor) {
+            prompt(ck, cv, b0, a.Tp, kColsAll);
+        } else {
+            prompt(ck, cv, b0, sa, kColsAll);
+            if (any_clean) prompt(ck, cv, sa, sb, kColsClean);
+            if (!a.zero_donor) prompt(a.dk + head_p, a.dv + head_p, sa, sb, any_clean ? kColsDonor : kColsAll);
+            prompt(ck, cv, sb, a.Tp, kColsAll);
+        }
+    }
+    const int gen_tile = list_tiles(L);   // tiles from here on are generated rows; key0 is then the row
+    list_add<TK>(L, a.gk + (pair * a.cap + g0) * grow, a.gv + (pair * a.cap + g0) * grow, step + a.T - g0, kColsAll, g0);
+    const int n_tiles = list_tiles(L);
+    const int t0 = (int)((int64_t)n_tiles * split / a.n_split), t1 = (int)((int64_t)n_tiles * (split + 1) / a.n_split);
+
+    // ---- staging: chunk u = i * 256 + tid of a tile is 16 bytes of key u / CPR
+    u32x4_t kr[X::NL], vr[X::NL];
+    uint32_t ke[X::NL], ve[X::NL];
+    auto is_gen = [&](int t) { return t >= gen_tile; };
+    auto load = [&](int t) {
+        const TileRef ref = list_tile<TK>(L, t, is_gen(t) ? grow : X::ROW);
+        if (F8 && is_gen(t)) {
+            const __amdgpu_buffer_rsrc_t rk = rows_rsrc(ref.k, ref.n * D), rv = rows_rsrc(ref.v, ref.n * D);
+            const __amdgpu_buffer_rsrc_t re = rows_rsrc(reinterpret_cast<const char *>(a.gke + pair * a.cap + ref.key0), ref.n);
+            const __amdgpu_buffer_rsrc_t rf = rows_rsrc(reinterpret_cast<const char *>(a.gve + pair * a.cap + ref.key0), ref.n);
+            static_for<0, X::NL8>([&](auto i) {
+                const int u = (int)i * 256 + tid;
+                kr[i] = row_load<0>(rk, u * 16);
+                vr[i] = row_load<0>(rv, u * 16);
+                ke[i] = __builtin_amdgcn_raw_buffer_load_b8(re, u / (D / 16), 0, 0);
+                ve[i] = __builtin_amdgcn_raw_buffer_load_b8(rf, u / (D / 16), 0, 0);
+            });
+        } else {
+            const __amdgpu_buffer_rsrc_t rk = rows_rsrc(ref.k, ref.n * X::ROW), rv = rows_rsrc(ref.v, ref.n * X::ROW);
+            static_for<0, X::NL>([&](auto i) {
+                const int u = (int)i * 256 + tid;
+                kr[i] = row_load<0>(rk, u * 16);
+                vr[i] = row_load<0>(rv, u * 16);
+            });
+        }
+    };
+    auto put = [&](char *buf, int key, int chunk, u32x4_t k, u32x4_t v) {
+        *reinterpret_cast<u32x4_t *>(buf + key * X::ROW + ((chunk ^ tree_swz_k<D>(key)) << 4)) = k;
+        *reinterpret_cast<u32x4_t *>(buf + X::TILE + key * X::ROW + ((chunk ^ tree_swz_v<D>(key)) << 4)) = v;
+    };
+    // whether some row of the work group does not see all of tile t
+    auto masked = [&](int t) {
+        const TileRef ref = list_tile<TK>(L, t, 0);
+        if (ref.n < TK || ref.cols != kColsAll) return true;
+        return is_gen(t) ? a.Tp + ref.key0 < low_max || ref.key0 + TK > step : ref.key0 < low_max;
+    };
+    // In a masked tile the values are looked at: rows of nodes that are not
+    // there count as 0, and s_bad tells of infinities and NaN (they must
+    // not reach the rows that do not see them: 0 * inf).
+    auto stage = [&](int t, int b) {
+        char *buf = lds + b * 2 * X::TILE;
+        const bool look = masked(t), f8 = F8 && is_gen(t);
+        const int key0 = list_tile<TK>(L, t, 0).key0;
+        bool bad = false;
+        auto value = [&](int key, u32x4_t v) {
+            if (look) {
+                const int u = key0 + key - step;
+                if (is_gen(t) && u >= 0 && (u >= 64 || !((alive >> u) & 1))) v = u32x4_t{0, 0, 0, 0};
+                bad |= has_non_finite(v);
+            }
+            return v;
+        };
+        if (f8) {
+            static_for<0, X::NL8>([&](auto i) {
+                const int u = (int)i * 256 + tid, key = u / (D / 16), ch = 2 * (u % (D / 16));
+                const u32x4_t k = kr[i], v = vr[i];
+                put(buf, key, ch, e4m3_to_bf16(make_uint2(k.x, k.y), ke[i]), value(key, e4m3_to_bf16(make_uint2(v.x, v.y), ve[i])));
+                put(buf, key, ch + 1, e4m3_to_bf16(make_uint2(k.z, k.w), ke[i]),
+                    value(key, e4m3_to_bf16(make_uint2(v.z, v.w), ve[i])));
+            });
+        } else {
+            static_for<0, X::NL>([&](auto i) {
+                const int u = (int)i * 256 + tid, key = u / X::CPR;
+                put(buf, key, u % X::CPR, kr[i], value(key, vr[i]));
+            });
+        }
+        if (bad) s_bad[b] = t + 1;
+    };
+
+    if (tid < 2) s_bad[tid] = 0;
+    if (t0 < t1) load(t0);
+
+    // ---- Q^T, in the lanes of the B operand: row r, d = 16 st + 8 h ..
+    bf16x8_t qb[NST];
+    {
+        const int64_t q_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
+        static_for<0, NST>([&](auto st) {
+            u32x4_t w = {0, 0, 0, 0};
+            if (valid) w = *reinterpret_cast<const u32x4_t *>(a.q + (q_row * D + 16 * (int)st + 8 * h) * 2);
+            qb[st] = __builtin_bit_cast(bf16x8_t, w);
+        });
+    }
+    // state of a row: o[db][i] is d = 32 db + 8 (i / 4) + 4 h + i % 4; a half's share of the sum
+    f32x16_t o[ND];
+    static_for<0, ND>([&](auto db) { static_for<0, 16>([&](auto i) { o[db][(int)i] = 0.f; }); });
+    float m = -INFINITY, l = 0.f;
+    // keys of the ZERO donor score 0 and add nothing to o
+    if (a.zero_donor && spliced && split == 0 && kw == 0) {
+        const int n_zero = a.span_hi - max(a.span_lo, max(low, 0));
+        if (n_zero > 0) {
+            m = 0.f;
+            l = h == 0 ? (float)n_zero : 0.f;
+        }
+    }
+
+    // ---- addresses of the operands within a buffer
+    int k_at[NST], v_at[ND];
+    static_for<0, NST>([&](auto st) { k_at[st] = (kw * 32 * KB + r) * X::ROW + (((2 * (int)st + h) ^ tree_swz_k<D>(r)) << 4); });
+    {
+        const int vrow = kw * 32 * KB + 4 * h + ((lane & 15) >> 2);
+        static_for<0, ND>([&](auto db) {
+            const int chunk = 4 * (int)db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            v_at[db] = X::TILE + vrow * X::ROW + ((chunk ^ tree_swz_v<D>(vrow)) << 4) + 8 * (lane & 1);
+        });
+    }
+
+    __syncthreads();   // s_bad
+    if (t0 < t1) stage(t0, 0);
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        const int b = (t - t0) & 1;
+        const char *buf = lds + b * 2 * X::TILE;
+        if (t + 1 < t1) load(t + 1);
+        const bool look = masked(t);
+        f32x16_t s[KB];
+        static_for<0, KB>([&](auto kb) {
+            static_for<0, 16>([&](auto i) { s[kb][(int)i] = 0.f; });
+            static_for<0, NST>([&](auto st) {
+                const bf16x8_t ka = *reinterpret_cast<const bf16x8_t *>(buf + k_at[st] + (int)kb * 32 * X::ROW);
+                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[st], s[kb], 0, 0, 0);
+            });
+        });
+        if (look) {
+            const TileRef ref = list_tile<TK>(L, t, 0);
+            const int first = ref.key0 + kw * 32 * KB, n = ref.n - kw * 32 * KB;
+            uint64_t see;
+            if (is_gen(t)) {
+                see = bits(low - a.Tp - first, min(step - first, n)) | (shifted(word, step - first) & bits(step - first, n));
+            } else {
+                see = (ref.cols == kColsAll || (ref.cols == kColsDonor) == spliced) ? bits(low - first, n) : 0;
+            }
+            see >>= 4 * h;
+            static_for<0, KB>([&](auto kb) {
+                static_for<0, 16>([&](auto i) {
+                    constexpr int key = 32 * kb + 8 * (i >> 2) + (i & 3);
+                    if (!((see >> key) & 1)) s[kb][(int)i] = -INFINITY;
+                });
+            });
+        }
+        float mt = -INFINITY;
+        static_for<0, KB>([&](auto kb) { static_for<0, 16>([&](auto i) { mt = fmaxf(mt, s[kb][(int)i]); }); });
+        mt *= a.qk_scale;
+        if (__any(mt > m + kSlack)) {
+            mt = fmaxf(mt, __shfl_xor(mt, 32));
+            const bool need = mt > m + kSlack;
+            const float mn = need ? mt : m;
+            const float al = need ? fast_exp2(m - mn) : 1.f;
+            l *= al;
+            static_for<0, ND>([&](auto db) { o[db] *= al; });
+            m = mn;
+        }
+        const float ms = m == -INFINITY ? 0.f : m;
+        bf16x8_t pb[2 * KB];
+        static_for<0, KB>([&](auto kb) {
+            static_for<0, 16>([&](auto i) {
+                const float p = fast_exp2(fmaf(s[kb][(int)i], a.qk_scale, -ms));
+                l += p;
+                pb[2 * kb + i / 8][i % 8] = (__bf16)p;
+            });
+        });
+        const bool bad = look && __builtin_amdgcn_readfirstlane(s_bad[b]) == t + 1;
+        static_for<0, ND>([&](auto db) {
+            f32x16_t up, down;
+            if (bad) static_for<0, 16>([&](auto i) { up[(int)i] = down[(int)i] = 0.f; });
+            static_for<0, 2 * KB>([&](auto kk) {
+                const char *at = buf + v_at[db] + 16 * (int)kk * X::ROW;
+                const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_t *)at);
+                const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_t *)(at + 8 * X::ROW));
+                const u32x2_t wl = __builtin_bit_cast(u32x2_t, lo), wh = __builtin_bit_cast(u32x2_t, hi);
+                u32x4_t va = {wl.x, wl.y, wh.x, wh.y};
+                if (bad) {
+                    u32x4_t above, under;
+                    split_non_finite(va, above, under);
+                    up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, above), pb[kk], up, 0, 0, 0);
+                    down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, under), pb[kk], down, 0, 0, 0);
+                }
+                o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, va), pb[kk], o[db], 0, 0, 0);
+            });
+            if (bad) {
+                static_for<0, 16>([&](auto i) {
+                    if (up[(int)i] > 0.f) o[db][(int)i] += INFINITY;
+                    if (down[(int)i] > 0.f) o[db][(int)i] -= INFINITY;
+                });
+            }
+        });
+        if (t + 1 < t1) stage(t + 1, b ^ 1);
+        __syncthreads();
+    }
+
+    // ---- results
+    l += __shfl_xor(l, 32);
+    const int64_t out_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
+    const int64_t n_part = (int64_t)a.n_active * a.T * a.Hkv * a.G;   // rows of a split
+    const int64_t part_row = (int64_t)split * n_part + ((int64_t)ci * a.T + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
+    float *part_ml = a.part + (int64_t)a.n_split * n_part * D;
+    if constexpr (KW > 1) {
+        // the waves of a row through LDS (every wave is done with the tiles)
+        float *s_o = reinterpret_cast<float *>(lds);   // [KW][32 RW][D], chunks of four swizzled by the row
+        const int wrow = 32 * rw + r;
+        static_for<0, ND>([&](auto db) {
+            static_for<0, 4>([&](auto i) {
+                const int d4 = 8 * (int)db + 2 * (int)i + h;
+                *reinterpret_cast<f32x4_t *>(s_o + ((kw * 32 * RW + wrow) * D + 4 * (d4 ^ (wrow & 15)))) =
+                    f32x4_t{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+            });
+        });
+        if (h == 0) {
+            s_ml[kw][wrow][0] = m;
+            s_ml[kw][wrow][1] = l;
+        }
+        __syncthreads();
+        for (int e = tid; e < 32 * RW * (D / 4); e += 256) {
+            const int w = e / (D / 4), d4 = e % (D / 4), rr = row0 + w;
+            if (rr >= rows) break;
+            const int nd = rr / a.G, hd = g * a.G + rr % a.G;
+            if (!((alive >> nd) & 1)) continue;
+            float M = -INFINITY, Lsum = 0.f;
+            static_for<0, KW>([&](auto k) { M = fmaxf(M, s_ml[k][w][0]); });
+            const float Ms = M == -INFINITY ? 0.f : M;
+            f32x4_t O = {0.f, 0.f, 0.f, 0.f};
+            static_for<0, KW>([&](auto k) {
+                const float f = fast_exp2(s_ml[k][w][0] - Ms);
+                Lsum = fmaf(f, s_ml[k][w][1], Lsum);
+                if (f != 0.f)
+                    O += f * *reinterpret_cast<const f32x4_t *>(s_o + (((int)k * 32 * RW + w) * D + 4 * (d4 ^ (w & 15))));
+            });
+            if (a.n_split > 1) {
+                const int64_t at = (int64_t)split * n_part + ((int64_t)ci * a.T + nd) * (a.Hkv * a.G) + hd;
+                *reinterpret_cast<f32x4_t *>(a.part + at * D + 4 * d4) = O;
+                if (d4 == 0) *reinterpret_cast<float2 *>(part_ml + 2 * at) = make_float2(M, Lsum);
+            } else {
+                const int64_t at = (node0 + nd) * (a.Hkv * a.G) + hd;
+                const float f = Lsum == 0.f ? 0.f : 1.f / Lsum;
+                *reinterpret_cast<bf16x4_t *>(a.out + at * D + 4 * d4) = __builtin_convertvector(O * f, bf16x4_t);
+                if (d4 == 0) a.lse[at] = kLn2 * (M + log2f(Lsum));
+            }
+        }
+    } else {
+        if (!valid) return;
+        if (a.n_split > 1) {
+            static_for<0, ND>([&](auto db) {
+                static_for<0, 4>([&](auto i) {
+                    *reinterpret_cast<f32x4_t *>(a.part + part_row * D + 32 * (int)db + 8 * (int)i + 4 * h) =
+                        f32x4_t{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+                });
+            });
+            if (h == 0) *reinterpret_cast<float2 *>(part_ml + 2 * part_row) = make_float2(m, l);
+        } else {
+            const float f = l == 0.f ? 0.f : 1.f / l;
+            static_for<0, ND>([&](auto db) {
+                static_for<0, 4>([&](auto i) {
+                    const f32x4_t v = f32x4_t{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]} * f;
+                    *reinterpret_cast<bf16x4_t *>(a.out + out_row * D + 32 * (int)db + 8 * (int)i + 4 * h) =
+                        __builtin_convertvector(v, bf16x4_t);
+                });
+            });
+            if (h == 0) a.lse[out_row] = kLn2 * (m + log2f(l));
+        }
+    }
+}
+
+// Joins the splits of every row: a thread has four values of a row.
+template <int D>
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
+    const int Hq = a.Hkv * a.G;
+    const int64_t n_part = (int64_t)a.n_active * a.T * Hq;
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, row = e / (D / 4);
+    const int d4 = (int)(e % (D / 4));
+    if (row >= n_part) return;
+    const int hd = (int)(row % Hq), node = (int)(row / Hq % a.T), ci = (int)(row / Hq / a.T);
+    const int64_t at_node = (int64_t)a.cells.cell[ci] * a.T + node;
+    if (a.depth[at_node] < 0) return;
+    const float *ml = a.part + (int64_t)a.n_split * n_part * D;
+    float M = -INFINITY, L = 0.f;
+    for (int s = 0; s < a.n_split; ++s) M = fmaxf(M, ml[2 * (s * n_part + row)]);
+    const float Ms = M == -INFINITY ? 0.f : M;
+    f32x4_t O = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.n_split; ++s) {
+        const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * (s * n_part + row));
+        const float f = fast_exp2(x.x - Ms);
+        L = fmaf(f, x.y, L);
+        if (f != 0.f) O += f * *reinterpret_cast<const f32x4_t *>(a.part + (s * n_part + row) * D + 4 * d4);
+    }
+    const int64_t at = at_node * Hq + hd;
+    const float f = L == 0.f ? 0.f : 1.f / L;
+    *reinterpret_cast<bf16x4_t *>(a.out + at * D + 4 * d4) = __builtin_convertvector(O * f, bf16x4_t);
+    if (d4 == 0) a.lse[at] = kLn2 * (M + log2f(L));
+}
+
+// Enqueues a call of plan p; 0 if a launch failed.
+typedef bool (*TreeLaunch)(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hipStream_t stream);
+
+template <int D, int RW, bool F8>
+bool launch_tree_kernel(const TreeArgs &a, hipStream_t stream) {
+    using X = TreeTile<D, RW>;
+    // more LDS than a kernel may take unasked; asked once a device
+    static std::atomic<uint64_t> raised{0};
+    int dev = 0;
+    if (X::LDS > 64 << 10) {
+        if (hipGetDevice(&dev) != hipSuccess) return false;
+        const uint64_t bit = 1ull << (dev & 63);
+        if (!(raised.load() & bit)) {
+            if (hipFuncSetAttribute(reinterpret_cast<const void *>(&tree_kernel<D, RW, F8>),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, X::LDS) != hipSuccess)
+                return false;
+            raised.fetch_or(bit);
+        }
+    }
+    const unsigned blocks = (unsigned)((int64_t)a.Hkv * a.n_active * a.row_tiles * a.n_split);
+    hipLaunchKernelGGL((tree_kernel<D, RW, F8>), dim3(blocks), dim3(256), X::LDS, stream, a);
+    return hipGetLastError() == hipSuccess;
+}
+
+template <int D>
+bool launch_tree(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hipStream_t stream) {
+    const bool f8 = kv_format == SPLICE_KV_E4M3;
+    bool ok;
+    if constexpr (D <= 128) {
+        if (p.row_waves == 1) ok = f8 ? launch_tree_kernel<D, 1, true>(a, stream) : launch_tree_kernel<D, 1, false>(a, stream);
+        else if (p.row_waves == 2) ok = f8 ? launch_tree_kernel<D, 2, true>(a, stream) : launch_tree_kernel<D, 2, false>(a, stream);
+        else ok = f8 ? launch_tree_kernel<D, 4, true>(a, stream) : launch_tree_kernel<D, 4, false>(a, stream);
+    } else {
+        if (p.row_waves == 2) ok = f8 ? launch_tree_kernel<D, 2, true>(a, stream) : launch_tree_kernel<D, 2, false>(a, stream);
+        else ok = f8 ? launch_tree_kernel<D, 4, true>(a, stream) : launch_tree_kernel<D, 4, false>(a, stream);
+    }
+    if (!ok || a.n_split == 1) return ok;
+    const int64_t units = (int64_t)a.n_active * a.T * a.Hkv * a.G * (D / 4);
+    hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, stream, a);
+    return hipGetLastError() == hipSuccess;
+}
+
+bool launch_tree_d64(const TreeArgs &, const splice::TreePlan &, int, hipStream_t);
+bool launch_tree_d128(const TreeArgs &, const splice::TreePlan &, int, hipStream_t);
+bool launch_tree_d256(const TreeArgs &, const splice::TreePlan &, int, hipStream_t);
+
+}  // namespace splice_dev

@@ -1,0 +1,129 @@
+"""splice_token_scores against the definition in float64."""
+import numpy as np
+import pytest
+import torch
+
+from tree_common import announce, f64, ref, sp
+
+pytestmark = pytest.mark.gpu
+
+
+def check(logits, tokens, k, scale=1.0, got=None):
+    got = got or sp.token_scores(logits, tokens, k, scale)
+    torch.cuda.synchronize()
+    raw = f64(logits)
+    vocab = raw.shape[1]
+    logp, lse, entropy, rank, top, top_logp = ref.scores(raw * scale, tokens.cpu().numpy(), k)
+    fine = np.isfinite(raw * scale)
+    size = np.abs(np.where(fine, raw * scale, 0)).max(-1)
+    # x log2(e) scale in one rounding each (3 * 2^-24 of |x|), v_exp_f32 and v_log_f32 (2^-22), sums of vocab weights in
+    # a tree under chains of vocab / 256 terms
+    tol = 2.0 ** -24 * (8 * size + vocab / 256 + 64)
+    def same(a, b, t):
+        a = f64(a)
+        ok = (np.isnan(a) & np.isnan(b)) | (a == b) | (np.abs(a - b) <= t)
+        assert ok.all(), (a[~ok][:4], b[~ok][:4])
+    same(got.lse, lse, tol)
+    same(got.logp, logp, 2 * tol)
+    # entropy: sum p (lse - x), the weights' errors times the distances
+    same(got.entropy, entropy, 2 * tol * (1 + np.log(vocab) + np.abs(np.nan_to_num(entropy))))
+    assert np.array_equal(got.rank.cpu().numpy(), rank)
+    if k:
+        assert np.array_equal(got.top.cpu().numpy(), top)
+        same(got.top_logp, top_logp, 2 * tol[:, None])
+    else:
+        assert got.top is None and got.top_logp is None
+
+
+def draw(seed, rows, vocab, dtype, spread=2.0, pad=0):
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(rows, vocab + pad, generator=g) * spread).to(dtype).cuda()
+    return x[:, pad // 2:pad // 2 + vocab], torch.randint(0, vocab, (rows,), generator=g).cuda()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (3, 2, 2), (5, 7, 0), (4, 63, 63), (2, 64, 64), (3, 65, 5), (1, 1000, 64),
+                                          (2, 8192, 20), (7, 8193, 1), (3, 33333, 64), (40, 4097, 3)])
+def test_sizes(rows, vocab, k, dtype):
+    announce(f"scores {rows} {vocab} {k} {dtype}")
+    check(*draw(vocab, rows, vocab, dtype), k)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad", [1, 2, 3, 5, 8, 15])
+def test_rows_at_any_offset(pad, dtype):
+    check(*draw(pad, 6, 1001, dtype, pad=pad), 4, 0.7)
+
+
+def test_ties_go_to_the_lower_index():
+    x = torch.zeros(4, 5000, device="cuda")
+    x[1] = -3.0
+    x[1, 17::100] = 2.5
+    x[2] = torch.randint(0, 3, (5000,), generator=torch.Generator().manual_seed(3)).float()
+    x[3, ::2] = -0.0
+    check(x, torch.tensor([4999, 117, 2500, 1], device="cuda"), 64)
+    check(x.to(torch.bfloat16), torch.tensor([0, 18, 4999, 0], device="cuda"), 64)
+
+
+def test_masked_infinite_and_nan():
+    x, t = draw(5, 12, 3000, torch.float32)
+    x = x.contiguous()
+    x[0] = -np.inf
+    x[1, 5:] = -np.inf
+    x[2, 1:] = -np.inf
+    x[3, 100] = np.inf
+    x[4, 7] = np.nan
+    x[5, 2999] = np.nan
+    x[5, 3] = np.nan
+    x[6] = torch.finfo(torch.float32).min
+    x[7, :2000] = torch.finfo(torch.float32).min
+    x[8] = np.nan
+    x[9, ::3] = -np.inf
+    t[1], t[2], t[4], t[5], t[9] = 200, 0, 7, 2999, 0
+    t[10], t[11] = -1, 3000   # no tokens
+    check(x, t, 8)
+    check(x.to(torch.bfloat16), t, 8)
+
+
+def test_peaked_and_flat_entropy():
+    x = torch.zeros(3, 4000, device="cuda")
+    x[0, 9] = 60.0
+    x[1, 9] = 15.0
+    check(x, torch.tensor([9, 8, 7], device="cuda"), 2)
+
+
+def test_scale_and_large_logits():
+    x, t = draw(6, 4, 999, torch.float32, spread=300.0)
+    for scale in (0.01, 1.0, 7.5):
+        check(x, t, 10, scale)
+
+
+def test_token_chunk_borders():
+    """The given token at either end of a 16-byte chunk and of a part, among equals."""
+    x = torch.zeros(40, 20000, device="cuda")
+    t = torch.tensor([0, 1, 3, 4, 5, 1023, 1024, 4095, 4096, 4097, 8191, 8192, 9999, 10000, 19996, 19999, 12, 15, 16, 17] * 2, device="cuda")
+    x[20:, ::2] = 1.0
+    check(x, t, 1)
+    check(x.to(torch.bfloat16), t, 1)
+
+
+def test_replayed_graph_and_same_bits():
+    x, t = draw(8, 3, 50000, torch.bfloat16)
+    x, ws = x.contiguous(), torch.empty(sp.splice_token_scores_workspace_bytes(3, 50000, 5), dtype=torch.uint8, device="cuda")
+    o = [torch.empty(3, device="cuda") for _ in range(3)] + [torch.empty(3, dtype=torch.int64, device="cuda"),
+                                                           torch.empty(3, 5, dtype=torch.int64, device="cuda"), torch.empty(3, 5, device="cuda")]
+    run = lambda: sp.splice_token_scores(x, t, *o, ws)  # noqa: E731
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for n in range(3):
+        x.copy_(draw(20 + n, 3, 50000, torch.bfloat16)[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = sp.token_scores(x, t, 5)
+        torch.cuda.synchronize()
+        for a, b in zip(o, eager):
+            assert torch.equal(a, b)
+        check(x, t, 5, got=sp.TokenScores(*o))
