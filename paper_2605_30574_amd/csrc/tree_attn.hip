@@ -54,23 +54,24 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     if (!splice::aligned(depth, 4) || !splice::aligned(visible, 8) || !splice::aligned(lse, 4)) return SPLICE_EINVAL;
 
     const int T = tree->n_nodes;
-    TreeArgs a;
-    const int n = splice::active_cells(sh, cell_step, a.cells);
+    TreeArgs args;
+    const int n = splice::active_cells(sh, cell_step, args.cells);
     if (n == 0) return SPLICE_OK;
     int64_t keys = 0;
     for (int i = 0; i < n; ++i) {
-        const int64_t k = splice::tree_keys(sh, checked, T, a.cells.step[i]);
+        const int64_t k = splice::tree_keys(sh, checked, T, args.cells.step[i]);
         keys = k > keys ? k : keys;
-        const int c = a.cells.cell[i];
-        const int64_t ahead = (int64_t)cell_LW[2 * c + 1] - a.cells.step[i];   // depth of the onset
+        const int c = args.cells.cell[i];
+        const int64_t ahead = (int64_t)cell_LW[2 * c + 1] - args.cells.step[i];   // depth of the onset
         const bool never = call->layer < cell_LW[2 * c] || ahead > SPLICE_MAX_NODES;
-        a.onset[i] = (uint8_t)(never ? SPLICE_MAX_NODES : (ahead > 0 ? ahead : 0));
+        args.onset[i] = (uint8_t)(never ? SPLICE_MAX_NODES : (ahead > 0 ? ahead : 0));
     }
     const splice::TreePlan p = splice::tree_plan(sh, checked, T, n, keys);
     if ((int64_t)sh.n_kv_heads * n * p.row_tiles * p.n_split > INT32_MAX ||
         (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30)
         return SPLICE_EUNSUPPORTED;
     if (p.bytes > 0 && (!workspace || !splice::aligned(workspace, 256) || workspace_bytes < p.bytes)) return SPLICE_EWORKSPACE;
+    splice_dev::TreeCall &a = args.call;
     a.q = (const char *)q;
     a.ck = (const char *)clean_k;
     a.cv = (const char *)clean_v;
@@ -99,9 +100,9 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     a.n_split = p.n_split;
     a.qk_scale = call->scale * splice_dev::kLog2e;
     hipStream_t st = (hipStream_t)stream;
-    const bool ok = sh.head_dim == 64    ? splice_dev::launch_tree_d64(a, p, tree->kv_format, st)
-                    : sh.head_dim == 128 ? splice_dev::launch_tree_d128(a, p, tree->kv_format, st)
-                                         : splice_dev::launch_tree_d256(a, p, tree->kv_format, st);
+    const bool ok = sh.head_dim == 64    ? splice_dev::launch_tree_d64(args, p, tree->kv_format, st)
+                    : sh.head_dim == 128 ? splice_dev::launch_tree_d128(args, p, tree->kv_format, st)
+                                         : splice_dev::launch_tree_d256(args, p, tree->kv_format, st);
     return ok ? SPLICE_OK : SPLICE_EHIP;
 }
 

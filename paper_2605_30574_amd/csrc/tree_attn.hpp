@@ -25,15 +25,14 @@
 
 #include "kv_format.hpp"
 #include "tree_plan.hpp"
-#include "wave_mfma.hpp"
+#include "prompt_wide.hpp"
 
 namespace splice_dev {
 
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef __attribute__((address_space(3))) i16x4_t lds_tr_t;
 
-struct TreeArgs {
+struct TreeCall {
     const char *q, *ck, *cv, *dk, *dv, *gk, *gv;
     const uint8_t *gke, *gve;
     const int32_t *depth;
@@ -43,8 +42,24 @@ struct TreeArgs {
     float *part;   // [split][active cell][node][q head][D], then [..][2] (m, l)
     int T, G, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, n_split;
     float qk_scale;   // scale * log2(e)
+};
+struct TreeArgs {
+    TreeCall call;
     splice::TreeCells cells;
     uint8_t onset[SPLICE_MAX_CELLS];   // depth from which an active cell's nodes are spliced (64: none)
+};
+
+// Where a work group is in its list of keys: the segment (0 the prompt before the span, or all
+// of it; 1 the span, clean; 2 the span from the donor; 3 the prompt behind it; 4
+// the generated rows with the tree's behind them), the rows left of it, the next tile's rows and
+// first key (a prompt position, or in segment 4 a generated row).
+struct TreeWalk {
+    const char *k, *v;
+    int seg, rem, key0;
+};
+struct TreeTileRef {
+    int seg, key0, n;
+    bool differ, mask;
 };
 
 template <int D, int RW>
@@ -110,7 +125,8 @@ __device__ __forceinline__ void split_non_finite(u32x4_t &w, u32x4_t &above, u32
 }
 
 template <int D, int RW, bool F8>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs a) {
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs args) {
+    const TreeCall a = args.call;   // what the lambdas use: captured, the whole arguments would go to memory
     using X = TreeTile<D, RW>;
     constexpr int KW = X::KW, KB = X::KB, TK = X::TK, ND = X::ND, NST = D / 16;
     extern __shared__ __align__(16) char lds[];
@@ -122,7 +138,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs a)
     // ---- which rows: KV heads run fastest, so that with eight (or a multiple) an XCD keeps to its own
     const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, n_items = a.n_active * a.row_tiles;
     const int split = rest / n_items, item = rest % n_items, ci = item / a.row_tiles, rt = item % a.row_tiles;
-    const int c = a.cells.cell[ci], step = a.cells.step[ci], onset = a.onset[ci], rows = a.T * a.G;
+    const int c = args.cells.cell[ci], step = args.cells.step[ci], onset = args.onset[ci], rows = a.T * a.G;
     const int row0 = 32 * RW * rt, row = row0 + 32 * rw + r;
     const int64_t node0 = (int64_t)c * a.T;
     int d_node = lane < a.T ? a.depth[node0 + lane] : -1;   // lane u: node u's depth
@@ -152,43 +168,78 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs a)
     const int low_all = a.window > 0 ? max(p0 + d_min - a.window + 1, 0) : 0;   // some row sees from here on,
     const int low_max = a.window > 0 ? p0 + d_max - a.window + 1 : 0;           // every row from here on
 
-    // ---- the list of keys
-    KeyListN<5> L;
-    list_init(L);
-    const size_t head_p = (size_t)g * a.Tp * X::ROW;
-    const int grow = F8 ? D : X::ROW;   // bytes of a generated row
-    const int64_t pair = (int64_t)c * a.Hkv + g;
+    // ---- the list of keys: segments 0 to 4, walked tile by tile
     const int b0 = min(low_all, a.Tp), sa = min(max(a.span_lo, b0), a.Tp), sb = max(a.span_hi, sa);
     const int g0 = min(max(low_all - a.Tp, 0), step);
-    {
-        const char *ck = a.ck + head_p, *cv = a.cv + head_p;
-        auto prompt = [&](const char *k, const char *v, int b, int e, int cols) {
-            list_add<TK>(L, k + (size_t)b * X::ROW, v + (size_t)b * X::ROW, e - b, cols, b);
-        };
-        if (!any_donor) {
-            prompt(ck, cv, b0, a.Tp, kColsAll);
-        } else {
-            prompt(ck, cv, b0, sa, kColsAll);
-            if (any_clean) prompt(ck, cv, sa, sb, kColsClean);
-            if (!a.zero_donor) prompt(a.dk + head_p, a.dv + head_p, sa, sb, any_clean ? kColsDonor : kColsAll);
-            prompt(ck, cv, sb, a.Tp, kColsAll);
-        }
-    }
-    const int gen_tile = list_tiles(L);   // tiles from here on are generated rows; key0 is then the row
-    list_add<TK>(L, a.gk + (pair * a.cap + g0) * grow, a.gv + (pair * a.cap + g0) * grow, step + a.T - g0, kColsAll, g0);
-    const int n_tiles = list_tiles(L);
+    const size_t head_p = (size_t)g * a.Tp * X::ROW;
+    const int64_t pair = (int64_t)c * a.Hkv + g;
+    auto seg_begin = [&](int i) { return i == 0 ? b0 : (i == 3 ? sb : (i == 4 ? g0 : sa)); };
+    auto seg_len = [&](int i) {
+        if (i == 4) return step + a.T - g0;
+        if (!any_donor) return i == 0 ? a.Tp - b0 : 0;
+        if (i == 0) return sa - b0;
+        if (i == 3) return a.Tp - sb;
+        return (i == 1 ? any_clean : !a.zero_donor) ? sb - sa : 0;
+    };
+    auto seg_tiles = [&](int i) { return (seg_len(i) + TK - 1) / TK; };
+    const int n_tiles = seg_tiles(0) + seg_tiles(1) + seg_tiles(2) + seg_tiles(3) + seg_tiles(4);
     const int t0 = (int)((int64_t)n_tiles * split / a.n_split), t1 = (int)((int64_t)n_tiles * (split + 1) / a.n_split);
+    TreeWalk w;
+    auto enter = [&](int i, int first) {   // segment i from its row `first` on
+        const int row_bytes = F8 && i == 4 ? D : X::ROW;
+        const char *k = i == 4 ? a.gk + pair * a.cap * row_bytes : pick_base(i == 2, a.ck, a.dk) + head_p;
+        const char *v = i == 4 ? a.gv + pair * a.cap * row_bytes : pick_base(i == 2, a.cv, a.dv) + head_p;
+        w.seg = i;
+        w.key0 = seg_begin(i) + first;
+        w.rem = seg_len(i) - first;
+        w.k = k + (size_t)w.key0 * row_bytes;
+        w.v = v + (size_t)w.key0 * row_bytes;
+    };
+    {
+        int i = 0, t = t0;
+        while (i < 4 && t >= seg_tiles(i)) t -= seg_tiles(i++);
+        enter(i, t * TK);
+    }
+    // The tile under way: how many keys, which, and what has to be looked at.
+    auto tile_of = [&]() {
+        TreeTileRef x;
+        x.seg = w.seg;
+        x.key0 = w.key0;
+        x.n = min(TK, w.rem);
+        // some row of the work group does not see some key: ...
+        x.differ = w.seg == 4   ? a.Tp + w.key0 < low_max || w.key0 + TK > step
+                   : w.seg == 0 ? w.key0 < low_max
+                                : w.key0 < low_max || (any_clean && (w.seg == 1 || w.seg == 2));
+        x.mask = x.differ || x.n < TK;   // ... or the tile is not full
+        return x;
+    };
+    auto advance = [&]() {
+        const int row_bytes = F8 && w.seg == 4 ? D : X::ROW;
+        w.k += TK * row_bytes;
+        w.v += TK * row_bytes;
+        w.key0 += TK;
+        w.rem -= TK;
+        while (w.rem <= 0 && w.seg < 4) enter(w.seg + 1, 0);
+    };
 
-    // ---- staging: chunk u = i * 256 + tid of a tile is 16 bytes of key u / CPR
-    u32x4_t kr[X::NL], vr[X::NL];
-    uint32_t ke[X::NL], ve[X::NL];
-    auto is_gen = [&](int t) { return t >= gen_tile; };
-    auto load = [&](int t) {
-        const TileRef ref = list_tile<TK>(L, t, is_gen(t) ? grow : X::ROW);
-        if (F8 && is_gen(t)) {
-            const __amdgpu_buffer_rsrc_t rk = rows_rsrc(ref.k, ref.n * D), rv = rows_rsrc(ref.v, ref.n * D);
-            const __amdgpu_buffer_rsrc_t re = rows_rsrc(reinterpret_cast<const char *>(a.gke + pair * a.cap + ref.key0), ref.n);
-            const __amdgpu_buffer_rsrc_t rf = rows_rsrc(reinterpret_cast<const char *>(a.gve + pair * a.cap + ref.key0), ref.n);
+    // ---- tiles into LDS.  bf16 rows go there straight from memory (lds_dma16:
+    // a lane names 16 bytes for chunk slot 64 q + lane); 8-bit ones by way of
+    // registers, where they become bf16
+    const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_offset(lds));
+    int k_src[X::NL], v_src[X::NL];
+    static_for<0, X::NL>([&](auto i) {
+        const int u = ((int)i * 4 + wave) * 64 + lane, key = u / X::CPR, slot = u % X::CPR;
+        k_src[i] = key * X::ROW + ((slot ^ tree_swz_k<D>(key)) << 4);
+        v_src[i] = key * X::ROW + ((slot ^ tree_swz_v<D>(key)) << 4);
+    });
+    u32x4_t kr[X::NL8], vr[X::NL8];
+    uint32_t ke[X::NL8], ve[X::NL8];
+    auto load = [&](int b) {   // of the walk's tile
+        const int n = min(TK, w.rem);
+        if (F8 && w.seg == 4) {
+            const __amdgpu_buffer_rsrc_t rk = rows_rsrc(w.k, n * D), rv = rows_rsrc(w.v, n * D);
+            const __amdgpu_buffer_rsrc_t re = rows_rsrc(reinterpret_cast<const char *>(a.gke + pair * a.cap + w.key0), n);
+            const __amdgpu_buffer_rsrc_t rf = rows_rsrc(reinterpret_cast<const char *>(a.gve + pair * a.cap + w.key0), n);
             static_for<0, X::NL8>([&](auto i) {
                 const int u = (int)i * 256 + tid;
                 kr[i] = row_load<0>(rk, u * 16);
@@ -197,68 +248,58 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs a)
                 ve[i] = __builtin_amdgcn_raw_buffer_load_b8(rf, u / (D / 16), 0, 0);
             });
         } else {
-            const __amdgpu_buffer_rsrc_t rk = rows_rsrc(ref.k, ref.n * X::ROW), rv = rows_rsrc(ref.v, ref.n * X::ROW);
+            const u32x4_t rk = rows_desc(w.k, n * X::ROW), rv = rows_desc(w.v, n * X::ROW);
+            const uint32_t base = lds0 + b * 2 * X::TILE;
             static_for<0, X::NL>([&](auto i) {
-                const int u = (int)i * 256 + tid;
-                kr[i] = row_load<0>(rk, u * 16);
-                vr[i] = row_load<0>(rv, u * 16);
+                const uint32_t at = base + (((int)i * 4 + wave) << 10);
+                lds_dma16(rk, at, k_src[i]);
+                lds_dma16(rv, at + X::TILE, v_src[i]);
             });
         }
     };
-    auto put = [&](char *buf, int key, int chunk, u32x4_t k, u32x4_t v) {
-        *reinterpret_cast<u32x4_t *>(buf + key * X::ROW + ((chunk ^ tree_swz_k<D>(key)) << 4)) = k;
-        *reinterpret_cast<u32x4_t *>(buf + X::TILE + key * X::ROW + ((chunk ^ tree_swz_v<D>(key)) << 4)) = v;
-    };
-    // whether some row of the work group does not see all of tile t
-    auto masked = [&](int t) {
-        const TileRef ref = list_tile<TK>(L, t, 0);
-        if (ref.n < TK || ref.cols != kColsAll) return true;
-        return is_gen(t) ? a.Tp + ref.key0 < low_max || ref.key0 + TK > step : ref.key0 < low_max;
-    };
-    // In a masked tile the values are looked at: rows of nodes that are not
-    // there count as 0, and s_bad tells of infinities and NaN (they must
-    // not reach the rows that do not see them: 0 * inf).
-    auto stage = [&](int t, int b) {
+    auto convert = [&](int b) {   // 8-bit rows from the registers
         char *buf = lds + b * 2 * X::TILE;
-        const bool look = masked(t), f8 = F8 && is_gen(t);
-        const int key0 = list_tile<TK>(L, t, 0).key0;
-        bool bad = false;
-        auto value = [&](int key, u32x4_t v) {
-            if (look) {
-                const int u = key0 + key - step;
-                if (is_gen(t) && u >= 0 && (u >= 64 || !((alive >> u) & 1))) v = u32x4_t{0, 0, 0, 0};
-                bad |= has_non_finite(v);
-            }
-            return v;
+        auto put = [&](int key, int chunk, u32x4_t k, u32x4_t v) {
+            *reinterpret_cast<u32x4_t *>(buf + key * X::ROW + ((chunk ^ tree_swz_k<D>(key)) << 4)) = k;
+            *reinterpret_cast<u32x4_t *>(buf + X::TILE + key * X::ROW + ((chunk ^ tree_swz_v<D>(key)) << 4)) = v;
         };
-        if (f8) {
-            static_for<0, X::NL8>([&](auto i) {
-                const int u = (int)i * 256 + tid, key = u / (D / 16), ch = 2 * (u % (D / 16));
-                const u32x4_t k = kr[i], v = vr[i];
-                put(buf, key, ch, e4m3_to_bf16(make_uint2(k.x, k.y), ke[i]), value(key, e4m3_to_bf16(make_uint2(v.x, v.y), ve[i])));
-                put(buf, key, ch + 1, e4m3_to_bf16(make_uint2(k.z, k.w), ke[i]),
-                    value(key, e4m3_to_bf16(make_uint2(v.z, v.w), ve[i])));
-            });
-        } else {
-            static_for<0, X::NL>([&](auto i) {
-                const int u = (int)i * 256 + tid, key = u / X::CPR;
-                put(buf, key, u % X::CPR, kr[i], value(key, vr[i]));
-            });
-        }
+        static_for<0, X::NL8>([&](auto i) {
+            const int u = (int)i * 256 + tid, key = u / (D / 16), ch = 2 * (u % (D / 16));
+            const u32x4_t k = kr[i], v = vr[i];
+            put(key, ch, e4m3_to_bf16(make_uint2(k.x, k.y), ke[i]), e4m3_to_bf16(make_uint2(v.x, v.y), ve[i]));
+            put(key, ch + 1, e4m3_to_bf16(make_uint2(k.z, k.w), ke[i]), e4m3_to_bf16(make_uint2(v.z, v.w), ve[i]));
+        });
+    };
+    // In a tile that rows see differently the values are looked at: those of
+    // nodes that are not there become 0, and s_bad tells of infinities and NaN
+    // (they must not reach the rows that do not see them: 0 * inf).
+    auto look = [&](const TreeTileRef &x, int b, int t) {
+        char *v = lds + b * 2 * X::TILE + X::TILE;
+        bool bad = false;
+        static_for<0, X::NL>([&](auto i) {
+            const int u = (int)i * 256 + tid, key = u / X::CPR, node = x.key0 + key - step;
+            u32x4_t *p = reinterpret_cast<u32x4_t *>(v + u * 16);
+            if (x.seg == 4 && node >= 0 && (node >= 64 || !((alive >> node) & 1))) *p = u32x4_t{0, 0, 0, 0};
+            else bad |= has_non_finite(*p);
+        });
         if (bad) s_bad[b] = t + 1;
     };
 
+    TreeTileRef cur = tile_of();
+    if (t0 < t1) {
+        load(0);
+        advance();
+    }
     if (tid < 2) s_bad[tid] = 0;
-    if (t0 < t1) load(t0);
 
     // ---- Q^T, in the lanes of the B operand: row r, d = 16 st + 8 h ..
     bf16x8_t qb[NST];
     {
         const int64_t q_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
         static_for<0, NST>([&](auto st) {
-            u32x4_t w = {0, 0, 0, 0};
-            if (valid) w = *reinterpret_cast<const u32x4_t *>(a.q + (q_row * D + 16 * (int)st + 8 * h) * 2);
-            qb[st] = __builtin_bit_cast(bf16x8_t, w);
+            u32x4_t x = {0, 0, 0, 0};
+            if (valid) x = *reinterpret_cast<const u32x4_t *>(a.q + (q_row * D + 16 * (int)st + 8 * h) * 2);
+            qb[st] = __builtin_bit_cast(bf16x8_t, x);
         });
     }
     // state of a row: o[db][i] is d = 32 db + 8 (i / 4) + 4 h + i % 4; a half's share of the sum
@@ -285,14 +326,23 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs a)
         });
     }
 
-    __syncthreads();   // s_bad
-    if (t0 < t1) stage(t0, 0);
-    __syncthreads();
+    wait_vmcnt<0>();   // this wave's part of the first tile
+    if (F8 && t0 < t1 && cur.seg == 4) convert(0);
     for (int t = t0; t < t1; ++t) {
         const int b = (t - t0) & 1;
+        __syncthreads();   // every wave's part of tile t is in LDS, and tile t - 1 has been read
+        const TreeTileRef next = tile_of();
+        if (t + 1 < t1) {
+            load(b ^ 1);
+            advance();
+        }
+        bool bad = false;
+        if (cur.differ) {
+            look(cur, b, t);
+            __syncthreads();
+            bad = __builtin_amdgcn_readfirstlane(s_bad[b]) == t + 1;
+        }
         const char *buf = lds + b * 2 * X::TILE;
-        if (t + 1 < t1) load(t + 1);
-        const bool look = masked(t);
         f32x16_t s[KB];
         static_for<0, KB>([&](auto kb) {
             static_for<0, 16>([&](auto i) { s[kb][(int)i] = 0.f; });
@@ -301,14 +351,13 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs a)
                 s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[st], s[kb], 0, 0, 0);
             });
         });
-        if (look) {
-            const TileRef ref = list_tile<TK>(L, t, 0);
-            const int first = ref.key0 + kw * 32 * KB, n = ref.n - kw * 32 * KB;
+        if (cur.mask) {
+            const int first = cur.key0 + kw * 32 * KB, n = cur.n - kw * 32 * KB;
             uint64_t see;
-            if (is_gen(t)) {
+            if (cur.seg == 4) {
                 see = bits(low - a.Tp - first, min(step - first, n)) | (shifted(word, step - first) & bits(step - first, n));
             } else {
-                see = (ref.cols == kColsAll || (ref.cols == kColsDonor) == spliced) ? bits(low - first, n) : 0;
+                see = !cur.differ || !any_clean || cur.seg == 0 || cur.seg == 3 || (cur.seg == 2) == spliced ? bits(low - first, n) : 0;
             }
             see >>= 4 * h;
             static_for<0, KB>([&](auto kb) {
@@ -339,34 +388,42 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs a)
                 pb[2 * kb + i / 8][i % 8] = (__bf16)p;
             });
         });
-        const bool bad = look && __builtin_amdgcn_readfirstlane(s_bad[b]) == t + 1;
-        static_for<0, ND>([&](auto db) {
-            f32x16_t up, down;
-            if (bad) static_for<0, 16>([&](auto i) { up[(int)i] = down[(int)i] = 0.f; });
-            static_for<0, 2 * KB>([&](auto kk) {
-                const char *at = buf + v_at[db] + 16 * (int)kk * X::ROW;
-                const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_t *)at);
-                const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_t *)(at + 8 * X::ROW));
-                const u32x2_t wl = __builtin_bit_cast(u32x2_t, lo), wh = __builtin_bit_cast(u32x2_t, hi);
-                u32x4_t va = {wl.x, wl.y, wh.x, wh.y};
-                if (bad) {
-                    u32x4_t above, under;
-                    split_non_finite(va, above, under);
-                    up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, above), pb[kk], up, 0, 0, 0);
-                    down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, under), pb[kk], down, 0, 0, 0);
-                }
-                o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, va), pb[kk], o[db], 0, 0, 0);
+        auto values = [&](int db, int kk) {   // 32 d of 16 keys, in the lanes of the A operand
+            const char *at = buf + v_at[db] + 16 * kk * X::ROW;
+            const u32x2_t lo = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)at));
+            const u32x2_t hi = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(at + 8 * X::ROW)));
+            return u32x4_t{lo.x, lo.y, hi.x, hi.y};
+        };
+        auto product = [&](u32x4_t v, bf16x8_t p, f32x16_t acc) {
+            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), p, acc, 0, 0, 0);
+        };
+        if (!bad) {
+            static_for<0, ND>([&](auto db) {
+                static_for<0, 2 * KB>([&](auto kk) { o[db] = product(values(db, kk), pb[kk], o[db]); });
             });
-            if (bad) {
+        } else {
+            // infinities and NaN apart: the weights that fall on them say which rows they reach
+            static_for<0, ND>([&](auto db) {
+                f32x16_t up, down;
+                static_for<0, 16>([&](auto i) { up[(int)i] = down[(int)i] = 0.f; });
+                static_for<0, 2 * KB>([&](auto kk) {
+                    u32x4_t v = values(db, kk), above, under;
+                    split_non_finite(v, above, under);
+                    o[db] = product(v, pb[kk], o[db]);
+                    up = product(above, pb[kk], up);
+                    down = product(under, pb[kk], down);
+                });
                 static_for<0, 16>([&](auto i) {
                     if (up[(int)i] > 0.f) o[db][(int)i] += INFINITY;
                     if (down[(int)i] > 0.f) o[db][(int)i] -= INFINITY;
                 });
-            }
-        });
-        if (t + 1 < t1) stage(t + 1, b ^ 1);
-        __syncthreads();
+            });
+        }
+        cur = next;
+        wait_vmcnt<0>();
+        if (F8 && t + 1 < t1 && cur.seg == 4) convert(b ^ 1);
     }
+    __syncthreads();
 
     // ---- results
     l += __shfl_xor(l, 32);
@@ -442,14 +499,15 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs a)
 
 // Joins the splits of every row: a thread has four values of a row.
 template <int D>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
+    const TreeCall a = args.call;
     const int Hq = a.Hkv * a.G;
     const int64_t n_part = (int64_t)a.n_active * a.T * Hq;
     const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, row = e / (D / 4);
     const int d4 = (int)(e % (D / 4));
     if (row >= n_part) return;
     const int hd = (int)(row % Hq), node = (int)(row / Hq % a.T), ci = (int)(row / Hq / a.T);
-    const int64_t at_node = (int64_t)a.cells.cell[ci] * a.T + node;
+    const int64_t at_node = (int64_t)args.cells.cell[ci] * a.T + node;
     if (a.depth[at_node] < 0) return;
     const float *ml = a.part + (int64_t)a.n_split * n_part * D;
     float M = -INFINITY, L = 0.f;
@@ -472,7 +530,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
 typedef bool (*TreeLaunch)(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hipStream_t stream);
 
 template <int D, int RW, bool F8>
-bool launch_tree_kernel(const TreeArgs &a, hipStream_t stream) {
+bool launch_tree_kernel(const TreeArgs &args, hipStream_t stream) {
     using X = TreeTile<D, RW>;
     // more LDS than a kernel may take unasked; asked once a device
     static std::atomic<uint64_t> raised{0};
@@ -487,8 +545,8 @@ bool launch_tree_kernel(const TreeArgs &a, hipStream_t stream) {
             raised.fetch_or(bit);
         }
     }
-    const unsigned blocks = (unsigned)((int64_t)a.Hkv * a.n_active * a.row_tiles * a.n_split);
-    hipLaunchKernelGGL((tree_kernel<D, RW, F8>), dim3(blocks), dim3(256), X::LDS, stream, a);
+    const unsigned blocks = (unsigned)((int64_t)args.call.Hkv * args.call.n_active * args.call.row_tiles * args.call.n_split);
+    hipLaunchKernelGGL((tree_kernel<D, RW, F8>), dim3(blocks), dim3(256), X::LDS, stream, args);
     return hipGetLastError() == hipSuccess;
 }
 
@@ -504,8 +562,9 @@ bool launch_tree(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hi
         if (p.row_waves == 2) ok = f8 ? launch_tree_kernel<D, 2, true>(a, stream) : launch_tree_kernel<D, 2, false>(a, stream);
         else ok = f8 ? launch_tree_kernel<D, 4, true>(a, stream) : launch_tree_kernel<D, 4, false>(a, stream);
     }
-    if (!ok || a.n_split == 1) return ok;
-    const int64_t units = (int64_t)a.n_active * a.T * a.Hkv * a.G * (D / 4);
+    const TreeCall &c = a.call;
+    if (!ok || c.n_split == 1) return ok;
+    const int64_t units = (int64_t)c.n_active * c.T * c.Hkv * c.G * (D / 4);
     hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess;
 }
