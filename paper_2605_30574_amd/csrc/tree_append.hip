@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
     constexpr int LPR = D / 8, ROWS = kAppendThreads / LPR;
     __shared__ float2 s_cs[D / 2];
     const int ci = blockIdx.x / a.T, t = blockIdx.x % a.T, tid = threadIdx.x;
-    const int c = a.cells.cell[ci], step = a.cells.step[ci];
+    const int c = (int)a.cells.cell[ci], step = a.cells.step[ci];
     const int64_t token = (int64_t)c * a.T + t;
     const int depth = a.depth[token];
     if (depth < 0) return;   // padding
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kAppendThreads) void keep_kernel(RowsArgs a) {
     constexpr int LPR = ROW / 16, U = SPLICE_MAX_NODES * LPR / kAppendThreads;
     __shared__ int s_from[SPLICE_MAX_NODES];
     const int ci = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, tid = threadIdx.x, lane = tid & 63;
-    const int c = a.cells.cell[ci];
+    const int c = (int)a.cells.cell[ci];
     const int64_t row0 = ((int64_t)c * a.Hkv + g) * a.cap + a.cells.step[ci];
     char *cache = blockIdx.y ? a.gv : a.gk;
     uint8_t *ex = blockIdx.y ? a.gve : a.gke;

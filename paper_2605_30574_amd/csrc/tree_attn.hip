@@ -5,6 +5,28 @@
 
 using splice_dev::TreeArgs;
 
+namespace {
+
+// Compute units of the current device (256 when HIP cannot tell: the plan then still holds, it only
+// balances for that many).
+int compute_units() {
+    static std::atomic<int> known[64];
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0) {
+        (void)hipGetLastError();
+        return 256;
+    }
+    if (dev < 64 && (n = known[dev].load()) > 0) return n;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) {
+        (void)hipGetLastError();
+        return 256;
+    }
+    if (dev < 64) known[dev].store(n);
+    return n;
+}
+
+}  // namespace
+
 extern "C" {
 
 int64_t splice_tree_attn_workspace_bytes(const splice_shape *shape, const splice_call *call, const splice_tree *tree) {
@@ -15,14 +37,7 @@ int64_t splice_tree_attn_workspace_bytes(const splice_shape *shape, const splice
     checked.step = 0;
     rc = splice::validate_call(*shape, &checked);
     if (rc != SPLICE_OK) return rc;
-    // any steps: every number of active cells, over as many keys as there may be
-    const int64_t keys = (int64_t)shape->prompt_len + shape->gen_capacity;
-    size_t bytes = 0;
-    for (int n = 1; n <= shape->n_cells; ++n) {
-        const size_t b = splice::tree_plan(*shape, checked, tree->n_nodes, n, keys).bytes;
-        bytes = b > bytes ? b : bytes;
-    }
-    return (int64_t)bytes;
+    return (int64_t)splice::tree_most_bytes(*shape, checked, tree->n_nodes, compute_units());
 }
 
 int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, const splice_tree *tree,
@@ -57,19 +72,26 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     TreeArgs args;
     const int n = splice::active_cells(sh, cell_step, args.cells);
     if (n == 0) return SPLICE_OK;
-    int64_t keys = 0;
+    int tiles[SPLICE_MAX_CELLS];
+    const int tile = splice::tree_tile_keys(sh.head_dim, splice::tree_row_waves(sh.head_dim, T * splice::group_of(sh)));
     for (int i = 0; i < n; ++i) {
-        const int64_t k = splice::tree_keys(sh, checked, T, args.cells.step[i]);
-        keys = k > keys ? k : keys;
-        const int c = args.cells.cell[i];
+        const int c = (int)args.cells.cell[i];
         const int64_t ahead = (int64_t)cell_LW[2 * c + 1] - args.cells.step[i];   // depth of the onset
-        const bool never = call->layer < cell_LW[2 * c] || ahead > SPLICE_MAX_NODES;
-        args.onset[i] = (uint8_t)(never ? SPLICE_MAX_NODES : (ahead > 0 ? ahead : 0));
+        const bool never = call->layer < cell_LW[2 * c] || ahead >= T;
+        args.slots.first_onset[i] = (uint32_t)(never ? SPLICE_MAX_NODES : (ahead > 0 ? ahead : 0));
+        tiles[i] = splice::tree_tiles(sh, checked, T, tile, args.cells.step[i], !never, ahead > 0);
     }
-    const splice::TreePlan p = splice::tree_plan(sh, checked, T, n, keys);
-    if ((int64_t)sh.n_kv_heads * n * p.row_tiles * p.n_split > INT32_MAX ||
-        (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30)
+    const splice::TreePlan p = splice::tree_plan(sh, checked, T, tiles, n, compute_units());
+    if ((int64_t)sh.n_kv_heads * p.n_slots * p.row_tiles > INT32_MAX || (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30)
         return SPLICE_EUNSUPPORTED;
+    uint32_t first = 0;
+    for (uint32_t &word : args.slots.cell) word = 0;
+    for (int i = 0; i < n; ++i) {
+        args.slots.first_onset[i] |= first << 8;
+        for (const uint32_t end = first + (uint32_t)splice::ceil_div(tiles[i], p.per); first < end; ++first)
+            args.slots.cell[first / 4] |= (uint32_t)i << (8 * (first % 4));
+    }
+    args.slots.first_onset[n] = first << 8;
     if (p.bytes > 0 && (!workspace || !splice::aligned(workspace, 256) || workspace_bytes < p.bytes)) return SPLICE_EWORKSPACE;
     splice_dev::TreeCall &a = args.call;
     a.q = (const char *)q;
@@ -97,7 +119,9 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     a.zero_donor = zero ? 1 : 0;
     a.n_active = n;
     a.row_tiles = p.row_tiles;
-    a.n_split = p.n_split;
+    a.n_slots = p.n_slots;
+    a.per = p.per;
+    a.split = p.split;
     a.qk_scale = call->scale * splice_dev::kLog2e;
     hipStream_t st = (hipStream_t)stream;
     const bool ok = sh.head_dim == 64    ? splice_dev::launch_tree_d64(args, p, tree->kv_format, st)

@@ -39,14 +39,15 @@ struct TreeCall {
     const uint64_t *visible;
     __bf16 *out;
     float *lse;
-    float *part;   // [split][active cell][node][q head][D], then [..][2] (m, l)
-    int T, G, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, n_split;
+    float *part;   // [slot][node][q head][D], then [..][2] (m, l)
+    int T, G, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, n_slots, per;
+    bool split;
     float qk_scale;   // scale * log2(e)
 };
 struct TreeArgs {
     TreeCall call;
     splice::TreeCells cells;
-    uint8_t onset[SPLICE_MAX_CELLS];   // depth from which an active cell's nodes are spliced (64: none)
+    splice::TreeSlots slots;
 };
 
 // Where a work group is in its list of keys: the segment (0 the prompt before the span, or all
@@ -64,15 +65,18 @@ struct TreeTileRef {
 
 template <int D, int RW>
 struct TreeTile {
+    static constexpr bool OWN = RW == 1;                       // every wave has tiles of its own
     static constexpr int KW = 4 / RW;                          // waves over keys
     static constexpr int KB = splice::tree_key_blocks(D, RW);  // 32-key blocks of a wave
     static constexpr int TK = splice::tree_tile_keys(D, RW);   // keys of a tile
     static constexpr int ROW = 2 * D;                          // bytes of a staged row
     static constexpr int CPR = D / 8;                          // 16-byte chunks of a row
     static constexpr int TILE = TK * ROW;                      // bytes of a K (or V) tile
-    static constexpr int LDS = 4 * TILE;                       // two buffers of K and V
-    static constexpr int NL = TK * CPR / 256;                  // chunks a thread loads of a K (or V) tile
+    static constexpr int LDS = (OWN ? 8 : 4) * TILE;           // K and V: a tile a wave, or two for all
+    static constexpr int NT = OWN ? 64 : 256;                  // threads that load a tile
+    static constexpr int NL = TK * CPR / NT;                   // chunks a thread loads of a K (or V) tile
     static constexpr int NL8 = NL / 2;                         // ... of 8-bit rows
+    static constexpr int NR = OWN ? NL : NL8;                  // ... by way of registers
     static constexpr int ND = D / 32;                          // 32-wide d blocks of the output
     static_assert(RW * KW == 4 && NL8 >= 1 && (KW == 1 || KW * 32 * RW * D * 4 <= LDS), "");
 };
@@ -95,6 +99,14 @@ __device__ __forceinline__ uint64_t bits(int b, int e) {
 __device__ __forceinline__ uint64_t shifted(uint64_t x, int by) {   // left, or right when by < 0
     if (by >= 64 || by <= -64) return 0;
     return by >= 0 ? x << by : x >> -by;
+}
+
+// Lanes of a wave that hand each other values through LDS: its operations run
+// in order, so only the compiler has to keep theirs.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
 }
 
 // Which words of two bf16 values hold an infinity or NaN.
@@ -136,9 +148,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     const int r = lane & 31, h = lane >> 5, rw = wave % RW, kw = wave / RW;
 
     // ---- which rows: KV heads run fastest, so that with eight (or a multiple) an XCD keeps to its own
-    const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, n_items = a.n_active * a.row_tiles;
-    const int split = rest / n_items, item = rest % n_items, ci = item / a.row_tiles, rt = item % a.row_tiles;
-    const int c = args.cells.cell[ci], step = args.cells.step[ci], onset = args.onset[ci], rows = a.T * a.G;
+    const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, slot = rest / a.row_tiles, rt = rest % a.row_tiles;
+    const int ci = (args.slots.cell[slot >> 2] >> (8 * (slot & 3))) & 255;
+    const uint32_t here = args.slots.first_onset[ci];
+    const int chunk = slot - (int)(here >> 8), onset = here & 255;
+    const bool last_chunk = slot + 1 == (int)(args.slots.first_onset[ci + 1] >> 8);
+    const int c = (int)args.cells.cell[ci], step = args.cells.step[ci], rows = a.T * a.G;
     const int row0 = 32 * RW * rt, row = row0 + 32 * rw + r;
     const int64_t node0 = (int64_t)c * a.T;
     int d_node = lane < a.T ? a.depth[node0 + lane] : -1;   // lane u: node u's depth
@@ -183,7 +198,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     };
     auto seg_tiles = [&](int i) { return (seg_len(i) + TK - 1) / TK; };
     const int n_tiles = seg_tiles(0) + seg_tiles(1) + seg_tiles(2) + seg_tiles(3) + seg_tiles(4);
-    const int t0 = (int)((int64_t)n_tiles * split / a.n_split), t1 = (int)((int64_t)n_tiles * (split + 1) / a.n_split);
+    const int t0 = min(chunk * a.per, n_tiles), t1 = last_chunk ? n_tiles : min(t0 + a.per, n_tiles);
     TreeWalk w;
     auto enter = [&](int i, int first) {   // segment i from its row `first` on
         const int row_bytes = F8 && i == 4 ? D : X::ROW;
@@ -196,7 +211,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         w.v = v + (size_t)w.key0 * row_bytes;
     };
     {
-        int i = 0, t = t0;
+        int i = 0, t = X::OWN ? t0 + kw : t0;
         while (i < 4 && t >= seg_tiles(i)) t -= seg_tiles(i++);
         enter(i, t * TK);
     }
@@ -213,39 +228,56 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         x.mask = x.differ || x.n < TK;   // ... or the tile is not full
         return x;
     };
-    auto advance = [&]() {
+    auto advance = [&]() {   // to the wave's next tile
         const int row_bytes = F8 && w.seg == 4 ? D : X::ROW;
-        w.k += TK * row_bytes;
-        w.v += TK * row_bytes;
-        w.key0 += TK;
-        w.rem -= TK;
-        while (w.rem <= 0 && w.seg < 4) enter(w.seg + 1, 0);
+        constexpr int N = X::OWN ? 4 : 1;
+        w.k += N * TK * row_bytes;
+        w.v += N * TK * row_bytes;
+        w.key0 += N * TK;
+        w.rem -= N * TK;
+        while (w.rem <= 0 && w.seg < 4) {   // -rem / TK tiles into the next segment
+            const int first = w.rem <= 0 ? -w.rem / TK * TK : 0;
+            enter(w.seg + 1, first);
+        }
     };
 
-    // ---- tiles into LDS.  bf16 rows go there straight from memory (lds_dma16:
-    // a lane names 16 bytes for chunk slot 64 q + lane); 8-bit ones by way of
-    // registers, where they become bf16
+    // ---- tiles into LDS.  A tile for all waves: bf16 rows go there straight
+    // from memory (lds_dma16: a lane names 16 bytes for chunk slot 64 q + lane)
+    // into the other of two buffers, 8-bit ones by way of registers, where they
+    // become bf16.  Tiles of a wave's own: the next one waits in registers, so
+    // that one buffer a wave is enough, two work groups fit a compute unit and
+    // no wave waits for another.
+    const int ltid = X::OWN ? lane : tid;
+    char *const own = lds + (X::OWN ? wave * 2 * X::TILE : 0);
     const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_offset(lds));
     int k_src[X::NL], v_src[X::NL];
-    static_for<0, X::NL>([&](auto i) {
-        const int u = ((int)i * 4 + wave) * 64 + lane, key = u / X::CPR, slot = u % X::CPR;
-        k_src[i] = key * X::ROW + ((slot ^ tree_swz_k<D>(key)) << 4);
-        v_src[i] = key * X::ROW + ((slot ^ tree_swz_v<D>(key)) << 4);
-    });
-    u32x4_t kr[X::NL8], vr[X::NL8];
+    if constexpr (!X::OWN) {
+        static_for<0, X::NL>([&](auto i) {
+            const int u = (int)i * 256 + tid, key = u / X::CPR, slot_of = u % X::CPR;
+            k_src[i] = key * X::ROW + ((slot_of ^ tree_swz_k<D>(key)) << 4);
+            v_src[i] = key * X::ROW + ((slot_of ^ tree_swz_v<D>(key)) << 4);
+        });
+    }
+    u32x4_t kr[X::NR], vr[X::NR];
     uint32_t ke[X::NL8], ve[X::NL8];
-    auto load = [&](int b) {   // of the walk's tile
+    auto load = [&](int b) {   // the walk's tile
         const int n = min(TK, w.rem);
         if (F8 && w.seg == 4) {
             const __amdgpu_buffer_rsrc_t rk = rows_rsrc(w.k, n * D), rv = rows_rsrc(w.v, n * D);
             const __amdgpu_buffer_rsrc_t re = rows_rsrc(reinterpret_cast<const char *>(a.gke + pair * a.cap + w.key0), n);
             const __amdgpu_buffer_rsrc_t rf = rows_rsrc(reinterpret_cast<const char *>(a.gve + pair * a.cap + w.key0), n);
             static_for<0, X::NL8>([&](auto i) {
-                const int u = (int)i * 256 + tid;
+                const int u = (int)i * X::NT + ltid;
                 kr[i] = row_load<0>(rk, u * 16);
                 vr[i] = row_load<0>(rv, u * 16);
                 ke[i] = __builtin_amdgcn_raw_buffer_load_b8(re, u / (D / 16), 0, 0);
                 ve[i] = __builtin_amdgcn_raw_buffer_load_b8(rf, u / (D / 16), 0, 0);
+            });
+        } else if constexpr (X::OWN) {
+            const __amdgpu_buffer_rsrc_t rk = rows_rsrc(w.k, n * X::ROW), rv = rows_rsrc(w.v, n * X::ROW);
+            static_for<0, X::NL>([&](auto i) {
+                kr[i] = row_load<0>(rk, ((int)i * X::NT + ltid) * 16);
+                vr[i] = row_load<0>(rv, ((int)i * X::NT + ltid) * 16);
             });
         } else {
             const u32x4_t rk = rows_desc(w.k, n * X::ROW), rv = rows_desc(w.v, n * X::ROW);
@@ -257,36 +289,49 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             });
         }
     };
-    auto convert = [&](int b) {   // 8-bit rows from the registers
-        char *buf = lds + b * 2 * X::TILE;
+    // What load() left in registers, into the tile.  8-bit rows: a lane has two
+    // neighbouring chunks, and every other lane begins with the second, so that
+    // a store of the wave meets every bank.
+    auto store = [&](char *buf, int seg) {
         auto put = [&](int key, int chunk, u32x4_t k, u32x4_t v) {
             *reinterpret_cast<u32x4_t *>(buf + key * X::ROW + ((chunk ^ tree_swz_k<D>(key)) << 4)) = k;
             *reinterpret_cast<u32x4_t *>(buf + X::TILE + key * X::ROW + ((chunk ^ tree_swz_v<D>(key)) << 4)) = v;
         };
-        static_for<0, X::NL8>([&](auto i) {
-            const int u = (int)i * 256 + tid, key = u / (D / 16), ch = 2 * (u % (D / 16));
-            const u32x4_t k = kr[i], v = vr[i];
-            put(key, ch, e4m3_to_bf16(make_uint2(k.x, k.y), ke[i]), e4m3_to_bf16(make_uint2(v.x, v.y), ve[i]));
-            put(key, ch + 1, e4m3_to_bf16(make_uint2(k.z, k.w), ke[i]), e4m3_to_bf16(make_uint2(v.z, v.w), ve[i]));
-        });
+        if (F8 && seg == 4) {
+            static_for<0, X::NL8>([&](auto i) {
+                const int u = (int)i * X::NT + ltid, key = u / (D / 16), ch = 2 * (u % (D / 16)), odd = (lane >> 3) & 1;
+                static_for<0, 2>([&](auto j) {
+                    const bool second = (int)j != odd;
+                    const u32x4_t k = kr[i], v = vr[i];
+                    put(key, ch + (second ? 1 : 0), e4m3_to_bf16(second ? make_uint2(k.z, k.w) : make_uint2(k.x, k.y), ke[i]),
+                        e4m3_to_bf16(second ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y), ve[i]));
+                });
+            });
+        } else if constexpr (X::OWN) {
+            static_for<0, X::NL>([&](auto i) {
+                const int u = (int)i * X::NT + ltid;
+                put(u / X::CPR, u % X::CPR, kr[i], vr[i]);
+            });
+        }
     };
     // In a tile that rows see differently the values are looked at: those of
-    // nodes that are not there become 0, and s_bad tells of infinities and NaN
-    // (they must not reach the rows that do not see them: 0 * inf).
-    auto look = [&](const TreeTileRef &x, int b, int t) {
-        char *v = lds + b * 2 * X::TILE + X::TILE;
+    // nodes that are not there become 0, and the answer tells of infinities and
+    // NaN (they must not reach the rows that do not see them: 0 * inf).
+    auto look = [&](const TreeTileRef &x, char *buf) {
         bool bad = false;
         static_for<0, X::NL>([&](auto i) {
-            const int u = (int)i * 256 + tid, key = u / X::CPR, node = x.key0 + key - step;
-            u32x4_t *p = reinterpret_cast<u32x4_t *>(v + u * 16);
-            if (x.seg == 4 && node >= 0 && (node >= 64 || !((alive >> node) & 1))) *p = u32x4_t{0, 0, 0, 0};
+            const int u = (int)i * X::NT + ltid, key = u / X::CPR, nd = x.key0 + key - step;
+            u32x4_t *p = reinterpret_cast<u32x4_t *>(buf + X::TILE + u * 16);
+            if (x.seg == 4 && nd >= 0 && (nd >= 64 || !((alive >> nd) & 1))) *p = u32x4_t{0, 0, 0, 0};
             else bad |= has_non_finite(*p);
         });
-        if (bad) s_bad[b] = t + 1;
+        return bad;
     };
 
+    const int t_first = X::OWN ? t0 + kw : t0;
+    constexpr int t_step = X::OWN ? 4 : 1;
     TreeTileRef cur = tile_of();
-    if (t0 < t1) {
+    if (t_first < t1) {
         load(0);
         advance();
     }
@@ -307,7 +352,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     static_for<0, ND>([&](auto db) { static_for<0, 16>([&](auto i) { o[db][(int)i] = 0.f; }); });
     float m = -INFINITY, l = 0.f;
     // keys of the ZERO donor score 0 and add nothing to o
-    if (a.zero_donor && spliced && split == 0 && kw == 0) {
+    if (a.zero_donor && spliced && chunk == 0 && kw == 0) {
         const int n_zero = a.span_hi - max(a.span_lo, max(low, 0));
         if (n_zero > 0) {
             m = 0.f;
@@ -317,32 +362,46 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
 
     // ---- addresses of the operands within a buffer
     int k_at[NST], v_at[ND];
-    static_for<0, NST>([&](auto st) { k_at[st] = (kw * 32 * KB + r) * X::ROW + (((2 * (int)st + h) ^ tree_swz_k<D>(r)) << 4); });
+    static_for<0, NST>([&](auto st) { k_at[st] = ((X::OWN ? 0 : kw * 32 * KB) + r) * X::ROW + (((2 * (int)st + h) ^ tree_swz_k<D>(r)) << 4); });
     {
-        const int vrow = kw * 32 * KB + 4 * h + ((lane & 15) >> 2);
+        const int vrow = (X::OWN ? 0 : kw * 32 * KB) + 4 * h + ((lane & 15) >> 2);
         static_for<0, ND>([&](auto db) {
             const int chunk = 4 * (int)db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
             v_at[db] = X::TILE + vrow * X::ROW + ((chunk ^ tree_swz_v<D>(vrow)) << 4) + 8 * (lane & 1);
         });
     }
 
-    wait_vmcnt<0>();   // this wave's part of the first tile
-    if (F8 && t0 < t1 && cur.seg == 4) convert(0);
-    for (int t = t0; t < t1; ++t) {
-        const int b = (t - t0) & 1;
-        __syncthreads();   // every wave's part of tile t is in LDS, and tile t - 1 has been read
+    if constexpr (!X::OWN) {
+        wait_vmcnt<0>();   // this wave's part of the first tile
+        if (t_first < t1) store(own, cur.seg);
+    }
+    for (int t = t_first; t < t1; t += t_step) {
+        const int b = X::OWN ? 0 : (t - t0) & 1;
+        char *const buf = own + b * 2 * X::TILE;
+        if constexpr (X::OWN) {
+            wave_fence();   // the wave has read the tile before
+            store(buf, cur.seg);
+            wave_fence();
+        } else {
+            __syncthreads();   // every wave's part of tile t is in LDS, and tile t - 1 has been read
+        }
         const TreeTileRef next = tile_of();
-        if (t + 1 < t1) {
+        if (t + t_step < t1) {
             load(b ^ 1);
             advance();
         }
         bool bad = false;
         if (cur.differ) {
-            look(cur, b, t);
-            __syncthreads();
-            bad = __builtin_amdgcn_readfirstlane(s_bad[b]) == t + 1;
+            bad = look(cur, buf);
+            if constexpr (X::OWN) {
+                bad = __any(bad);
+                wave_fence();
+            } else {
+                if (bad) s_bad[b] = t + 1;
+                __syncthreads();
+                bad = __builtin_amdgcn_readfirstlane(s_bad[b]) == t + 1;
+            }
         }
-        const char *buf = lds + b * 2 * X::TILE;
         f32x16_t s[KB];
         static_for<0, KB>([&](auto kb) {
             static_for<0, 16>([&](auto i) { s[kb][(int)i] = 0.f; });
@@ -352,7 +411,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             });
         });
         if (cur.mask) {
-            const int first = cur.key0 + kw * 32 * KB, n = cur.n - kw * 32 * KB;
+            const int skip = X::OWN ? 0 : kw * 32 * KB, first = cur.key0 + skip, n = cur.n - skip;
             uint64_t see;
             if (cur.seg == 4) {
                 see = bits(low - a.Tp - first, min(step - first, n)) | (shifted(word, step - first) & bits(step - first, n));
@@ -420,17 +479,19 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             });
         }
         cur = next;
-        wait_vmcnt<0>();
-        if (F8 && t + 1 < t1 && cur.seg == 4) convert(b ^ 1);
+        if constexpr (!X::OWN) {
+            wait_vmcnt<0>();
+            if (t + 1 < t1) store(own + (b ^ 1) * 2 * X::TILE, cur.seg);
+        }
     }
     __syncthreads();
 
     // ---- results
     l += __shfl_xor(l, 32);
     const int64_t out_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
-    const int64_t n_part = (int64_t)a.n_active * a.T * a.Hkv * a.G;   // rows of a split
-    const int64_t part_row = (int64_t)split * n_part + ((int64_t)ci * a.T + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
-    float *part_ml = a.part + (int64_t)a.n_split * n_part * D;
+    const int64_t n_part = (int64_t)a.n_slots * a.T * a.Hkv * a.G;   // rows of the partial results
+    const int64_t part_row = ((int64_t)slot * a.T + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
+    float *part_ml = a.part + n_part * D;
     if constexpr (KW > 1) {
         // the waves of a row through LDS (every wave is done with the tiles)
         float *s_o = reinterpret_cast<float *>(lds);   // [KW][32 RW][D], chunks of four swizzled by the row
@@ -462,8 +523,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
                 if (f != 0.f)
                     O += f * *reinterpret_cast<const f32x4_t *>(s_o + (((int)k * 32 * RW + w) * D + 4 * (d4 ^ (w & 15))));
             });
-            if (a.n_split > 1) {
-                const int64_t at = (int64_t)split * n_part + ((int64_t)ci * a.T + nd) * (a.Hkv * a.G) + hd;
+            if (a.split) {
+                const int64_t at = ((int64_t)slot * a.T + nd) * (a.Hkv * a.G) + hd;
                 *reinterpret_cast<f32x4_t *>(a.part + at * D + 4 * d4) = O;
                 if (d4 == 0) *reinterpret_cast<float2 *>(part_ml + 2 * at) = make_float2(M, Lsum);
             } else {
@@ -475,7 +536,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         }
     } else {
         if (!valid) return;
-        if (a.n_split > 1) {
+        if (a.split) {
             static_for<0, ND>([&](auto db) {
                 static_for<0, 4>([&](auto i) {
                     *reinterpret_cast<f32x4_t *>(a.part + part_row * D + 32 * (int)db + 8 * (int)i + 4 * h) =
@@ -497,33 +558,59 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     }
 }
 
-// Joins the splits of every row: a thread has four values of a row.
+// Joins the chunks of every row: a work group has 256 / (D / 4) q heads of one
+// node (blockIdx.x the active cell and node, blockIdx.y the heads), a thread
+// four values of a row.  The lanes of a row read its chunks' maxima and sums
+// together, then each chunk's values with several loads in flight.
 template <int D>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
+    constexpr int LPR = D / 4, ROWS = 256 / LPR;
+    __shared__ float s_w[ROWS][splice::kTreeMaxChunks];
     const TreeCall a = args.call;
-    const int Hq = a.Hkv * a.G;
-    const int64_t n_part = (int64_t)a.n_active * a.T * Hq;
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, row = e / (D / 4);
-    const int d4 = (int)(e % (D / 4));
-    if (row >= n_part) return;
-    const int hd = (int)(row % Hq), node = (int)(row / Hq % a.T), ci = (int)(row / Hq / a.T);
+    const int Hq = a.Hkv * a.G, ci = blockIdx.x / a.T, node = blockIdx.x % a.T;
     const int64_t at_node = (int64_t)args.cells.cell[ci] * a.T + node;
     if (a.depth[at_node] < 0) return;
-    const float *ml = a.part + (int64_t)a.n_split * n_part * D;
-    float M = -INFINITY, L = 0.f;
-    for (int s = 0; s < a.n_split; ++s) M = fmaxf(M, ml[2 * (s * n_part + row)]);
+    const int rw = threadIdx.x / LPR, l = threadIdx.x % LPR, hd = blockIdx.y * ROWS + rw;
+    const int first = (int)(args.slots.first_onset[ci] >> 8), n = (int)(args.slots.first_onset[ci + 1] >> 8) - first;
+    const bool on = hd < Hq;
+    const int64_t stride = (int64_t)a.T * Hq, row = (int64_t)first * stride + (int64_t)node * Hq + (on ? hd : 0);
+    const float *ml = a.part + (int64_t)a.n_slots * stride * D;
+    constexpr int PER = splice::kTreeMaxChunks / LPR;
+    float ms[PER], ls[PER], M = -INFINITY, L = 0.f;
+    static_for<0, PER>([&](auto i) {
+        const int s = l + (int)i * LPR;
+        ms[i] = -INFINITY;
+        ls[i] = 0.f;
+        if (s < n) {
+            const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * (row + s * stride));
+            ms[i] = x.x;
+            ls[i] = x.y;
+        }
+        M = fmaxf(M, ms[i]);
+    });
+    for (int o = 1; o < LPR; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
     const float Ms = M == -INFINITY ? 0.f : M;
+    static_for<0, PER>([&](auto i) {
+        const int s = l + (int)i * LPR;
+        const float f = fast_exp2(ms[i] - Ms);
+        if (s < n) s_w[rw][s] = f;
+        L = fmaf(f, ls[i], L);
+    });
+    for (int o = 1; o < LPR; o <<= 1) L += __shfl_xor(L, o);
+    __syncthreads();
+    if (!on) return;
+    const float *src = a.part + row * D + 4 * l;
     f32x4_t O = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.n_split; ++s) {
-        const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * (s * n_part + row));
-        const float f = fast_exp2(x.x - Ms);
-        L = fmaf(f, x.y, L);
-        if (f != 0.f) O += f * *reinterpret_cast<const f32x4_t *>(a.part + (s * n_part + row) * D + 4 * d4);
+#pragma unroll 8
+    for (int s = 0; s < n; ++s) {
+        const float f = s_w[rw][s];
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(src + s * stride * D);
+        O += f == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : f * x;   // a chunk of nothing may hold anything
     }
     const int64_t at = at_node * Hq + hd;
     const float f = L == 0.f ? 0.f : 1.f / L;
-    *reinterpret_cast<bf16x4_t *>(a.out + at * D + 4 * d4) = __builtin_convertvector(O * f, bf16x4_t);
-    if (d4 == 0) a.lse[at] = kLn2 * (M + log2f(L));
+    *reinterpret_cast<bf16x4_t *>(a.out + at * D + 4 * l) = __builtin_convertvector(O * f, bf16x4_t);
+    if (l == 0) a.lse[at] = kLn2 * (M + log2f(L));
 }
 
 // Enqueues a call of plan p; 0 if a launch failed.
@@ -545,7 +632,7 @@ bool launch_tree_kernel(const TreeArgs &args, hipStream_t stream) {
             raised.fetch_or(bit);
         }
     }
-    const unsigned blocks = (unsigned)((int64_t)args.call.Hkv * args.call.n_active * args.call.row_tiles * args.call.n_split);
+    const unsigned blocks = (unsigned)((int64_t)args.call.Hkv * args.call.n_slots * args.call.row_tiles);
     hipLaunchKernelGGL((tree_kernel<D, RW, F8>), dim3(blocks), dim3(256), X::LDS, stream, args);
     return hipGetLastError() == hipSuccess;
 }
@@ -563,9 +650,10 @@ bool launch_tree(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hi
         else ok = f8 ? launch_tree_kernel<D, 4, true>(a, stream) : launch_tree_kernel<D, 4, false>(a, stream);
     }
     const TreeCall &c = a.call;
-    if (!ok || c.n_split == 1) return ok;
-    const int64_t units = (int64_t)c.n_active * c.T * c.Hkv * c.G * (D / 4);
-    hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, stream, a);
+    if (!ok || !c.split) return ok;
+    const int heads = 256 / (D / 4);
+    hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)(c.n_active * c.T), (unsigned)((c.Hkv * c.G + heads - 1) / heads)),
+                       dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess;
 }
 

@@ -11,10 +11,13 @@
 
 namespace splice {
 
-// The cells that are not finished, in order: their index and step.
+// The cells that are not finished, in order: their steps and indexes.  Words
+// throughout, as kernels read these at a computed place: a byte array beside a
+// word array under one index has been compiled into a scalar load whose base
+// is no multiple of four, and the hardware drops those bits.
 struct TreeCells {
     int32_t step[SPLICE_MAX_CELLS];
-    uint8_t cell[SPLICE_MAX_CELLS];
+    uint32_t cell[SPLICE_MAX_CELLS];
 };
 
 inline int active_cells(const splice_shape &sh, const int32_t *cell_step, TreeCells &out) {
@@ -22,7 +25,7 @@ inline int active_cells(const splice_shape &sh, const int32_t *cell_step, TreeCe
     for (int c = 0; c < sh.n_cells; ++c)
         if (cell_step[c] >= 0) {
             out.step[n] = cell_step[c];
-            out.cell[n++] = (uint8_t)c;
+            out.cell[n++] = (uint32_t)c;
         }
     return n;
 }
@@ -66,44 +69,111 @@ void with_format(int D, int kv_format, F f) {
 constexpr int tree_row_waves(int D, int rows) { return rows <= 32 && D <= 128 ? 1 : (rows <= 64 ? 2 : 4); }
 // 32-key blocks a wave takes of a tile.
 constexpr int tree_key_blocks(int D, int row_waves) { return row_waves == 4 && D <= 128 ? 2 : 1; }
-constexpr int tree_tile_keys(int D, int row_waves) { return 32 * tree_key_blocks(D, row_waves) * (4 / row_waves); }
+// With one wave a row every wave has tiles of its own.
+constexpr int tree_tile_keys(int D, int row_waves) {
+    return row_waves == 1 ? 32 : 32 * tree_key_blocks(D, row_waves) * (4 / row_waves);
+}
+constexpr int tree_resident(int D) { return D <= 128 ? 2 : 1; }   // work groups a compute unit holds
 
-constexpr int kTreeMaxSplits = 64;
-constexpr int kTreeItemsTarget = 1024;   // work groups a split aims for
-constexpr int kTreeMinTiles = 2;         // tiles of keys a split takes at least
+// A cell's list of keys is cut into chunks of `per` tiles, one work group
+// each (per KV head and row tile); a slot is one chunk of one cell.
+constexpr int kTreeMaxSlots = 640;
+constexpr int kTreeRounds = 6;    // rounds of resident work groups a plan may take to balance its chunks
+constexpr int kTreeStart = 4;     // what a work group costs beside its tiles, in tiles
+constexpr int kTreeMaxChunks = 64;
 
 struct TreePlan {
-    int row_waves, row_tiles, n_split;
-    size_t bytes;   // partial results: [split][active cell][node][q head] of D + 2 floats
+    int row_waves, row_tiles, per, n_slots;
+    bool split;     // some cell has more than one chunk
+    size_t bytes;   // partial results: [slot][node][q head] of D + 2 floats
 };
 
-// keys: the most any cell of the call sees.
-inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, int n_active, int64_t keys) {
+// Where the active cells' chunks are, and at which depth their nodes begin to
+// be spliced (64: none): first slot << 8 | onset, and one more first slot; and
+// the active cell of every slot, four a word.
+struct TreeSlots {
+    uint32_t first_onset[SPLICE_MAX_CELLS + 1];
+    uint32_t cell[kTreeMaxSlots / 4];
+};
+
+inline size_t tree_slot_bytes(const splice_shape &sh, int T) { return (size_t)T * sh.n_q_heads * (sh.head_dim + 2) * 4; }
+
+// The most tiles that a cell at `step` walks: prompt slots (a replaced span
+// twice when nodes on both sides of the onset may share a row tile) and
+// generated rows; every segment may end in a tile of its own.
+inline int tree_tiles(const splice_shape &sh, const splice_call &call, int T, int tile, int64_t step, bool spliced, bool mixed) {
+    int64_t low = call.window > 0 ? sh.prompt_len + step - call.window + 1 : 0;   // the first position that the root sees
+    if (low < 0) low = 0;
+    const int64_t Tp = sh.prompt_len, b0 = low < Tp ? low : Tp, g0 = low > Tp ? (low - Tp < step ? low - Tp : step) : 0;
+    const int64_t sa = sh.span_lo > b0 ? sh.span_lo : b0, sb = sh.span_hi > sa ? sh.span_hi : sa;
+    int64_t n = ceil_div(step + T - g0, tile);
+    if (!spliced) return (int)(n + ceil_div(Tp - b0, tile));
+    n += ceil_div(sa - b0, tile) + ceil_div(Tp - sb, tile);
+    const int span = ceil_div(sb - sa, tile);
+    return (int)(n + (mixed ? span : 0) + (sh.donor_kind == SPLICE_DONOR_ZERO ? 0 : span));
+}
+
+inline int64_t tree_chunks(const int *tiles, int n, int per) {
+    int64_t slots = 0;
+    for (int i = 0; i < n; ++i) slots += ceil_div(tiles[i], per);
+    return slots;
+}
+
+// Chunks of equal length, so that the work groups of all cells fill k rounds
+// of what the GPU holds at once; k is the one that takes least by
+// k * (per + kTreeStart).
+inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, int n_cu) {
     TreePlan p;
     const int rows = T * group_of(sh);
     p.row_waves = tree_row_waves(sh.head_dim, rows);
     p.row_tiles = ceil_div(rows, 32 * p.row_waves);
-    const int64_t items = (int64_t)n_active * sh.n_kv_heads * p.row_tiles;
-    const int tile = tree_tile_keys(sh.head_dim, p.row_waves);
-    int64_t n = call.split_keys > 0 ? ceil_div(keys, call.split_keys) : ceil_div(kTreeItemsTarget, items);
-    const int64_t most = ceil_div(keys, (call.split_keys > 0 ? 1 : kTreeMinTiles) * tile);
-    n = n < most ? n : most;
-    n = n < kTreeMaxSplits ? n : kTreeMaxSplits;
-    p.n_split = n > 1 ? (int)n : 1;
-    p.bytes = p.n_split > 1 ? (size_t)p.n_split * n_active * T * sh.n_q_heads * (sh.head_dim + 2) * 4 : 0;
+    const int tile = tree_tile_keys(sh.head_dim, p.row_waves), step = p.row_waves == 1 ? 4 : 1;   // four waves, four tiles
+    const int64_t items = (int64_t)sh.n_kv_heads * p.row_tiles, room = (int64_t)n_cu * tree_resident(sh.head_dim);
+    int64_t sum = 0;
+    int most = 1;
+    for (int i = 0; i < n; ++i) {
+        sum += tiles[i];
+        most = tiles[i] > most ? tiles[i] : most;
+    }
+    const int least = step * ceil_div(most, (int64_t)step * kTreeMaxChunks);   // no cell in more than kTreeMaxChunks
+    auto fits = [&](int per, int64_t limit) { return tree_chunks(tiles, n, per) <= limit; };
+    if (call.split_keys > 0) {
+        p.per = step * ceil_div(call.split_keys, tile * step);
+        if (p.per < least) p.per = least;
+        while (!fits(p.per, kTreeMaxSlots)) p.per *= 2;
+    } else {
+        p.per = most;
+        int64_t best = INT64_MAX;
+        for (int k = 1; k <= kTreeRounds; ++k) {
+            int64_t limit = k * room / items;
+            limit = limit < kTreeMaxSlots ? limit : kTreeMaxSlots;
+            if (limit < n) continue;   // not even whole lists fit
+            int per = step * ceil_div(sum, limit * step);
+            if (per < least) per = least;
+            while (per < most && !fits(per, limit)) per += step * (1 + per / (16 * step));
+            const int64_t cost = k * ((int64_t)per / step + kTreeStart);
+            if (cost < best) {
+                best = cost;
+                p.per = per;
+            }
+        }
+    }
+    p.n_slots = (int)tree_chunks(tiles, n, p.per);
+    p.split = p.n_slots > n;
+    p.bytes = p.split ? p.n_slots * tree_slot_bytes(sh, T) : 0;
     return p;
 }
 
-// Keys a cell at `step` may see: prompt slots (both of a replaced span's if
-// nodes on either side of the onset share a tile) and generated rows.
-inline int64_t tree_keys(const splice_shape &sh, const splice_call &call, int T, int64_t step) {
-    int64_t prompt = sh.prompt_len, gen = step;
-    if (call.window > 0) {
-        const int64_t low = sh.prompt_len + step - call.window + 1;   // of the root
-        if (low > 0) prompt -= low < prompt ? low : prompt;
-        if (low > sh.prompt_len) gen -= low - sh.prompt_len < gen ? low - sh.prompt_len : gen;
-    }
-    return prompt + gen + T;
+// Bytes that no plan of this shape passes, whatever the steps.
+inline size_t tree_most_bytes(const splice_shape &sh, const splice_call &call, int T, int n_cu) {
+    const int rows = T * group_of(sh), rw = tree_row_waves(sh.head_dim, rows);
+    const int64_t items = (int64_t)sh.n_kv_heads * ceil_div(rows, 32 * rw);
+    int64_t slots = kTreeMaxSlots;
+    if (call.split_keys == 0 && (int64_t)kTreeRounds * n_cu * tree_resident(sh.head_dim) / items < slots)
+        slots = (int64_t)kTreeRounds * n_cu * tree_resident(sh.head_dim) / items;
+    const int64_t chunks = (int64_t)sh.n_cells * kTreeMaxChunks;
+    slots = slots < chunks ? slots : chunks;
+    return slots * tree_slot_bytes(sh, T);
 }
 
 }  // namespace splice
