@@ -54,6 +54,10 @@ struct TreeArgs {
 // of it; 1 the span, clean; 2 the span from the donor; 3 the prompt behind it; 4
 // the generated rows with the tree's behind them), the rows left of it, the next tile's rows and
 // first key (a prompt position, or in segment 4 a generated row).
+struct TreeSegment {
+    const char *k, *v;
+    int key0, len;
+};
 struct TreeWalk {
     const char *k, *v;
     int seg, rem, key0;
@@ -72,13 +76,15 @@ struct TreeTile {
     static constexpr int ROW = 2 * D;                          // bytes of a staged row
     static constexpr int CPR = D / 8;                          // 16-byte chunks of a row
     static constexpr int TILE = TK * ROW;                      // bytes of a K (or V) tile
-    static constexpr int LDS = (OWN ? 8 : 4) * TILE;           // K and V: a tile a wave, or two for all
+    static constexpr int TILES = (OWN ? 8 : 4) * TILE;         // K and V: a tile a wave, or two for all
+    static constexpr int LDS = TILES + (OWN ? 32 * ROW : 0);   // ... and Q, for which a wave with a tile in
+                                                               // registers has none left
     static constexpr int NT = OWN ? 64 : 256;                  // threads that load a tile
     static constexpr int NL = TK * CPR / NT;                   // chunks a thread loads of a K (or V) tile
     static constexpr int NL8 = NL / 2;                         // ... of 8-bit rows
     static constexpr int NR = OWN ? NL : NL8;                  // ... by way of registers
     static constexpr int ND = D / 32;                          // 32-wide d blocks of the output
-    static_assert(RW * KW == 4 && NL8 >= 1 && (KW == 1 || KW * 32 * RW * D * 4 <= LDS), "");
+    static_assert(RW * KW == 4 && NL8 >= 1 && (KW == 1 || KW * 32 * RW * D * 4 <= TILES), "");
 };
 
 // Chunk-slot swizzles (XOR on the 16-byte chunk index) of key r: the 16 rows
@@ -99,6 +105,15 @@ __device__ __forceinline__ uint64_t bits(int b, int e) {
 __device__ __forceinline__ uint64_t shifted(uint64_t x, int by) {   // left, or right when by < 0
     if (by >= 64 || by <= -64) return 0;
     return by >= 0 ? x << by : x >> -by;
+}
+
+// A pointer that is the same in every lane, in scalar registers (a buffer
+// descriptor from vector registers costs a loop a load).
+__device__ __forceinline__ const char *uniform(const char *p) {
+    const uint64_t x = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32));
+    return reinterpret_cast<const char *>(((uint64_t)hi << 32) | lo);
 }
 
 // Lanes of a wave that hand each other values through LDS: its operations run
@@ -143,6 +158,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     constexpr int KW = X::KW, KB = X::KB, TK = X::TK, ND = X::ND, NST = D / 16;
     extern __shared__ __align__(16) char lds[];
     __shared__ int s_bad[2];
+    __shared__ TreeSegment s_seg[5];
     __shared__ float s_ml[KW > 1 ? KW : 1][32 * RW][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, h = lane >> 5, rw = wave % RW, kw = wave / RW;
@@ -188,33 +204,38 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     const int g0 = min(max(low_all - a.Tp, 0), step);
     const size_t head_p = (size_t)g * a.Tp * X::ROW;
     const int64_t pair = (int64_t)c * a.Hkv + g;
-    auto seg_begin = [&](int i) { return i == 0 ? b0 : (i == 3 ? sb : (i == 4 ? g0 : sa)); };
-    auto seg_len = [&](int i) {
-        if (i == 4) return step + a.T - g0;
-        if (!any_donor) return i == 0 ? a.Tp - b0 : 0;
-        if (i == 0) return sa - b0;
-        if (i == 3) return a.Tp - sb;
-        return (i == 1 ? any_clean : !a.zero_donor) ? sb - sa : 0;
-    };
-    auto seg_tiles = [&](int i) { return (seg_len(i) + TK - 1) / TK; };
-    const int n_tiles = seg_tiles(0) + seg_tiles(1) + seg_tiles(2) + seg_tiles(3) + seg_tiles(4);
-    const int t0 = min(chunk * a.per, n_tiles), t1 = last_chunk ? n_tiles : min(t0 + a.per, n_tiles);
-    TreeWalk w;
-    auto enter = [&](int i, int first) {   // segment i from its row `first` on
-        const int row_bytes = F8 && i == 4 ? D : X::ROW;
+    if (tid < 5) {
+        const int i = tid, row_bytes = F8 && i == 4 ? D : X::ROW;
+        int begin = i == 0 ? b0 : (i == 3 ? sb : (i == 4 ? g0 : sa)), end = begin;
+        if (i == 4) end = step + a.T;
+        else if (i == 0) end = any_donor ? sa : a.Tp;
+        else if (any_donor) end = i == 3 ? a.Tp : ((i == 1 ? any_clean : !a.zero_donor) ? sb : begin);
         const char *k = i == 4 ? a.gk + pair * a.cap * row_bytes : pick_base(i == 2, a.ck, a.dk) + head_p;
         const char *v = i == 4 ? a.gv + pair * a.cap * row_bytes : pick_base(i == 2, a.cv, a.dv) + head_p;
-        w.seg = i;
-        w.key0 = seg_begin(i) + first;
-        w.rem = seg_len(i) - first;
-        w.k = k + (size_t)w.key0 * row_bytes;
-        w.v = v + (size_t)w.key0 * row_bytes;
-    };
-    {
-        int i = 0, t = X::OWN ? t0 + kw : t0;
-        while (i < 4 && t >= seg_tiles(i)) t -= seg_tiles(i++);
-        enter(i, t * TK);
+        s_seg[i] = TreeSegment{k + (size_t)begin * row_bytes, v + (size_t)begin * row_bytes, begin, end - begin};
     }
+    if (tid < 2) s_bad[tid] = 0;
+    __syncthreads();
+    int n_tiles = 0;
+    static_for<0, 5>([&](auto i) { n_tiles += (s_seg[i].len + TK - 1) / TK; });
+    n_tiles = __builtin_amdgcn_readfirstlane(n_tiles);
+    const int t0 = min(chunk * a.per, n_tiles), t1 = last_chunk ? n_tiles : min(t0 + a.per, n_tiles);
+    TreeWalk w;
+    // `skip` tiles on from the end of segment i - 1, over the segments that are shorter
+    auto enter = [&](int i, int skip) {
+        TreeSegment x = s_seg[i];
+        while (i < 4 && skip * TK >= x.len) {
+            skip -= (x.len + TK - 1) / TK;
+            x = s_seg[++i];
+        }
+        const int row_bytes = F8 && i == 4 ? D : X::ROW;
+        w.seg = __builtin_amdgcn_readfirstlane(i);
+        w.k = uniform(x.k + (size_t)skip * TK * row_bytes);
+        w.v = uniform(x.v + (size_t)skip * TK * row_bytes);
+        w.key0 = __builtin_amdgcn_readfirstlane(x.key0 + skip * TK);
+        w.rem = __builtin_amdgcn_readfirstlane(x.len - skip * TK);
+    };
+    enter(0, X::OWN ? t0 + kw : t0);
     // The tile under way: how many keys, which, and what has to be looked at.
     auto tile_of = [&]() {
         TreeTileRef x;
@@ -235,10 +256,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         w.v += N * TK * row_bytes;
         w.key0 += N * TK;
         w.rem -= N * TK;
-        while (w.rem <= 0 && w.seg < 4) {   // -rem / TK tiles into the next segment
-            const int first = w.rem <= 0 ? -w.rem / TK * TK : 0;
-            enter(w.seg + 1, first);
-        }
+        if (w.rem <= 0 && w.seg < 4) enter(w.seg + 1, -w.rem / TK);
     };
 
     // ---- tiles into LDS.  A tile for all waves: bf16 rows go there straight
@@ -247,7 +265,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     // become bf16.  Tiles of a wave's own: the next one waits in registers, so
     // that one buffer a wave is enough, two work groups fit a compute unit and
     // no wave waits for another.
-    const int ltid = X::OWN ? lane : tid;
+    int ltid = X::OWN ? lane : tid;
     char *const own = lds + (X::OWN ? wave * 2 * X::TILE : 0);
     const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_offset(lds));
     int k_src[X::NL], v_src[X::NL];
@@ -263,9 +281,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     auto load = [&](int b) {   // the walk's tile
         const int n = min(TK, w.rem);
         if (F8 && w.seg == 4) {
+            const int64_t ex = pair * a.cap + w.key0;
             const __amdgpu_buffer_rsrc_t rk = rows_rsrc(w.k, n * D), rv = rows_rsrc(w.v, n * D);
-            const __amdgpu_buffer_rsrc_t re = rows_rsrc(reinterpret_cast<const char *>(a.gke + pair * a.cap + w.key0), n);
-            const __amdgpu_buffer_rsrc_t rf = rows_rsrc(reinterpret_cast<const char *>(a.gve + pair * a.cap + w.key0), n);
+            const __amdgpu_buffer_rsrc_t re = rows_rsrc(uniform(reinterpret_cast<const char *>(a.gke + ex)), n);
+            const __amdgpu_buffer_rsrc_t rf = rows_rsrc(uniform(reinterpret_cast<const char *>(a.gve + ex)), n);
             static_for<0, X::NL8>([&](auto i) {
                 const int u = (int)i * X::NT + ltid;
                 kr[i] = row_load<0>(rk, u * 16);
@@ -335,17 +354,26 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         load(0);
         advance();
     }
-    if (tid < 2) s_bad[tid] = 0;
 
     // ---- Q^T, in the lanes of the B operand: row r, d = 16 st + 8 h ..
-    bf16x8_t qb[NST];
+    bf16x8_t qb[X::OWN ? 1 : NST];
+    char *const s_q = lds + X::TILES;   // chunk slots as those of K
     {
         const int64_t q_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
-        static_for<0, NST>([&](auto st) {
-            u32x4_t x = {0, 0, 0, 0};
-            if (valid) x = *reinterpret_cast<const u32x4_t *>(a.q + (q_row * D + 16 * (int)st + 8 * h) * 2);
-            qb[st] = __builtin_bit_cast(bf16x8_t, x);
-        });
+        if constexpr (X::OWN) {
+            for (int ch = 2 * kw + h; ch < X::CPR; ch += 8) {
+                u32x4_t x = {0, 0, 0, 0};
+                if (valid) x = *reinterpret_cast<const u32x4_t *>(a.q + (q_row * D + 8 * ch) * 2);
+                *reinterpret_cast<u32x4_t *>(s_q + r * X::ROW + ((ch ^ tree_swz_k<D>(r)) << 4)) = x;
+            }
+            __syncthreads();
+        } else {
+            static_for<0, NST>([&](auto st) {
+                u32x4_t x = {0, 0, 0, 0};
+                if (valid) x = *reinterpret_cast<const u32x4_t *>(a.q + (q_row * D + 16 * (int)st + 8 * h) * 2);
+                qb[st] = __builtin_bit_cast(bf16x8_t, x);
+            });
+        }
     }
     // state of a row: o[db][i] is d = 32 db + 8 (i / 4) + 4 h + i % 4; a half's share of the sum
     f32x16_t o[ND];
@@ -360,15 +388,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         }
     }
 
-    // ---- addresses of the operands within a buffer
-    int k_at[NST], v_at[ND];
-    static_for<0, NST>([&](auto st) { k_at[st] = ((X::OWN ? 0 : kw * 32 * KB) + r) * X::ROW + (((2 * (int)st + h) ^ tree_swz_k<D>(r)) << 4); });
+    // ---- addresses of the operands within a buffer: K at k_at ^ 32 st, V at v_at ^ 64 db
+    int k_at = ((X::OWN ? 0 : kw * 32 * KB) + r) * X::ROW + ((h ^ tree_swz_k<D>(r)) << 4), v_at;
     {
         const int vrow = (X::OWN ? 0 : kw * 32 * KB) + 4 * h + ((lane & 15) >> 2);
-        static_for<0, ND>([&](auto db) {
-            const int chunk = 4 * (int)db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            v_at[db] = X::TILE + vrow * X::ROW + ((chunk ^ tree_swz_v<D>(vrow)) << 4) + 8 * (lane & 1);
-        });
+        const int chunk_of = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        v_at = X::TILE + vrow * X::ROW + ((chunk_of ^ tree_swz_v<D>(vrow)) << 4) + 8 * (lane & 1);
     }
 
     if constexpr (!X::OWN) {
@@ -378,6 +403,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     for (int t = t_first; t < t1; t += t_step) {
         const int b = X::OWN ? 0 : (t - t0) & 1;
         char *const buf = own + b * 2 * X::TILE;
+        // addresses are worked out anew for every tile: kept, they would take the registers of the tile in flight
+        asm volatile("" : "+v"(ltid), "+v"(k_at), "+v"(v_at));
         if constexpr (X::OWN) {
             wave_fence();   // the wave has read the tile before
             store(buf, cur.seg);
@@ -406,8 +433,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         static_for<0, KB>([&](auto kb) {
             static_for<0, 16>([&](auto i) { s[kb][(int)i] = 0.f; });
             static_for<0, NST>([&](auto st) {
-                const bf16x8_t ka = *reinterpret_cast<const bf16x8_t *>(buf + k_at[st] + (int)kb * 32 * X::ROW);
-                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[st], s[kb], 0, 0, 0);
+                const bf16x8_t ka = *reinterpret_cast<const bf16x8_t *>(buf + (k_at ^ 32 * (int)st) + (int)kb * 32 * X::ROW);
+                bf16x8_t q;
+                if constexpr (X::OWN) q = *reinterpret_cast<const bf16x8_t *>(s_q + (k_at ^ 32 * (int)st));
+                else q = qb[st];
+                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, q, s[kb], 0, 0, 0);
             });
         });
         if (cur.mask) {
@@ -448,7 +478,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             });
         });
         auto values = [&](int db, int kk) {   // 32 d of 16 keys, in the lanes of the A operand
-            const char *at = buf + v_at[db] + 16 * kk * X::ROW;
+            const char *at = buf + (v_at ^ 64 * db) + 16 * kk * X::ROW;
             const u32x2_t lo = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)at));
             const u32x2_t hi = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(at + 8 * X::ROW)));
             return u32x4_t{lo.x, lo.y, hi.x, hi.y};
