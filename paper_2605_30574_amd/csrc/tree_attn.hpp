@@ -133,22 +133,30 @@ __device__ __forceinline__ bool has_non_finite(u32x4_t w) {
     return bad;
 }
 
-// The words with every infinity and NaN replaced by 0, and 1.0 where a value
-// is +inf or NaN (above) or -inf or NaN (under).
-__device__ __forceinline__ void split_non_finite(u32x4_t &w, u32x4_t &above, u32x4_t &under) {
+// 1.0 where a value is +inf or NaN (above) or -inf or NaN (under), else 0.
+__device__ __forceinline__ void find_non_finite(u32x4_t w, u32x4_t &above, u32x4_t &under) {
     static_for<0, 4>([&](auto i) {
-        uint32_t fin = 0, up = 0, down = 0;
+        uint32_t up = 0, down = 0;
         static_for<0, 2>([&](auto h) {
             const uint32_t x = (w[(int)i] >> (16 * h)) & 0xffffu;
             const bool bad = (x & 0x7f80u) == 0x7f80u, nan = bad && (x & 0x7fu);
-            fin |= (bad ? 0u : x) << (16 * h);
             up |= (bad && (nan || !(x >> 15)) ? 0x3f80u : 0u) << (16 * h);
             down |= (bad && (nan || (x >> 15)) ? 0x3f80u : 0u) << (16 * h);
         });
-        w[(int)i] = fin;
         above[(int)i] = up;
         under[(int)i] = down;
     });
+}
+
+// The words with 0 for every infinity and NaN.
+__device__ __forceinline__ u32x4_t finite_only(u32x4_t w) {
+    static_for<0, 4>([&](auto i) {
+        uint32_t x = w[(int)i];
+        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+        w[(int)i] = x;
+    });
+    return w;
 }
 
 template <int D, int RW, bool F8>
@@ -157,7 +165,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     using X = TreeTile<D, RW>;
     constexpr int KW = X::KW, KB = X::KB, TK = X::TK, ND = X::ND, NST = D / 16;
     extern __shared__ __align__(16) char lds[];
-    __shared__ int s_bad[2];
+    __shared__ int s_bad;
     __shared__ TreeSegment s_seg[5];
     __shared__ float s_ml[KW > 1 ? KW : 1][32 * RW][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -214,7 +222,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         const char *v = i == 4 ? a.gv + pair * a.cap * row_bytes : pick_base(i == 2, a.cv, a.dv) + head_p;
         s_seg[i] = TreeSegment{k + (size_t)begin * row_bytes, v + (size_t)begin * row_bytes, begin, end - begin};
     }
-    if (tid < 2) s_bad[tid] = 0;
+    if (tid == 0) s_bad = 0;
     __syncthreads();
     int n_tiles = 0;
     static_for<0, 5>([&](auto i) { n_tiles += (s_seg[i].len + TK - 1) / TK; });
@@ -308,6 +316,14 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             });
         }
     };
+    // ---- addresses of the operands within a buffer: K at k_at ^ 32 st, V at v_at ^ 64 db
+    int k_at = ((X::OWN ? 0 : kw * 32 * KB) + r) * X::ROW + ((h ^ tree_swz_k<D>(r)) << 4), v_at;
+    {
+        const int vrow = (X::OWN ? 0 : kw * 32 * KB) + 4 * h + ((lane & 15) >> 2);
+        const int chunk_of = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        v_at = X::TILE + vrow * X::ROW + ((chunk_of ^ tree_swz_v<D>(vrow)) << 4) + 8 * (lane & 1);
+    }
+
     // What load() left in registers, into the tile.  8-bit rows: a lane has two
     // neighbouring chunks, and every other lane begins with the second, so that
     // a store of the wave meets every bank.
@@ -334,17 +350,39 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         }
     };
     // In a tile that rows see differently the values are looked at: those of
-    // nodes that are not there become 0, and the answer tells of infinities and
-    // NaN (they must not reach the rows that do not see them: 0 * inf).
+    // nodes that are not there become 0, and so do infinities and NaN, which
+    // must not reach the rows that do not see them (0 * inf); s_bad tells
+    // that there were some, and the rows that do see them are settled behind
+    // the loop.
     auto look = [&](const TreeTileRef &x, char *buf) {
-        bool bad = false;
         static_for<0, X::NL>([&](auto i) {
             const int u = (int)i * X::NT + ltid, key = u / X::CPR, nd = x.key0 + key - step;
             u32x4_t *p = reinterpret_cast<u32x4_t *>(buf + X::TILE + u * 16);
-            if (x.seg == 4 && nd >= 0 && (nd >= 64 || !((alive >> nd) & 1))) *p = u32x4_t{0, 0, 0, 0};
-            else bad |= has_non_finite(*p);
+            const u32x4_t v = *p;
+            if (x.seg == 4 && nd >= 0 && (nd >= 64 || !((alive >> nd) & 1))) {
+                *p = u32x4_t{0, 0, 0, 0};
+            } else if (has_non_finite(v)) {
+                *p = finite_only(v);
+                s_bad = 1;
+            }
         });
-        return bad;
+    };
+    // Bit k: the lane's row sees key k of the tile, from the wave's first key on.
+    auto seen = [&](const TreeTileRef &x) {
+        const int skip = X::OWN ? 0 : kw * 32 * KB, first = x.key0 + skip, n = x.n - skip;
+        if (x.seg == 4)
+            return bits(low - a.Tp - first, min(step - first, n)) | (shifted(word, step - first) & bits(step - first, n));
+        const bool other = any_clean && any_donor && (x.seg == 1 || x.seg == 2) && (x.seg == 2) != spliced;
+        return other ? 0 : bits(low - first, n);
+    };
+    auto values = [&](const char *buf, int db, int kk) {   // 32 d of 16 keys, in the lanes of the A operand
+        const char *at = buf + (v_at ^ 64 * db) + 16 * kk * X::ROW;
+        const u32x2_t lo = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)at));
+        const u32x2_t hi = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(at + 8 * X::ROW)));
+        return u32x4_t{lo.x, lo.y, hi.x, hi.y};
+    };
+    auto product = [&](u32x4_t x, bf16x8_t p, f32x16_t acc) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), p, acc, 0, 0, 0);
     };
 
     const int t_first = X::OWN ? t0 + kw : t0;
@@ -388,14 +426,6 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         }
     }
 
-    // ---- addresses of the operands within a buffer: K at k_at ^ 32 st, V at v_at ^ 64 db
-    int k_at = ((X::OWN ? 0 : kw * 32 * KB) + r) * X::ROW + ((h ^ tree_swz_k<D>(r)) << 4), v_at;
-    {
-        const int vrow = (X::OWN ? 0 : kw * 32 * KB) + 4 * h + ((lane & 15) >> 2);
-        const int chunk_of = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        v_at = X::TILE + vrow * X::ROW + ((chunk_of ^ tree_swz_v<D>(vrow)) << 4) + 8 * (lane & 1);
-    }
-
     if constexpr (!X::OWN) {
         wait_vmcnt<0>();   // this wave's part of the first tile
         if (t_first < t1) store(own, cur.seg);
@@ -417,38 +447,27 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             load(b ^ 1);
             advance();
         }
-        bool bad = false;
         if (cur.differ) {
-            bad = look(cur, buf);
-            if constexpr (X::OWN) {
-                bad = __any(bad);
-                wave_fence();
-            } else {
-                if (bad) s_bad[b] = t + 1;
-                __syncthreads();
-                bad = __builtin_amdgcn_readfirstlane(s_bad[b]) == t + 1;
-            }
+            look(cur, buf);
+            if constexpr (X::OWN) wave_fence();
+            else __syncthreads();
         }
         f32x16_t s[KB];
         static_for<0, KB>([&](auto kb) {
+            u32x4_t ka[NST];
+            static_for<0, NST>([&](auto st) {
+                ka[st] = *reinterpret_cast<const u32x4_t *>(buf + (k_at ^ 32 * (int)st) + (int)kb * 32 * X::ROW);
+            });
             static_for<0, 16>([&](auto i) { s[kb][(int)i] = 0.f; });
             static_for<0, NST>([&](auto st) {
-                const bf16x8_t ka = *reinterpret_cast<const bf16x8_t *>(buf + (k_at ^ 32 * (int)st) + (int)kb * 32 * X::ROW);
                 bf16x8_t q;
                 if constexpr (X::OWN) q = *reinterpret_cast<const bf16x8_t *>(s_q + (k_at ^ 32 * (int)st));
                 else q = qb[st];
-                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, q, s[kb], 0, 0, 0);
+                s[kb] = product(ka[st], q, s[kb]);
             });
         });
         if (cur.mask) {
-            const int skip = X::OWN ? 0 : kw * 32 * KB, first = cur.key0 + skip, n = cur.n - skip;
-            uint64_t see;
-            if (cur.seg == 4) {
-                see = bits(low - a.Tp - first, min(step - first, n)) | (shifted(word, step - first) & bits(step - first, n));
-            } else {
-                see = !cur.differ || !any_clean || cur.seg == 0 || cur.seg == 3 || (cur.seg == 2) == spliced ? bits(low - first, n) : 0;
-            }
-            see >>= 4 * h;
+            const uint64_t see = seen(cur) >> 4 * h;
             static_for<0, KB>([&](auto kb) {
                 static_for<0, 16>([&](auto i) {
                     constexpr int key = 32 * kb + 8 * (i >> 2) + (i & 3);
@@ -477,37 +496,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
                 pb[2 * kb + i / 8][i % 8] = (__bf16)p;
             });
         });
-        auto values = [&](int db, int kk) {   // 32 d of 16 keys, in the lanes of the A operand
-            const char *at = buf + (v_at ^ 64 * db) + 16 * kk * X::ROW;
-            const u32x2_t lo = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)at));
-            const u32x2_t hi = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(at + 8 * X::ROW)));
-            return u32x4_t{lo.x, lo.y, hi.x, hi.y};
-        };
-        auto product = [&](u32x4_t v, bf16x8_t p, f32x16_t acc) {
-            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), p, acc, 0, 0, 0);
-        };
-        if (!bad) {
-            static_for<0, ND>([&](auto db) {
-                static_for<0, 2 * KB>([&](auto kk) { o[db] = product(values(db, kk), pb[kk], o[db]); });
-            });
-        } else {
-            // infinities and NaN apart: the weights that fall on them say which rows they reach
-            static_for<0, ND>([&](auto db) {
-                f32x16_t up, down;
-                static_for<0, 16>([&](auto i) { up[(int)i] = down[(int)i] = 0.f; });
-                static_for<0, 2 * KB>([&](auto kk) {
-                    u32x4_t v = values(db, kk), above, under;
-                    split_non_finite(v, above, under);
-                    o[db] = product(v, pb[kk], o[db]);
-                    up = product(above, pb[kk], up);
-                    down = product(under, pb[kk], down);
-                });
-                static_for<0, 16>([&](auto i) {
-                    if (up[(int)i] > 0.f) o[db][(int)i] += INFINITY;
-                    if (down[(int)i] > 0.f) o[db][(int)i] -= INFINITY;
-                });
-            });
-        }
+        static_for<0, ND>([&](auto db) {
+            static_for<0, 2 * KB>([&](auto kk) { o[db] = product(values(buf, db, kk), pb[kk], o[db]); });
+        });
         cur = next;
         if constexpr (!X::OWN) {
             wait_vmcnt<0>();
@@ -515,6 +506,45 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         }
     }
     __syncthreads();
+    if (s_bad) {
+        // infinities and NaN among the values of tiles that rows see differently:
+        // the tiles once more, and which of them each row sees
+        enter(0, t_first);
+        for (int t = t_first; t < t1; t += t_step) {
+            const TreeTileRef x = tile_of();
+            if (x.differ) {
+                if constexpr (!X::OWN) __syncthreads();
+                load(0);
+                wait_vmcnt<0>();
+                if constexpr (X::OWN) wave_fence();
+                store(own, x.seg);
+                if constexpr (X::OWN) wave_fence();
+                else __syncthreads();
+                const uint64_t see = seen(x) >> 4 * h;
+                bf16x8_t on[2 * KB];
+                static_for<0, 32 * KB / 2>([&](auto i) {
+                    constexpr int key = 32 * (i / 16) + 8 * ((i % 16) >> 2) + (i & 3);
+                    on[i / 8][i % 8] = (__bf16)((see >> key) & 1 ? 1.f : 0.f);
+                });
+                static_for<0, ND>([&](auto db) {
+                    f32x16_t up, down;
+                    static_for<0, 16>([&](auto i) { up[(int)i] = down[(int)i] = 0.f; });
+                    static_for<0, 2 * KB>([&](auto kk) {
+                        u32x4_t above, under;
+                        find_non_finite(values(own, db, kk), above, under);
+                        up = product(above, on[kk], up);
+                        down = product(under, on[kk], down);
+                    });
+                    static_for<0, 16>([&](auto i) {
+                        if (up[(int)i] > 0.f) o[db][(int)i] += INFINITY;
+                        if (down[(int)i] > 0.f) o[db][(int)i] -= INFINITY;
+                    });
+                });
+            }
+            advance();
+        }
+        __syncthreads();
+    }
 
     // ---- results
     l += __shfl_xor(l, 32);
