@@ -70,28 +70,24 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
 
     const int T = tree->n_nodes;
     TreeArgs args;
-    const int n = splice::active_cells(sh, cell_step, args.cells);
+    splice::TreeCells cells;
+    const int n = splice::active_cells(sh, cell_step, cells);
     if (n == 0) return SPLICE_OK;
     int tiles[SPLICE_MAX_CELLS];
+    uint8_t onset[SPLICE_MAX_CELLS];
     const int tile = splice::tree_tile_keys(sh.head_dim, splice::tree_row_waves(sh.head_dim, T * splice::group_of(sh)));
     for (int i = 0; i < n; ++i) {
-        const int c = (int)args.cells.cell[i];
-        const int64_t ahead = (int64_t)cell_LW[2 * c + 1] - args.cells.step[i];   // depth of the onset
-        const bool never = call->layer < cell_LW[2 * c] || ahead >= T;
-        args.slots.first_onset[i] = (uint32_t)(never ? SPLICE_MAX_NODES : (ahead > 0 ? ahead : 0));
-        tiles[i] = splice::tree_tiles(sh, checked, T, tile, args.cells.step[i], !never, ahead > 0);
+        const int32_t *lw = cell_LW + 2 * cells.cell[i];
+        const int64_t ahead = (int64_t)lw[1] - cells.step[i];   // depth of the onset
+        const bool never = call->layer < lw[0] || ahead >= T;
+        onset[i] = (uint8_t)(never ? SPLICE_MAX_NODES : (ahead > 0 ? ahead : 0));
+        tiles[i] = splice::tree_tiles(sh, checked, T, tile, cells.step[i], !never, ahead > 0);
+        args.step[i] = cells.step[i];
     }
     const splice::TreePlan p = splice::tree_plan(sh, checked, T, tiles, n, compute_units());
     if ((int64_t)sh.n_kv_heads * p.n_slots * p.row_tiles > INT32_MAX || (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30)
         return SPLICE_EUNSUPPORTED;
-    uint32_t first = 0;
-    for (uint32_t &word : args.slots.cell) word = 0;
-    for (int i = 0; i < n; ++i) {
-        args.slots.first_onset[i] |= first << 8;
-        for (const uint32_t end = first + (uint32_t)splice::ceil_div(tiles[i], p.per); first < end; ++first)
-            args.slots.cell[first / 4] |= (uint32_t)i << (8 * (first % 4));
-    }
-    args.slots.first_onset[n] = first << 8;
+    splice::tree_slots(cells, onset, tiles, n, p.per, args.slots);
     if (p.bytes > 0 && (!workspace || !splice::aligned(workspace, 256) || workspace_bytes < p.bytes)) return SPLICE_EWORKSPACE;
     splice_dev::TreeCall &a = args.call;
     a.q = (const char *)q;

@@ -46,7 +46,7 @@ struct TreeCall {
 };
 struct TreeArgs {
     TreeCall call;
-    splice::TreeCells cells;
+    int32_t step[SPLICE_MAX_CELLS];   // of the active cells
     splice::TreeSlots slots;
 };
 
@@ -172,12 +172,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     const int r = lane & 31, h = lane >> 5, rw = wave % RW, kw = wave / RW;
 
     // ---- which rows: KV heads run fastest, so that with eight (or a multiple) an XCD keeps to its own
-    const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, slot = rest / a.row_tiles, rt = rest % a.row_tiles;
-    const int ci = (args.slots.cell[slot >> 2] >> (8 * (slot & 3))) & 255;
-    const uint32_t here = args.slots.first_onset[ci];
-    const int chunk = slot - (int)(here >> 8), onset = here & 255;
-    const bool last_chunk = slot + 1 == (int)(args.slots.first_onset[ci + 1] >> 8);
-    const int c = (int)args.cells.cell[ci], step = args.cells.step[ci], rows = a.T * a.G;
+    const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, place = rest / a.row_tiles, rt = rest % a.row_tiles;
+    const uint32_t here = args.slots.order[place >> 1] >> (16 * (place & 1));
+    const int ci = here & 255, chunk = (here >> 8) & 255;
+    const uint32_t info = args.slots.info[ci];
+    const int c = info & 255, onset = (info >> 8) & 255, slot = (int)(info >> 16) + chunk, step = args.step[ci], rows = a.T * a.G;
+    const bool last_chunk = slot + 1 == (int)(args.slots.info[ci + 1] >> 16);
     const int row0 = 32 * RW * rt, row = row0 + 32 * rw + r;
     const int64_t node0 = (int64_t)c * a.T;
     int d_node = lane < a.T ? a.depth[node0 + lane] : -1;   // lane u: node u's depth
@@ -628,10 +628,11 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
     __shared__ float s_w[ROWS][splice::kTreeMaxChunks];
     const TreeCall a = args.call;
     const int Hq = a.Hkv * a.G, ci = blockIdx.x / a.T, node = blockIdx.x % a.T;
-    const int64_t at_node = (int64_t)args.cells.cell[ci] * a.T + node;
+    const uint32_t info = args.slots.info[ci];
+    const int64_t at_node = (int64_t)(info & 255) * a.T + node;
     if (a.depth[at_node] < 0) return;
     const int rw = threadIdx.x / LPR, l = threadIdx.x % LPR, hd = blockIdx.y * ROWS + rw;
-    const int first = (int)(args.slots.first_onset[ci] >> 8), n = (int)(args.slots.first_onset[ci + 1] >> 8) - first;
+    const int first = (int)(info >> 16), n = (int)(args.slots.info[ci + 1] >> 16) - first;
     const bool on = hd < Hq;
     const int64_t stride = (int64_t)a.T * Hq, row = (int64_t)first * stride + (int64_t)node * Hq + (on ? hd : 0);
     const float *ml = a.part + (int64_t)a.n_slots * stride * D;

@@ -88,13 +88,35 @@ struct TreePlan {
     size_t bytes;   // partial results: [slot][node][q head] of D + 2 floats
 };
 
-// Where the active cells' chunks are, and at which depth their nodes begin to
-// be spliced (64: none): first slot << 8 | onset, and one more first slot; and
-// the active cell of every slot, four a word.
+// An active cell: its index, the depth from which its nodes are spliced (64:
+// none) and its first slot (there is one more, for the end).  A slot of
+// the grid: its active cell and chunk, two slots a word; chunks of one number
+// stand together, so that work groups that run together read the same part of
+// the prompt, and among them the unspliced cells, which read the clean span.
 struct TreeSlots {
-    uint32_t first_onset[SPLICE_MAX_CELLS + 1];
-    uint32_t cell[kTreeMaxSlots / 4];
+    uint32_t info[SPLICE_MAX_CELLS + 1];   // cell | onset << 8 | first slot << 16
+    uint32_t order[kTreeMaxSlots / 2];     // active cell | chunk << 8, in 16 bits
 };
+
+inline void tree_slots(const TreeCells &cells, const uint8_t *onset, const int *tiles, int n, int per, TreeSlots &out) {
+    uint32_t first = 0;
+    int most = 0;
+    for (int i = 0; i < n; ++i) {
+        out.info[i] = cells.cell[i] | (uint32_t)onset[i] << 8 | first << 16;
+        first += (uint32_t)ceil_div(tiles[i], per);
+        most = tiles[i] > most ? tiles[i] : most;
+    }
+    out.info[n] = first << 16;
+    int at = 0;
+    for (int chunk = 0; chunk * per < most; ++chunk)
+        for (int spliced = 0; spliced < 2; ++spliced)
+            for (int i = 0; i < n; ++i)
+                if ((onset[i] < SPLICE_MAX_NODES) == (spliced == 1) && chunk * per < tiles[i]) {
+                    const uint32_t x = (uint32_t)i | (uint32_t)chunk << 8;
+                    out.order[at / 2] = at % 2 ? out.order[at / 2] | x << 16 : x;
+                    ++at;
+                }
+}
 
 inline size_t tree_slot_bytes(const splice_shape &sh, int T) { return (size_t)T * sh.n_q_heads * (sh.head_dim + 2) * 4; }
 
