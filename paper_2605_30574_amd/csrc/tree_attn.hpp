@@ -64,7 +64,10 @@ struct TreeWalk {
 };
 struct TreeTileRef {
     int seg, key0, n;
-    bool differ, mask;
+    bool edge;     // some row's view begins or ends in it, or it is not full
+    bool other;    // the span's form of nodes on one side of the onset, in a list with nodes on both
+    bool dead;     // it holds rows of nodes that are not there
+    bool differ;   // some row does not see some key of it
 };
 
 template <int D, int RW>
@@ -165,7 +168,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     using X = TreeTile<D, RW>;
     constexpr int KW = X::KW, KB = X::KB, TK = X::TK, ND = X::ND, NST = D / 16;
     extern __shared__ __align__(16) char lds[];
-    __shared__ int s_bad;
+    __shared__ int s_bad, s_again;
     __shared__ TreeSegment s_seg[5];
     __shared__ float s_ml[KW > 1 ? KW : 1][32 * RW][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -222,7 +225,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         const char *v = i == 4 ? a.gv + pair * a.cap * row_bytes : pick_base(i == 2, a.cv, a.dv) + head_p;
         s_seg[i] = TreeSegment{k + (size_t)begin * row_bytes, v + (size_t)begin * row_bytes, begin, end - begin};
     }
-    if (tid == 0) s_bad = 0;
+    if (tid == 0) s_bad = s_again = 0;
     __syncthreads();
     int n_tiles = 0;
     static_for<0, 5>([&](auto i) { n_tiles += (s_seg[i].len + TK - 1) / TK; });
@@ -243,18 +246,16 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         w.key0 = __builtin_amdgcn_readfirstlane(x.key0 + skip * TK);
         w.rem = __builtin_amdgcn_readfirstlane(x.len - skip * TK);
     };
-    enter(0, X::OWN ? t0 + kw : t0);
     // The tile under way: how many keys, which, and what has to be looked at.
     auto tile_of = [&]() {
         TreeTileRef x;
         x.seg = w.seg;
         x.key0 = w.key0;
         x.n = min(TK, w.rem);
-        // some row of the work group does not see some key: ...
-        x.differ = w.seg == 4   ? a.Tp + w.key0 < low_max || w.key0 + TK > step
-                   : w.seg == 0 ? w.key0 < low_max
-                                : w.key0 < low_max || (any_clean && (w.seg == 1 || w.seg == 2));
-        x.mask = x.differ || x.n < TK;   // ... or the tile is not full
+        x.other = any_clean && any_donor && (w.seg == 1 || w.seg == 2);
+        x.dead = w.seg == 4 && w.key0 + TK > step && alive != bits(0, a.T);
+        x.differ = x.other || (w.seg == 4 ? a.Tp + w.key0 < low_max || w.key0 + TK > step : w.key0 < low_max);
+        x.edge = x.n < TK || (x.differ && !x.other) || (x.other && w.key0 < low_max);
         return x;
     };
     auto advance = [&]() {   // to the wave's next tile
@@ -349,11 +350,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             });
         }
     };
-    // In a tile that rows see differently the values are looked at: those of
-    // nodes that are not there become 0, and so do infinities and NaN, which
-    // must not reach the rows that do not see them (0 * inf); s_bad tells
-    // that there were some, and the rows that do see them are settled behind
-    // the loop.
+    // Values that are looked at: those of nodes that are not there become 0, and
+    // so do infinities and NaN, which must not reach the rows that do not see
+    // them (0 * inf); s_bad tells that there were some, and the rows that do
+    // see them are settled behind the loop.
     auto look = [&](const TreeTileRef &x, char *buf) {
         static_for<0, X::NL>([&](auto i) {
             const int u = (int)i * X::NT + ltid, key = u / X::CPR, nd = x.key0 + key - step;
@@ -372,8 +372,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         const int skip = X::OWN ? 0 : kw * 32 * KB, first = x.key0 + skip, n = x.n - skip;
         if (x.seg == 4)
             return bits(low - a.Tp - first, min(step - first, n)) | (shifted(word, step - first) & bits(step - first, n));
-        const bool other = any_clean && any_donor && (x.seg == 1 || x.seg == 2) && (x.seg == 2) != spliced;
-        return other ? 0 : bits(low - first, n);
+        return x.other && (x.seg == 2) != spliced ? 0 : bits(low - first, n);
     };
     auto values = [&](const char *buf, int db, int kk) {   // 32 d of 16 keys, in the lanes of the A operand
         const char *at = buf + (v_at ^ 64 * db) + 16 * kk * X::ROW;
@@ -387,11 +386,16 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
 
     const int t_first = X::OWN ? t0 + kw : t0;
     constexpr int t_step = X::OWN ? 4 : 1;
-    TreeTileRef cur = tile_of();
-    if (t_first < t1) {
-        load(0);
-        advance();
-    }
+    TreeTileRef cur;
+    auto begin = [&]() {   // the wave's first tile
+        enter(0, t_first);
+        cur = tile_of();
+        if (t_first < t1) {
+            load(0);
+            advance();
+        }
+    };
+    begin();
 
     // ---- Q^T, in the lanes of the B operand: row r, d = 16 st + 8 h ..
     bf16x8_t qb[X::OWN ? 1 : NST];
@@ -413,10 +417,17 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             });
         }
     }
-    // state of a row: o[db][i] is d = 32 db + 8 (i / 4) + 4 h + i % 4; a half's share of the sum
-    f32x16_t o[ND];
+    const bool wave_clean = __any(valid && !spliced), wave_donor = __any(valid && spliced);
+
+    // The list is walked as if every value were finite. If a row's result then
+    // is not, it is walked once more, and the values of every tile that
+    // rows see differently are looked at.
+    f32x16_t o[ND];   // o[db][i] is d = 32 db + 8 (i / 4) + 4 h + i % 4 of the row
+    float m, l;       // its maximum; its sum, of which either half has a share
+    for (bool careful = false;; careful = true) {
     static_for<0, ND>([&](auto db) { static_for<0, 16>([&](auto i) { o[db][(int)i] = 0.f; }); });
-    float m = -INFINITY, l = 0.f;
+    m = -INFINITY;
+    l = 0.f;
     // keys of the ZERO donor score 0 and add nothing to o
     if (a.zero_donor && spliced && chunk == 0 && kw == 0) {
         const int n_zero = a.span_hi - max(a.span_lo, max(low, 0));
@@ -447,11 +458,13 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             load(b ^ 1);
             advance();
         }
-        if (cur.differ) {
+        if (careful ? cur.differ : cur.dead) {
             look(cur, buf);
             if constexpr (X::OWN) wave_fence();
             else __syncthreads();
         }
+        // (a wave may have no row that sees its tile)
+        if (!cur.other || (cur.seg == 2 ? wave_donor : wave_clean)) {
         f32x16_t s[KB];
         static_for<0, KB>([&](auto kb) {
             u32x4_t ka[NST];
@@ -466,7 +479,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
                 s[kb] = product(ka[st], q, s[kb]);
             });
         });
-        if (cur.mask) {
+        if (cur.edge || (careful && cur.other)) {
             const uint64_t see = seen(cur) >> 4 * h;
             static_for<0, KB>([&](auto kb) {
                 static_for<0, 16>([&](auto i) {
@@ -478,6 +491,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         float mt = -INFINITY;
         static_for<0, KB>([&](auto kb) { static_for<0, 16>([&](auto i) { mt = fmaxf(mt, s[kb][(int)i]); }); });
         mt *= a.qk_scale;
+        const bool hidden = cur.other && (cur.seg == 2) != spliced;   // the row sees none of it
+        if (hidden) mt = -INFINITY;
         if (__any(mt > m + kSlack)) {
             mt = fmaxf(mt, __shfl_xor(mt, 32));
             const bool need = mt > m + kSlack;
@@ -487,7 +502,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             static_for<0, ND>([&](auto db) { o[db] *= al; });
             m = mn;
         }
-        const float ms = m == -INFINITY ? 0.f : m;
+        const float ms = hidden ? INFINITY : (m == -INFINITY ? 0.f : m);
         bf16x8_t pb[2 * KB];
         static_for<0, KB>([&](auto kb) {
             static_for<0, 16>([&](auto i) {
@@ -499,6 +514,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         static_for<0, ND>([&](auto db) {
             static_for<0, 2 * KB>([&](auto kk) { o[db] = product(values(buf, db, kk), pb[kk], o[db]); });
         });
+        }
         cur = next;
         if constexpr (!X::OWN) {
             wait_vmcnt<0>();
@@ -506,6 +522,14 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         }
     }
     __syncthreads();
+    if (careful) break;
+    float zero = 0.f * l;   // NaN if anything is not finite
+    static_for<0, ND>([&](auto db) { static_for<0, 16>([&](auto i) { zero = fmaf(0.f, o[db][(int)i], zero); }); });
+    if (valid && zero != zero) s_again = 1;
+    __syncthreads();
+    if (!s_again) break;
+    begin();
+    }
     if (s_bad) {
         // infinities and NaN among the values of tiles that rows see differently:
         // the tiles once more, and which of them each row sees
