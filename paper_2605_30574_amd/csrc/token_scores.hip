@@ -5,9 +5,11 @@
 // z = (logit - m) scale log2(e) the sums s = sum 2^z and t = sum 2^z z; then
 //   lse = m scale + ln2 log2 s,   entropy = ln2 (log2 s - t / s).
 // When m rises, all z fall by some r: t becomes 2^-r (t - r s) and s 2^-r s.
-// (m stays a logit: the lowest float, a usual mask, times log2(e) is no float.)  The k largest
-// logits are kept sorted in a wave, one a lane, as 64-bit keys (the value's
-// order, then the lower index); a logit below the k-th costs one comparison.
+// (m stays a logit: the lowest float, a usual mask, times log2(e) is no float.)
+// The k largest logits, as 64-bit keys (the value's order, then the lower
+// index), are the first k of the candidates that each wave keeps in a list in
+// LDS: what is below the k-th that it has seen costs a comparison a 16-byte
+// chunk, and waves do not wait for each other before the row's end.
 // A row is cut into parts when there are too few rows for the GPU, and a
 // second kernel joins the parts' sums and lists.
 
@@ -26,8 +28,12 @@ constexpr int kScoreThreads = 256;
 constexpr int kScoreWaves = kScoreThreads / 64;
 constexpr int kChunks = 4;            // 16-byte chunks a thread has in flight
 constexpr int kMaxParts = 64;
-constexpr int kPartBytes = 16 << 10;  // a part is at least this long
-constexpr int kPartsTarget = 2048;    // work groups that fill the GPU
+constexpr int kPartBytes = 8 << 10;  // a part is at least this long
+constexpr int kPartsTarget = 1024;    // work groups that fill the GPU
+constexpr int kWaveKeys = 256;        // a wave's list
+constexpr int kSlackKeys = 32;        // one this much longer than k is cut
+constexpr int kCandidates = 1024;     // a work group's four lists; a row's parts have no more
+static_assert(SPLICE_MAX_TOP + kSlackKeys <= 128 && kWaveKeys * kScoreWaves == kCandidates, "two kept keys a lane");
 
 struct PartSums {
     float m, s, t;
@@ -59,36 +65,127 @@ __device__ __forceinline__ float key_value(uint64_t key) {
 }
 __device__ __forceinline__ int key_index(uint64_t key) { return (int)~(uint32_t)key; }
 
+// Lists of candidates, in any order; joined, n of them from the start.
+struct Candidates {
+    uint64_t key[kCandidates];
+    uint64_t first[SPLICE_MAX_TOP];   // the first k of the list, in order
+    uint64_t least;
+    int n;
+};
+
+// Lanes of a wave that hand each other values through LDS: its operations run
+// in order, so only the compiler has to keep theirs.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+
 __device__ __forceinline__ uint64_t lane_value(uint64_t x, int lane) {
     const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, lane);
     const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane);
     return ((uint64_t)hi << 32) | lo;
 }
 
-// The first k of all keys offered to a wave: lane i holds the i-th largest.
-struct TopList {
-    uint64_t key = 0;   // this lane's
-    uint64_t least = 0; // the k-th
-    int k;
+// A wave's list: n keys (the same n in every lane), of which those that find
+// room are there.
+struct WaveList {
+    uint64_t *key;
+    int n, k;
 
-    __device__ __forceinline__ explicit TopList(int k) : k(k) {}
+    __device__ __forceinline__ void append(bool on, uint64_t x) {
+        const uint64_t lanes = __ballot(on);
+        if (lanes == 0) return;
+        const int at = n + __popcll(lanes & ((1ull << (threadIdx.x & 63)) - 1));
+        if (on && at < kWaveKeys) key[at] = x;
+        n += __popcll(lanes);
+    }
 
-    // Every lane of the wave offers one key (0: none).
-    __device__ __forceinline__ void offer(uint64_t x) {
+    // The k-th key, of the keys that found room; sort: the first k are moved to
+    // the list's front, in order.  A lane counts for each of its entries the
+    // larger ones; keys are all different.
+    __device__ __forceinline__ uint64_t kth(bool sort) {
+        constexpr int PER = kWaveKeys / 64;
+        const int lane = threadIdx.x & 63, have = min(n, kWaveKeys);
+        wave_fence();
+        uint64_t mine[PER];
+        int rank[PER];
+        static_for<0, PER>([&](auto i) {
+            mine[i] = lane + 64 * (int)i < have ? key[lane + 64 * (int)i] : 0;
+            rank[i] = lane + 64 * (int)i < have ? 0 : kWaveKeys;
+        });
+        auto count = [&](auto entries) {   // a lane's first `entries` against all
+#pragma unroll 4
+            for (int j = 0; j < have; ++j) {
+                const uint64_t x = key[j];
+                static_for<0, decltype(entries)::value>([&](auto i) { rank[i] += x > mine[i]; });
+            }
+        };
+        if (have <= 64) count(std::integral_constant<int, 1>{});
+        else if (have <= 128) count(std::integral_constant<int, 2>{});
+        else count(std::integral_constant<int, PER>{});
+        wave_fence();
+        uint64_t found = 0;
+        static_for<0, PER>([&](auto i) {
+            if (sort && rank[i] < k) key[rank[i]] = mine[i];
+            const uint64_t at = __ballot(rank[i] == k - 1);
+            if (at) found = lane_value(mine[i], __builtin_ctzll(at));
+        });
+        if (sort) n = min(n, k);
+        wave_fence();
+        return found;   // 0 of fewer than k
+    }
+
+    // Only those of the first `had` keys that are not below x are left.
+    __device__ __forceinline__ void only(int had, uint64_t x) {
         const int lane = threadIdx.x & 63;
-        uint64_t todo = __ballot(x > least);
-        while (todo) {
-            const int from = __builtin_ctzll(todo);
-            const uint64_t y = lane_value(x, from);
-            const int at = __popcll(__ballot(key > y));
-            const uint64_t up = __shfl_up((unsigned long long)key, 1);
-            key = lane < at ? key : (lane == at ? y : up);
-            least = lane_value(key, k - 1);
-            todo &= todo - 1;
-            todo &= __ballot(x > least);
-        }
+        wave_fence();
+        const uint64_t y0 = lane < had ? key[lane] : 0, y1 = lane + 64 < had ? key[lane + 64] : 0;
+        wave_fence();
+        n = 0;
+        append(lane < had && y0 >= x, y0);
+        append(lane + 64 < had && y1 >= x, y1);
     }
 };
+
+// What does not fit is left out, and n tells.
+__device__ __forceinline__ void append(Candidates &c, uint64_t key) {
+    const int at = atomicAdd(&c.n, 1);
+    if (at < kCandidates) c.key[at] = key;
+}
+
+// first[0..k) = the first k of the list's n entries (0 beyond n), in order: a
+// thread counts for each of its entries the larger ones; keys are all
+// different.  Called by all threads, after a barrier; ends in one.
+__device__ __forceinline__ void rank_first(Candidates &c, int n, int k) {
+    constexpr int PER = kCandidates / kScoreThreads;
+    const int tid = threadIdx.x;
+    uint64_t mine[PER];
+    int rank[PER];
+    static_for<0, PER>([&](auto i) {
+        const int e = tid + (int)i * kScoreThreads;
+        mine[i] = e < n ? c.key[e] : ~0ull;
+        rank[i] = 0;
+    });
+    if (tid < k) c.first[tid] = 0;
+    __syncthreads();
+    if ((tid & ~63) >= n) {
+        // no entries in this wave
+    } else if (n <= kScoreThreads) {
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) rank[0] += c.key[j] > mine[0];
+    } else {
+#pragma unroll 2
+        for (int j = 0; j < n; ++j) {
+            const uint64_t x = c.key[j];
+            static_for<0, PER>([&](auto i) { rank[i] += x > mine[i]; });
+        }
+    }
+    static_for<0, PER>([&](auto i) {
+        if (tid + (int)i * kScoreThreads < n && rank[i] < k) c.first[rank[i]] = mine[i];
+    });
+    __syncthreads();
+}
 
 // Where weights are 0 their z, which may be -inf, stops here: 0 times a finite number.
 constexpr float kLeastZ = -1e4f;
@@ -110,28 +207,30 @@ __device__ __forceinline__ void wave_join(float scale2, float &m, float &s, floa
     }
 }
 
-// The row's results from its joined sums; called by one wave.
+template <bool BF16>
+__device__ __forceinline__ float logit(const char *row, int i) {
+    return BF16 ? bf16_hi((uint32_t)reinterpret_cast<const uint16_t *>(row)[i] << 16) : reinterpret_cast<const float *>(row)[i];
+}
+
+// The row's results from its joined sums and its first k keys; called by one wave.
 template <bool BF16>
 __device__ __forceinline__ void finish(const ScoreArgs &a, int64_t row, float m, float s, float t, int before,
-                                       const TopList &list) {
+                                       const uint64_t *first) {
     const int lane = threadIdx.x & 63;
     const float log_s = kLn2 * log2f(s);   // -inf for a row of nothing
     if (lane == 0) {
         const int64_t tok = a.tokens[row];
         const bool in = tok >= 0 && tok < a.vocab;
-        float x = 0.f;
-        if (in) {
-            const char *p = a.logits + row * a.stride;
-            x = BF16 ? bf16_hi((uint32_t)reinterpret_cast<const uint16_t *>(p)[tok] << 16) : reinterpret_cast<const float *>(p)[tok];
-        }
+        const float x = in ? logit<BF16>(a.logits + row * a.stride, (int)tok) : 0.f;
         a.logp[row] = in ? (x - m) * a.scale - log_s : __uint_as_float(0x7fc00000u);
         a.lse[row] = fmaf(m, a.scale, log_s);
         a.entropy[row] = log_s - kLn2 * (t / s);
         a.rank[row] = in ? before : -1;
     }
     if (lane < a.k) {
-        a.top[row * a.k + lane] = key_index(list.key);
-        a.top_logp[row * a.k + lane] = (key_value(list.key) - m) * a.scale - log_s;
+        const uint64_t key = first[lane];
+        a.top[row * a.k + lane] = key_index(key);
+        a.top_logp[row * a.k + lane] = (key_value(key) - m) * a.scale - log_s;
     }
 }
 
@@ -139,21 +238,24 @@ template <bool BF16>
 __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreArgs a) {
     constexpr int VE = BF16 ? 8 : 4, ES = BF16 ? 2 : 4;   // values of a chunk, bytes of a value
     __shared__ PartSums s_sums[kScoreWaves];
-    __shared__ uint64_t s_keys[kScoreWaves][64];
+    __shared__ Candidates s_top;
+    __shared__ int s_count[kScoreWaves];
     const int64_t row = blockIdx.x / a.parts;
     const int part = (int)(blockIdx.x % a.parts), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const char *p = a.logits + row * a.stride;
-    // 16-byte chunks from the last boundary at or below the row's start
-    const int skew = (int)((uintptr_t)p & 15) / ES;
-    const char *base = p - skew * ES;
-    const int n_chunks = (int)(((int64_t)skew + a.vocab + VE - 1) / VE);
-    const int per = (n_chunks + a.parts - 1) / a.parts, c0 = part * per, c1 = min(c0 + per, n_chunks);
+    // 16-byte chunks of the row; what lies before the first boundary and behind
+    // the last are single values, which the first and the last part take, one a thread
+    int head = (int)(-(uintptr_t)p & 15) / ES;
+    head = min(head, a.vocab);
+    const int n_chunks = (a.vocab - head) / VE, tail = a.vocab - head - n_chunks * VE;
+    const char *base = p + head * ES;
+    const int per = (n_chunks + a.parts - 1) / a.parts, c0 = min(part * per, n_chunks), c1 = min(c0 + per, n_chunks);
 
     const int64_t tok = a.tokens[row];
     const bool in = tok >= 0 && tok < a.vocab;
     const int token = in ? (int)tok : 0;
-    const float xt = BF16 ? bf16_hi((uint32_t)reinterpret_cast<const uint16_t *>(p)[token] << 16)
-                          : reinterpret_cast<const float *>(p)[token];
+    const float xt = logit<BF16>(p, token);
+    const bool xt_nan = xt != xt;
     // before the token x >= xt comes first, behind it x > xt: the former is
     // x > the float below xt (a NaN for -inf: then every value comes first)
     const uint32_t xb = __float_as_uint(xt);
@@ -163,98 +265,185 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreArgs a) {
 
     float m = -INFINITY, s = 0.f, t = 0.f;
     int before = 0;
-    TopList list(a.k);
-    float least = -INFINITY;
+    WaveList list{s_top.key + wave * kWaveKeys, 0, a.k};
+    uint64_t kth = 0;            // a key that k keys of the row are not below
+    float least = -INFINITY;     // its value
+    auto raise = [&](float top) {   // m to at least top
+        if (top > m) {
+            const float r = (m - top) * a.scale2, f = fast_exp2(r);
+            t = f * fmaf(fmaxf(r, kLeastZ), s, t);
+            s *= f;
+            m = top;
+        }
+    };
+    auto add = [&](float z) {
+        const float e = fast_exp2(z);
+        s += e;
+        t = fmaf(e, fmaxf(z, kLeastZ), t);
+    };
 
-    for (int c = c0; c < c1; c += kScoreThreads * kChunks) {   // the same trips in every lane
-        float x[kChunks][VE];
+    float single = -INFINITY;
+    int single_id = -1;
+    if (part == 0 && tid < head) single_id = tid;
+    if (part == a.parts - 1 && tid >= 64 && tid - 64 < tail) single_id = a.vocab - tail + tid - 64;
+    if (single_id >= 0) {
+        single = logit<BF16>(p, single_id);
+        raise(single);
+        add((single - (m == -INFINITY ? 0.f : m)) * a.scale2);
+        before += xt_nan ? single != single && single_id < token
+                         : single > xt || single != single || (single == xt && single_id < token);
+    }
+    if (a.k > 0) list.append(single_id >= 0, key_of(single, single_id));
+
+    u32x4_t w[kChunks];   // the next trip's
+    auto load = [&](int c) {
         static_for<0, kChunks>([&](auto u) {
-            const int j = c + (int)u * kScoreThreads + tid, id0 = j * VE - skew;
-            if (j < c1 && id0 >= 0 && id0 + VE <= a.vocab) {
-                const u32x4_t w = *reinterpret_cast<const u32x4_t *>(base + (int64_t)j * 16);
-                static_for<0, 4>([&](auto i) {
-                    const uint32_t v = w[(int)i];
-                    if constexpr (BF16) {
-                        x[u][2 * i] = bf16_lo(v);
-                        x[u][2 * i + 1] = bf16_hi(v);
-                    } else {
-                        x[u][i] = __uint_as_float(v);
-                    }
-                });
-            } else {
-                static_for<0, VE>([&](auto i) {   // a row's ends: only what is its own is read
-                    const int id = id0 + (int)i;
-                    x[u][i] = -INFINITY;
-                    if (j < c1 && id >= 0 && id < a.vocab)
-                        x[u][i] = BF16 ? bf16_hi((uint32_t)reinterpret_cast<const uint16_t *>(p)[id] << 16)
-                                       : reinterpret_cast<const float *>(p)[id];
-                });
-            }
+            const int j = c + (int)u * kScoreThreads + tid;
+            if (j < c1) w[u] = *reinterpret_cast<const u32x4_t *>(base + (int64_t)j * 16);
         });
+    };
+    load(c0);
+    for (int c = c0; c < c1; c += kScoreThreads * kChunks) {   // the same trips in every lane
+        float x[kChunks][VE], top[kChunks];
         static_for<0, kChunks>([&](auto u) {
-            const int j = c + (int)u * kScoreThreads + tid, id0 = j * VE - skew;
-            float top = x[u][0];
-            static_for<1, VE>([&](auto i) { top = fmaxf(top, x[u][i]); });
-            if (top > m) {
-                const float r = (m - top) * a.scale2, f = fast_exp2(r);
-                t = f * fmaf(fmaxf(r, kLeastZ), s, t);
-                s *= f;
-                m = top;
-            }
-            const float ref = m == -INFINITY ? 0.f : m;
-            static_for<0, VE>([&](auto i) {
-                const float z = (x[u][i] - ref) * a.scale2, e = fast_exp2(z);
-                s += e;
-                t = fmaf(e, fmaxf(z, kLeastZ), t);
+            static_for<0, 4>([&](auto i) {
+                const uint32_t v = w[u][(int)i];
+                if constexpr (BF16) {
+                    x[u][2 * i] = bf16_lo(v);
+                    x[u][2 * i + 1] = bf16_hi(v);
+                } else {
+                    x[u][i] = __uint_as_float(v);
+                }
             });
-            if (xt == xt && id0 >= 0 && j < c1 && id0 + VE <= a.vocab && (token < id0 || token >= id0 + VE)) {
-                const float bar = token >= id0 ? below : xt;
-                static_for<0, VE>([&](auto i) { before += !(x[u][i] <= bar); });
-            } else if (j < c1) {
-                static_for<0, VE>([&](auto i) {
-                    const int id = id0 + (int)i;
-                    const float y = x[u][i];
-                    const bool first = xt == xt ? (y > xt || y != y || (y == xt && id < token)) : (y != y && id < token);
-                    before += id >= 0 && id < a.vocab && first;
-                });
-            }
-            if (a.k > 0) {
-                bool any = false;
-                static_for<0, VE>([&](auto i) { any |= !(x[u][i] < least); });
-                if (__any(any)) {
-                    static_for<0, VE>([&](auto i) {
-                        const int id = id0 + (int)i;
-                        list.offer(j < c1 && id >= 0 && id < a.vocab ? key_of(x[u][i], id) : 0);
-                    });
-                    least = list.least ? key_value(list.least) : -INFINITY;
+        });
+        load(c + kScoreThreads * kChunks);
+        static_for<0, kChunks>([&](auto u) {
+            const int j = c + (int)u * kScoreThreads + tid, id0 = head + j * VE;
+            top[u] = -INFINITY;
+            if (j < c1) {
+                static_for<0, VE>([&](auto i) { top[u] = fmaxf(top[u], x[u][i]); });
+                raise(top[u]);
+                if (__any(m < -1e30f)) {   // m * scale2 may be no float
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    static_for<0, VE>([&](auto i) { add((x[u][i] - ref) * a.scale2); });
+                } else {
+                    const float ref = -m * a.scale2;
+                    static_for<0, VE>([&](auto i) { add(fmaf(x[u][i], a.scale2, ref)); });
+                }
+                if (xt_nan) {
+                    static_for<0, VE>([&](auto i) { before += x[u][i] != x[u][i] && id0 + (int)i < token; });
+                } else {
+                    const float bar = token >= id0 + VE ? below : xt;
+                    static_for<0, VE>([&](auto i) { before += !(x[u][i] <= bar); });
+                    if (token >= id0 && token < id0 + VE)
+                        static_for<0, VE>([&](auto i) { before += x[u][i] == xt && id0 + (int)i < token; });
                 }
             }
         });
+        if (a.k == 0) continue;
+        if (c == c0) {
+            // to begin with: the largest of the lanes' maxima that k of them are not below
+            float best = top[0];
+            static_for<1, kChunks>([&](auto u) { best = fmaxf(best, top[u]); });
+            int over = 0;
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+                over += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(best), j)) >= best;
+            least = over >= a.k ? best : -INFINITY;
+            for (int o = 32; o > 0; o >>= 1) least = fmaxf(least, __shfl_xor(least, o));
+        }
+        for (;;) {
+            const int had = list.n;
+            static_for<0, kChunks>([&](auto u) {
+                const int j = c + (int)u * kScoreThreads + tid;
+                const bool any = j < c1 && (!(top[u] < least) || s != s);   // s is a NaN where a logit is
+                if (__any(any)) {
+                    int id0 = head + j * VE;
+                    asm volatile("" : "+v"(id0));   // else every value's id and key are worked out before the loop
+                    static_for<0, VE>([&](auto i) {
+                        const bool maybe = any && !(x[u][i] < least);
+                        if (__any(maybe)) {
+                            float y = x[u][i];
+                            asm volatile("" : "+v"(y));
+                            const uint64_t key = key_of(y, id0 + (int)i);
+                            list.append(maybe && key >= kth, key);
+                        }
+                    });
+                }
+            });
+            if (list.n <= a.k + kSlackKeys) break;
+            const bool again = list.n > kWaveKeys;   // not all found room
+            kth = list.kth(!again);
+            least = key_value(kth);
+            if (!again) break;
+            list.only(had, kth);   // and the trip again: its keys that are not below
+        }
+    }
+    if (a.k > 0) {
+        // the waves' first k together
+        list.kth(true);
+        __syncthreads();
+        const int n = kScoreWaves * a.k, w_of = tid / a.k, i_of = tid % a.k;
+        if (lane == 0) s_count[wave] = list.n;
+        __syncthreads();
+        const uint64_t mine = tid < n && i_of < s_count[w_of] ? s_top.key[w_of * kWaveKeys + i_of] : 0;
+        __syncthreads();
+        if (tid == 0) s_top.n = 0;
+        __syncthreads();
+        if (mine) append(s_top, mine);
+        __syncthreads();
+        rank_first(s_top, s_top.n, a.k);
     }
 
     wave_join(a.scale2, m, s, t, before);
-    s_keys[wave][lane] = list.key;
     if (lane == 0) s_sums[wave] = PartSums{m, s, t, before};
     __syncthreads();
     if (wave != 0) return;
     for (int w = 1; w < kScoreWaves; ++w) {
         join(a.scale2, m, s, t, s_sums[w].m, s_sums[w].s, s_sums[w].t);
         before += s_sums[w].before;
-        if (a.k > 0) list.offer(s_keys[w][lane]);
     }
     if (a.parts == 1) {
-        finish<BF16>(a, row, m, s, t, before, list);
+        finish<BF16>(a, row, m, s, t, before, s_top.first);
         return;
     }
     if (lane == 0) a.sums[blockIdx.x] = PartSums{m, s, t, before};
-    if (lane < a.k) a.keys[(int64_t)blockIdx.x * a.k + lane] = list.key;
+    if (lane < a.k) a.keys[(int64_t)blockIdx.x * a.k + lane] = s_top.first[lane];
 }
 
-// Joins the parts of a row: one wave a row.
+// Joins the parts of a row, a work group a row.  With q = ceil(k / parts), the
+// least of the parts' q-th keys has at least k keys not below it.
 template <bool BF16>
-__global__ __launch_bounds__(64) void score_join_kernel(ScoreArgs a) {
+__global__ __launch_bounds__(kScoreThreads) void score_join_kernel(ScoreArgs a) {
+    __shared__ Candidates s_top;
     const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (a.k > 0) {
+        constexpr int PER = kCandidates / kScoreThreads;
+        const int n = a.parts * a.k, q = (a.k + a.parts - 1) / a.parts;
+        uint64_t key[PER];
+        static_for<0, PER>([&](auto i) {
+            const int e = tid + (int)i * kScoreThreads;
+            key[i] = e < n ? a.keys[row * n + e] : 0;
+        });
+        uint64_t least = tid < a.parts ? a.keys[row * n + tid * a.k + q - 1] : ~0ull;
+        if (wave == 0) {   // at most 64 parts
+            for (int o = 32; o > 0; o >>= 1) {
+                const uint64_t x = __shfl_xor((unsigned long long)least, o);
+                least = x < least ? x : least;
+            }
+            if (lane == 0) {
+                s_top.least = least;
+                s_top.n = 0;
+            }
+        }
+        __syncthreads();
+        least = s_top.least;
+        static_for<0, PER>([&](auto i) { if (key[i] != 0 && key[i] >= least) append(s_top, key[i]); });
+        __syncthreads();
+        rank_first(s_top, s_top.n, a.k);
+    }
+    if (wave != 0) return;
     float m = -INFINITY, s = 0.f, t = 0.f;
     int before = 0;
     if (lane < a.parts) {
@@ -265,17 +454,15 @@ __global__ __launch_bounds__(64) void score_join_kernel(ScoreArgs a) {
         before = p.before;
     }
     wave_join(a.scale2, m, s, t, before);
-    TopList list(a.k);
-    const int n = a.parts * a.k;
-    for (int i = 0; i < n; i += 64) list.offer(i + lane < n ? a.keys[row * n + i + lane] : 0);
-    finish<BF16>(a, row, m, s, t, before, list);
+    finish<BF16>(a, row, m, s, t, before, s_top.first);
 }
 
-int parts_of(int64_t rows, int64_t vocab) {
+int parts_of(int64_t rows, int64_t vocab, int k) {
     int64_t parts = (kPartsTarget + rows - 1) / rows;
     const int64_t most = (vocab * 2 + kPartBytes - 1) / kPartBytes;   // in bf16; the same for both types
     parts = parts < most ? parts : most;
-    return (int)(parts < kMaxParts ? parts : kMaxParts);
+    const int fit = k > 0 && kCandidates / k < kMaxParts ? kCandidates / k : kMaxParts;   // of the parts' lists in one
+    return (int)(parts < fit ? parts : fit);
 }
 
 bool takes(int64_t rows, int64_t vocab, int32_t k) {
@@ -289,7 +476,7 @@ extern "C" {
 int64_t splice_token_scores_workspace_bytes(int64_t rows, int64_t vocab, int32_t k) {
     if (!takes(rows, vocab, k)) return SPLICE_ESHAPE;
     if (rows == 0) return 0;
-    const int parts = parts_of(rows, vocab);
+    const int parts = parts_of(rows, vocab, k);
     return parts == 1 ? 0 : rows * parts * ((int64_t)sizeof(PartSums) + 8 * k);
 }
 
@@ -311,7 +498,7 @@ int32_t splice_token_scores(const void *logits, int32_t dtype, int64_t rows, int
         return SPLICE_EINVAL;
     if (need > 0 && (!workspace || !splice::aligned(workspace, 16) || workspace_bytes < (size_t)need))
         return SPLICE_EWORKSPACE;
-    const int parts = parts_of(rows, vocab);
+    const int parts = parts_of(rows, vocab, k);
     ScoreArgs a{(const char *)logits, tokens, logp, lse, entropy, top_logp, rank, top, (PartSums *)workspace, nullptr,
                 row_stride * es, (int)vocab, k, parts, scale, scale * kLog2e};
     if (parts > 1) a.keys = (uint64_t *)((char *)workspace + rows * parts * sizeof(PartSums));
@@ -320,8 +507,8 @@ int32_t splice_token_scores(const void *logits, int32_t dtype, int64_t rows, int
     if (dtype == SPLICE_BF16) hipLaunchKernelGGL(score_kernel<true>, grid, dim3(kScoreThreads), 0, st, a);
     else hipLaunchKernelGGL(score_kernel<false>, grid, dim3(kScoreThreads), 0, st, a);
     if (parts > 1) {
-        if (dtype == SPLICE_BF16) hipLaunchKernelGGL(score_join_kernel<true>, dim3((unsigned)rows), dim3(64), 0, st, a);
-        else hipLaunchKernelGGL(score_join_kernel<false>, dim3((unsigned)rows), dim3(64), 0, st, a);
+        if (dtype == SPLICE_BF16) hipLaunchKernelGGL(score_join_kernel<true>, dim3((unsigned)rows), dim3(kScoreThreads), 0, st, a);
+        else hipLaunchKernelGGL(score_join_kernel<false>, dim3((unsigned)rows), dim3(kScoreThreads), 0, st, a);
     }
     return hipGetLastError() == hipSuccess ? SPLICE_OK : SPLICE_EHIP;
 }
