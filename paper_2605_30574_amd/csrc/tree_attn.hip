@@ -103,7 +103,8 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     a.visible = visible;
     a.out = (__bf16 *)out;
     a.lse = lse;
-    a.part = (float *)workspace;
+    a.part = (_Float16 *)workspace;
+    a.record = (float4 *)((char *)workspace + (size_t)p.n_slots * T * sh.n_q_heads * sh.head_dim * 2);
     a.T = T;
     a.G = splice::group_of(sh);
     a.Hkv = sh.n_kv_heads;

@@ -30,6 +30,9 @@
 namespace splice_dev {
 
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 struct TreeCall {
@@ -39,7 +42,12 @@ struct TreeCall {
     const uint64_t *visible;
     __bf16 *out;
     float *lse;
-    float *part;   // [slot][node][q head][D], then [..][2] (m, l)
+    // Partial results, [slot][node][q head]: o / l in fp16 (a convex combination
+    // of value rows; where one passes 2^15, times a power of two sc), and m,
+    // l, l / sc.  A rounding of 2^-12 of them is small beside the bf16 result's,
+    // and in 32 bits they would be 53% of what a call of many chunks writes and reads again.
+    _Float16 *part;
+    float4 *record;
     int T, G, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, n_slots, per;
     bool split;
     float qk_scale;   // scale * log2(e)
@@ -108,6 +116,14 @@ __device__ __forceinline__ uint64_t bits(int b, int e) {
 __device__ __forceinline__ uint64_t shifted(uint64_t x, int by) {   // left, or right when by < 0
     if (by >= 64 || by <= -64) return 0;
     return by >= 0 ? x << by : x >> -by;
+}
+
+// |x|, 0 for an infinity or NaN; and the power of two that brings a largest
+// value down to 2^15 where it is above.
+__device__ __forceinline__ float finite_size(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
+__device__ __forceinline__ float half_scale(float top) {
+    if (!(top > 32768.f)) return 1.f;
+    return __uint_as_float((uint32_t)(127 + 14 + 127 - (int)(__float_as_uint(top) >> 23)) << 23);
 }
 
 // A pointer that is the same in every lane, in scalar registers (a buffer
@@ -573,9 +589,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     // ---- results
     l += __shfl_xor(l, 32);
     const int64_t out_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
-    const int64_t n_part = (int64_t)a.n_slots * a.T * a.Hkv * a.G;   // rows of the partial results
     const int64_t part_row = ((int64_t)slot * a.T + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
-    float *part_ml = a.part + n_part * D;
     if constexpr (KW > 1) {
         // the waves of a row through LDS (every wave is done with the tiles)
         float *s_o = reinterpret_cast<float *>(lds);   // [KW][32 RW][D], chunks of four swizzled by the row
@@ -607,95 +621,87 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
                 if (f != 0.f)
                     O += f * *reinterpret_cast<const f32x4_t *>(s_o + (((int)k * 32 * RW + w) * D + 4 * (d4 ^ (w & 15))));
             });
+            const float f = Lsum == 0.f ? 0.f : 1.f / Lsum;
+            O *= f;
             if (a.split) {
                 const int64_t at = ((int64_t)slot * a.T + nd) * (a.Hkv * a.G) + hd;
-                *reinterpret_cast<f32x4_t *>(a.part + at * D + 4 * d4) = O;
-                if (d4 == 0) *reinterpret_cast<float2 *>(part_ml + 2 * at) = make_float2(M, Lsum);
+                float top = 0.f;
+                static_for<0, 4>([&](auto i) { top = fmaxf(top, finite_size(O[(int)i])); });
+                for (int x = 1; x < (D / 4 < 64 ? D / 4 : 64); x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+                const float sc = half_scale(top);
+                *reinterpret_cast<f16x4_t *>(a.part + at * D + 4 * d4) = __builtin_convertvector(O * sc, f16x4_t);
+                if (d4 == 0) a.record[at] = make_float4(M, Lsum, Lsum / sc, 0.f);
             } else {
                 const int64_t at = (node0 + nd) * (a.Hkv * a.G) + hd;
-                const float f = Lsum == 0.f ? 0.f : 1.f / Lsum;
-                *reinterpret_cast<bf16x4_t *>(a.out + at * D + 4 * d4) = __builtin_convertvector(O * f, bf16x4_t);
+                *reinterpret_cast<bf16x4_t *>(a.out + at * D + 4 * d4) = __builtin_convertvector(O, bf16x4_t);
                 if (d4 == 0) a.lse[at] = kLn2 * (M + log2f(Lsum));
             }
         }
     } else {
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        float top = 0.f;
+        static_for<0, ND>([&](auto db) {
+            static_for<0, 16>([&](auto i) {
+                o[db][(int)i] *= f;
+                top = fmaxf(top, finite_size(o[db][(int)i]));
+            });
+        });
+        const float sc = half_scale(fmaxf(top, __shfl_xor(top, 32)));
         if (!valid) return;
-        if (a.split) {
-            static_for<0, ND>([&](auto db) {
-                static_for<0, 4>([&](auto i) {
-                    *reinterpret_cast<f32x4_t *>(a.part + part_row * D + 32 * (int)db + 8 * (int)i + 4 * h) =
-                        f32x4_t{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
-                });
+        static_for<0, ND>([&](auto db) {
+            static_for<0, 4>([&](auto i) {
+                const f32x4_t v = {o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+                const int d = 32 * (int)db + 8 * (int)i + 4 * h;
+                if (a.split) *reinterpret_cast<f16x4_t *>(a.part + part_row * D + d) = __builtin_convertvector(v * sc, f16x4_t);
+                else *reinterpret_cast<bf16x4_t *>(a.out + out_row * D + d) = __builtin_convertvector(v, bf16x4_t);
             });
-            if (h == 0) *reinterpret_cast<float2 *>(part_ml + 2 * part_row) = make_float2(m, l);
-        } else {
-            const float f = l == 0.f ? 0.f : 1.f / l;
-            static_for<0, ND>([&](auto db) {
-                static_for<0, 4>([&](auto i) {
-                    const f32x4_t v = f32x4_t{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]} * f;
-                    *reinterpret_cast<bf16x4_t *>(a.out + out_row * D + 32 * (int)db + 8 * (int)i + 4 * h) =
-                        __builtin_convertvector(v, bf16x4_t);
-                });
-            });
-            if (h == 0) a.lse[out_row] = kLn2 * (m + log2f(l));
+        });
+        if (h == 0) {
+            if (a.split) a.record[part_row] = make_float4(m, l, l / sc, 0.f);
+            else a.lse[out_row] = kLn2 * (m + log2f(l));
         }
     }
 }
 
-// Joins the chunks of every row: a work group has 256 / (D / 4) q heads of one
-// node (blockIdx.x the active cell and node, blockIdx.y the heads), a thread
-// four values of a row.  The lanes of a row read its chunks' maxima and sums
-// together, then each chunk's values with several loads in flight.
+// Joins the chunks of every row: a wave a row (blockIdx.x the active cell and
+// node, blockIdx.y four q heads).  Its lanes read a chunk's record each, then
+// D / 8 lanes a chunk its values, 64 / (D / 8) chunks at once.
 template <int D>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
-    constexpr int LPR = D / 4, ROWS = 256 / LPR;
-    __shared__ float s_w[ROWS][splice::kTreeMaxChunks];
+    constexpr int LPR = D / 8, SP = 64 / LPR;
+    static_assert(splice::kTreeMaxChunks == 64, "a chunk a lane");
     const TreeCall a = args.call;
     const int Hq = a.Hkv * a.G, ci = blockIdx.x / a.T, node = blockIdx.x % a.T;
     const uint32_t info = args.slots.info[ci];
     const int64_t at_node = (int64_t)(info & 255) * a.T + node;
-    if (a.depth[at_node] < 0) return;
-    const int rw = threadIdx.x / LPR, l = threadIdx.x % LPR, hd = blockIdx.y * ROWS + rw;
+    const int lane = threadIdx.x & 63, hd = blockIdx.y * 4 + (threadIdx.x >> 6);
     const int first = (int)(info >> 16), n = (int)(args.slots.info[ci + 1] >> 16) - first;
-    const bool on = hd < Hq;
-    const int64_t stride = (int64_t)a.T * Hq, row = (int64_t)first * stride + (int64_t)node * Hq + (on ? hd : 0);
-    const float *ml = a.part + (int64_t)a.n_slots * stride * D;
-    constexpr int PER = splice::kTreeMaxChunks / LPR;
-    float ms[PER], ls[PER], M = -INFINITY, L = 0.f;
-    static_for<0, PER>([&](auto i) {
-        const int s = l + (int)i * LPR;
-        ms[i] = -INFINITY;
-        ls[i] = 0.f;
-        if (s < n) {
-            const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * (row + s * stride));
-            ms[i] = x.x;
-            ls[i] = x.y;
-        }
-        M = fmaxf(M, ms[i]);
-    });
-    for (int o = 1; o < LPR; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-    const float Ms = M == -INFINITY ? 0.f : M;
-    static_for<0, PER>([&](auto i) {
-        const int s = l + (int)i * LPR;
-        const float f = fast_exp2(ms[i] - Ms);
-        if (s < n) s_w[rw][s] = f;
-        L = fmaf(f, ls[i], L);
-    });
-    for (int o = 1; o < LPR; o <<= 1) L += __shfl_xor(L, o);
-    __syncthreads();
-    if (!on) return;
-    const float *src = a.part + row * D + 4 * l;
-    f32x4_t O = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = 0; s < n; ++s) {
-        const float f = s_w[rw][s];
-        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(src + s * stride * D);
-        O += f == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : f * x;   // a chunk of nothing may hold anything
+    if (hd >= Hq || a.depth[at_node] < 0) return;
+    const int64_t stride = (int64_t)a.T * Hq, row = (int64_t)first * stride + (int64_t)node * Hq + hd;
+    float4 x = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    if (lane < n) x = a.record[row + lane * stride];
+    float M = x.x;
+    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    const float f = fast_exp2(x.x - (M == -INFINITY ? 0.f : M)), weight = f * x.z;
+    float L = f * x.y;
+    for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o);
+    const int sp = lane / LPR, l = lane % LPR;
+    const _Float16 *src = a.part + row * D + 8 * l;
+    f32x8_t O = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < n; s0 += 4 * SP) {
+        static_for<0, 4>([&](auto u) {
+            const int s = s0 + (int)u * SP + sp, from = min(s, n - 1);
+            float w = __shfl(weight, from);
+            if (s >= n) w = 0.f;
+            const f32x8_t v = __builtin_convertvector(*reinterpret_cast<const f16x8_t *>(src + from * stride * D), f32x8_t);
+            static_for<0, 8>([&](auto i) { O[(int)i] = w == 0.f ? O[(int)i] : fmaf(w, v[(int)i], O[(int)i]); });   // 0 * inf
+        });
     }
+    for (int o = LPR; o < 64; o <<= 1) static_for<0, 8>([&](auto i) { O[(int)i] += __shfl_xor(O[(int)i], o); });
     const int64_t at = at_node * Hq + hd;
-    const float f = L == 0.f ? 0.f : 1.f / L;
-    *reinterpret_cast<bf16x4_t *>(a.out + at * D + 4 * l) = __builtin_convertvector(O * f, bf16x4_t);
-    if (l == 0) a.lse[at] = kLn2 * (M + log2f(L));
+    const float r = L == 0.f ? 0.f : 1.f / L;
+    if (sp == 0) *reinterpret_cast<bf16x8_t *>(a.out + at * D + 8 * l) = __builtin_convertvector(O * r, bf16x8_t);
+    if (lane == 0) a.lse[at] = kLn2 * (M + log2f(L));
 }
 
 // Enqueues a call of plan p; 0 if a launch failed.
@@ -736,9 +742,8 @@ bool launch_tree(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hi
     }
     const TreeCall &c = a.call;
     if (!ok || !c.split) return ok;
-    const int heads = 256 / (D / 4);
-    hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)(c.n_active * c.T), (unsigned)((c.Hkv * c.G + heads - 1) / heads)),
-                       dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)(c.n_active * c.T), (unsigned)((c.Hkv * c.G + 3) / 4)), dim3(256),
+                       0, stream, a);
     return hipGetLastError() == hipSuccess;
 }
 

@@ -85,7 +85,7 @@ constexpr int kTreeMaxChunks = 64;
 struct TreePlan {
     int row_waves, row_tiles, per, n_slots;
     bool split;     // some cell has more than one chunk
-    size_t bytes;   // partial results: [slot][node][q head] of D + 2 floats
+    size_t bytes;   // partial results: [slot][node][q head] of D fp16 and four floats
 };
 
 // An active cell: its index, the depth from which its nodes are spliced (64:
@@ -118,7 +118,7 @@ inline void tree_slots(const TreeCells &cells, const uint8_t *onset, const int *
                 }
 }
 
-inline size_t tree_slot_bytes(const splice_shape &sh, int T) { return (size_t)T * sh.n_q_heads * (sh.head_dim + 2) * 4; }
+inline size_t tree_slot_bytes(const splice_shape &sh, int T) { return (size_t)T * sh.n_q_heads * (2 * sh.head_dim + 16); }
 
 // The most tiles that a cell at `step` walks: prompt slots (a replaced span
 // twice when nodes on both sides of the onset may share a row tile) and
