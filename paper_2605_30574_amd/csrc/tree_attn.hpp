@@ -94,6 +94,7 @@ struct TreeTile {
     static constexpr int NL = TK * CPR / NT;                   // chunks a thread loads of a K (or V) tile
     static constexpr int NL8 = NL / 2;                         // ... of 8-bit rows
     static constexpr int NR = OWN ? NL : NL8;                  // ... by way of registers
+    static constexpr bool EARLY = !OWN && KB == 1 && D <= 128; // values are read before the softmax
     static constexpr int ND = D / 32;                          // 32-wide d blocks of the output
     static_assert(RW * KW == 4 && NL8 >= 1 && (KW == 1 || KW * 32 * RW * D * 4 <= TILES), "");
 };
@@ -470,6 +471,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             __syncthreads();   // every wave's part of tile t is in LDS, and tile t - 1 has been read
         }
         const TreeTileRef next = tile_of();
+        // the matrix products of one wave go before the softmax of another on its SIMD
+        __builtin_amdgcn_s_setprio(1);
         if (t + t_step < t1) {
             load(b ^ 1);
             advance();
@@ -495,6 +498,13 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
                 s[kb] = product(ka[st], q, s[kb]);
             });
         });
+        // with registers to spare the values are on their way while the softmax runs
+        u32x4_t vv[X::EARLY ? 2 * KB : 1][ND];
+        if constexpr (X::EARLY) {
+            static_for<0, 2 * KB>([&](auto kk) { static_for<0, ND>([&](auto db) { vv[kk][db] = values(buf, db, kk); }); });
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
         if (cur.edge || (careful && cur.other)) {
             const uint64_t see = seen(cur) >> 4 * h;
             static_for<0, KB>([&](auto kb) {
@@ -528,7 +538,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             });
         });
         static_for<0, ND>([&](auto db) {
-            static_for<0, 2 * KB>([&](auto kk) { o[db] = product(values(buf, db, kk), pb[kk], o[db]); });
+            static_for<0, 2 * KB>([&](auto kk) {
+                if constexpr (X::EARLY) o[db] = product(vv[kk][db], pb[kk], o[db]);
+                else o[db] = product(values(buf, db, kk), pb[kk], o[db]);
+            });
         });
         }
         cur = next;
