@@ -48,7 +48,8 @@ struct TreeCall {
     // and in 32 bits they would be 53% of what a call of many chunks writes and reads again.
     _Float16 *part;
     float4 *record;
-    int T, G, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, n_slots, per;
+    int T, G, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, per;
+    int n_p, p_tiles;   // packed calls: chunks of the prompt and tiles of 128 rows; else 0
     bool split;
     float qk_scale;   // scale * log2(e)
 };
@@ -179,63 +180,120 @@ __device__ __forceinline__ u32x4_t finite_only(u32x4_t w) {
     return w;
 }
 
-template <int D, int RW, bool F8>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs args) {
-    const TreeCall a = args.call;   // what the lambdas use: captured, the whole arguments would go to memory
+// One work group's item.  PACKED: 128 rows of any cells of a KV head over a chunk of
+// the prompt; otherwise rows of one cell over a chunk of its list, which in a
+// packed call is that of its generated rows.
+template <int D, int RW, bool F8, bool PACKED>
+__device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
     using X = TreeTile<D, RW>;
     constexpr int KW = X::KW, KB = X::KB, TK = X::TK, ND = X::ND, NST = D / 16;
     extern __shared__ __align__(16) char lds[];
     __shared__ int s_bad, s_again;
     __shared__ TreeSegment s_seg[5];
+    __shared__ int s_rows[PACKED ? 4 : 1][4];
     __shared__ float s_ml[KW > 1 ? KW : 1][32 * RW][2];
+    const TreeCall a = args.call;   // what the lambdas use: captured, the whole arguments would go to memory
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, h = lane >> 5, rw = wave % RW, kw = wave / RW;
 
     // ---- which rows: KV heads run fastest, so that with eight (or a multiple) an XCD keeps to its own
-    const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, place = rest / a.row_tiles, rt = rest % a.row_tiles;
-    const uint32_t here = args.slots.order[place >> 1] >> (16 * (place & 1));
-    const int ci = here & 255, chunk = (here >> 8) & 255;
-    const uint32_t info = args.slots.info[ci];
-    const int c = info & 255, onset = (info >> 8) & 255, slot = (int)(info >> 16) + chunk, step = args.step[ci], rows = a.T * a.G;
-    const bool last_chunk = slot + 1 == (int)(args.slots.info[ci + 1] >> 16);
-    const int row0 = 32 * RW * rt, row = row0 + 32 * rw + r;
-    const int64_t node0 = (int64_t)c * a.T;
-    int d_node = lane < a.T ? a.depth[node0 + lane] : -1;   // lane u: node u's depth
-    d_node = min(d_node, a.T - 1);
-    const uint64_t alive = __ballot(d_node >= 0);
-    const uint64_t mine = bits(row0 / a.G, min(row0 + 32 * RW - 1, rows - 1) / a.G + 1) & alive;   // the work group's nodes
-    if (mine == 0) return;
-    const int node = min(row / a.G, a.T - 1), depth = __shfl(d_node, node), p0 = a.Tp + step;
-    const bool valid = row < rows && depth >= 0;
-    const bool spliced = depth >= onset;
-    const int low = a.window > 0 ? p0 + max(depth, 0) - a.window + 1 : 0;   // first position the row sees
-    uint64_t word = valid ? a.visible[node0 + node] & alive : 0;
-    if (a.window > 0 && a.window < a.T) {
-        for (int u = 0; u < a.T; ++u)
-            if (depth - __shfl(d_node, u) >= a.window) word &= ~(1ull << u);
+    const int g = block % a.Hkv, rest = block / a.Hkv, rows = a.T * a.G;
+    int row0, row, chunk, slot, step = 0, node, depth, low, low_all, low_max;
+    int64_t node0, pair = 0;
+    bool last_chunk = false, valid, spliced, any_clean, any_donor;
+    uint64_t alive = 0, word = 0;
+    if constexpr (PACKED) {
+        chunk = rest / a.p_tiles;
+        row0 = 0;
+        const int at = 32 * RW * (rest % a.p_tiles) + 32 * rw + r, n_rows = a.n_active * rows;
+        const int ci = min(at, n_rows - 1) / rows;
+        row = at - ci * rows;
+        const uint32_t info = args.slots.info[ci];
+        const int at_step = args.step[ci];
+        node0 = (int64_t)(info & 255) * a.T;
+        slot = (int)(info >> 16) + chunk;
+        node = min(row / a.G, a.T - 1);
+        depth = min(a.depth[node0 + node], a.T - 1);
+        valid = at < n_rows && depth >= 0;
+        spliced = depth >= (int)((info >> 8) & 255);
+        low = a.window > 0 ? a.Tp + at_step + max(depth, 0) - a.window + 1 : 0;   // first position the row sees
+        int lo = valid ? low : INT32_MAX, hi = valid ? low : INT32_MIN;
+        for (int o = 32; o > 0; o >>= 1) {
+            lo = min(lo, __shfl_xor(lo, o));
+            hi = max(hi, __shfl_xor(hi, o));
+        }
+        const int clean = __any(valid && !spliced), donor = __any(valid && spliced);
+        if (lane == 0) {
+            s_rows[wave][0] = lo;
+            s_rows[wave][1] = hi;
+            s_rows[wave][2] = clean;
+            s_rows[wave][3] = donor;
+        }
+        __syncthreads();
+        static_for<0, 4>([&](auto w) {
+            lo = min(lo, s_rows[w][0]);
+            hi = max(hi, s_rows[w][1]);
+        });
+        any_clean = __builtin_amdgcn_readfirstlane(s_rows[0][2] | s_rows[1][2] | s_rows[2][2] | s_rows[3][2]) != 0;
+        any_donor = __builtin_amdgcn_readfirstlane(s_rows[0][3] | s_rows[1][3] | s_rows[2][3] | s_rows[3][3]) != 0;
+        if (!any_clean && !any_donor) return;
+        low_all = __builtin_amdgcn_readfirstlane(max(lo, 0));   // some row sees from here on,
+        low_max = __builtin_amdgcn_readfirstlane(hi);           // every row from here on
+    } else {
+        const int place = rest / a.row_tiles, rt = rest % a.row_tiles;
+        const uint32_t here = args.slots.order[place >> 1] >> (16 * (place & 1));
+        const int ci = here & 255;
+        chunk = (here >> 8) & 255;
+        const uint32_t info = args.slots.info[ci];
+        const int c = info & 255, onset = (info >> 8) & 255;
+        slot = (int)(info >> 16) + a.n_p + chunk;
+        step = args.step[ci];
+        last_chunk = slot + 1 == (int)(args.slots.info[ci + 1] >> 16);
+        row0 = 32 * RW * rt;
+        row = row0 + 32 * rw + r;
+        node0 = (int64_t)c * a.T;
+        pair = (int64_t)c * a.Hkv + g;
+        int d_node = lane < a.T ? a.depth[node0 + lane] : -1;   // lane u: node u's depth
+        d_node = min(d_node, a.T - 1);
+        alive = __ballot(d_node >= 0);
+        const uint64_t mine = bits(row0 / a.G, min(row0 + 32 * RW - 1, rows - 1) / a.G + 1) & alive;   // the work group's nodes
+        if (mine == 0) return;
+        node = min(row / a.G, a.T - 1);
+        depth = __shfl(d_node, node);
+        const int p0 = a.Tp + step;
+        valid = row < rows && depth >= 0;
+        spliced = depth >= onset;
+        low = a.window > 0 ? p0 + max(depth, 0) - a.window + 1 : 0;
+        word = valid ? a.visible[node0 + node] & alive : 0;
+        if (a.window > 0 && a.window < a.T) {
+            for (int u = 0; u < a.T; ++u)
+                if (depth - __shfl(d_node, u) >= a.window) word &= ~(1ull << u);
+        }
+        // of the work group's nodes: the least and the largest depth, and whether spliced and unspliced ones are there
+        const bool in = (mine >> lane) & 1;
+        int d_min = in ? d_node : SPLICE_MAX_NODES, d_max = in ? d_node : 0;
+        for (int o = 32; o > 0; o >>= 1) {
+            d_min = min(d_min, __shfl_xor(d_min, o));
+            d_max = max(d_max, __shfl_xor(d_max, o));
+        }
+        d_min = __builtin_amdgcn_readfirstlane(d_min);
+        d_max = __builtin_amdgcn_readfirstlane(d_max);
+        any_clean = d_min < onset;
+        any_donor = d_max >= onset;
+        low_all = a.window > 0 ? max(p0 + d_min - a.window + 1, 0) : 0;
+        low_max = a.window > 0 ? p0 + d_max - a.window + 1 : 0;
     }
-    // of the work group's nodes: the least and the largest depth, and whether spliced and unspliced ones are there
-    const bool in = (mine >> lane) & 1;
-    int d_min = in ? d_node : SPLICE_MAX_NODES, d_max = in ? d_node : 0;
-    for (int o = 32; o > 0; o >>= 1) {
-        d_min = min(d_min, __shfl_xor(d_min, o));
-        d_max = max(d_max, __shfl_xor(d_max, o));
-    }
-    d_min = __builtin_amdgcn_readfirstlane(d_min);
-    d_max = __builtin_amdgcn_readfirstlane(d_max);
-    const bool any_clean = d_min < onset, any_donor = d_max >= onset;
-    const int low_all = a.window > 0 ? max(p0 + d_min - a.window + 1, 0) : 0;   // some row sees from here on,
-    const int low_max = a.window > 0 ? p0 + d_max - a.window + 1 : 0;           // every row from here on
 
     // ---- the list of keys: segments 0 to 4, walked tile by tile
     const int b0 = min(low_all, a.Tp), sa = min(max(a.span_lo, b0), a.Tp), sb = max(a.span_hi, sa);
     const int g0 = min(max(low_all - a.Tp, 0), step);
     const size_t head_p = (size_t)g * a.Tp * X::ROW;
-    const int64_t pair = (int64_t)c * a.Hkv + g;
+    const bool prompt = PACKED || a.n_p == 0;   // a packed call's prompt has items of its own
     if (tid < 5) {
         const int i = tid, row_bytes = F8 && i == 4 ? D : X::ROW;
         int begin = i == 0 ? b0 : (i == 3 ? sb : (i == 4 ? g0 : sa)), end = begin;
-        if (i == 4) end = step + a.T;
+        if (i == 4) end = PACKED ? begin : step + a.T;
+        else if (!prompt) end = begin;
         else if (i == 0) end = any_donor ? sa : a.Tp;
         else if (any_donor) end = i == 3 ? a.Tp : ((i == 1 ? any_clean : !a.zero_donor) ? sb : begin);
         const char *k = i == 4 ? a.gk + pair * a.cap * row_bytes : pick_base(i == 2, a.ck, a.dk) + head_p;
@@ -247,7 +305,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     int n_tiles = 0;
     static_for<0, 5>([&](auto i) { n_tiles += (s_seg[i].len + TK - 1) / TK; });
     n_tiles = __builtin_amdgcn_readfirstlane(n_tiles);
-    const int t0 = min(chunk * a.per, n_tiles), t1 = last_chunk ? n_tiles : min(t0 + a.per, n_tiles);
+    const int t0 = PACKED ? n_tiles * chunk / a.n_p : min(chunk * a.per, n_tiles);
+    const int t1 = PACKED ? n_tiles * (chunk + 1) / a.n_p : (last_chunk ? n_tiles : min(t0 + a.per, n_tiles));
     TreeWalk w;
     // `skip` tiles on from the end of segment i - 1, over the segments that are shorter
     auto enter = [&](int i, int skip) {
@@ -270,8 +329,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
         x.key0 = w.key0;
         x.n = min(TK, w.rem);
         x.other = any_clean && any_donor && (w.seg == 1 || w.seg == 2);
-        x.dead = w.seg == 4 && w.key0 + TK > step && alive != bits(0, a.T);
-        x.differ = x.other || (w.seg == 4 ? a.Tp + w.key0 < low_max || w.key0 + TK > step : w.key0 < low_max);
+        const bool gen = !PACKED && w.seg == 4;
+        x.dead = gen && w.key0 + TK > step && alive != bits(0, a.T);
+        x.differ = x.other || (gen ? a.Tp + w.key0 < low_max || w.key0 + TK > step : w.key0 < low_max);
         x.edge = x.n < TK || (x.differ && !x.other) || (x.other && w.key0 < low_max);
         return x;
     };
@@ -376,7 +436,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             const int u = (int)i * X::NT + ltid, key = u / X::CPR, nd = x.key0 + key - step;
             u32x4_t *p = reinterpret_cast<u32x4_t *>(buf + X::TILE + u * 16);
             const u32x4_t v = *p;
-            if (x.seg == 4 && nd >= 0 && (nd >= 64 || !((alive >> nd) & 1))) {
+            if (!PACKED && x.seg == 4 && nd >= 0 && (nd >= 64 || !((alive >> nd) & 1))) {
                 *p = u32x4_t{0, 0, 0, 0};
             } else if (has_non_finite(v)) {
                 *p = finite_only(v);
@@ -387,7 +447,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     // Bit k: the lane's row sees key k of the tile, from the wave's first key on.
     auto seen = [&](const TreeTileRef &x) {
         const int skip = X::OWN ? 0 : kw * 32 * KB, first = x.key0 + skip, n = x.n - skip;
-        if (x.seg == 4)
+        if (!PACKED && x.seg == 4)
             return bits(low - a.Tp - first, min(step - first, n)) | (shifted(word, step - first) & bits(step - first, n));
         return x.other && (x.seg == 2) != spliced ? 0 : bits(low - first, n);
     };
@@ -446,7 +506,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
     m = -INFINITY;
     l = 0.f;
     // keys of the ZERO donor score 0 and add nothing to o
-    if (a.zero_donor && spliced && chunk == 0 && kw == 0) {
+    if (a.zero_donor && prompt && spliced && chunk == 0 && kw == 0) {
         const int n_zero = a.span_hi - max(a.span_lo, max(low, 0));
         if (n_zero > 0) {
             m = 0.f;
@@ -665,15 +725,28 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs ar
             static_for<0, 4>([&](auto i) {
                 const f32x4_t v = {o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
                 const int d = 32 * (int)db + 8 * (int)i + 4 * h;
-                if (a.split) *reinterpret_cast<f16x4_t *>(a.part + part_row * D + d) = __builtin_convertvector(v * sc, f16x4_t);
+                if (PACKED || a.split) *reinterpret_cast<f16x4_t *>(a.part + part_row * D + d) = __builtin_convertvector(v * sc, f16x4_t);
                 else *reinterpret_cast<bf16x4_t *>(a.out + out_row * D + d) = __builtin_convertvector(v, bf16x4_t);
             });
         });
         if (h == 0) {
-            if (a.split) a.record[part_row] = make_float4(m, l, l / sc, 0.f);
+            if (PACKED || a.split) a.record[part_row] = make_float4(m, l, l / sc, 0.f);
             else a.lse[out_row] = kLn2 * (m + log2f(l));
         }
     }
+}
+
+template <int D, int RW, bool F8>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs args) {
+    tree_item<D, RW, F8, false>(args, (int)blockIdx.x);
+}
+
+// Items of the prompt, then items of the generated rows.
+template <int D, int RW, bool F8>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_packed_kernel(TreeArgs args) {
+    const int n = args.call.p_tiles * args.call.n_p * args.call.Hkv;
+    if ((int)blockIdx.x < n) tree_item<D, 4, false, true>(args, (int)blockIdx.x);
+    else tree_item<D, RW, F8, false>(args, (int)blockIdx.x - n);
 }
 
 // Joins the chunks of every row: a wave a row (blockIdx.x the active cell and
@@ -720,39 +793,49 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
 // Enqueues a call of plan p; 0 if a launch failed.
 typedef bool (*TreeLaunch)(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hipStream_t stream);
 
-template <int D, int RW, bool F8>
-bool launch_tree_kernel(const TreeArgs &args, hipStream_t stream) {
-    using X = TreeTile<D, RW>;
+template <int D, int RW, bool F8, bool PACKED>
+bool launch_tree_kernel(const TreeArgs &args, int blocks, hipStream_t stream) {
+    constexpr int LDS = PACKED && TreeTile<D, 4>::LDS > TreeTile<D, RW>::LDS ? TreeTile<D, 4>::LDS : TreeTile<D, RW>::LDS;
+    void (*kernel)(TreeArgs);
+    if constexpr (PACKED) kernel = tree_packed_kernel<D, RW, F8>;
+    else kernel = tree_kernel<D, RW, F8>;
     // more LDS than a kernel may take unasked; asked once a device
     static std::atomic<uint64_t> raised{0};
     int dev = 0;
-    if (X::LDS > 64 << 10) {
+    if (LDS > 64 << 10) {
         if (hipGetDevice(&dev) != hipSuccess) return false;
         const uint64_t bit = 1ull << (dev & 63);
         if (!(raised.load() & bit)) {
-            if (hipFuncSetAttribute(reinterpret_cast<const void *>(&tree_kernel<D, RW, F8>),
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, X::LDS) != hipSuccess)
+            if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) !=
+                hipSuccess)
                 return false;
             raised.fetch_or(bit);
         }
     }
-    const unsigned blocks = (unsigned)((int64_t)args.call.Hkv * args.call.n_slots * args.call.row_tiles);
-    hipLaunchKernelGGL((tree_kernel<D, RW, F8>), dim3(blocks), dim3(256), X::LDS, stream, args);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), LDS, stream, args);
     return hipGetLastError() == hipSuccess;
 }
 
 template <int D>
 bool launch_tree(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hipStream_t stream) {
     const bool f8 = kv_format == SPLICE_KV_E4M3;
-    bool ok;
-    if constexpr (D <= 128) {
-        if (p.row_waves == 1) ok = f8 ? launch_tree_kernel<D, 1, true>(a, stream) : launch_tree_kernel<D, 1, false>(a, stream);
-        else if (p.row_waves == 2) ok = f8 ? launch_tree_kernel<D, 2, true>(a, stream) : launch_tree_kernel<D, 2, false>(a, stream);
-        else ok = f8 ? launch_tree_kernel<D, 4, true>(a, stream) : launch_tree_kernel<D, 4, false>(a, stream);
-    } else {
-        if (p.row_waves == 2) ok = f8 ? launch_tree_kernel<D, 2, true>(a, stream) : launch_tree_kernel<D, 2, false>(a, stream);
-        else ok = f8 ? launch_tree_kernel<D, 4, true>(a, stream) : launch_tree_kernel<D, 4, false>(a, stream);
-    }
+    bool ok = false;
+    auto go = [&](auto rw) {
+        constexpr int RW = decltype(rw)::value;
+        if (p.row_waves != RW) return;
+        if constexpr (RW < 4) {
+            if (p.n_p > 0) {
+                ok = f8 ? launch_tree_kernel<D, RW, true, true>(a, p.blocks, stream)
+                        : launch_tree_kernel<D, RW, false, true>(a, p.blocks, stream);
+                return;
+            }
+        }
+        ok = f8 ? launch_tree_kernel<D, RW, true, false>(a, p.blocks, stream)
+                : launch_tree_kernel<D, RW, false, false>(a, p.blocks, stream);
+    };
+    if constexpr (D <= 128) go(std::integral_constant<int, 1>{});
+    go(std::integral_constant<int, 2>{});
+    go(std::integral_constant<int, 4>{});
     const TreeCall &c = a.call;
     if (!ok || !c.split) return ok;
     hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)(c.n_active * c.T), (unsigned)((c.Hkv * c.G + 3) / 4)), dim3(256),

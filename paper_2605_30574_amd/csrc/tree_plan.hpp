@@ -83,39 +83,41 @@ constexpr int kTreeStart = 4;     // what a work group costs beside its tiles, i
 constexpr int kTreeMaxChunks = 64;
 
 struct TreePlan {
-    int row_waves, row_tiles, per, n_slots;
-    bool split;     // some cell has more than one chunk
-    size_t bytes;   // partial results: [slot][node][q head] of D fp16 and four floats
+    int row_waves, row_tiles, per;
+    int n_p, p_tiles;      // packed: chunks of the prompt, tiles of 128 rows; else 0
+    int n_slots, blocks;   // partial results a (node, q head) may have, over all cells; work groups
+    bool split;            // some cell has more than one chunk
+    size_t bytes;          // partial results: [slot][node][q head] of D fp16 and four floats
 };
 
 // An active cell: its index, the depth from which its nodes are spliced (64:
-// none) and its first slot (there is one more, for the end).  A slot of
-// the grid: its active cell and chunk, two slots a word; chunks of one number
+// none) and its first slot (there is one more, for the end).  An item of the
+// grid: its active cell and chunk, two items a word; chunks of one number
 // stand together, so that work groups that run together read the same part of
-// the prompt, and among them the unspliced cells, which read the clean span.
+// the prompt, and the active cells are in the order of their class (unspliced,
+// on both sides of the onset, spliced), so that they read the same span.
 struct TreeSlots {
     uint32_t info[SPLICE_MAX_CELLS + 1];   // cell | onset << 8 | first slot << 16
     uint32_t order[kTreeMaxSlots / 2];     // active cell | chunk << 8, in 16 bits
 };
 
-inline void tree_slots(const TreeCells &cells, const uint8_t *onset, const int *tiles, int n, int per, TreeSlots &out) {
+inline void tree_slots(const TreeCells &cells, const uint8_t *onset, const int *tiles, int n, const TreePlan &p, TreeSlots &out) {
     uint32_t first = 0;
     int most = 0;
     for (int i = 0; i < n; ++i) {
         out.info[i] = cells.cell[i] | (uint32_t)onset[i] << 8 | first << 16;
-        first += (uint32_t)ceil_div(tiles[i], per);
+        first += (uint32_t)(p.n_p + ceil_div(tiles[i], p.per));
         most = tiles[i] > most ? tiles[i] : most;
     }
     out.info[n] = first << 16;
     int at = 0;
-    for (int chunk = 0; chunk * per < most; ++chunk)
-        for (int spliced = 0; spliced < 2; ++spliced)
-            for (int i = 0; i < n; ++i)
-                if ((onset[i] < SPLICE_MAX_NODES) == (spliced == 1) && chunk * per < tiles[i]) {
-                    const uint32_t x = (uint32_t)i | (uint32_t)chunk << 8;
-                    out.order[at / 2] = at % 2 ? out.order[at / 2] | x << 16 : x;
-                    ++at;
-                }
+    for (int chunk = 0; chunk * p.per < most; ++chunk)
+        for (int i = 0; i < n; ++i)
+            if (chunk * p.per < tiles[i]) {
+                const uint32_t x = (uint32_t)i | (uint32_t)chunk << 8;
+                out.order[at / 2] = at % 2 ? out.order[at / 2] | x << 16 : x;
+                ++at;
+            }
 }
 
 inline size_t tree_slot_bytes(const splice_shape &sh, int T) { return (size_t)T * sh.n_q_heads * (2 * sh.head_dim + 16); }
@@ -123,12 +125,15 @@ inline size_t tree_slot_bytes(const splice_shape &sh, int T) { return (size_t)T 
 // The most tiles that a cell at `step` walks: prompt slots (a replaced span
 // twice when nodes on both sides of the onset may share a row tile) and
 // generated rows; every segment may end in a tile of its own.
-inline int tree_tiles(const splice_shape &sh, const splice_call &call, int T, int tile, int64_t step, bool spliced, bool mixed) {
+// prompt, gen: whether the parts count.
+inline int tree_tiles(const splice_shape &sh, const splice_call &call, int T, int tile, int64_t step, bool spliced, bool mixed,
+                      bool prompt, bool gen) {
     int64_t low = call.window > 0 ? sh.prompt_len + step - call.window + 1 : 0;   // the first position that the root sees
     if (low < 0) low = 0;
     const int64_t Tp = sh.prompt_len, b0 = low < Tp ? low : Tp, g0 = low > Tp ? (low - Tp < step ? low - Tp : step) : 0;
     const int64_t sa = sh.span_lo > b0 ? sh.span_lo : b0, sb = sh.span_hi > sa ? sh.span_hi : sa;
-    int64_t n = ceil_div(step + T - g0, tile);
+    int64_t n = gen ? ceil_div(step + T - g0, tile) : 0;
+    if (!prompt) return (int)n;
     if (!spliced) return (int)(n + ceil_div(Tp - b0, tile));
     n += ceil_div(sa - b0, tile) + ceil_div(Tp - sb, tile);
     const int span = ceil_div(sb - sa, tile);
@@ -141,14 +146,22 @@ inline int64_t tree_chunks(const int *tiles, int n, int per) {
     return slots;
 }
 
+// A packed call: the cells' rows of a KV head, 128 a work group, share the
+// prompt's tiles, and each cell's generated rows have items of their own.
+constexpr int kTreeMaxPrompt = 16;     // chunks of the prompt
+constexpr int kTreePackedTiles = 4;    // tiles of prompt that a call has at least
+
 // Chunks of equal length, so that the work groups of all cells fill k rounds
 // of what the GPU holds at once; k is the one that takes least by
-// k * (per + kTreeStart).
-inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, int n_cu) {
+// k * (per + kTreeStart).  tiles: of the cells' lists, in a packed call without
+// the prompt, whose list is prompt_tiles long.
+inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, int n_cu, bool packed,
+                          int prompt_tiles) {
     TreePlan p;
     const int rows = T * group_of(sh);
     p.row_waves = tree_row_waves(sh.head_dim, rows);
     p.row_tiles = ceil_div(rows, 32 * p.row_waves);
+    p.n_p = p.p_tiles = 0;
     const int tile = tree_tile_keys(sh.head_dim, p.row_waves), step = p.row_waves == 1 ? 4 : 1;   // four waves, four tiles
     const int64_t items = (int64_t)sh.n_kv_heads * p.row_tiles, room = (int64_t)n_cu * tree_resident(sh.head_dim);
     int64_t sum = 0;
@@ -157,7 +170,8 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
         sum += tiles[i];
         most = tiles[i] > most ? tiles[i] : most;
     }
-    const int least = step * ceil_div(most, (int64_t)step * kTreeMaxChunks);   // no cell in more than kTreeMaxChunks
+    const int most_chunks = kTreeMaxChunks - (packed ? kTreeMaxPrompt : 0);
+    const int least = step * ceil_div(most, (int64_t)step * most_chunks);   // no cell in more than kTreeMaxChunks
     auto fits = [&](int per, int64_t limit) { return tree_chunks(tiles, n, per) <= limit; };
     if (call.split_keys > 0) {
         p.per = step * ceil_div(call.split_keys, tile * step);
@@ -181,21 +195,53 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
         }
     }
     p.n_slots = (int)tree_chunks(tiles, n, p.per);
+    p.blocks = (int)(items * p.n_slots);
     p.split = p.n_slots > n;
+    if (packed) {
+        p.p_tiles = ceil_div((int64_t)n * rows, 128);
+        const int64_t row_items = (int64_t)sh.n_kv_heads * p.p_tiles;
+        int64_t best = INT64_MAX;
+        for (int np = 1; np <= kTreeMaxPrompt && np <= prompt_tiles; ++np) {
+            if (np > 1 && call.split_keys == 0 && row_items * np > kTreeRounds * room) break;
+            const int64_t per = ceil_div(prompt_tiles, np);
+            const int64_t cost = call.split_keys > 0 ? (per * 64 >= call.split_keys ? -np : np)
+                                                     : ceil_div(row_items * np, room) * (per + kTreeStart);
+            if (cost < best) {
+                best = cost;
+                p.n_p = np;
+            }
+        }
+        p.blocks += (int)(row_items * p.n_p);
+        p.n_slots += n * p.n_p;
+        p.split = true;
+    }
     p.bytes = p.split ? p.n_slots * tree_slot_bytes(sh, T) : 0;
     return p;
+}
+
+// Whether n active cells share the prompt's tiles.
+inline bool tree_packed(const splice_shape &sh, int T, int n, int prompt_tiles) {
+    const int rows = T * group_of(sh);
+    return rows <= 64 && (int64_t)n * rows >= 64 && n > 1 && prompt_tiles >= kTreePackedTiles;
 }
 
 // Bytes that no plan of this shape passes, whatever the steps.
 inline size_t tree_most_bytes(const splice_shape &sh, const splice_call &call, int T, int n_cu) {
     const int rows = T * group_of(sh), rw = tree_row_waves(sh.head_dim, rows);
-    const int64_t items = (int64_t)sh.n_kv_heads * ceil_div(rows, 32 * rw);
-    int64_t slots = kTreeMaxSlots;
-    if (call.split_keys == 0 && (int64_t)kTreeRounds * n_cu * tree_resident(sh.head_dim) / items < slots)
-        slots = (int64_t)kTreeRounds * n_cu * tree_resident(sh.head_dim) / items;
-    const int64_t chunks = (int64_t)sh.n_cells * kTreeMaxChunks;
-    slots = slots < chunks ? slots : chunks;
-    return slots * tree_slot_bytes(sh, T);
+    const int64_t items = (int64_t)sh.n_kv_heads * ceil_div(rows, 32 * rw), room = (int64_t)kTreeRounds * n_cu * tree_resident(sh.head_dim);
+    int64_t most = 0;
+    for (int n = 1; n <= sh.n_cells; ++n) {
+        int64_t slots = call.split_keys == 0 && room / items < kTreeMaxSlots ? room / items : kTreeMaxSlots;
+        slots = slots < (int64_t)n * kTreeMaxChunks ? slots : (int64_t)n * kTreeMaxChunks;
+        slots = slots > n ? slots : n;
+        if (tree_packed(sh, T, n, INT32_MAX)) {
+            int64_t np = room / ((int64_t)sh.n_kv_heads * ceil_div((int64_t)n * rows, 128));
+            np = call.split_keys > 0 || np > kTreeMaxPrompt ? kTreeMaxPrompt : (np > 1 ? np : 1);
+            slots += n * np;
+        }
+        most = slots > most ? slots : most;
+    }
+    return most * tree_slot_bytes(sh, T);
 }
 
 }  // namespace splice

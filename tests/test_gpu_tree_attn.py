@@ -212,3 +212,91 @@ def test_far_rows_of_a_large_cache():
     got = s.attend(64)
     s.expected = lambda: want
     s.check(*got, "far rows")
+
+
+# ---------------------------------------------------------------- many cells over one prompt
+
+def many(seed, C, T, Tp=400, window=0, **kw):
+    """Cells of every class: never spliced, from their first step on, from a depth within the tree on; some finished."""
+    rng = np.random.default_rng(seed)
+    cap = T + 60
+    steps = rng.integers(0, cap - T + 1, C)
+    if C > 4:
+        steps[C // 2] = -1
+    LW = [[9, 0] if c % 3 == 0 else ([0, 0] if c % 3 == 1 else [1, max(int(steps[c]), 0) + 1 + c % 2]) for c in range(C)]
+    span = kw.pop("span", (Tp // 5, Tp - Tp // 7))
+    return Sweep(seed, C=C, T=T, Tp=Tp, span=span, cap=cap, steps=steps, LW=LW, window=window, **kw)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads", [(8, 2, 64), (2, 2, 64), (8, 1, 128), (8, 2, 128), (8, 4, 256)])
+@pytest.mark.parametrize("C,T", [(17, 1), (40, 2), (12, 5), (9, 16), (2, 16)])
+def test_shared_prompt(C, T, heads, kv):
+    Hq, Hkv, D = heads
+    run(many(200 + C + T, C, T, Hq=Hq, Hkv=Hkv, D=D, kv=kv), what=f"shared prompt {C} {T} {heads} {kv}")
+
+
+@pytest.mark.parametrize("window", [1, 20, 64, 130, 300, 470])
+@pytest.mark.parametrize("donor", ["diff", "zero"])
+def test_shared_prompt_windows(window, donor):
+    run(many(211, 14, 6, window=window, donor=donor, D=128), what=f"shared prompt, window {window} {donor}")
+
+
+@pytest.mark.parametrize("span", [(0, 400), (0, 0), (1, 399), (64, 128), (399, 400)])
+@pytest.mark.parametrize("donor", ["diff", "zero"])
+def test_shared_prompt_spans(span, donor):
+    run(many(223, 11, 7, span=span, donor=donor, D=64), what=f"shared prompt, span {span} {donor}")
+
+
+@pytest.mark.parametrize("split", [64, 128, 1024])
+def test_shared_prompt_splits(split):
+    run(many(227, 13, 9, Tp=1100, D=128), split, what=f"shared prompt, split {split}")
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_shared_prompt_hides_what_is_not_seen(D):
+    """NaN and infinities in the clean span, which only unspliced nodes see, and in the donor's outside of the span."""
+    s = many(229, 12, 5, D=D, Hkv=4, window=450)
+    want = s.expected()
+    a, b = s.span
+    bad = torch.tensor([float("nan"), float("inf"), float("-inf"), 3.0e38], dtype=torch.bfloat16, device="cuda")
+    for x in s.donor:
+        x[:, :a] = float("nan")
+        x[:, b:, :4] = bad
+    s.expected = lambda: want
+    s.check(*s.attend(), "NaN in the donor's scaffold")
+    for x in s.clean:
+        x[:, a + 3:b - 5, :4] = bad
+    out, lse = s.attend()
+    torch.cuda.synchronize()
+    step = s.steps[:, None] + s.depth
+    on = (s.depth >= 0) & (s.steps[:, None] >= 0)
+    spliced = on & (s.layer >= s.LW[:, :1]) & (step >= s.LW[:, 1:])
+    assert (spliced.any(1) & (on & ~spliced).any(1)).any()
+    o, l = f64(out), f64(lse)
+    assert not np.isfinite(o[on & ~spliced]).all(-1).any()
+    o[on & ~spliced], l[on & ~spliced] = want[0][on & ~spliced], want[1][on & ~spliced]
+    s.check(torch.from_numpy(o), torch.from_numpy(l), "NaN in the clean span")
+
+
+def test_shared_prompt_of_every_cell():
+    """As many cells as a call takes, one node each, and cells of one tile of rows that are all finished."""
+    C = 256
+    s = many(233, C, 1, Hq=4, Hkv=1, D=64, Tp=300)
+    s.steps[32:64] = -1
+    run(s, what="256 cells")
+
+
+def test_large_values_keep_their_scale():
+    """Values far beyond fp16's range go through the partial results by a power of two."""
+    s = Sweep(239, C=2, T=9, D=128, Tp=900, span=(100, 800), cap=600, steps=[500, 20], LW=[[0, 0], [9, 0]])
+    out, lse = s.attend(128)
+    for x in (s.clean[1], s.donor[1], s.gen[1]):
+        x.mul_(2.0 ** 100)
+    big, lse2 = s.attend(128)
+    torch.cuda.synchronize()
+    assert torch.equal(lse, lse2)
+    on = torch.from_numpy(s.depth >= 0).cuda()
+    # the scaled partial results are rounded alike up to fp16's subnormals, the result after it
+    got, want = big[on].double() * 2.0 ** -100, out[on].double()
+    assert ((got - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -14).all()
