@@ -99,7 +99,9 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     for (int i = 1; i < n; ++i) min_step = sorted.step[i] < min_step ? sorted.step[i] : min_step;
     const int prompt_tiles = splice::tree_tiles(sh, checked, T, splice::tree_tile_keys(sh.head_dim, 4), min_step, n_of[1] + n_of[2] > 0,
                                                 n_of[1] > 0, true, false);
-    const bool packed = splice::tree_packed(sh, T, n, prompt_tiles);
+    int64_t prompt_keys = sh.prompt_len;   // that the first of them sees
+    if (call->window > 0 && (int64_t)call->window - min_step - 1 < prompt_keys) prompt_keys = (int64_t)call->window - min_step - 1;
+    const bool packed = splice::tree_packed(sh, *call, T, n, prompt_keys);
     int tiles[SPLICE_MAX_CELLS];
     const int tile = splice::tree_tile_keys(sh.head_dim, splice::tree_row_waves(sh.head_dim, T * splice::group_of(sh)));
     for (int i = 0; i < n; ++i)

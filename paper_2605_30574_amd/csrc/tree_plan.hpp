@@ -148,8 +148,20 @@ inline int64_t tree_chunks(const int *tiles, int n, int per) {
 
 // A packed call: the cells' rows of a KV head, 128 a work group, share the
 // prompt's tiles, and each cell's generated rows have items of their own.
-constexpr int kTreeMaxPrompt = 16;     // chunks of the prompt
-constexpr int kTreePackedTiles = 4;    // tiles of prompt that a call has at least
+// That takes another partial result a row, and pays where the cells together
+// walk much prompt: n cells times its keys times head_dim from 5 * 2^20 on
+// (us, apart / packed: 64 cells of 5 nodes, D = 128, 512 keys 24 / 33, 1024
+// 45 / 37, 2048 60 / 42; 40 cells of 12 nodes 512 keys 34 / 38, 2048 58 / 48; 8 cells
+// of 5 nodes 2048 keys 19 / 22; D = 256, 64 cells of one node 256 keys 21 / 25,
+// 1024 44 / 26; D = 64, 64 cells of 5 nodes 1024 keys 29 / 24). A call that sets
+// split_keys packs whenever it can.
+constexpr int kTreeMaxPrompt = 16;                 // chunks of the prompt
+constexpr int64_t kTreePackedWork = 5 << 20;
+
+inline bool tree_packed(const splice_shape &sh, const splice_call &call, int T, int n, int64_t prompt_keys) {
+    if (T * group_of(sh) > 64 || n < 2 || prompt_keys < 1) return false;
+    return call.split_keys > 0 || n * prompt_keys * sh.head_dim >= kTreePackedWork;
+}
 
 // Chunks of equal length, so that the work groups of all cells fill k rounds
 // of what the GPU holds at once; k is the one that takes least by
@@ -219,12 +231,6 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
     return p;
 }
 
-// Whether n active cells share the prompt's tiles.
-inline bool tree_packed(const splice_shape &sh, int T, int n, int prompt_tiles) {
-    const int rows = T * group_of(sh);
-    return rows <= 64 && (int64_t)n * rows >= 64 && n > 1 && prompt_tiles >= kTreePackedTiles;
-}
-
 // Bytes that no plan of this shape passes, whatever the steps.
 inline size_t tree_most_bytes(const splice_shape &sh, const splice_call &call, int T, int n_cu) {
     const int rows = T * group_of(sh), rw = tree_row_waves(sh.head_dim, rows);
@@ -234,7 +240,7 @@ inline size_t tree_most_bytes(const splice_shape &sh, const splice_call &call, i
         int64_t slots = call.split_keys == 0 && room / items < kTreeMaxSlots ? room / items : kTreeMaxSlots;
         slots = slots < (int64_t)n * kTreeMaxChunks ? slots : (int64_t)n * kTreeMaxChunks;
         slots = slots > n ? slots : n;
-        if (tree_packed(sh, T, n, INT32_MAX)) {
+        if (tree_packed(sh, call, T, n, sh.prompt_len)) {
             int64_t np = room / ((int64_t)sh.n_kv_heads * ceil_div((int64_t)n * rows, 128));
             np = call.split_keys > 0 || np > kTreeMaxPrompt ? kTreeMaxPrompt : (np > 1 ? np : 1);
             slots += n * np;

@@ -232,20 +232,23 @@ def many(seed, C, T, Tp=400, window=0, **kw):
 @pytest.mark.parametrize("heads", [(8, 2, 64), (2, 2, 64), (8, 1, 128), (8, 2, 128), (8, 4, 256)])
 @pytest.mark.parametrize("C,T", [(17, 1), (40, 2), (12, 5), (9, 16), (2, 16)])
 def test_shared_prompt(C, T, heads, kv):
+    """split_keys has the cells share the prompt's tiles at any size."""
     Hq, Hkv, D = heads
-    run(many(200 + C + T, C, T, Hq=Hq, Hkv=Hkv, D=D, kv=kv), what=f"shared prompt {C} {T} {heads} {kv}")
+    s = many(200 + C + T, C, T, Hq=Hq, Hkv=Hkv, D=D, kv=kv)
+    run(s, 256, f"shared prompt {C} {T} {heads} {kv}")
+    run(s, what=f"apart {C} {T} {heads} {kv}")
 
 
 @pytest.mark.parametrize("window", [1, 20, 64, 130, 300, 470])
 @pytest.mark.parametrize("donor", ["diff", "zero"])
 def test_shared_prompt_windows(window, donor):
-    run(many(211, 14, 6, window=window, donor=donor, D=128), what=f"shared prompt, window {window} {donor}")
+    run(many(211, 14, 6, window=window, donor=donor, D=128), 256, f"shared prompt, window {window} {donor}")
 
 
 @pytest.mark.parametrize("span", [(0, 400), (0, 0), (1, 399), (64, 128), (399, 400)])
 @pytest.mark.parametrize("donor", ["diff", "zero"])
 def test_shared_prompt_spans(span, donor):
-    run(many(223, 11, 7, span=span, donor=donor, D=64), what=f"shared prompt, span {span} {donor}")
+    run(many(223, 11, 7, span=span, donor=donor, D=64), 256, f"shared prompt, span {span} {donor}")
 
 
 @pytest.mark.parametrize("split", [64, 128, 1024])
@@ -264,10 +267,10 @@ def test_shared_prompt_hides_what_is_not_seen(D):
         x[:, :a] = float("nan")
         x[:, b:, :4] = bad
     s.expected = lambda: want
-    s.check(*s.attend(), "NaN in the donor's scaffold")
+    s.check(*s.attend(256), "NaN in the donor's scaffold")
     for x in s.clean:
         x[:, a + 3:b - 5, :4] = bad
-    out, lse = s.attend()
+    out, lse = s.attend(256)
     torch.cuda.synchronize()
     step = s.steps[:, None] + s.depth
     on = (s.depth >= 0) & (s.steps[:, None] >= 0)
@@ -284,7 +287,12 @@ def test_shared_prompt_of_every_cell():
     C = 256
     s = many(233, C, 1, Hq=4, Hkv=1, D=64, Tp=300)
     s.steps[32:64] = -1
-    run(s, what="256 cells")
+    run(s, 256, "256 cells")
+    run(s, what="256 cells apart")
+
+
+def test_shared_prompt_by_default():
+    run(many(241, 64, 2, Hq=2, Hkv=1, Tp=1400, D=64), what="64 cells over 1400 slots")
 
 
 def test_large_values_keep_their_scale():
