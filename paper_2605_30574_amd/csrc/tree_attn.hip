@@ -94,11 +94,12 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
         sorted.step[to] = args.step[to] = cells.step[i];
         sorted_onset[to] = onset[i];
     }
-    // a packed call's list of the prompt, for the widest view and both forms of the span
+    // a packed call's list of the prompt, for the widest view (row tiles with nodes on
+    // both sides of the onset, few, walk both forms of the span)
     int min_step = sorted.step[0];
     for (int i = 1; i < n; ++i) min_step = sorted.step[i] < min_step ? sorted.step[i] : min_step;
     const int prompt_tiles = splice::tree_tiles(sh, checked, T, splice::tree_tile_keys(sh.head_dim, 4), min_step, n_of[1] + n_of[2] > 0,
-                                                n_of[1] > 0, true, false);
+                                                n_of[1] == n, true, false);
     int64_t prompt_keys = sh.prompt_len;   // that the first of them sees
     if (call->window > 0 && (int64_t)call->window - min_step - 1 < prompt_keys) prompt_keys = (int64_t)call->window - min_step - 1;
     const bool packed = splice::tree_packed(sh, *call, T, n, prompt_keys);

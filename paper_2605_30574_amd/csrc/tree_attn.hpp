@@ -749,49 +749,51 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_packed_kernel(Tree
     else tree_item<D, RW, F8, false>(args, (int)blockIdx.x - n);
 }
 
-// Joins the chunks of every row: a wave a row (blockIdx.x the active cell and
-// node, blockIdx.y four q heads).  Its lanes read a chunk's record each, then
-// D / 8 lanes a chunk its values, 64 / (D / 8) chunks at once.
-template <int D>
+// Joins the chunks of every row (blockIdx.x the active cell and node).  D / 8
+// lanes read a chunk's values.  MANY: a wave a row, whose lanes read a chunk's
+// record each, and 64 / (D / 8) chunks at once; otherwise, with at most D / 8
+// and at most 8 chunks, 64 / (D / 8) rows a wave.
+template <int D, bool MANY>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
-    constexpr int LPR = D / 8, SP = 64 / LPR;
-    static_assert(splice::kTreeMaxChunks == 64, "a chunk a lane");
+    constexpr int LPR = D / 8, SP = 64 / LPR, GROUP = MANY ? 64 : LPR;
+    static_assert(splice::kTreeMaxChunks == 64 && LPR >= 8, "a chunk a lane");
     const TreeCall a = args.call;
     const int Hq = a.Hkv * a.G, ci = blockIdx.x / a.T, node = blockIdx.x % a.T;
     const uint32_t info = args.slots.info[ci];
     const int64_t at_node = (int64_t)(info & 255) * a.T + node;
-    const int lane = threadIdx.x & 63, hd = blockIdx.y * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = blockIdx.y * 4 + (threadIdx.x >> 6), sp = lane / LPR, l = lane % LPR;
+    const int hd = MANY ? wave : wave * SP + sp, head = min(hd, Hq - 1);   // rows behind the last are the last again
     const int first = (int)(info >> 16), n = (int)(args.slots.info[ci + 1] >> 16) - first;
-    if (hd >= Hq || a.depth[at_node] < 0) return;
-    const int64_t stride = (int64_t)a.T * Hq, row = (int64_t)first * stride + (int64_t)node * Hq + hd;
+    if (a.depth[at_node] < 0) return;
+    const int64_t stride = (int64_t)a.T * Hq, row = (int64_t)first * stride + (int64_t)node * Hq + head;
+    const int mine = MANY ? lane : l;
     float4 x = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-    if (lane < n) x = a.record[row + lane * stride];
+    if (mine < n) x = a.record[row + mine * stride];
     float M = x.x;
-    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    for (int o = 1; o < GROUP; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
     const float f = fast_exp2(x.x - (M == -INFINITY ? 0.f : M)), weight = f * x.z;
     float L = f * x.y;
-    for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o);
-    const int sp = lane / LPR, l = lane % LPR;
+    for (int o = 1; o < GROUP; o <<= 1) L += __shfl_xor(L, o);
     const _Float16 *src = a.part + row * D + 8 * l;
     f32x8_t O = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < n; s0 += 4 * SP) {
-        static_for<0, 4>([&](auto u) {
-            const int s = s0 + (int)u * SP + sp, from = min(s, n - 1);
-            float w = __shfl(weight, from);
+    constexpr int U = MANY ? 4 : 8, STEP = MANY ? SP : 1;
+    for (int s0 = 0; s0 < n; s0 += U * STEP) {
+        static_for<0, U>([&](auto u) {
+            const int s = s0 + (int)u * STEP + (MANY ? sp : 0), from = min(s, n - 1);
+            float w = __shfl(weight, MANY ? from : sp * LPR + from);
             if (s >= n) w = 0.f;
             const f32x8_t v = __builtin_convertvector(*reinterpret_cast<const f16x8_t *>(src + from * stride * D), f32x8_t);
             static_for<0, 8>([&](auto i) { O[(int)i] = w == 0.f ? O[(int)i] : fmaf(w, v[(int)i], O[(int)i]); });   // 0 * inf
         });
     }
-    for (int o = LPR; o < 64; o <<= 1) static_for<0, 8>([&](auto i) { O[(int)i] += __shfl_xor(O[(int)i], o); });
+    if constexpr (MANY)
+        for (int o = LPR; o < 64; o <<= 1) static_for<0, 8>([&](auto i) { O[(int)i] += __shfl_xor(O[(int)i], o); });
+    if (hd >= Hq || (MANY && sp != 0)) return;
     const int64_t at = at_node * Hq + hd;
     const float r = L == 0.f ? 0.f : 1.f / L;
-    if (sp == 0) *reinterpret_cast<bf16x8_t *>(a.out + at * D + 8 * l) = __builtin_convertvector(O * r, bf16x8_t);
-    if (lane == 0) a.lse[at] = kLn2 * (M + log2f(L));
+    *reinterpret_cast<bf16x8_t *>(a.out + at * D + 8 * l) = __builtin_convertvector(O * r, bf16x8_t);
+    if (l == 0) a.lse[at] = kLn2 * (M + log2f(L));
 }
-
-// Enqueues a call of plan p; 0 if a launch failed.
-typedef bool (*TreeLaunch)(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hipStream_t stream);
 
 template <int D, int RW, bool F8, bool PACKED>
 bool launch_tree_kernel(const TreeArgs &args, int blocks, hipStream_t stream) {
@@ -838,8 +840,10 @@ bool launch_tree(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hi
     go(std::integral_constant<int, 4>{});
     const TreeCall &c = a.call;
     if (!ok || !c.split) return ok;
-    hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)(c.n_active * c.T), (unsigned)((c.Hkv * c.G + 3) / 4)), dim3(256),
-                       0, stream, a);
+    const int Hq = c.Hkv * c.G, rows = p.most_chunks > 8 ? 4 : 4 * 64 / (D / 8);   // a work group's
+    const dim3 grid((unsigned)(c.n_active * c.T), (unsigned)((Hq + rows - 1) / rows));
+    if (p.most_chunks > 8) hipLaunchKernelGGL((tree_join_kernel<D, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((tree_join_kernel<D, false>), grid, dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess;
 }
 

@@ -86,6 +86,7 @@ struct TreePlan {
     int row_waves, row_tiles, per;
     int n_p, p_tiles;      // packed: chunks of the prompt, tiles of 128 rows; else 0
     int n_slots, blocks;   // partial results a (node, q head) may have, over all cells; work groups
+    int most_chunks;       // of a cell
     bool split;            // some cell has more than one chunk
     size_t bytes;          // partial results: [slot][node][q head] of D fp16 and four floats
 };
@@ -192,7 +193,7 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
     } else {
         p.per = most;
         int64_t best = INT64_MAX;
-        for (int k = 1; k <= kTreeRounds; ++k) {
+        for (int k = 1; k <= (packed ? 1 : kTreeRounds); ++k) {   // the prompt's items fill the further rounds
             int64_t limit = k * room / items;
             limit = limit < kTreeMaxSlots ? limit : kTreeMaxSlots;
             if (limit < n) continue;   // not even whole lists fit
@@ -227,6 +228,7 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
         p.n_slots += n * p.n_p;
         p.split = true;
     }
+    p.most_chunks = p.n_p + ceil_div(most, p.per);
     p.bytes = p.split ? p.n_slots * tree_slot_bytes(sh, T) : 0;
     return p;
 }
