@@ -70,48 +70,11 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
 
     const int T = tree->n_nodes;
     TreeArgs args;
-    splice::TreeCells cells;
-    const int n = splice::active_cells(sh, cell_step, cells);
+    int n = 0;
+    const splice::TreePlan p = splice::tree_prepare(sh, checked, T, cell_LW, cell_step, compute_units(), n, args.step, args.slots);
     if (n == 0) return SPLICE_OK;
-    // the cells in the order of their class, and what each has to walk
-    uint8_t onset[SPLICE_MAX_CELLS], cls[SPLICE_MAX_CELLS];
-    for (int i = 0; i < n; ++i) {
-        const int32_t *lw = cell_LW + 2 * cells.cell[i];
-        const int64_t ahead = (int64_t)lw[1] - cells.step[i];   // depth of the onset
-        const bool never = call->layer < lw[0] || ahead >= T;
-        onset[i] = (uint8_t)(never ? SPLICE_MAX_NODES : (ahead > 0 ? ahead : 0));
-        cls[i] = never ? 0 : (ahead > 0 ? 1 : 2);
-    }
-    splice::TreeCells sorted;
-    uint8_t sorted_onset[SPLICE_MAX_CELLS];
-    int at[3] = {0, 0, 0}, n_of[3] = {0, 0, 0};
-    for (int i = 0; i < n; ++i) ++n_of[cls[i]];
-    at[1] = n_of[0];
-    at[2] = n_of[0] + n_of[1];
-    for (int i = 0; i < n; ++i) {
-        const int to = at[cls[i]]++;
-        sorted.cell[to] = cells.cell[i];
-        sorted.step[to] = args.step[to] = cells.step[i];
-        sorted_onset[to] = onset[i];
-    }
-    // a packed call's list of the prompt, for the widest view (row tiles with nodes on
-    // both sides of the onset, few, walk both forms of the span)
-    int min_step = sorted.step[0];
-    for (int i = 1; i < n; ++i) min_step = sorted.step[i] < min_step ? sorted.step[i] : min_step;
-    const int prompt_tiles = splice::tree_tiles(sh, checked, T, splice::tree_tile_keys(sh.head_dim, 4), min_step, n_of[1] + n_of[2] > 0,
-                                                n_of[1] == n, true, false);
-    int64_t prompt_keys = sh.prompt_len;   // that the first of them sees
-    if (call->window > 0 && (int64_t)call->window - min_step - 1 < prompt_keys) prompt_keys = (int64_t)call->window - min_step - 1;
-    const bool packed = splice::tree_packed(sh, *call, T, n, prompt_keys);
-    int tiles[SPLICE_MAX_CELLS];
-    const int tile = splice::tree_tile_keys(sh.head_dim, splice::tree_row_waves(sh.head_dim, T * splice::group_of(sh)));
-    for (int i = 0; i < n; ++i)
-        tiles[i] = splice::tree_tiles(sh, checked, T, tile, sorted.step[i], i >= n_of[0], i >= n_of[0] && i < n_of[0] + n_of[1],
-                                      !packed, true);
-    const splice::TreePlan p = splice::tree_plan(sh, checked, T, tiles, n, compute_units(), packed, prompt_tiles);
     if ((int64_t)sh.n_kv_heads * p.n_slots * p.row_tiles > INT32_MAX || (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30)
         return SPLICE_EUNSUPPORTED;
-    splice::tree_slots(sorted, sorted_onset, tiles, n, p, args.slots);
     if (p.bytes > 0 && (!workspace || !splice::aligned(workspace, 256) || workspace_bytes < p.bytes)) return SPLICE_EWORKSPACE;
     splice_dev::TreeCall &a = args.call;
     a.q = (const char *)q;

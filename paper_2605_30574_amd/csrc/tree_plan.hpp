@@ -233,6 +233,47 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
     return p;
 }
 
+// A call's plan, and what its kernels read: n active cells in the order of
+// their class, their steps, and the grid's items.
+inline TreePlan tree_prepare(const splice_shape &sh, const splice_call &call, int T, const int32_t *cell_LW,
+                             const int32_t *cell_step, int n_cu, int &n, int32_t *step, TreeSlots &slots) {
+    TreeCells cells, sorted;
+    n = active_cells(sh, cell_step, cells);
+    if (n == 0) return TreePlan{};
+    uint8_t onset[SPLICE_MAX_CELLS], sorted_onset[SPLICE_MAX_CELLS], cls[SPLICE_MAX_CELLS];
+    int n_of[3] = {0, 0, 0};
+    for (int i = 0; i < n; ++i) {
+        const int32_t *lw = cell_LW + 2 * cells.cell[i];
+        const int64_t ahead = (int64_t)lw[1] - cells.step[i];   // depth of the onset
+        const bool never = call.layer < lw[0] || ahead >= T;
+        onset[i] = (uint8_t)(never ? SPLICE_MAX_NODES : (ahead > 0 ? ahead : 0));
+        cls[i] = never ? 0 : (ahead > 0 ? 1 : 2);
+        ++n_of[cls[i]];
+    }
+    int at[3] = {0, n_of[0], n_of[0] + n_of[1]}, min_step = cells.step[0];
+    for (int i = 0; i < n; ++i) {
+        const int to = at[cls[i]]++;
+        sorted.cell[to] = cells.cell[i];
+        sorted.step[to] = step[to] = cells.step[i];
+        sorted_onset[to] = onset[i];
+        min_step = cells.step[i] < min_step ? cells.step[i] : min_step;
+    }
+    // a packed call's list of the prompt, for the widest view (row tiles with nodes on
+    // both sides of the onset, few, walk both forms of the span)
+    const int prompt_tiles = tree_tiles(sh, call, T, tree_tile_keys(sh.head_dim, 4), min_step, n_of[1] + n_of[2] > 0, n_of[1] == n,
+                                        true, false);
+    int64_t prompt_keys = sh.prompt_len;
+    if (call.window > 0 && (int64_t)call.window - min_step - 1 < prompt_keys) prompt_keys = (int64_t)call.window - min_step - 1;
+    const bool packed = tree_packed(sh, call, T, n, prompt_keys);
+    int tiles[SPLICE_MAX_CELLS];
+    const int tile = tree_tile_keys(sh.head_dim, tree_row_waves(sh.head_dim, T * group_of(sh)));
+    for (int i = 0; i < n; ++i)
+        tiles[i] = tree_tiles(sh, call, T, tile, sorted.step[i], i >= n_of[0], i >= n_of[0] && i < n_of[0] + n_of[1], !packed, true);
+    const TreePlan p = tree_plan(sh, call, T, tiles, n, n_cu, packed, prompt_tiles);
+    tree_slots(sorted, sorted_onset, tiles, n, p, slots);
+    return p;
+}
+
 // Bytes that no plan of this shape passes, whatever the steps.
 inline size_t tree_most_bytes(const splice_shape &sh, const splice_call &call, int T, int n_cu) {
     const int rows = T * group_of(sh), rw = tree_row_waves(sh.head_dim, rows);

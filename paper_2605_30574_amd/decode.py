@@ -12,6 +12,8 @@ library's kernel. Around it, with dense bf16 weights on the GPU, what lies
 between the products, the head, the argmax and the products it has better
 tiles for are this library's kernels too (``include/splice_decoder.h``); the
 other products, and passes with other weights, are PyTorch operations.
+``SweepDecoder.score_tree`` is a pass over a tree of candidate tokens per cell
+(``tree``): what the model says about each of them, without a pass per token.
 
 Readings of what the paper leaves to the model (the same on the CPU
 reference in ``oracle.decoder``):
@@ -25,7 +27,7 @@ reference in ``oracle.decoder``):
 from __future__ import annotations
 
 import ctypes
-from typing import List, Optional
+from typing import List, NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -33,6 +35,7 @@ from torch.autograd import forward_ad
 from torch.utils._device import DeviceContext
 
 from . import splice as S
+from . import tree as T
 
 ARGMAX_PARTS = 64   # SPLICE_ARGMAX_PARTS
 _declared = None
@@ -119,6 +122,34 @@ def rope(x: torch.Tensor, pos: torch.Tensor, theta: float) -> torch.Tensor:
     return torch.cat([x1 * cos - x2 * sin, x2 * cos + x1 * sin], dim=-1)
 
 
+class DecoderTree(NamedTuple):
+    """A tree per cell on the decoder's device (SweepDecoder.make_tree)."""
+    spec: T.SpliceTree
+    depth: torch.Tensor       # int32 [C][T]
+    visible: torch.Tensor     # int64 [C][T]
+    workspace: torch.Tensor
+    parents: np.ndarray       # int64 [C][T]
+
+
+def accept(parents: np.ndarray, tokens: np.ndarray, first: np.ndarray, best: np.ndarray):
+    """(keep int32 [C][T], number int64 [C]) of the nodes of each cell that a greedy decode would have taken: a root whose
+    token is first[c] (what the last pass chose), then, from node to node, a child whose token is best[c][t] (what
+    the pass chose behind node t).  Of several children with that token the lowest index."""
+    parents, tokens = np.asarray(parents), np.asarray(tokens)
+    keep, number = np.full(parents.shape, -1, np.int32), np.zeros(parents.shape[0], np.int64)
+    for c in range(parents.shape[0]):
+        at, want = -1, first[c]
+        while True:
+            hits = np.flatnonzero((parents[c] == at) & (tokens[c] == want))
+            if len(hits) == 0:
+                break
+            at = int(hits[0])
+            keep[c, number[c]] = at
+            number[c] += 1
+            want = best[c][at]
+    return keep, number
+
+
 class SweepDecoder:
     """C sweep cells (L_c, W_c) decoding over one prompt, all N layers.
 
@@ -176,10 +207,10 @@ class SweepDecoder:
                      @ p["w_down"]).float()
         return (rms_norm(x, wt["norm_f"], m.rms_eps).to(cdt) @ wt["lm_head"]).float()
 
-    def _fused(self, x: torch.Tensor, pos: Optional[torch.Tensor]) -> bool:
-        """Whether the library's kernels take this pass (x: the embedded tokens)."""
+    def _fused(self, x: torch.Tensor, pos: Optional[torch.Tensor], rows: Optional[int] = None) -> bool:
+        """Whether the library's kernels take this pass (x: the embedded tokens, a row per cell or ``rows``)."""
         w, wt = self.w, self.wt
-        C, Hq, Hkv, D, dev, d = self.C, w.n_q_heads, w.n_kv_heads, w.head_dim, x.device, x.shape[-1]
+        C, Hq, Hkv, D, dev, d = rows or self.C, w.n_q_heads, w.n_kv_heads, w.head_dim, x.device, x.shape[-1]
         if torch.is_autocast_enabled("cuda") and torch.get_autocast_dtype("cuda") != torch.bfloat16:
             return False   # the products are another type's
         if not (_unwatched() and x.is_cuda and _current(dev) and C > 0 and d % 8 == 0 and _plain(x, dev, C, d) and
@@ -273,6 +304,109 @@ class SweepDecoder:
         ok(lib.splice_decoder_head(hp, head.data_ptr(), logits.data_ptr(), C, d, vocab, part.data_ptr(), need, stream),
            "splice_decoder_head")
         return logits
+
+    # ------------------------------------------------------------- trees of candidate tokens
+
+    def _kv_format(self) -> str:
+        kinds = {(c["gen_k"].dtype, c["gen_v"].dtype) for c in self.caches}
+        if kinds == {(torch.bfloat16, torch.bfloat16)}:
+            return "bf16"
+        if kinds == {(torch.uint8, torch.uint8)}:
+            return "e4m3"
+        raise ValueError(f"generated caches are bfloat16, or uint8 with exponents, in every layer: got {kinds}")
+
+    def make_tree(self, parents) -> DecoderTree:
+        """Trees of T nodes per cell (``tree.tree_layout``: parents [C][T], -1 a root, less padding) for score_tree and
+        keep_nodes.  Generated caches may be bfloat16, or uint8 (e4m3) with ``gen_k_exp`` and ``gen_v_exp``."""
+        parents = np.asarray(parents)
+        depth, visible = T.tree_layout(parents)
+        if depth.shape[0] != self.C:
+            raise ValueError(f"parents has {depth.shape[0]} rows, the decoder {self.C} cells")
+        spec = T.make_tree(depth.shape[1], self._kv_format())
+        need = max((T.splice_tree_attn_workspace_bytes(self.shape, call, spec) for call in self.calls), default=0)
+        return DecoderTree(spec, torch.from_numpy(depth).to(self.device), torch.from_numpy(visible.view(np.int64)).to(self.device),
+                           torch.empty(need, dtype=torch.uint8, device=self.device), parents.astype(np.int64))
+
+    @torch.no_grad()
+    def tree_logits(self, tokens: torch.Tensor, tree: DecoderTree, steps: np.ndarray) -> torch.Tensor:
+        """Logits [C * T][V] of one pass over the trees' nodes: node t of cell c is the token tokens[c][t] (int64) at
+        decode step steps[c] + its depth, behind the steps[c] rows of the cell's generated caches and its ancestors.
+        Its K/V become row steps[c] + t, so steps[c] + T must not pass the caches' rows; cells with a
+        negative step are skipped.  Rows of padding and of skipped cells hold no meaning (their tokens are any of the
+        vocabulary).  No gradients."""
+        w, m, wt = self.w, self.m, self.wt
+        C, Hq, Hkv, D, n = self.C, w.n_q_heads, w.n_kv_heads, w.head_dim, tree.spec.n_nodes
+        if tuple(tokens.shape) != (C, n):
+            raise ValueError(f"tokens has shape {tuple(tokens.shape)}, expected ({C}, {n})")
+        st, _ = S._steps(steps, C)
+        pos = None
+        if getattr(self.positions, "__func__", None) is not SweepDecoder.positions:   # not T_p + s
+            pos = (self.positions(st).to(torch.int64)[:, None] + tree.depth).contiguous()
+        x = wt["embed"][tokens.reshape(-1)]
+        cdt, dev, rows = x.dtype, x.device, C * n
+        freq = torch.from_numpy(T.rope_frequencies(D, float(m.rope_theta))[0]).to(dev)
+        rope_of, bf16 = T.make_rope("half", D), torch.bfloat16
+        out = torch.zeros((C, n, Hq, D), dtype=bf16, device=dev)
+        lse = torch.empty((C, n, Hq), dtype=torch.float32, device=dev)
+        exps = ("gen_k_exp", "gen_v_exp") if tree.spec.kv_format == T.SPLICE_KV_E4M3 else ()
+        fused = self._fused(x, None, rows) and x.shape[1] <= 8192   # SPLICE_ADD_NORM_MAX_D
+
+        def attend(l, q, k, v):
+            c = self.caches[l]
+            e = [c[name] for name in exps] or [None, None]
+            q, k, v = q.to(bf16).view(C, n, Hq, D), k.to(bf16).view(C, n, Hkv, D), v.to(bf16).view(C, n, Hkv, D)
+            T.splice_tree_append(self.shape, tree.spec, rope_of, freq, st, tree.depth, q, k, v, q, c["gen_k"], c["gen_v"], *e,
+                                 pos=pos)
+            T.splice_tree_attn(self.shape, self.calls[l], tree.spec, self.lw, st, tree.depth, tree.visible, q, c["clean_k"],
+                               c["clean_v"], c["donor_k"], c["donor_v"], c["gen_k"], c["gen_v"], *e, out, lse, tree.workspace)
+            return out.view(rows, Hq * D)
+
+        if not fused:
+            x = x.float()
+            for l in range(self.N):
+                p = wt["layers"][l]
+                h = rms_norm(x, p["norm_1"], m.rms_eps).to(cdt)
+                x = x + (attend(l, h @ p["w_q"], h @ p["w_k"], h @ p["w_v"]).to(cdt) @ p["w_o"]).float()
+                h = rms_norm(x, p["norm_2"], m.rms_eps).to(cdt)
+                x = x + ((torch.nn.functional.silu((h @ p["w_gate"]).float()).to(cdt) * (h @ p["w_up"])) @ p["w_down"]).float()
+            return rms_norm(x, wt["norm_f"], m.rms_eps).to(cdt) @ wt["lm_head"]
+
+        lib, ok, stream, d = _library(), S._check, S._stream_ptr(None, dev), x.shape[1]
+        res, h = torch.empty((rows, d), dtype=torch.float32, device=dev), torch.empty((rows, d), dtype=bf16, device=dev)
+
+        def norm(delta, gain, assign=0):
+            ok(lib.splice_decoder_add_norm(res.data_ptr(), delta.data_ptr(), gain.data_ptr(), h.data_ptr(), None, rows, d,
+                                           m.rms_eps, assign, stream), "splice_decoder_add_norm")
+
+        delta, first = x, 1
+        for l in range(self.N):
+            p = wt["layers"][l]
+            norm(delta, p["norm_1"], first)
+            first = 0
+            norm(attend(l, h @ p["w_q"], h @ p["w_k"], h @ p["w_v"]) @ p["w_o"], p["norm_2"])
+            gate, up = h @ p["w_gate"], h @ p["w_up"]
+            ok(lib.splice_decoder_silu(gate.data_ptr(), up.data_ptr(), gate.data_ptr(), rows, gate.shape[1], 0, stream),
+               "splice_decoder_silu")
+            delta = gate @ p["w_down"]
+        norm(delta, wt["norm_f"], first)
+        return h @ wt["lm_head"]
+
+    def score_tree(self, tokens: torch.Tensor, tree: DecoderTree, steps: np.ndarray, targets: torch.Tensor, top: int = 0,
+                   scale: float = 1.0) -> T.TokenScores:
+        """What the model says behind every node of the trees (tree_logits): log probability, entropy, rank of the token
+        targets[c][t] (int64 [C][T]), and the ``top`` most probable tokens; fields [C][T] and [C][T][top].  scale: an
+        inverse temperature."""
+        logits = self.tree_logits(tokens, tree, steps)
+        got = T.token_scores(logits, targets.reshape(-1).contiguous(), top, scale)
+        shape = (self.C, tree.spec.n_nodes)
+        return T.TokenScores(*(None if f is None else f.view(*shape, *f.shape[1:]) for f in got))
+
+    def keep_nodes(self, tree: DecoderTree, steps: np.ndarray, keep: torch.Tensor) -> None:
+        """Move the K/V of each cell's nodes keep[c] (int32 [C][T], ascending, ended by -1: ``accept``) to its rows
+        steps[c], steps[c] + 1, ... in every layer: the decode goes on at steps[c] + their number."""
+        for c in self.caches:
+            e = [c[name] for name in ("gen_k_exp", "gen_v_exp")] if tree.spec.kv_format == T.SPLICE_KV_E4M3 else []
+            T.splice_tree_keep(self.shape, tree.spec, steps, keep, c["gen_k"], c["gen_v"], *e)
 
     def step(self, tokens: torch.Tensor, steps: np.ndarray, pos: Optional[torch.Tensor] = None):
         """One decode pass: (next tokens [C] int64, logits [C][V]); of equal

@@ -125,25 +125,6 @@ def test_attention_refusals():
     assert attn(sh=sh, call=small, bytes=1024) == sp.SPLICE_EWORKSPACE
 
 
-def test_workspace_serves_any_steps():
-    """The bytes asked for cover whichever cells are active at whichever steps."""
-    lib = T._library()
-    call = sp.make_call(1, 0, 0, 0.1)
-    for C in (1, 3, 64):
-        for n in (1, 5, 64):
-            sh, tree = shape(n_cells=C, prompt_len=3000, gen_capacity=900), sp.make_tree(n)
-            need = sp.splice_tree_attn_workspace_bytes(sh, call, tree)
-            for active in {1, (C + 1) // 2, C}:
-                for step in (0, 100, 900 - n):
-                    steps = ints(*([step] * active + [-1] * (C - active)))
-                    # one byte short of a 256-byte aligned block is refused only if some call needs it all: the call's own need
-                    # is found by asking with ever less
-                    a = [FAKE] * 9 + [None, None, FAKE + 1, FAKE, FAKE]   # a misaligned out: refused before the launch
-                    rc = lib.splice_tree_attn(ctypes.byref(sh), ctypes.byref(call), ctypes.byref(tree), ints(*([0, 0] * C)), steps,
-                                              *a, need, None)
-                    assert rc == sp.SPLICE_EINVAL
-
-
 def test_workspace_refusals():
     assert T._library().splice_tree_attn_workspace_bytes(None, None, None) == sp.SPLICE_EINVAL
     sh, tree = shape(), sp.make_tree(4)
@@ -253,3 +234,14 @@ def test_frequencies():
     with pytest.raises(ValueError):
         sp.rope_frequencies(63, 1e4)
     assert sp.rope_frequencies(0, 1e4)[0].size == 0
+
+
+def test_accepted_paths():
+    from paper_2605_30574_amd.decode import accept
+    parents = [[-1, -1, 0, 1, 1, 4], [-1, 0, 1, -2, -2, -2], [-1, 0, 0, 2, 3, 4]]
+    tokens = [[7, 8, 9, 3, 4, 5], [1, 2, 3, 9, 9, 9], [6, 6, 6, 6, 6, 6]]
+    best = [[9, 4, 0, 0, 5, 0], [2, 0, 0, 0, 0, 0], [6, 6, 6, 6, 6, 6]]
+    keep, n = accept(parents, tokens, [8, 1, 5], best)
+    assert keep.dtype == np.int32 and keep.tolist() == [[1, 4, 5, -1, -1, -1], [0, 1, -1, -1, -1, -1], [-1] * 6]
+    assert n.tolist() == [3, 2, 0]
+    assert accept(parents, tokens, [8, 1, 6], best)[0][2].tolist() == [0, 1, -1, -1, -1, -1]   # the lower of two children
