@@ -71,7 +71,7 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     const int T = tree->n_nodes;
     TreeArgs args;
     int n = 0;
-    const splice::TreePlan p = splice::tree_prepare(sh, checked, T, cell_LW, cell_step, compute_units(), n, args.step, args.slots);
+    const splice::TreePlan p = splice::tree_prepare(sh, checked, *tree, cell_LW, cell_step, compute_units(), n, args.step, args.slots);
     if (n == 0) return SPLICE_OK;
     if ((int64_t)sh.n_kv_heads * p.n_slots * p.row_tiles > INT32_MAX || (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30)
         return SPLICE_EUNSUPPORTED;

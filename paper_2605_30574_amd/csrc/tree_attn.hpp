@@ -79,7 +79,7 @@ struct TreeTileRef {
     bool differ;   // some row does not see some key of it
 };
 
-template <int D, int RW>
+template <int D, int RW, bool F8>
 struct TreeTile {
     static constexpr bool OWN = RW == 1;                       // every wave has tiles of its own
     static constexpr int KW = 4 / RW;                          // waves over keys
@@ -88,7 +88,11 @@ struct TreeTile {
     static constexpr int ROW = 2 * D;                          // bytes of a staged row
     static constexpr int CPR = D / 8;                          // 16-byte chunks of a row
     static constexpr int TILE = TK * ROW;                      // bytes of a K (or V) tile
-    static constexpr int TILES = (OWN ? 8 : 4) * TILE;         // K and V: a tile a wave, or two for all
+    // Buffers of tiles for all waves: two, or one where two would leave room for a single work group on a compute unit (D =
+    // 256, tiles of 64 keys; two groups then cover each other's loads. 8-bit rows in flight take the registers that a
+    // second group would need)
+    static constexpr int NBUF = OWN || (D > 128 && RW == 2 && !F8) ? 1 : 2;
+    static constexpr int TILES = (OWN ? 4 : NBUF) * 2 * TILE;  // K and V: a tile a wave, or NBUF for all
     static constexpr int LDS = TILES + (OWN ? 32 * ROW : 0);   // ... and Q, for which a wave with a tile in
                                                                // registers has none left
     static constexpr int NT = OWN ? 64 : 256;                  // threads that load a tile
@@ -97,7 +101,8 @@ struct TreeTile {
     static constexpr int NR = OWN ? NL : NL8;                  // ... by way of registers
     static constexpr bool EARLY = !OWN && KB == 1 && D <= 128; // values are read before the softmax
     static constexpr int ND = D / 32;                          // 32-wide d blocks of the output
-    static_assert(RW * KW == 4 && NL8 >= 1 && (KW == 1 || KW * 32 * RW * D * 4 <= TILES), "");
+    static constexpr int PARTS = KW > 1 && KW * 32 * RW * D * 4 > TILES ? 2 : 1;   // in which the waves' results are joined
+    static_assert(RW * KW == 4 && NL8 >= 1 && (KW == 1 || KW * 32 * RW * D * 4 <= TILES * PARTS), "");
 };
 
 // Chunk-slot swizzles (XOR on the 16-byte chunk index) of key r: the 16 rows
@@ -185,13 +190,13 @@ __device__ __forceinline__ u32x4_t finite_only(u32x4_t w) {
 // packed call is that of its generated rows.
 template <int D, int RW, bool F8, bool PACKED>
 __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
-    using X = TreeTile<D, RW>;
+    using X = TreeTile<D, RW, F8>;
     constexpr int KW = X::KW, KB = X::KB, TK = X::TK, ND = X::ND, NST = D / 16;
     extern __shared__ __align__(16) char lds[];
     __shared__ int s_bad, s_again;
     __shared__ TreeSegment s_seg[5];
     __shared__ int s_rows[PACKED ? 4 : 1][4];
-    __shared__ float s_ml[KW > 1 ? KW : 1][32 * RW][2];
+    __shared__ float s_ml[KW > 1 ? KW : 1][32 * RW][3];
     const TreeCall a = args.call;   // what the lambdas use: captured, the whole arguments would go to memory
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, h = lane >> 5, rw = wave % RW, kw = wave / RW;
@@ -514,12 +519,12 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
         }
     }
 
-    if constexpr (!X::OWN) {
+    if constexpr (!X::OWN && X::NBUF == 2) {
         wait_vmcnt<0>();   // this wave's part of the first tile
         if (t_first < t1) store(own, cur.seg);
     }
     for (int t = t_first; t < t1; t += t_step) {
-        const int b = X::OWN ? 0 : (t - t0) & 1;
+        const int b = X::NBUF == 1 ? 0 : (t - t0) & 1;
         char *const buf = own + b * 2 * X::TILE;
         // addresses are worked out anew for every tile: kept, they would take the registers of the tile in flight
         asm volatile("" : "+v"(ltid), "+v"(k_at), "+v"(v_at));
@@ -527,13 +532,17 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
             wave_fence();   // the wave has read the tile before
             store(buf, cur.seg);
             wave_fence();
+        } else if constexpr (X::NBUF == 1) {
+            wait_vmcnt<0>();
+            store(buf, cur.seg);
+            __syncthreads();
         } else {
             __syncthreads();   // every wave's part of tile t is in LDS, and tile t - 1 has been read
         }
         const TreeTileRef next = tile_of();
         // the matrix products of one wave go before the softmax of another on its SIMD
         __builtin_amdgcn_s_setprio(1);
-        if (t + t_step < t1) {
+        if (t + t_step < t1 && (X::OWN || X::NBUF == 2)) {
             load(b ^ 1);
             advance();
         }
@@ -605,7 +614,14 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
         });
         }
         cur = next;
-        if constexpr (!X::OWN) {
+        if constexpr (!X::OWN && X::NBUF == 1) {
+            __syncthreads();   // tile t has been read
+            if (t + 1 < t1) {
+                cur = tile_of();
+                load(0);
+                advance();
+            }
+        } else if constexpr (!X::OWN) {
             wait_vmcnt<0>();
             if (t + 1 < t1) store(own + (b ^ 1) * 2 * X::TILE, cur.seg);
         }
@@ -665,51 +681,60 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
     const int64_t part_row = ((int64_t)slot * a.T + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
     if constexpr (KW > 1) {
         // the waves of a row through LDS (every wave is done with the tiles)
-        float *s_o = reinterpret_cast<float *>(lds);   // [KW][32 RW][D], chunks of four swizzled by the row
+        constexpr int DP = D / X::PARTS;               // values of a row at once
+        float *s_o = reinterpret_cast<float *>(lds);   // [KW][32 RW][DP], chunks of four swizzled by the row
         const int wrow = 32 * rw + r;
-        static_for<0, ND>([&](auto db) {
-            static_for<0, 4>([&](auto i) {
-                const int d4 = 8 * (int)db + 2 * (int)i + h;
-                *reinterpret_cast<f32x4_t *>(s_o + ((kw * 32 * RW + wrow) * D + 4 * (d4 ^ (wrow & 15)))) =
-                    f32x4_t{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
-            });
-        });
+        float top = 0.f;   // the joined row's values are between the waves': none is larger
+        static_for<0, ND>([&](auto db) { static_for<0, 16>([&](auto i) { top = fmaxf(top, finite_size(o[db][(int)i])); }); });
+        top = fmaxf(top, __shfl_xor(top, 32));
         if (h == 0) {
             s_ml[kw][wrow][0] = m;
             s_ml[kw][wrow][1] = l;
+            s_ml[kw][wrow][2] = l == 0.f ? 0.f : finite_size(top / l);
         }
-        __syncthreads();
-        for (int e = tid; e < 32 * RW * (D / 4); e += 256) {
-            const int w = e / (D / 4), d4 = e % (D / 4), rr = row0 + w;
-            if (rr >= rows) break;
-            const int nd = rr / a.G, hd = g * a.G + rr % a.G;
-            if (!((alive >> nd) & 1)) continue;
-            float M = -INFINITY, Lsum = 0.f;
-            static_for<0, KW>([&](auto k) { M = fmaxf(M, s_ml[k][w][0]); });
-            const float Ms = M == -INFINITY ? 0.f : M;
-            f32x4_t O = {0.f, 0.f, 0.f, 0.f};
-            static_for<0, KW>([&](auto k) {
-                const float f = fast_exp2(s_ml[k][w][0] - Ms);
-                Lsum = fmaf(f, s_ml[k][w][1], Lsum);
-                if (f != 0.f)
-                    O += f * *reinterpret_cast<const f32x4_t *>(s_o + (((int)k * 32 * RW + w) * D + 4 * (d4 ^ (w & 15))));
+        static_for<0, X::PARTS>([&](auto part) {
+            if (part > 0) __syncthreads();
+            static_for<0, ND / X::PARTS>([&](auto e) {
+                constexpr int db = part * (ND / X::PARTS) + e;
+                static_for<0, 4>([&](auto i) {
+                    const int d4 = 8 * (int)e + 2 * (int)i + h;
+                    *reinterpret_cast<f32x4_t *>(s_o + ((kw * 32 * RW + wrow) * DP + 4 * (d4 ^ (wrow & 15)))) =
+                        f32x4_t{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+                });
             });
-            const float f = Lsum == 0.f ? 0.f : 1.f / Lsum;
-            O *= f;
-            if (a.split) {
-                const int64_t at = ((int64_t)slot * a.T + nd) * (a.Hkv * a.G) + hd;
-                float top = 0.f;
-                static_for<0, 4>([&](auto i) { top = fmaxf(top, finite_size(O[(int)i])); });
-                for (int x = 1; x < (D / 4 < 64 ? D / 4 : 64); x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-                const float sc = half_scale(top);
-                *reinterpret_cast<f16x4_t *>(a.part + at * D + 4 * d4) = __builtin_convertvector(O * sc, f16x4_t);
-                if (d4 == 0) a.record[at] = make_float4(M, Lsum, Lsum / sc, 0.f);
-            } else {
-                const int64_t at = (node0 + nd) * (a.Hkv * a.G) + hd;
-                *reinterpret_cast<bf16x4_t *>(a.out + at * D + 4 * d4) = __builtin_convertvector(O, bf16x4_t);
-                if (d4 == 0) a.lse[at] = kLn2 * (M + log2f(Lsum));
+            __syncthreads();
+            for (int e = tid; e < 32 * RW * (DP / 4); e += 256) {
+                const int w = e / (DP / 4), d4 = e % (DP / 4), rr = row0 + w, d = (int)part * DP + 4 * d4;
+                if (rr >= rows) break;
+                const int nd = rr / a.G, hd = g * a.G + rr % a.G;
+                if (!((alive >> nd) & 1)) continue;
+                float M = -INFINITY, Lsum = 0.f, size = 0.f;
+                static_for<0, KW>([&](auto k) {
+                    M = fmaxf(M, s_ml[k][w][0]);
+                    size = fmaxf(size, s_ml[k][w][2]);
+                });
+                const float Ms = M == -INFINITY ? 0.f : M;
+                f32x4_t O = {0.f, 0.f, 0.f, 0.f};
+                static_for<0, KW>([&](auto k) {
+                    const float f = fast_exp2(s_ml[k][w][0] - Ms);
+                    Lsum = fmaf(f, s_ml[k][w][1], Lsum);
+                    if (f != 0.f)
+                        O += f * *reinterpret_cast<const f32x4_t *>(s_o + (((int)k * 32 * RW + w) * DP + 4 * (d4 ^ (w & 15))));
+                });
+                const float f = Lsum == 0.f ? 0.f : 1.f / Lsum;
+                O *= f;
+                if (a.split) {
+                    const int64_t at = ((int64_t)slot * a.T + nd) * (a.Hkv * a.G) + hd;
+                    const float sc = half_scale(size);
+                    *reinterpret_cast<f16x4_t *>(a.part + at * D + d) = __builtin_convertvector(O * sc, f16x4_t);
+                    if (d == 0) a.record[at] = make_float4(M, Lsum, Lsum / sc, 0.f);
+                } else {
+                    const int64_t at = (node0 + nd) * (a.Hkv * a.G) + hd;
+                    *reinterpret_cast<bf16x4_t *>(a.out + at * D + d) = __builtin_convertvector(O, bf16x4_t);
+                    if (d == 0) a.lse[at] = kLn2 * (M + log2f(Lsum));
+                }
             }
-        }
+        });
     } else {
         const float f = l == 0.f ? 0.f : 1.f / l;
         float top = 0.f;
@@ -737,13 +762,13 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
 }
 
 template <int D, int RW, bool F8>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_kernel(TreeArgs args) {
+__global__ __launch_bounds__(256, splice::tree_resident(D, F8)) void tree_kernel(TreeArgs args) {
     tree_item<D, RW, F8, false>(args, (int)blockIdx.x);
 }
 
 // Items of the prompt, then items of the generated rows.
 template <int D, int RW, bool F8>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tree_packed_kernel(TreeArgs args) {
+__global__ __launch_bounds__(256, splice::tree_resident(D, F8)) void tree_packed_kernel(TreeArgs args) {
     const int n = args.call.p_tiles * args.call.n_p * args.call.Hkv;
     if ((int)blockIdx.x < n) tree_item<D, 4, false, true>(args, (int)blockIdx.x);
     else tree_item<D, RW, F8, false>(args, (int)blockIdx.x - n);
@@ -797,7 +822,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
 
 template <int D, int RW, bool F8, bool PACKED>
 bool launch_tree_kernel(const TreeArgs &args, int blocks, hipStream_t stream) {
-    constexpr int LDS = PACKED && TreeTile<D, 4>::LDS > TreeTile<D, RW>::LDS ? TreeTile<D, 4>::LDS : TreeTile<D, RW>::LDS;
+    constexpr int LDS = PACKED && TreeTile<D, 4, false>::LDS > TreeTile<D, RW, F8>::LDS ? TreeTile<D, 4, false>::LDS : TreeTile<D, RW, F8>::LDS;
     void (*kernel)(TreeArgs);
     if constexpr (PACKED) kernel = tree_packed_kernel<D, RW, F8>;
     else kernel = tree_kernel<D, RW, F8>;

@@ -73,13 +73,13 @@ constexpr int tree_key_blocks(int D, int row_waves) { return row_waves == 4 && D
 constexpr int tree_tile_keys(int D, int row_waves) {
     return row_waves == 1 ? 32 : 32 * tree_key_blocks(D, row_waves) * (4 / row_waves);
 }
-constexpr int tree_resident(int D) { return D <= 128 ? 2 : 1; }   // work groups a compute unit holds
+constexpr int tree_resident(int D, bool f8) { return D > 128 && f8 ? 1 : 2; }   // work groups a compute unit holds
 
 // A cell's list of keys is cut into chunks of `per` tiles, one work group
 // each (per KV head and row tile); a slot is one chunk of one cell.
 constexpr int kTreeMaxSlots = 640;
 constexpr int kTreeRounds = 6;    // rounds of resident work groups a plan may take to balance its chunks
-constexpr int kTreeStart = 4;     // what a work group costs beside its tiles, in tiles
+constexpr int kTreeStart = 8;     // what a work group costs beside its tiles, in tiles
 constexpr int kTreeMaxChunks = 64;
 
 struct TreePlan {
@@ -168,7 +168,7 @@ inline bool tree_packed(const splice_shape &sh, const splice_call &call, int T, 
 // of what the GPU holds at once; k is the one that takes least by
 // k * (per + kTreeStart).  tiles: of the cells' lists, in a packed call without
 // the prompt, whose list is prompt_tiles long.
-inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, int n_cu, bool packed,
+inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, int n_cu, bool f8, bool packed,
                           int prompt_tiles) {
     TreePlan p;
     const int rows = T * group_of(sh);
@@ -176,7 +176,7 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
     p.row_tiles = ceil_div(rows, 32 * p.row_waves);
     p.n_p = p.p_tiles = 0;
     const int tile = tree_tile_keys(sh.head_dim, p.row_waves), step = p.row_waves == 1 ? 4 : 1;   // four waves, four tiles
-    const int64_t items = (int64_t)sh.n_kv_heads * p.row_tiles, room = (int64_t)n_cu * tree_resident(sh.head_dim);
+    const int64_t items = (int64_t)sh.n_kv_heads * p.row_tiles, room = (int64_t)n_cu * tree_resident(sh.head_dim, f8);
     int64_t sum = 0;
     int most = 1;
     for (int i = 0; i < n; ++i) {
@@ -235,8 +235,10 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
 
 // A call's plan, and what its kernels read: n active cells in the order of
 // their class, their steps, and the grid's items.
-inline TreePlan tree_prepare(const splice_shape &sh, const splice_call &call, int T, const int32_t *cell_LW,
+inline TreePlan tree_prepare(const splice_shape &sh, const splice_call &call, const splice_tree &tree, const int32_t *cell_LW,
                              const int32_t *cell_step, int n_cu, int &n, int32_t *step, TreeSlots &slots) {
+    const int T = tree.n_nodes;
+    const bool f8 = tree.kv_format == SPLICE_KV_E4M3;
     TreeCells cells, sorted;
     n = active_cells(sh, cell_step, cells);
     if (n == 0) return TreePlan{};
@@ -269,7 +271,7 @@ inline TreePlan tree_prepare(const splice_shape &sh, const splice_call &call, in
     const int tile = tree_tile_keys(sh.head_dim, tree_row_waves(sh.head_dim, T * group_of(sh)));
     for (int i = 0; i < n; ++i)
         tiles[i] = tree_tiles(sh, call, T, tile, sorted.step[i], i >= n_of[0], i >= n_of[0] && i < n_of[0] + n_of[1], !packed, true);
-    const TreePlan p = tree_plan(sh, call, T, tiles, n, n_cu, packed, prompt_tiles);
+    const TreePlan p = tree_plan(sh, call, T, tiles, n, n_cu, f8, packed, prompt_tiles);
     tree_slots(sorted, sorted_onset, tiles, n, p, slots);
     return p;
 }
@@ -277,7 +279,7 @@ inline TreePlan tree_prepare(const splice_shape &sh, const splice_call &call, in
 // Bytes that no plan of this shape passes, whatever the steps.
 inline size_t tree_most_bytes(const splice_shape &sh, const splice_call &call, int T, int n_cu) {
     const int rows = T * group_of(sh), rw = tree_row_waves(sh.head_dim, rows);
-    const int64_t items = (int64_t)sh.n_kv_heads * ceil_div(rows, 32 * rw), room = (int64_t)kTreeRounds * n_cu * tree_resident(sh.head_dim);
+    const int64_t items = (int64_t)sh.n_kv_heads * ceil_div(rows, 32 * rw), room = (int64_t)kTreeRounds * n_cu * 2;
     int64_t most = 0;
     for (int n = 1; n <= sh.n_cells; ++n) {
         int64_t slots = call.split_keys == 0 && room / items < kTreeMaxSlots ? room / items : kTreeMaxSlots;

@@ -22,7 +22,7 @@ int64_t prepare(const splice_shape *sh, const splice_call *call, const splice_tr
     if (validate_tree(sh, tree, steps) != SPLICE_OK) return -1;
     TreeSlots s{};
     int n = 0;
-    const TreePlan p = tree_prepare(*sh, *call, tree->n_nodes, lw, steps, n_cu, n, step, s);
+    const TreePlan p = tree_prepare(*sh, *call, *tree, lw, steps, n_cu, n, step, s);
     for (int i = 0; i <= SPLICE_MAX_CELLS; ++i) info[i] = s.info[i];
     for (int i = 0; i < kTreeMaxSlots; ++i) order[i] = (s.order[i / 2] >> (16 * (i % 2))) & 0xffff;
     const int64_t v[] = {n, p.row_waves, p.row_tiles, p.per, p.n_p, p.p_tiles, p.n_slots, p.blocks, p.most_chunks, p.split};
@@ -58,7 +58,7 @@ def draw(rng):
     call = sp.make_call(3, 0, rng.choice((0, 0, log(1, 5000))), 0.1, rng.choice((0, 0, 0, 64, 256, 65536)))
     steps = [rng.choice((-1, 0, cap - n, rng.randint(0, cap - n))) if rng.random() < 0.5 else rng.randint(0, cap - n) for _ in range(C)]
     lw = [(rng.randint(0, 8), rng.choice((0, max(s, 0) + rng.randint(0, 70), 10**9))) for s in steps]
-    return sh, call, sp.make_tree(n), lw, steps
+    return sh, call, sp.make_tree(n, rng.choice(("bf16", "e4m3"))), lw, steps
 
 
 def test_plans(plan):
