@@ -73,8 +73,7 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     int n = 0;
     const splice::TreePlan p = splice::tree_prepare(sh, checked, *tree, cell_LW, cell_step, compute_units(), n, args.step, args.slots);
     if (n == 0) return SPLICE_OK;
-    if ((int64_t)sh.n_kv_heads * p.n_slots * p.row_tiles > INT32_MAX || (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30)
-        return SPLICE_EUNSUPPORTED;
+    if (p.blocks > 65535 || (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30) return SPLICE_EUNSUPPORTED;
     if (p.bytes > 0 && (!workspace || !splice::aligned(workspace, 256) || workspace_bytes < p.bytes)) return SPLICE_EWORKSPACE;
     splice_dev::TreeCall &a = args.call;
     a.q = (const char *)q;
@@ -94,6 +93,7 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     a.record = (float4 *)((char *)workspace + (size_t)p.n_slots * T * sh.n_q_heads * sh.head_dim * 2);
     a.T = T;
     a.G = splice::group_of(sh);
+    a.lgG = a.G == 1 ? 0 : (a.G == 2 ? 1 : (a.G == 4 ? 2 : 3));
     a.Hkv = sh.n_kv_heads;
     a.Tp = sh.prompt_len;
     a.cap = sh.gen_capacity;

@@ -48,7 +48,7 @@ struct TreeCall {
     // and in 32 bits they would be 53% of what a call of many chunks writes and reads again.
     _Float16 *part;
     float4 *record;
-    int T, G, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, per;
+    int T, G, lgG, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, per;
     int n_p, p_tiles;   // packed calls: chunks of the prompt and tiles of 128 rows; else 0
     bool split;
     float qk_scale;   // scale * log2(e)
@@ -189,7 +189,7 @@ __device__ __forceinline__ u32x4_t finite_only(u32x4_t w) {
 // the prompt; otherwise rows of one cell over a chunk of its list, which in a
 // packed call is that of its generated rows.
 template <int D, int RW, bool F8, bool PACKED>
-__device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
+__device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     using X = TreeTile<D, RW, F8>;
     constexpr int KW = X::KW, KB = X::KB, TK = X::TK, ND = X::ND, NST = D / 16;
     extern __shared__ __align__(16) char lds[];
@@ -201,8 +201,9 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, h = lane >> 5, rw = wave % RW, kw = wave / RW;
 
-    // ---- which rows: KV heads run fastest, so that with eight (or a multiple) an XCD keeps to its own
-    const int g = block % a.Hkv, rest = block / a.Hkv, rows = a.T * a.G;
+    // ---- which rows: KV heads run fastest (blockIdx.x), so that with eight (or a multiple) an XCD keeps to its own.
+    // What a division takes counts here: a work group may have few tiles
+    const int g = blockIdx.x, rows = a.T << a.lgG, G1 = a.G - 1;
     int row0, row, chunk, slot, step = 0, node, depth, low, low_all, low_max;
     int64_t node0, pair = 0;
     bool last_chunk = false, valid, spliced, any_clean, any_donor;
@@ -210,14 +211,14 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
     if constexpr (PACKED) {
         chunk = rest / a.p_tiles;
         row0 = 0;
-        const int at = 32 * RW * (rest % a.p_tiles) + 32 * rw + r, n_rows = a.n_active * rows;
+        const int at = 32 * RW * (rest - chunk * a.p_tiles) + 32 * rw + r, n_rows = a.n_active * rows;
         const int ci = min(at, n_rows - 1) / rows;
         row = at - ci * rows;
         const uint32_t info = args.slots.info[ci];
         const int at_step = args.step[ci];
         node0 = (int64_t)(info & 255) * a.T;
         slot = (int)(info >> 16) + chunk;
-        node = min(row / a.G, a.T - 1);
+        node = min(row >> a.lgG, a.T - 1);
         depth = min(a.depth[node0 + node], a.T - 1);
         valid = at < n_rows && depth >= 0;
         spliced = depth >= (int)((info >> 8) & 255);
@@ -245,7 +246,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
         low_all = __builtin_amdgcn_readfirstlane(max(lo, 0));   // some row sees from here on,
         low_max = __builtin_amdgcn_readfirstlane(hi);           // every row from here on
     } else {
-        const int place = rest / a.row_tiles, rt = rest % a.row_tiles;
+        const int place = a.row_tiles == 1 ? rest : rest / a.row_tiles, rt = rest - place * a.row_tiles;
         const uint32_t here = args.slots.order[place >> 1] >> (16 * (place & 1));
         const int ci = here & 255;
         chunk = (here >> 8) & 255;
@@ -258,18 +259,19 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
         row = row0 + 32 * rw + r;
         node0 = (int64_t)c * a.T;
         pair = (int64_t)c * a.Hkv + g;
+        node = min(row >> a.lgG, a.T - 1);
         int d_node = lane < a.T ? a.depth[node0 + lane] : -1;   // lane u: node u's depth
+        word = a.visible[node0 + node];
         d_node = min(d_node, a.T - 1);
         alive = __ballot(d_node >= 0);
-        const uint64_t mine = bits(row0 / a.G, min(row0 + 32 * RW - 1, rows - 1) / a.G + 1) & alive;   // the work group's nodes
+        const uint64_t mine = bits(row0 >> a.lgG, (min(row0 + 32 * RW - 1, rows - 1) >> a.lgG) + 1) & alive;   // the work group's nodes
         if (mine == 0) return;
-        node = min(row / a.G, a.T - 1);
         depth = __shfl(d_node, node);
         const int p0 = a.Tp + step;
         valid = row < rows && depth >= 0;
         spliced = depth >= onset;
         low = a.window > 0 ? p0 + max(depth, 0) - a.window + 1 : 0;
-        word = valid ? a.visible[node0 + node] & alive : 0;
+        word = valid ? word & alive : 0;
         if (a.window > 0 && a.window < a.T) {
             for (int u = 0; u < a.T; ++u)
                 if (depth - __shfl(d_node, u) >= a.window) word &= ~(1ull << u);
@@ -483,7 +485,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
     bf16x8_t qb[X::OWN ? 1 : NST];
     char *const s_q = lds + X::TILES;   // chunk slots as those of K
     {
-        const int64_t q_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
+        const int64_t q_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + (row & G1);
         if constexpr (X::OWN) {
             for (int ch = 2 * kw + h; ch < X::CPR; ch += 8) {
                 u32x4_t x = {0, 0, 0, 0};
@@ -677,8 +679,8 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
 
     // ---- results
     l += __shfl_xor(l, 32);
-    const int64_t out_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
-    const int64_t part_row = ((int64_t)slot * a.T + node) * (a.Hkv * a.G) + g * a.G + row % a.G;
+    const int64_t out_row = (node0 + node) * (a.Hkv * a.G) + g * a.G + (row & G1);
+    const int64_t part_row = ((int64_t)slot * a.T + node) * (a.Hkv * a.G) + g * a.G + (row & G1);
     if constexpr (KW > 1) {
         // the waves of a row through LDS (every wave is done with the tiles)
         constexpr int DP = D / X::PARTS;               // values of a row at once
@@ -706,7 +708,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
             for (int e = tid; e < 32 * RW * (DP / 4); e += 256) {
                 const int w = e / (DP / 4), d4 = e % (DP / 4), rr = row0 + w, d = (int)part * DP + 4 * d4;
                 if (rr >= rows) break;
-                const int nd = rr / a.G, hd = g * a.G + rr % a.G;
+                const int nd = rr >> a.lgG, hd = g * a.G + (rr & G1);
                 if (!((alive >> nd) & 1)) continue;
                 float M = -INFINITY, Lsum = 0.f, size = 0.f;
                 static_for<0, KW>([&](auto k) {
@@ -763,15 +765,15 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int block) {
 
 template <int D, int RW, bool F8>
 __global__ __launch_bounds__(256, splice::tree_resident(D, F8)) void tree_kernel(TreeArgs args) {
-    tree_item<D, RW, F8, false>(args, (int)blockIdx.x);
+    tree_item<D, RW, F8, false>(args, (int)blockIdx.y);
 }
 
 // Items of the prompt, then items of the generated rows.
 template <int D, int RW, bool F8>
 __global__ __launch_bounds__(256, splice::tree_resident(D, F8)) void tree_packed_kernel(TreeArgs args) {
-    const int n = args.call.p_tiles * args.call.n_p * args.call.Hkv;
-    if ((int)blockIdx.x < n) tree_item<D, 4, false, true>(args, (int)blockIdx.x);
-    else tree_item<D, RW, F8, false>(args, (int)blockIdx.x - n);
+    const int n = args.call.p_tiles * args.call.n_p;
+    if ((int)blockIdx.y < n) tree_item<D, 4, false, true>(args, (int)blockIdx.y);
+    else tree_item<D, RW, F8, false>(args, (int)blockIdx.y - n);
 }
 
 // Joins the chunks of every row (blockIdx.x the active cell and node).  D / 8
@@ -839,7 +841,7 @@ bool launch_tree_kernel(const TreeArgs &args, int blocks, hipStream_t stream) {
             raised.fetch_or(bit);
         }
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), LDS, stream, args);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)args.call.Hkv, (unsigned)blocks), dim3(256), LDS, stream, args);
     return hipGetLastError() == hipSuccess;
 }
 

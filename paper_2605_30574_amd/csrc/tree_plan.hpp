@@ -85,7 +85,7 @@ constexpr int kTreeMaxChunks = 64;
 struct TreePlan {
     int row_waves, row_tiles, per;
     int n_p, p_tiles;      // packed: chunks of the prompt, tiles of 128 rows; else 0
-    int n_slots, blocks;   // partial results a (node, q head) may have, over all cells; work groups
+    int n_slots, blocks;   // partial results a (node, q head) may have, over all cells; work groups a KV head
     int most_chunks;       // of a cell
     bool split;            // some cell has more than one chunk
     size_t bytes;          // partial results: [slot][node][q head] of D fp16 and four floats
@@ -208,7 +208,7 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
         }
     }
     p.n_slots = (int)tree_chunks(tiles, n, p.per);
-    p.blocks = (int)(items * p.n_slots);
+    p.blocks = p.row_tiles * p.n_slots;
     p.split = p.n_slots > n;
     if (packed) {
         p.p_tiles = ceil_div((int64_t)n * rows, 128);
@@ -224,7 +224,7 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
                 p.n_p = np;
             }
         }
-        p.blocks += (int)(row_items * p.n_p);
+        p.blocks += p.p_tiles * p.n_p;
         p.n_slots += n * p.n_p;
         p.split = true;
     }

@@ -95,7 +95,7 @@ def test_plans(plan):
             assert 1 <= first[i + 1] - first[i] - n_p <= chunks_max and first[i + 1] - first[i] <= min(64, most_chunks)
         assert first[0] == 0 and first[n] == n_slots
         items = n_slots - n * n_p
-        assert items <= slots_max and n_p <= prompt_max and blocks == sh.n_kv_heads * (row_tiles * items + n_p * p_tiles)
+        assert items <= slots_max and n_p <= prompt_max and blocks == row_tiles * items + n_p * p_tiles <= 65535
         assert not n_p or (p_tiles * 128 >= n * rows > (p_tiles - 1) * 128 and rows <= 64)
         seen = {(order[i] & 255, order[i] >> 8) for i in range(items)}
         assert seen == {(i, k) for i in range(n) for k in range(first[i + 1] - first[i] - n_p)}
