@@ -143,19 +143,28 @@ def rope_frequencies(rotary_dim: int, theta: float, scaling: Optional[str] = Non
 
 # ------------------------------------------------------------------ checks
 
-def _here(dev) -> None:
-    """Kernels are launched on the current device: its tensors are the only ones that they may read."""
-    if dev[0] != S._torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {dev[1]}, which is not the current device")
-
-
 def _anchor(t, name: str):
-    """(device index, device) of the tensor that the others of a call are compared with."""
+    """(device index, device) of the tensor that the others of a call are compared with: the current device, on which
+    kernels are launched."""
     if t is None or not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    dev = (t.get_device(), t.device)
-    _here(dev)
-    return dev
+    index = t.get_device()
+    if index != S._torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+    return index, t.device
+
+
+def _ptr(t, name: str, numel: int, dtype, dev) -> Optional[int]:
+    """S._ptr, the usual case first: a call makes up to a dozen of these checks."""
+    if t is not None and t.dtype is dtype and t.get_device() == dev[0] and t.numel() == numel > 0 and t.is_contiguous():
+        return t.data_ptr()
+    return S._ptr(t, name, numel, dtype, dev)
+
+
+def _stream(stream, dev) -> int:
+    if stream is None and S._current_raw_stream is not None:
+        return S._current_raw_stream(dev[0])
+    return S._stream_ptr(stream, dev[1])
 
 
 def _caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp):
@@ -164,11 +173,11 @@ def _caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp):
         if gen_k_exp is not None or gen_v_exp is not None:
             raise ValueError("bf16 caches take no exponents")
         dt = S._torch.bfloat16
-        return (S._ptr(gen_k, "gen_k", n * shape.head_dim, dt, dev), S._ptr(gen_v, "gen_v", n * shape.head_dim, dt, dev),
+        return (_ptr(gen_k, "gen_k", n * shape.head_dim, dt, dev), _ptr(gen_v, "gen_v", n * shape.head_dim, dt, dev),
                 None, None)
     u8 = S._torch.uint8
-    return (S._ptr(gen_k, "gen_k", n * shape.head_dim, u8, dev), S._ptr(gen_v, "gen_v", n * shape.head_dim, u8, dev),
-            S._ptr(gen_k_exp, "gen_k_exp", n, u8, dev), S._ptr(gen_v_exp, "gen_v_exp", n, u8, dev))
+    return (_ptr(gen_k, "gen_k", n * shape.head_dim, u8, dev), _ptr(gen_v, "gen_v", n * shape.head_dim, u8, dev),
+            _ptr(gen_k_exp, "gen_k_exp", n, u8, dev), _ptr(gen_v_exp, "gen_v_exp", n, u8, dev))
 
 
 def _rows(t, name: str, shape, T: int, heads: int, dev) -> Tuple[int, int]:
@@ -203,17 +212,17 @@ def splice_tree_append(shape, tree, rope, freq, cell_step, depth, q, k, v, q_out
     dev = _anchor(q_out, "q_out")
     T, C = tree.n_nodes, shape.n_cells
     t, n_q = S._torch, C * T * shape.n_q_heads * shape.head_dim
-    qo = S._ptr(q_out, "q_out", n_q, t.bfloat16, dev)
+    qo = _ptr(q_out, "q_out", n_q, t.bfloat16, dev)
     qp, qs = _rows(q, "q", shape, T, shape.n_q_heads, dev)
     kp, ks = _rows(k, "k", shape, T, shape.n_kv_heads, dev)
     vp, vs = _rows(v, "v", shape, T, shape.n_kv_heads, dev)
-    dp = S._ptr(depth, "depth", C * T, t.int32, dev)
-    pp = None if pos is None else S._ptr(pos, "pos", C * T, t.int64, dev)
-    fp = None if rope.rotary_dim == 0 and freq is None else S._ptr(freq, "freq", rope.rotary_dim // 2, t.float64, dev)
+    dp = _ptr(depth, "depth", C * T, t.int32, dev)
+    pp = None if pos is None else _ptr(pos, "pos", C * T, t.int64, dev)
+    fp = None if rope.rotary_dim == 0 and freq is None else _ptr(freq, "freq", rope.rotary_dim // 2, t.float64, dev)
     st, stp = S._steps(cell_step, C)
     S._check(lib.splice_tree_append(ctypes.byref(shape), ctypes.byref(tree), ctypes.byref(rope), stp, dp, pp, fp, qp, qs, kp,
                                     ks, vp, vs, qo, *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp),
-                                    S._stream_ptr(stream, dev[1])), "splice_tree_append")
+                                    _stream(stream, dev)), "splice_tree_append")
 
 
 def splice_tree_read(shape, tree, cell_step, gen_k, gen_v, gen_k_exp, gen_v_exp, rows_k, rows_v, stream=None) -> None:
@@ -221,11 +230,11 @@ def splice_tree_read(shape, tree, cell_step, gen_k, gen_v, gen_k_exp, gen_v_exp,
     lib = _library()
     dev = _anchor(rows_k, "rows_k")
     n = shape.n_cells * shape.n_kv_heads * tree.n_nodes * shape.head_dim
-    rk, rv = (S._ptr(x, name, n, S._torch.bfloat16, dev) for x, name in ((rows_k, "rows_k"), (rows_v, "rows_v")))
+    rk, rv = (_ptr(x, name, n, S._torch.bfloat16, dev) for x, name in ((rows_k, "rows_k"), (rows_v, "rows_v")))
     st, stp = S._steps(cell_step, shape.n_cells)
     S._check(lib.splice_tree_read(ctypes.byref(shape), ctypes.byref(tree), stp,
                                   *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp), rk, rv,
-                                  S._stream_ptr(stream, dev[1])), "splice_tree_read")
+                                  _stream(stream, dev)), "splice_tree_read")
 
 
 def splice_tree_attn_workspace_bytes(shape, call, tree) -> int:
@@ -249,35 +258,35 @@ def splice_tree_attn(shape, call, tree, cell_LW, cell_step, depth, visible, q, c
     dev = _anchor(q, "q")
     t, C, T, Hq, D = S._torch, shape.n_cells, tree.n_nodes, shape.n_q_heads, shape.head_dim
     n_prompt, bf16 = shape.n_kv_heads * shape.prompt_len * D, t.bfloat16
-    qp = S._ptr(q, "q", C * T * Hq * D, bf16, dev)
-    ck, cv = S._ptr(clean_k, "clean_k", n_prompt, bf16, dev), S._ptr(clean_v, "clean_v", n_prompt, bf16, dev)
+    qp = _ptr(q, "q", C * T * Hq * D, bf16, dev)
+    ck, cv = _ptr(clean_k, "clean_k", n_prompt, bf16, dev), _ptr(clean_v, "clean_v", n_prompt, bf16, dev)
     if shape.donor_kind == S.SPLICE_DONOR_ZERO:
         if donor_k is not None or donor_v is not None:
             raise ValueError("the ZERO donor takes no donor buffers")
         dk = dv = None
     else:
-        dk, dv = S._ptr(donor_k, "donor_k", n_prompt, bf16, dev), S._ptr(donor_v, "donor_v", n_prompt, bf16, dev)
+        dk, dv = _ptr(donor_k, "donor_k", n_prompt, bf16, dev), _ptr(donor_v, "donor_v", n_prompt, bf16, dev)
     gen = _caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp)
-    dp = S._ptr(depth, "depth", C * T, t.int32, dev)
+    dp = _ptr(depth, "depth", C * T, t.int32, dev)
     words = t.int64 if visible is None or visible.dtype is t.int64 else getattr(t, "uint64", t.int64)
-    vp = S._ptr(visible, "visible", C * T, words, dev)
-    op, lp = S._ptr(out, "out", C * T * Hq * D, bf16, dev), S._ptr(lse, "lse", C * T * Hq, t.float32, dev)
+    vp = _ptr(visible, "visible", C * T, words, dev)
+    op, lp = _ptr(out, "out", C * T * Hq * D, bf16, dev), _ptr(lse, "lse", C * T * Hq, t.float32, dev)
     wp, wbytes = _workspace(workspace, dev)
     lw, lwp = S._cells(cell_LW, C)
     st, stp = S._steps(cell_step, C)
     S._check(lib.splice_tree_attn(ctypes.byref(shape), ctypes.byref(call), ctypes.byref(tree), lwp, stp, dp, vp, qp, ck, cv,
-                                  dk, dv, *gen, op, lp, wp, wbytes, S._stream_ptr(stream, dev[1])), "splice_tree_attn")
+                                  dk, dv, *gen, op, lp, wp, wbytes, _stream(stream, dev)), "splice_tree_attn")
 
 
 def splice_tree_keep(shape, tree, cell_step, keep, gen_k, gen_v, gen_k_exp=None, gen_v_exp=None, stream=None) -> None:
     """Row s_c + i of the generated caches = row s_c + keep[c][i] (``keep`` int32 [C][T], ascending, ended by -1)."""
     lib = _library()
     dev = _anchor(keep, "keep")
-    kp = S._ptr(keep, "keep", shape.n_cells * tree.n_nodes, S._torch.int32, dev)
+    kp = _ptr(keep, "keep", shape.n_cells * tree.n_nodes, S._torch.int32, dev)
     st, stp = S._steps(cell_step, shape.n_cells)
     S._check(lib.splice_tree_keep(ctypes.byref(shape), ctypes.byref(tree), stp, kp,
                                   *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp),
-                                  S._stream_ptr(stream, dev[1])), "splice_tree_keep")
+                                  _stream(stream, dev)), "splice_tree_keep")
 
 
 def splice_token_scores_workspace_bytes(rows: int, vocab: int, k: int) -> int:
@@ -306,15 +315,15 @@ def splice_token_scores(logits, tokens, logp, lse, entropy, rank, top, top_logp,
             raise ValueError(f"top has shape {tuple(top.shape)}, expected ({rows}, k)")
         k = top.shape[1]
     f32, i64 = t.float32, t.int64
-    tok, rk = S._ptr(tokens, "tokens", rows, i64, dev), S._ptr(rank, "rank", rows, i64, dev)
-    out = [S._ptr(x, name, rows, f32, dev) for x, name in ((logp, "logp"), (lse, "lse"), (entropy, "entropy"))]
+    tok, rk = _ptr(tokens, "tokens", rows, i64, dev), _ptr(rank, "rank", rows, i64, dev)
+    out = [_ptr(x, name, rows, f32, dev) for x, name in ((logp, "logp"), (lse, "lse"), (entropy, "entropy"))]
     tp = tl = None
     if k:
-        tp, tl = S._ptr(top, "top", rows * k, i64, dev), S._ptr(top_logp, "top_logp", rows * k, f32, dev)
+        tp, tl = _ptr(top, "top", rows * k, i64, dev), _ptr(top_logp, "top_logp", rows * k, f32, dev)
     wp, wbytes = _workspace(workspace, dev)
     S._check(lib.splice_token_scores(logits.data_ptr(), S.SPLICE_BF16 if logits.dtype is t.bfloat16 else S.SPLICE_F32, rows,
                                      vocab, stride, float(scale), tok, k, *out, rk, tp, tl, wp, wbytes,
-                                     S._stream_ptr(stream, dev[1])), "splice_token_scores")
+                                     _stream(stream, dev)), "splice_token_scores")
 
 
 class TokenScores(NamedTuple):
