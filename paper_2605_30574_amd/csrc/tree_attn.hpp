@@ -42,10 +42,11 @@ struct TreeCall {
     const uint64_t *visible;
     __bf16 *out;
     float *lse;
-    // Partial results, [slot][node][q head]: o / l in fp16 (a convex combination
-    // of value rows; where one passes 2^15, times a power of two sc), and m,
-    // l, l / sc.  A rounding of 2^-12 of them is small beside the bf16 result's,
-    // and in 32 bits they would be 53% of what a call of many chunks writes and reads again.
+    // Partial results, [slot][node][q head]: o / l (a convex combination of
+    // value rows) in fp16, times a power of two sc that brings a row's
+    // largest value to 2^14 .. 2^15, and m, l, 1 / sc.  A rounding of 2^-12 of
+    // it is small beside the bf16 result's, and 32 bits would be 1.9 times the
+    // bytes that a call of many chunks writes and reads again.
     _Float16 *part;
     float4 *record;
     int T, G, lgG, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, per;
@@ -125,12 +126,11 @@ __device__ __forceinline__ uint64_t shifted(uint64_t x, int by) {   // left, or 
     return by >= 0 ? x << by : x >> -by;
 }
 
-// |x|, 0 for an infinity or NaN; and the power of two that brings a largest
-// value down to 2^15 where it is above.
+// |x|, 0 for an infinity or NaN; and the power of two, 2^60 at most, that
+// brings a largest value to 2^14 .. 2^15.
 __device__ __forceinline__ float finite_size(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
 __device__ __forceinline__ float half_scale(float top) {
-    if (!(top > 32768.f)) return 1.f;
-    return __uint_as_float((uint32_t)(127 + 14 + 127 - (int)(__float_as_uint(top) >> 23)) << 23);
+    return __uint_as_float((uint32_t)min(127 + 14 + 127 - (int)(__float_as_uint(top) >> 23), 127 + 60) << 23);
 }
 
 // A pointer that is the same in every lane, in scalar registers (a buffer
@@ -729,7 +729,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
                     const int64_t at = ((int64_t)slot * a.T + nd) * (a.Hkv * a.G) + hd;
                     const float sc = half_scale(size);
                     *reinterpret_cast<f16x4_t *>(a.part + at * D + d) = __builtin_convertvector(O * sc, f16x4_t);
-                    if (d == 0) a.record[at] = make_float4(M, Lsum, Lsum / sc, 0.f);
+                    if (d == 0) a.record[at] = make_float4(M, Lsum, 1.f / sc, 0.f);
                 } else {
                     const int64_t at = (node0 + nd) * (a.Hkv * a.G) + hd;
                     *reinterpret_cast<bf16x4_t *>(a.out + at * D + d) = __builtin_convertvector(O, bf16x4_t);
@@ -757,7 +757,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
             });
         });
         if (h == 0) {
-            if (PACKED || a.split) a.record[part_row] = make_float4(m, l, l / sc, 0.f);
+            if (PACKED || a.split) a.record[part_row] = make_float4(m, l, 1.f / sc, 0.f);
             else a.lse[out_row] = kLn2 * (m + log2f(l));
         }
     }
@@ -798,9 +798,10 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
     if (mine < n) x = a.record[row + mine * stride];
     float M = x.x;
     for (int o = 1; o < GROUP; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-    const float f = fast_exp2(x.x - (M == -INFINITY ? 0.f : M)), weight = f * x.z;
-    float L = f * x.y;
+    const float share = fast_exp2(x.x - (M == -INFINITY ? 0.f : M)) * x.y;
+    float L = share;
     for (int o = 1; o < GROUP; o <<= 1) L += __shfl_xor(L, o);
+    const float weight = share == 0.f ? 0.f : share / L * x.z;
     const _Float16 *src = a.part + row * D + 8 * l;
     f32x8_t O = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     constexpr int U = MANY ? 4 : 8, STEP = MANY ? SP : 1;
@@ -817,8 +818,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
         for (int o = LPR; o < 64; o <<= 1) static_for<0, 8>([&](auto i) { O[(int)i] += __shfl_xor(O[(int)i], o); });
     if (hd >= Hq || (MANY && sp != 0)) return;
     const int64_t at = at_node * Hq + hd;
-    const float r = L == 0.f ? 0.f : 1.f / L;
-    *reinterpret_cast<bf16x8_t *>(a.out + at * D + 8 * l) = __builtin_convertvector(O * r, bf16x8_t);
+    *reinterpret_cast<bf16x8_t *>(a.out + at * D + 8 * l) = __builtin_convertvector(O, bf16x8_t);
     if (l == 0) a.lse[at] = kLn2 * (M + log2f(L));
 }
 

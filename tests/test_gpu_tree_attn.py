@@ -308,3 +308,36 @@ def test_large_values_keep_their_scale():
     # the scaled partial results are rounded alike up to fp16's subnormals, the result after it
     got, want = big[on].double() * 2.0 ** -100, out[on].double()
     assert ((got - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -14).all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** -20, 2.0 ** -50, 2.0 ** -100])
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("T,D", [(2, 64), (9, 128), (12, 256)])
+def test_small_values_keep_their_scale(T, D, shared, size):
+    """Values far below fp16's range go through the partial results by a power of two of up to 2^60: at least ten bits of a
+    row's largest value are left at 2^-60, and with it at 2^-100 the absolute error is 2^-25 2^-60."""
+    s = Sweep(251, C=6 if shared else 2, T=T, D=D, Hq=4, Hkv=1, Tp=900, span=(100, 800), cap=600)
+    for x in (s.clean[1], s.donor[1], s.gen[1]):
+        x.mul_(size)
+    out, lse = s.attend(128)
+    if size >= 2.0 ** -50:
+        s.check(out, lse, f"values of {size}")
+    else:
+        torch.cuda.synchronize()
+        want = s.expected()[0]
+        on = s.depth >= 0
+        assert np.abs(f64(out) - want)[on].max() <= 2.0 ** -85
+
+
+def test_no_cells():
+    """A call of no cells checks its tensors and returns."""
+    s = Sweep(257, C=0, T=3)
+    out, lse = s.attend()
+    rope = sp.make_rope("half", 64)
+    freq = torch.ones(32, dtype=torch.float64, device="cuda")
+    k = torch.empty(0, 3, s.Hkv, s.D, dtype=torch.bfloat16, device="cuda")
+    sp.splice_tree_append(s.shape, s.tree, rope, freq, s.steps, s.depth_dev, s.q, k, k, out, *s.gen)
+    sp.splice_tree_keep(s.shape, s.tree, s.steps, s.depth_dev, *s.gen)
+    rows = torch.empty(0, s.Hkv, 3, s.D, dtype=torch.bfloat16, device="cuda")
+    sp.splice_tree_read(s.shape, s.tree, s.steps, *s.gen, None, None, rows, rows.clone())
+    torch.cuda.synchronize()
