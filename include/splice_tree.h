@@ -41,8 +41,8 @@
  * Otherwise the conventions of splice_attn.h hold: shapes, splices, ownership,
  * alignment (16 bytes; exponents, depth, lse and logits as their types),
  * streams, errors.  Every entry takes shape->dtype == SPLICE_BF16 only
- * (SPLICE_EUNSUPPORTED otherwise).  s_c + T <= gen_capacity for every active
- * cell (SPLICE_ESHAPE).  Results are deterministic.
+ * and fewer than 2^16 query heads (SPLICE_EUNSUPPORTED otherwise).  s_c + T <=
+ * gen_capacity for every active cell (SPLICE_ESHAPE).  Results are deterministic.
  */
 #ifndef SPLICE_TREE_H
 #define SPLICE_TREE_H
@@ -99,7 +99,10 @@ SPLICE_API int32_t splice_tree_read(const splice_shape *shape, const splice_tree
 /*
  * out [C][T][Hq][D] bf16 and lse [C][T][Hq] fp32 (natural log) of the nodes
  * of every active cell; q [C][T][Hq][D] bf16, rotated.  call->step and
- * call->merge_wait are ignored.  workspace: 256-byte aligned,
+ * call->merge_wait are ignored.  Weighted values are summed in fp32 before the
+ * division by the weights' sum, and a weight may be 2^8: values of a size that
+ * times 2^8 times the number of keys passes fp32's range may give infinities.
+ * workspace: 256-byte aligned,
  * splice_tree_attn_workspace_bytes(shape, call, tree) bytes (enough for any
  * steps; it may be 0), no initialisation.  Calls that share a workspace must
  * be ordered on one stream.
@@ -139,7 +142,7 @@ SPLICE_API int32_t splice_tree_keep(const splice_shape *shape, const splice_tree
  * Logits of -inf have probability 0 (a row of nothing else: lse -inf,
  * entropy and logp NaN).  NaN logits make the row's lse, entropy and log
  * probabilities NaN and come first in its order; ranks count them as above every number.
- * Sums are fp32.  logp, lse, entropy fp32 [rows]; rank, tokens, top int64.
+ * Sums are fp32; rows < 2^24, vocab <= 2^28.  logp, lse, entropy fp32 [rows]; rank, tokens, top int64.
  * workspace: 16-byte aligned, splice_token_scores_workspace_bytes bytes, no
  * initialisation.
  */

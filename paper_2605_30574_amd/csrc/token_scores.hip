@@ -465,8 +465,9 @@ int parts_of(int64_t rows, int64_t vocab, int k) {
     return (int)(parts < fit ? parts : fit);
 }
 
+// (a work group a row: a launch has fewer than 2^32 threads)
 bool takes(int64_t rows, int64_t vocab, int32_t k) {
-    return rows >= 0 && rows <= 1 << 24 && vocab >= 1 && vocab <= 1 << 28 && k >= 0 && k <= SPLICE_MAX_TOP && k <= vocab;
+    return rows >= 0 && rows < 1 << 24 && vocab >= 1 && vocab <= 1 << 28 && k >= 0 && k <= SPLICE_MAX_TOP && k <= vocab;
 }
 
 }  // namespace

@@ -249,9 +249,7 @@ int32_t splice_tree_append(const splice_shape *shape, const splice_tree *tree, c
     const int n = splice::active_cells(sh, cell_step, a.cells);
     if (n == 0) return SPLICE_OK;
     const int rows = kAppendThreads / (D / 8);
-    const int64_t heads = (int64_t)sh.n_q_heads + 2 * (int64_t)sh.n_kv_heads;
-    if ((heads + rows - 1) / rows > 65535) return SPLICE_EUNSUPPORTED;
-    const dim3 grid((unsigned)(n * tree->n_nodes), (unsigned)((heads + rows - 1) / rows));
+    const dim3 grid((unsigned)(n * tree->n_nodes), (unsigned)splice::ceil_div(sh.n_q_heads + 2 * sh.n_kv_heads, rows));
     splice::with_format(D, tree->kv_format, [&](auto d, auto f8) {
         hipLaunchKernelGGL((append_kernel<decltype(d)::value, decltype(f8)::value>), grid, dim3(kAppendThreads), 0,
                            (hipStream_t)stream, a);
@@ -273,7 +271,6 @@ int32_t splice_tree_read(const splice_shape *shape, const splice_tree *tree, con
                shape->n_kv_heads, shape->gen_capacity, {}};
     const int n = splice::active_cells(*shape, cell_step, a.cells);
     if (n == 0) return SPLICE_OK;
-    if ((int64_t)n * shape->n_kv_heads > INT32_MAX) return SPLICE_EUNSUPPORTED;
     const dim3 grid((unsigned)(n * shape->n_kv_heads), 2);
     splice::with_format(shape->head_dim, tree->kv_format, [&](auto d, auto f8) {
         hipLaunchKernelGGL((read_kernel<decltype(d)::value, decltype(f8)::value>), grid, dim3(kAppendThreads), 0,
@@ -293,7 +290,6 @@ int32_t splice_tree_keep(const splice_shape *shape, const splice_tree *tree, con
                shape->n_kv_heads, shape->gen_capacity, {}};
     const int n = splice::active_cells(*shape, cell_step, a.cells);
     if (n == 0) return SPLICE_OK;
-    if ((int64_t)n * shape->n_kv_heads > INT32_MAX) return SPLICE_EUNSUPPORTED;
     const dim3 grid((unsigned)(n * shape->n_kv_heads), 2);
     splice::with_format(shape->head_dim, tree->kv_format, [&](auto d, auto f8) {
         constexpr int ROW = decltype(d)::value * (decltype(f8)::value ? 1 : 2);

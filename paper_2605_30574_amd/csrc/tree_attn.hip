@@ -54,6 +54,7 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     checked.step = 0;   // every node takes its own step
     rc = splice::validate_call(sh, &checked);
     if (rc != SPLICE_OK) return rc;
+    if (!isfinite(call->scale * splice_dev::kLog2e)) return SPLICE_EINVAL;
     rc = splice::validate_cells(sh, cell_LW);
     if (rc != SPLICE_OK) return rc;
     if (sh.n_cells == 0) return SPLICE_OK;
@@ -73,7 +74,6 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     int n = 0;
     const splice::TreePlan p = splice::tree_prepare(sh, checked, *tree, cell_LW, cell_step, compute_units(), n, args.step, args.slots);
     if (n == 0) return SPLICE_OK;
-    if (p.blocks > 65535 || (int64_t)n * T * sh.n_q_heads > (int64_t)1 << 30) return SPLICE_EUNSUPPORTED;
     if (p.bytes > 0 && (!workspace || !splice::aligned(workspace, 256) || workspace_bytes < p.bytes)) return SPLICE_EWORKSPACE;
     splice_dev::TreeCall &a = args.call;
     a.q = (const char *)q;

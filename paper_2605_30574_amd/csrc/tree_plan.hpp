@@ -36,6 +36,8 @@ inline int32_t validate_tree_shape(const splice_shape *shape, const splice_tree 
     if (!tree || (tree->kv_format != SPLICE_KV_BF16 && tree->kv_format != SPLICE_KV_E4M3)) return SPLICE_EINVAL;
     if (tree->n_nodes < 1) return SPLICE_ESHAPE;
     if (tree->n_nodes > SPLICE_MAX_NODES || shape->dtype != SPLICE_BF16) return SPLICE_EUNSUPPORTED;
+    // a launch has fewer than 2^32 threads along x (256 cells, a work group a KV head each) and 2^16 work groups along y
+    if (shape->n_q_heads >= 1 << 16) return SPLICE_EUNSUPPORTED;
     if (tree->n_nodes > shape->gen_capacity) return SPLICE_ESHAPE;
     return SPLICE_OK;
 }

@@ -101,7 +101,14 @@ def test_shapes_trees_and_steps(entry):
     assert entry(sh=shape(n_cells=0), steps=None) == sp.SPLICE_OK
 
 
+@pytest.mark.parametrize("entry", EVERY)
+def test_more_heads_than_a_grid_has_work_groups(entry):
+    assert entry(sh=shape(n_q_heads=1 << 16, n_kv_heads=1 << 16)) == sp.SPLICE_EUNSUPPORTED
+    assert entry(sh=shape(n_q_heads=1 << 30, n_kv_heads=1 << 30)) == sp.SPLICE_EUNSUPPORTED
+
+
 def test_attention_refusals():
+    assert attn(call=sp.make_call(1, 0, 0, 3e38)) == sp.SPLICE_EINVAL     # no float in base 2
     assert attn(call=sp.make_call(4, 0, 0, 0.1)) == sp.SPLICE_ESHAPE
     assert attn(call=sp.make_call(1, 0, -1, 0.1)) == sp.SPLICE_ESHAPE
     for scale in (0.0, -1.0, float("nan"), float("inf")):
@@ -157,7 +164,7 @@ def test_keep_and_read_refusals():
 def test_scores_refusals():
     assert scores(dtype=2) == sp.SPLICE_EINVAL
     for kw in (dict(rows=-1), dict(vocab=0), dict(k=-1), dict(k=65), dict(vocab=4), dict(vocab=(1 << 28) + 1, stride=1 << 29),
-               dict(rows=(1 << 24) + 1), dict(stride=99), dict(stride=-100), dict(stride=1 << 33)):
+               dict(rows=1 << 24), dict(stride=99), dict(stride=-100), dict(stride=1 << 33)):
         assert scores(**kw) == sp.SPLICE_ESHAPE, kw
     for scale in (0.0, -1.0, float("nan"), float("inf"), 3e38):
         assert scores(scale=scale) == sp.SPLICE_EINVAL
