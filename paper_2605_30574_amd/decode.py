@@ -127,7 +127,8 @@ class DecoderTree(NamedTuple):
     spec: T.SpliceTree
     depth: torch.Tensor       # int32 [C][T]
     visible: torch.Tensor     # int64 [C][T]
-    workspace: torch.Tensor
+    workspace: torch.Tensor   # of one pass at a time
+    freq: torch.Tensor        # float64 [D / 2], of the rotary positions
     parents: np.ndarray       # int64 [C][T]
 
 
@@ -317,7 +318,8 @@ class SweepDecoder:
 
     def make_tree(self, parents) -> DecoderTree:
         """Trees of T nodes per cell (``tree.tree_layout``: parents [C][T], -1 a root, less padding) for score_tree and
-        keep_nodes.  Generated caches may be bfloat16, or uint8 (e4m3) with ``gen_k_exp`` and ``gen_v_exp``."""
+        keep_nodes.  Generated caches may be bfloat16, or uint8 (e4m3) with ``gen_k_exp`` and ``gen_v_exp`` (which
+        ``step`` does not take).  Passes over one tree object share its workspace: order them on one stream."""
         parents = np.asarray(parents)
         depth, visible = T.tree_layout(parents)
         if depth.shape[0] != self.C:
@@ -325,7 +327,9 @@ class SweepDecoder:
         spec = T.make_tree(depth.shape[1], self._kv_format())
         need = max((T.splice_tree_attn_workspace_bytes(self.shape, call, spec) for call in self.calls), default=0)
         return DecoderTree(spec, torch.from_numpy(depth).to(self.device), torch.from_numpy(visible.view(np.int64)).to(self.device),
-                           torch.empty(need, dtype=torch.uint8, device=self.device), parents.astype(np.int64))
+                           torch.empty(need, dtype=torch.uint8, device=self.device),
+                           torch.from_numpy(T.rope_frequencies(self.w.head_dim, float(self.m.rope_theta))[0]).to(self.device),
+                           parents.astype(np.int64))
 
     @torch.no_grad()
     def tree_logits(self, tokens: torch.Tensor, tree: DecoderTree, steps: np.ndarray) -> torch.Tensor:
@@ -344,7 +348,6 @@ class SweepDecoder:
             pos = (self.positions(st).to(torch.int64)[:, None] + tree.depth).contiguous()
         x = wt["embed"][tokens.reshape(-1)]
         cdt, dev, rows = x.dtype, x.device, C * n
-        freq = torch.from_numpy(T.rope_frequencies(D, float(m.rope_theta))[0]).to(dev)
         rope_of, bf16 = T.make_rope("half", D), torch.bfloat16
         out = torch.zeros((C, n, Hq, D), dtype=bf16, device=dev)
         lse = torch.empty((C, n, Hq), dtype=torch.float32, device=dev)
@@ -355,7 +358,7 @@ class SweepDecoder:
             c = self.caches[l]
             e = [c[name] for name in exps] or [None, None]
             q, k, v = q.to(bf16).view(C, n, Hq, D), k.to(bf16).view(C, n, Hkv, D), v.to(bf16).view(C, n, Hkv, D)
-            T.splice_tree_append(self.shape, tree.spec, rope_of, freq, st, tree.depth, q, k, v, q, c["gen_k"], c["gen_v"], *e,
+            T.splice_tree_append(self.shape, tree.spec, rope_of, tree.freq, st, tree.depth, q, k, v, q, c["gen_k"], c["gen_v"], *e,
                                  pos=pos)
             T.splice_tree_attn(self.shape, self.calls[l], tree.spec, self.lw, st, tree.depth, tree.visible, q, c["clean_k"],
                                c["clean_v"], c["donor_k"], c["donor_v"], c["gen_k"], c["gen_v"], *e, out, lse, tree.workspace)

@@ -336,8 +336,9 @@ class TokenScores(NamedTuple):
     top_logp: object
 
 
-def token_scores(logits, tokens, top: int = 0, scale: float = 1.0, stream=None) -> TokenScores:
-    """``splice_token_scores`` with its outputs and workspace allocated by torch."""
+def token_scores(logits, tokens, top: int = 0, scale: float = 1.0) -> TokenScores:
+    """``splice_token_scores`` on the current stream, with its outputs and workspace allocated by torch (whose
+    memory is that stream's: for another one, ``with torch.cuda.stream(...)``)."""
     S.load_library()
     t, dev = S._torch, logits.device
     if logits.dim() != 2:
@@ -348,5 +349,5 @@ def token_scores(logits, tokens, top: int = 0, scale: float = 1.0, stream=None) 
     ids = t.empty((rows, top), dtype=t.int64, device=dev) if top else None
     vals = t.empty((rows, top), dtype=t.float32, device=dev) if top else None
     ws = t.empty(splice_token_scores_workspace_bytes(rows, vocab, top), dtype=t.uint8, device=dev)
-    splice_token_scores(logits, tokens, logp, lse, entropy, rank, ids, vals, ws, scale, stream)
+    splice_token_scores(logits, tokens, logp, lse, entropy, rank, ids, vals, ws, scale)
     return TokenScores(logp, lse, entropy, rank, ids, vals)
