@@ -168,7 +168,10 @@ inline bool tree_packed(const splice_shape &sh, const splice_call &call, int T, 
 
 // Chunks of equal length, so that the work groups of all cells fill k rounds
 // of what the GPU holds at once; k is the one that takes least by
-// k * (per + kTreeStart).  tiles: of the cells' lists, in a packed call without
+// k * (per + kTreeStart); of a packed call's prompt one more kTreeStart where the
+// generated rows' items do not fit beside its last round (40 cells of 12 nodes,
+// D = 256, 1024 keys in view: 16 chunks of two tiles 44 us, 8 of four, beside
+// which they fit, 32).  tiles: of the cells' lists, in a packed call without
 // the prompt, whose list is prompt_tiles long.
 inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, int n_cu, bool f8, bool packed,
                           int prompt_tiles) {
@@ -215,12 +218,14 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
     if (packed) {
         p.p_tiles = ceil_div((int64_t)n * rows, 128);
         const int64_t row_items = (int64_t)sh.n_kv_heads * p.p_tiles;
+        const int64_t gen_items = (int64_t)sh.n_kv_heads * p.blocks;
         int64_t best = INT64_MAX;
         for (int np = 1; np <= kTreeMaxPrompt && np <= prompt_tiles; ++np) {
             if (np > 1 && call.split_keys == 0 && row_items * np > kTreeRounds * room) break;
             const int64_t per = ceil_div(prompt_tiles, np);
+            const int64_t rounds = ceil_div(row_items * np, room), spare = rounds * room - row_items * np;
             const int64_t cost = call.split_keys > 0 ? (per * 64 >= call.split_keys ? -np : np)
-                                                     : ceil_div(row_items * np, room) * (per + kTreeStart);
+                                                     : rounds * (per + kTreeStart) + (spare < gen_items ? kTreeStart : 0);
             if (cost < best) {
                 best = cost;
                 p.n_p = np;
