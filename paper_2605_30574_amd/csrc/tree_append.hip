@@ -62,6 +62,30 @@ __device__ __forceinline__ uint2 quantise(const f32x8v_t &x, uint32_t bits, uint
     return make_uint2((uint32_t)lo, (uint32_t)hi);
 }
 
+// (cos, sin) of so many turns, times a factor, each rounded once: an 8-bit code
+// next to a border falls on the side where the exact rotation lies.  To
+// the nearest quarter turn, then the series of sine and cosine on
+// [-pi / 4, pi / 4], whose first term left out is below 2^-33.
+__device__ __forceinline__ float2 turned(double turns, double factor) {
+    turns -= rint(turns);
+    const double n = rint(4. * turns);
+    const double x = (turns - 0.25 * n) * 6.28318530717958647693, y = x * x;
+    double sn = 1. / 39916800., cs = -1. / 3628800.;
+    sn = fma(-sn, y, 1. / 362880.);
+    cs = fma(cs, y, 1. / 40320.);
+    sn = fma(sn, y, -1. / 5040.);
+    cs = fma(cs, y, -1. / 720.);
+    sn = fma(sn, y, 1. / 120.);
+    cs = fma(cs, y, 1. / 24.);
+    sn = fma(sn, y, -1. / 6.);
+    cs = fma(cs, y, -1. / 2.);
+    sn = fma(sn * y, x, x);
+    cs = fma(cs, y, 1.);
+    const int k = (int)n & 3;   // quarters
+    const double c = k & 1 ? sn : cs, s = k & 1 ? cs : sn;
+    return make_float2((float)((k == 1 || k == 2 ? -c : c) * factor), (float)((k & 2 ? -s : s) * factor));
+}
+
 // A work group takes one node's heads kAppendThreads / LPR at a time (LPR = D / 8
 // lanes a head row, eight values a lane): blockIdx.x the node, blockIdx.y the
 // heads.  The angles of the node are computed once and shared.  Launch and
@@ -77,10 +101,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
     if (depth < 0) return;   // padding
     if (tid < a.half_rotary) {
         const double p = a.pos ? (double)a.pos[token] : (double)(a.Tp + step) + (double)min(depth, a.T - 1);
-        const double turns = p * (a.freq[tid] * 0.15915494309189533577);   // 1 / (2 pi)
-        float sn, cs;
-        sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
-        s_cs[tid] = make_float2(cs * a.mscale, sn * a.mscale);
+        s_cs[tid] = turned(p * (a.freq[tid] * 0.15915494309189533577), (double)a.mscale);   // 1 / (2 pi)
     }
     __syncthreads();
     const int hd = blockIdx.y * ROWS + tid / LPR, l = tid % LPR;
@@ -96,8 +117,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
             static_for<0, 4>([&](auto i) {
                 const float2 cs = s_cs[d / 2 + (int)i];
                 const float u = x[2 * (int)i], w = x[2 * (int)i + 1];
-                x[2 * (int)i] = u * cs.x - w * cs.y;
-                x[2 * (int)i + 1] = w * cs.x + u * cs.y;
+                x[2 * (int)i] = fmaf(u, cs.x, -(w * cs.y));
+                x[2 * (int)i + 1] = fmaf(w, cs.x, u * cs.y);
             });
         } else {
             const bool low = d < half;
@@ -107,7 +128,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
             static_for<0, 8>([&](auto i) {
                 const float2 cs = s_cs[f + (int)i];
                 const float u = x[(int)i], w = o[(int)i];
-                x[(int)i] = low ? u * cs.x - w * cs.y : u * cs.x + w * cs.y;
+                x[(int)i] = fmaf(u, cs.x, low ? -(w * cs.y) : w * cs.y);
             });
         }
     }
