@@ -226,16 +226,13 @@ __device__ __forceinline__ float logit(const char *row, int i) {
     return BF16 ? bf16_hi((uint32_t)reinterpret_cast<const uint16_t *>(row)[i] << 16) : reinterpret_cast<const float *>(row)[i];
 }
 
-// The row's results from its joined sums and its first k keys; called by one wave.
-template <bool BF16>
-__device__ __forceinline__ void finish(const ScoreArgs &a, int64_t row, float m, float s, float t, int before,
+// The row's results from its joined sums and its first k keys; in, x: whether
+// the token is one of the vocabulary, its logit.  Called by one wave.
+__device__ __forceinline__ void finish(const ScoreArgs &a, int64_t row, bool in, float x, float m, float s, float t, int before,
                                        const uint64_t *first) {
     const int lane = threadIdx.x & 63;
     const float log_s = kLn2 * log2f(s);   // -inf for a row of nothing
     if (lane == 0) {
-        const int64_t tok = a.tokens[row];
-        const bool in = tok >= 0 && tok < a.vocab;
-        const float x = in ? logit<BF16>(a.logits + row * a.stride, (int)tok) : 0.f;
         a.logp[row] = in ? (x - m) * a.scale - log_s : __uint_as_float(0x7fc00000u);
         a.lse[row] = fmaf(m, a.scale, log_s);
         a.entropy[row] = log_s - kLn2 * (t / s);
@@ -265,6 +262,16 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreArgs a) {
     const int n_chunks = (a.vocab - head) / VE, tail = a.vocab - head - n_chunks * VE;
     const char *base = p + head * ES;
     const int per = (n_chunks + a.parts - 1) / a.parts, c0 = min(part * per, n_chunks), c1 = min(c0 + per, n_chunks);
+
+    u32x4_t w[kChunks];   // the next trip's; the first is on its way while the token's logit is looked up
+    auto load = [&](int c) {
+        static_for<0, kChunks>([&](auto u) {
+            const int j = c + (int)u * kScoreThreads + tid;
+            if (j < c1) w[u] = *reinterpret_cast<const u32x4_t *>(base + (int64_t)j * 16);
+        });
+    };
+    load(c0);
+    __builtin_amdgcn_sched_barrier(0);
 
     const int64_t tok = a.tokens[row];
     const bool in = tok >= 0 && tok < a.vocab;
@@ -342,14 +349,6 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreArgs a) {
     }
     if (a.k > 0) list.append(single_id >= 0, key_of(single, single_id));
 
-    u32x4_t w[kChunks];   // the next trip's
-    auto load = [&](int c) {
-        static_for<0, kChunks>([&](auto u) {
-            const int j = c + (int)u * kScoreThreads + tid;
-            if (j < c1) w[u] = *reinterpret_cast<const u32x4_t *>(base + (int64_t)j * 16);
-        });
-    };
-    load(c0);
     for (int c = c0; c < c1; c += kScoreThreads * kChunks) {   // the same trips in every lane
         float x[kChunks][VE], top[kChunks];
         static_for<0, kChunks>([&](auto u) {
@@ -427,7 +426,7 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreArgs a) {
             list.only(again ? had : list.n, kth);
             if (!again) break;   // else the trip again: its keys that are not below
         }
-        if (list.n >= told_n + (q + 1) / 2) tell(list.bound(q));
+        if (c + kScoreThreads * kChunks < c1 && list.n >= told_n + (q + 1) / 2) tell(list.bound(q));
     }
     if (a.k > 0) {
         // the waves' lists together
@@ -456,7 +455,7 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreArgs a) {
         before += s_sums[w].before;
     }
     if (a.parts == 1) {
-        finish<BF16>(a, row, m, s, t, before, s_top.first);
+        finish(a, row, in, xt, m, s, t, before, s_top.first);
         return;
     }
     if (lane == 0) a.sums[blockIdx.x] = PartSums{m, s, t, before};
@@ -464,12 +463,18 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreArgs a) {
 }
 
 // Joins the parts of a row, a work group a row.  With q = ceil(k / parts), the
-// least of the parts' q-th keys has at least k keys not below it.
+// ceil(k / q)-th of the parts' q-th keys has at least k keys not below it.
 template <bool BF16>
 __global__ __launch_bounds__(kScoreThreads) void score_join_kernel(ScoreArgs a) {
     __shared__ Candidates s_top;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // all that is read of the row, at once
+    const int64_t tok = a.tokens[row];
+    PartSums p{-INFINITY, 0.f, 0.f, 0};
+    if (lane < a.parts) p = a.sums[row * a.parts + lane];
+    const bool in = tok >= 0 && tok < a.vocab;
+    const float xt = logit<BF16>(a.logits + row * a.stride, in ? (int)tok : 0);
     if (a.k > 0) {
         constexpr int PER = kCandidates / kScoreThreads;
         const int n = a.parts * a.k, q = (a.k + a.parts - 1) / a.parts;
@@ -478,35 +483,23 @@ __global__ __launch_bounds__(kScoreThreads) void score_join_kernel(ScoreArgs a) 
             const int e = tid + (int)i * kScoreThreads;
             key[i] = e < n ? a.keys[row * n + e] : 0;
         });
-        uint64_t least = tid < a.parts ? a.keys[row * n + tid * a.k + q - 1] : ~0ull;
         if (wave == 0) {   // at most 64 parts
-            for (int o = 32; o > 0; o >>= 1) {
-                const uint64_t x = __shfl_xor((unsigned long long)least, o);
-                least = x < least ? x : least;
-            }
+            const uint32_t u[1] = {lane < a.parts ? (uint32_t)(a.keys[row * n + lane * a.k + q - 1] >> 32) : 0};
+            const uint32_t bound = nth_word(u, (a.k + q - 1) / q, kBoundBit);
             if (lane == 0) {
-                s_top.least = least;
+                s_top.least = (uint64_t)bound << 32;
                 s_top.n = 0;
             }
         }
         __syncthreads();
-        least = s_top.least;
+        const uint64_t least = s_top.least;
         static_for<0, PER>([&](auto i) { if (key[i] != 0 && key[i] >= least) append(s_top, key[i]); });
         __syncthreads();
         rank_first(s_top, s_top.n, a.k);
     }
     if (wave != 0) return;
-    float m = -INFINITY, s = 0.f, t = 0.f;
-    int before = 0;
-    if (lane < a.parts) {
-        const PartSums p = a.sums[row * a.parts + lane];
-        m = p.m;
-        s = p.s;
-        t = p.t;
-        before = p.before;
-    }
-    wave_join(a.scale2, m, s, t, before);
-    finish<BF16>(a, row, m, s, t, before, s_top.first);
+    wave_join(a.scale2, p.m, p.s, p.t, p.before);
+    finish(a, row, in, xt, p.m, p.s, p.t, p.before, s_top.first);
 }
 
 int parts_of(int64_t rows, int64_t vocab, int k) {
