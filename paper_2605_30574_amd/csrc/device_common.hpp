@@ -90,4 +90,12 @@ __device__ __forceinline__ const char *pick_base(bool second, const char *first_
     return first_base + (second ? delta : (uintptr_t)0);
 }
 
+// Lanes of a wave that hand each other values through LDS: its operations run
+// in order, so only the compiler has to keep theirs.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+
 }  // namespace splice_dev

@@ -32,7 +32,7 @@ constexpr int kScoreThreads = 256;
 constexpr int kScoreWaves = kScoreThreads / 64;
 constexpr int kChunks = 4;            // 16-byte chunks a thread has in flight
 constexpr int kMaxParts = 64;
-constexpr int kPartBytes = 8 << 10;  // a part is at least this long
+constexpr int kPartBytes = 8 << 10;   // a part is at least this long
 constexpr int kPartsTarget = 1024;    // work groups that fill the GPU
 constexpr int kWaveKeys = 256;        // a wave's list
 constexpr int kCutKeys = 128;         // one longer than this is cut to its first k
@@ -74,14 +74,6 @@ struct Candidates {
     uint64_t least;
     int n;
 };
-
-// Lanes of a wave that hand each other values through LDS: its operations run
-// in order, so only the compiler has to keep theirs.
-__device__ __forceinline__ void wave_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
-}
 
 // The need-th largest of the wave's words, N a lane (0: none), with the bits
 // below `last` zero: a bound that need words are not below.  Bit by bit, as a

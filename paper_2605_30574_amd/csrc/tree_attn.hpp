@@ -1,24 +1,38 @@
 // tree_attn.hpp -- attention of a tree of drafted nodes per cell over the
 // cell's spliced prompt, its generated rows and the tree's own rows
-// (splice_tree_attn).
+// (splice_tree_attn): out = sum_j 2^(s_j - m) v_j / l with s_j = scale log2(e) q.k_j
+// over the keys j that a node sees, l = sum_j 2^(s_j - m), in one pass with
+// a running m.
 //
 // The queries of a (cell, KV head) are its T * G (node, head) rows.  A work
 // group takes 32 RW of them (RW waves of 32 rows; the other 4 / RW waves of a
-// row take other keys) and walks a list of keys in tiles that it stages in LDS
-// for all its waves, two tiles deep: the next tile's loads are in flight in
-// registers while one is computed.  Per wave and 32 keys
-//   S^T = K Q^T   v_mfma_f32_32x32x16_bf16, A = K from LDS, B = Q^T held in
-//                 registers: lane (half h, r) gets row r's scores of the keys
-//                 8 b + 4 h + i, so a row's statistics take one exchange
-//                 between the halves;
-//   softmax       running maximum with lazy rescaling, sums in fp32;
+// row take other keys) over a chunk of the cell's list of keys, which it walks
+// tile by tile.  Per wave and 32 keys
+//   S^T = K Q^T   v_mfma_f32_32x32x16_bf16, A = K from LDS, B = Q^T: lane (half
+//                 h, r) gets row r's scores of the keys 8 b + 4 h + i, so a
+//                 row's statistics take one exchange between the halves, and
+//                 that only where its maximum rises by more than kSlack;
+//   softmax       sums in fp32;
 //   O^T += V^T P  A = V^T by transposing LDS reads, in the order of keys in
 //                 which P lies in the lanes; P rounded to bf16 (weights of at
 //                 most 2^kSlack with relative errors of 2^-9 that average
 //                 out; their sum is not rounded).
-// Keys are listed in segments (prompt before, in and behind the span, each
-// span form that the tile's rows need, the generated rows with the tree's
-// behind them); only tiles that some row does not see wholly are masked.
+// RW = 1: every wave has a tile of its own, with the next one in registers, and
+// waits for no other; else a tile is for all waves, and bf16 rows go straight
+// to one of two buffers in LDS while the other is computed.
+//
+// The list has up to five segments (prompt before, in and behind the span, each
+// span form that the work group's rows need, the generated rows with the
+// tree's behind them); only tiles that some row does not see wholly are masked.
+// It is walked as if all values were finite, and again, with the values of those
+// tiles looked at, where a result is not (0 * inf is no 0).
+//
+// Packed calls: the prompt is the same for all cells, so work groups of 128
+// rows of any cells walk chunks of it, and the cells' generated rows have work groups
+// of their own.  Chunks' results go to memory in 16 bits and tree_join_kernel joins them.
+//
+// What bounds it: the matrix products where many rows share keys, else bytes in
+// flight, and in small calls the chain of loads before the first tile.
 #pragma once
 
 #include <atomic>
@@ -140,14 +154,6 @@ __device__ __forceinline__ const char *uniform(const char *p) {
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32));
     return reinterpret_cast<const char *>(((uint64_t)hi << 32) | lo);
-}
-
-// Lanes of a wave that hand each other values through LDS: its operations run
-// in order, so only the compiler has to keep theirs.
-__device__ __forceinline__ void wave_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
 }
 
 // Which words of two bf16 values hold an infinity or NaN.
@@ -509,133 +515,133 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     f32x16_t o[ND];   // o[db][i] is d = 32 db + 8 (i / 4) + 4 h + i % 4 of the row
     float m, l;       // its maximum; its sum, of which either half has a share
     for (bool careful = false;; careful = true) {
-    static_for<0, ND>([&](auto db) { static_for<0, 16>([&](auto i) { o[db][(int)i] = 0.f; }); });
-    m = -INFINITY;
-    l = 0.f;
-    // keys of the ZERO donor score 0 and add nothing to o
-    if (a.zero_donor && prompt && spliced && chunk == 0 && kw == 0) {
-        const int n_zero = a.span_hi - max(a.span_lo, max(low, 0));
-        if (n_zero > 0) {
-            m = 0.f;
-            l = h == 0 ? (float)n_zero : 0.f;
+        static_for<0, ND>([&](auto db) { static_for<0, 16>([&](auto i) { o[db][(int)i] = 0.f; }); });
+        m = -INFINITY;
+        l = 0.f;
+        // keys of the ZERO donor score 0 and add nothing to o
+        if (a.zero_donor && prompt && spliced && chunk == 0 && kw == 0) {
+            const int n_zero = a.span_hi - max(a.span_lo, max(low, 0));
+            if (n_zero > 0) {
+                m = 0.f;
+                l = h == 0 ? (float)n_zero : 0.f;
+            }
         }
-    }
 
-    if constexpr (!X::OWN && X::NBUF == 2) {
-        wait_vmcnt<0>();   // this wave's part of the first tile
-        if (t_first < t1) store(own, cur.seg);
-    }
-    for (int t = t_first; t < t1; t += t_step) {
-        const int b = X::NBUF == 1 ? 0 : (t - t0) & 1;
-        char *const buf = own + b * 2 * X::TILE;
-        // addresses are worked out anew for every tile: kept, they would take the registers of the tile in flight
-        asm volatile("" : "+v"(ltid), "+v"(k_at), "+v"(v_at));
-        if constexpr (X::OWN) {
-            wave_fence();   // the wave has read the tile before
-            store(buf, cur.seg);
-            wave_fence();
-        } else if constexpr (X::NBUF == 1) {
-            wait_vmcnt<0>();
-            store(buf, cur.seg);
-            __syncthreads();
-        } else {
-            __syncthreads();   // every wave's part of tile t is in LDS, and tile t - 1 has been read
+        if constexpr (!X::OWN && X::NBUF == 2) {
+            wait_vmcnt<0>();   // this wave's part of the first tile
+            if (t_first < t1) store(own, cur.seg);
         }
-        const TreeTileRef next = tile_of();
-        // the matrix products of one wave go before the softmax of another on its SIMD
-        __builtin_amdgcn_s_setprio(1);
-        if (t + t_step < t1 && (X::OWN || X::NBUF == 2)) {
-            load(b ^ 1);
-            advance();
-        }
-        if (careful ? cur.differ : cur.dead) {
-            look(cur, buf);
-            if constexpr (X::OWN) wave_fence();
-            else __syncthreads();
-        }
-        // (a wave may have no row that sees its tile)
-        if (!cur.other || (cur.seg == 2 ? wave_donor : wave_clean)) {
-        f32x16_t s[KB];
-        static_for<0, KB>([&](auto kb) {
-            u32x4_t ka[NST];
-            static_for<0, NST>([&](auto st) {
-                ka[st] = *reinterpret_cast<const u32x4_t *>(buf + (k_at ^ 32 * (int)st) + (int)kb * 32 * X::ROW);
-            });
-            static_for<0, 16>([&](auto i) { s[kb][(int)i] = 0.f; });
-            static_for<0, NST>([&](auto st) {
-                bf16x8_t q;
-                if constexpr (X::OWN) q = *reinterpret_cast<const bf16x8_t *>(s_q + (k_at ^ 32 * (int)st));
-                else q = qb[st];
-                s[kb] = product(ka[st], q, s[kb]);
-            });
-        });
-        // with registers to spare the values are on their way while the softmax runs
-        u32x4_t vv[X::EARLY ? 2 * KB : 1][ND];
-        if constexpr (X::EARLY) {
-            static_for<0, 2 * KB>([&](auto kk) { static_for<0, ND>([&](auto db) { vv[kk][db] = values(buf, db, kk); }); });
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        __builtin_amdgcn_s_setprio(0);
-        if (cur.edge || (careful && cur.other)) {
-            const uint64_t see = seen(cur) >> 4 * h;
-            static_for<0, KB>([&](auto kb) {
-                static_for<0, 16>([&](auto i) {
-                    constexpr int key = 32 * kb + 8 * (i >> 2) + (i & 3);
-                    if (!((see >> key) & 1)) s[kb][(int)i] = -INFINITY;
-                });
-            });
-        }
-        float mt = -INFINITY;
-        static_for<0, KB>([&](auto kb) { static_for<0, 16>([&](auto i) { mt = fmaxf(mt, s[kb][(int)i]); }); });
-        mt *= a.qk_scale;
-        const bool hidden = cur.other && (cur.seg == 2) != spliced;   // the row sees none of it
-        if (hidden) mt = -INFINITY;
-        if (__any(mt > m + kSlack)) {
-            mt = fmaxf(mt, __shfl_xor(mt, 32));
-            const bool need = mt > m + kSlack;
-            const float mn = need ? mt : m;
-            const float al = need ? fast_exp2(m - mn) : 1.f;
-            l *= al;
-            static_for<0, ND>([&](auto db) { o[db] *= al; });
-            m = mn;
-        }
-        const float ms = hidden ? INFINITY : (m == -INFINITY ? 0.f : m);
-        bf16x8_t pb[2 * KB];
-        static_for<0, KB>([&](auto kb) {
-            static_for<0, 16>([&](auto i) {
-                const float p = fast_exp2(fmaf(s[kb][(int)i], a.qk_scale, -ms));
-                l += p;
-                pb[2 * kb + i / 8][i % 8] = (__bf16)p;
-            });
-        });
-        static_for<0, ND>([&](auto db) {
-            static_for<0, 2 * KB>([&](auto kk) {
-                if constexpr (X::EARLY) o[db] = product(vv[kk][db], pb[kk], o[db]);
-                else o[db] = product(values(buf, db, kk), pb[kk], o[db]);
-            });
-        });
-        }
-        cur = next;
-        if constexpr (!X::OWN && X::NBUF == 1) {
-            __syncthreads();   // tile t has been read
-            if (t + 1 < t1) {
-                cur = tile_of();
-                load(0);
+        for (int t = t_first; t < t1; t += t_step) {
+            const int b = X::NBUF == 1 ? 0 : (t - t0) & 1;
+            char *const buf = own + b * 2 * X::TILE;
+            // addresses are worked out anew for every tile: kept, they would take the registers of the tile in flight
+            asm volatile("" : "+v"(ltid), "+v"(k_at), "+v"(v_at));
+            if constexpr (X::OWN) {
+                wave_fence();   // the wave has read the tile before
+                store(buf, cur.seg);
+                wave_fence();
+            } else if constexpr (X::NBUF == 1) {
+                wait_vmcnt<0>();
+                store(buf, cur.seg);
+                __syncthreads();
+            } else {
+                __syncthreads();   // every wave's part of tile t is in LDS, and tile t - 1 has been read
+            }
+            const TreeTileRef next = tile_of();
+            // the matrix products of one wave go before the softmax of another on its SIMD
+            __builtin_amdgcn_s_setprio(1);
+            if (t + t_step < t1 && (X::OWN || X::NBUF == 2)) {
+                load(b ^ 1);
                 advance();
             }
-        } else if constexpr (!X::OWN) {
-            wait_vmcnt<0>();
-            if (t + 1 < t1) store(own + (b ^ 1) * 2 * X::TILE, cur.seg);
+            if (careful ? cur.differ : cur.dead) {
+                look(cur, buf);
+                if constexpr (X::OWN) wave_fence();
+                else __syncthreads();
+            }
+            // (a wave may have no row that sees its tile)
+            if (!cur.other || (cur.seg == 2 ? wave_donor : wave_clean)) {
+                f32x16_t s[KB];
+                static_for<0, KB>([&](auto kb) {
+                    u32x4_t ka[NST];
+                    static_for<0, NST>([&](auto st) {
+                        ka[st] = *reinterpret_cast<const u32x4_t *>(buf + (k_at ^ 32 * (int)st) + (int)kb * 32 * X::ROW);
+                    });
+                    static_for<0, 16>([&](auto i) { s[kb][(int)i] = 0.f; });
+                    static_for<0, NST>([&](auto st) {
+                        bf16x8_t q;
+                        if constexpr (X::OWN) q = *reinterpret_cast<const bf16x8_t *>(s_q + (k_at ^ 32 * (int)st));
+                        else q = qb[st];
+                        s[kb] = product(ka[st], q, s[kb]);
+                    });
+                });
+                // with registers to spare the values are on their way while the softmax runs
+                u32x4_t vv[X::EARLY ? 2 * KB : 1][ND];
+                if constexpr (X::EARLY) {
+                    static_for<0, 2 * KB>([&](auto kk) { static_for<0, ND>([&](auto db) { vv[kk][db] = values(buf, db, kk); }); });
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                __builtin_amdgcn_s_setprio(0);
+                if (cur.edge || (careful && cur.other)) {
+                    const uint64_t see = seen(cur) >> 4 * h;
+                    static_for<0, KB>([&](auto kb) {
+                        static_for<0, 16>([&](auto i) {
+                            constexpr int key = 32 * kb + 8 * (i >> 2) + (i & 3);
+                            if (!((see >> key) & 1)) s[kb][(int)i] = -INFINITY;
+                        });
+                    });
+                }
+                float mt = -INFINITY;
+                static_for<0, KB>([&](auto kb) { static_for<0, 16>([&](auto i) { mt = fmaxf(mt, s[kb][(int)i]); }); });
+                mt *= a.qk_scale;
+                const bool hidden = cur.other && (cur.seg == 2) != spliced;   // the row sees none of it
+                if (hidden) mt = -INFINITY;
+                if (__any(mt > m + kSlack)) {
+                    mt = fmaxf(mt, __shfl_xor(mt, 32));
+                    const bool need = mt > m + kSlack;
+                    const float mn = need ? mt : m;
+                    const float al = need ? fast_exp2(m - mn) : 1.f;
+                    l *= al;
+                    static_for<0, ND>([&](auto db) { o[db] *= al; });
+                    m = mn;
+                }
+                const float ms = hidden ? INFINITY : (m == -INFINITY ? 0.f : m);
+                bf16x8_t pb[2 * KB];
+                static_for<0, KB>([&](auto kb) {
+                    static_for<0, 16>([&](auto i) {
+                        const float p = fast_exp2(fmaf(s[kb][(int)i], a.qk_scale, -ms));
+                        l += p;
+                        pb[2 * kb + i / 8][i % 8] = (__bf16)p;
+                    });
+                });
+                static_for<0, ND>([&](auto db) {
+                    static_for<0, 2 * KB>([&](auto kk) {
+                        if constexpr (X::EARLY) o[db] = product(vv[kk][db], pb[kk], o[db]);
+                        else o[db] = product(values(buf, db, kk), pb[kk], o[db]);
+                    });
+                });
+            }
+            cur = next;
+            if constexpr (!X::OWN && X::NBUF == 1) {
+                __syncthreads();   // tile t has been read
+                if (t + 1 < t1) {
+                    cur = tile_of();
+                    load(0);
+                    advance();
+                }
+            } else if constexpr (!X::OWN) {
+                wait_vmcnt<0>();
+                if (t + 1 < t1) store(own + (b ^ 1) * 2 * X::TILE, cur.seg);
+            }
         }
-    }
-    __syncthreads();
-    if (careful) break;
-    float zero = 0.f * l;   // NaN if anything is not finite
-    static_for<0, ND>([&](auto db) { static_for<0, 16>([&](auto i) { zero = fmaf(0.f, o[db][(int)i], zero); }); });
-    if (valid && zero != zero) s_again = 1;
-    __syncthreads();
-    if (!s_again) break;
-    begin();
+        __syncthreads();
+        if (careful) break;
+        float zero = 0.f * l;   // NaN if anything is not finite
+        static_for<0, ND>([&](auto db) { static_for<0, 16>([&](auto i) { zero = fmaf(0.f, o[db][(int)i], zero); }); });
+        if (valid && zero != zero) s_again = 1;
+        __syncthreads();
+        if (!s_again) break;
+        begin();
     }
     if (s_bad) {
         // infinities and NaN among the values of tiles that rows see differently:
@@ -859,6 +865,7 @@ bool launch_tree(const TreeArgs &a, const splice::TreePlan &p, int kv_format, hi
                 return;
             }
         }
+        if (p.n_p > 0) return;   // no kernel: the plan has none such
         ok = f8 ? launch_tree_kernel<D, RW, true, false>(a, p.blocks, stream)
                 : launch_tree_kernel<D, RW, false, false>(a, p.blocks, stream);
     };

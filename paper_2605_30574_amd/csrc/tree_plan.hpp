@@ -159,10 +159,13 @@ inline int64_t tree_chunks(const int *tiles, int n, int per) {
 // 1024 44 / 26; D = 64, 64 cells of 5 nodes 1024 keys 29 / 24). A call that sets
 // split_keys packs whenever it can.
 constexpr int kTreeMaxPrompt = 16;                 // chunks of the prompt
+constexpr int kTreePackedRows = 64;                // rows of a cell (more fill the waves of a work group by themselves)
+static_assert(tree_row_waves(64, kTreePackedRows) < 4 && tree_row_waves(128, kTreePackedRows) < 4 &&
+              tree_row_waves(256, kTreePackedRows) < 4, "the packed kernels take up to two row waves for the generated rows");
 constexpr int64_t kTreePackedWork = 5 << 20;
 
 inline bool tree_packed(const splice_shape &sh, const splice_call &call, int T, int n, int64_t prompt_keys) {
-    if (T * group_of(sh) > 64 || n < 2 || prompt_keys < 1) return false;
+    if (T * group_of(sh) > kTreePackedRows || n < 2 || prompt_keys < 1) return false;
     return call.split_keys > 0 || n * prompt_keys * sh.head_dim >= kTreePackedWork;
 }
 

@@ -399,6 +399,8 @@ class SweepDecoder:
         """What the model says behind every node of the trees (tree_logits): log probability, entropy, rank of the token
         targets[c][t] (int64 [C][T]), and the ``top`` most probable tokens; fields [C][T] and [C][T][top].  scale: an
         inverse temperature."""
+        if targets.shape != tokens.shape:
+            raise ValueError(f"targets has shape {tuple(targets.shape)}, tokens {tuple(tokens.shape)}")
         logits = self.tree_logits(tokens, tree, steps)
         got = T.token_scores(logits, targets.reshape(-1).contiguous(), top, scale)
         shape = (self.C, tree.spec.n_nodes)
@@ -407,6 +409,8 @@ class SweepDecoder:
     def keep_nodes(self, tree: DecoderTree, steps: np.ndarray, keep: torch.Tensor) -> None:
         """Move the K/V of each cell's nodes keep[c] (int32 [C][T], ascending, ended by -1: ``accept``) to its rows
         steps[c], steps[c] + 1, ... in every layer: the decode goes on at steps[c] + their number."""
+        if tuple(keep.shape) != (self.C, tree.spec.n_nodes):
+            raise ValueError(f"keep has shape {tuple(keep.shape)}, expected ({self.C}, {tree.spec.n_nodes})")
         for c in self.caches:
             e = [c[name] for name in ("gen_k_exp", "gen_v_exp")] if tree.spec.kv_format == T.SPLICE_KV_E4M3 else []
             T.splice_tree_keep(self.shape, tree.spec, steps, keep, c["gen_k"], c["gen_v"], *e)

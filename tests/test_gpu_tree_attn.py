@@ -341,3 +341,21 @@ def test_no_cells():
     rows = torch.empty(0, s.Hkv, 3, s.D, dtype=torch.bfloat16, device="cuda")
     sp.splice_tree_read(s.shape, s.tree, s.steps, *s.gen, None, None, rows, rows.clone())
     torch.cuda.synchronize()
+
+
+def test_two_calls_at_once():
+    """Calls with workspaces of their own, on two streams at the same time, do not touch each other."""
+    a, b = Sweep(263, C=3, T=9, D=128, Tp=900, span=(100, 800), cap=600), many(269, 40, 2)
+    alone = [a.attend(128), b.attend(256)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    held = [[(s.outputs(), s.workspace(split)) for _ in range(8)] for s, split in ((a, 128), (b, 256))]
+    torch.cuda.synchronize()
+    for n in range(8):
+        for s, split, stream, h in zip((a, b), (128, 256), streams, held):
+            (out, lse), ws = h[n]
+            s.attend(split, out, lse, ws, stream)
+    torch.cuda.synchronize()
+    for (out, lse), h in zip(alone, held):
+        for (o, l), _ in h:
+            assert torch.equal(o, out) and torch.equal(l, lse)

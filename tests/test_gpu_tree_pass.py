@@ -164,3 +164,15 @@ def test_refusals():
     caches[0]["gen_k"] = caches[0]["gen_k"].float()
     with pytest.raises(ValueError):
         gpu.make_tree(chain(C, 2))
+
+
+def test_targets_and_nodes_of_another_shape():
+    w, m, lw, _, gpu, _, _ = setup(decode_bar.CASES[0])
+    C, T = lw.shape[0], lw.shape[0] + 1
+    steps = np.zeros(C, np.int32)
+    tree = gpu.make_tree(chain(C, T))
+    tokens = torch.zeros((C, T), dtype=torch.int64, device="cuda")
+    with pytest.raises(ValueError):
+        gpu.score_tree(tokens, tree, steps, tokens.t().contiguous())
+    with pytest.raises(ValueError):
+        gpu.keep_nodes(tree, steps, torch.zeros((T, C), dtype=torch.int32, device="cuda"))

@@ -195,3 +195,57 @@ def test_read_and_keep(T, D, kv):
                 want[c, :, s:s + count[c]] = \
                     before[n][c][:, s + keep[c, :count[c]]]
         assert np.array_equal(after[n], want)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+def test_captured_append_attend_keep(kv):
+    """A pass's calls in one graph, replayed on new inputs between eager work: the bits of eager calls."""
+    s = Rows(31, C=4, T=6, D=64, Tp=100, cap=40, kv=kv, fused=False)
+    g = torch.Generator().manual_seed(32)
+    bf = torch.bfloat16
+    randn = lambda *shape: torch.randn(*shape, generator=g).to(bf).cuda()  # noqa: E731
+    shape = sp.make_shape(s.C, 4, s.Hq, s.Hkv, s.D, s.Tp, (10, 70), s.cap, False, "bf16")
+    prompt = [randn(s.Hkv, s.Tp, s.D) for _ in range(4)]
+    call, rope = sp.make_call(1, 0, 0, s.D ** -0.5, 64), sp.make_rope("half", s.D)
+    freq = torch.from_numpy(sp.rope_frequencies(s.D, 1e4)[0]).cuda()
+    _, visible = sp.tree_layout(random_parents(np.random.default_rng(31), s.C, s.T))
+    visible = torch.from_numpy(visible.view(np.int64)).cuda()
+    keep = torch.tensor([[0, 2, 5, -1, -1, -1], [1, 3, -1, -1, -1, -1], [-1] * 6, [0, 1, 2, 3, 4, 5]], dtype=torch.int32).cuda()
+    lw = np.array([[0, 0], [0, 8], [9, 0], [1, 6]], np.int32)
+    start = [x.clone() for x in s.gen]
+    start_e = [None if x is None else x.clone() for x in s.exps]
+
+    def buffers():
+        n = sp.splice_tree_attn_workspace_bytes(shape, call, s.tree)
+        return dict(q=torch.zeros_like(s.q_out), gen=[x.clone() for x in start], e=[None if x is None else x.clone() for x in start_e],
+                    out=torch.zeros_like(s.q_out), lse=torch.zeros(s.C, s.T, s.Hq, device="cuda"),
+                    ws=torch.empty(n, dtype=torch.uint8, device="cuda"))
+
+    def calls(b):
+        sp.splice_tree_append(shape, s.tree, rope, freq, s.steps, s.depth_dev, s.q, s.k, s.v, b["q"], *b["gen"], *b["e"])
+        sp.splice_tree_attn(shape, call, s.tree, lw, s.steps, s.depth_dev, visible, b["q"], *prompt, *b["gen"], *b["e"], b["out"],
+                            b["lse"], b["ws"])
+        sp.splice_tree_keep(shape, s.tree, s.steps, keep, *b["gen"], *b["e"])
+
+    cap = buffers()
+    calls(cap)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(cap)
+    for n in range(4):
+        announce(f"captured pass {kv}, replay {n}")
+        for x in (s.q, s.k, s.v):
+            x.copy_(randn(*x.shape))
+        for x, y in zip(cap["gen"] + cap["e"], start + start_e):
+            if x is not None:
+                x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = buffers()
+        calls(eager)
+        torch.cuda.synchronize()
+        for name in ("q", "out", "lse"):
+            assert torch.equal(cap[name], eager[name]), name
+        for x, y in zip(cap["gen"] + cap["e"], eager["gen"] + eager["e"]):
+            assert x is None or torch.equal(x, y)
