@@ -64,7 +64,7 @@ struct TreeCall {
     _Float16 *part;
     float4 *record;
     int T, G, lgG, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, per;
-    int n_p, p_tiles;   // packed calls: chunks of the prompt and tiles of 128 rows; else 0
+    int n_p, p_tiles, p_heavy;   // packed calls: chunks of the prompt, tiles of 128 rows, those that may walk the span twice; else 0
     bool split;
     float qk_scale;   // scale * log2(e)
 };
@@ -215,9 +215,13 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     bool last_chunk = false, valid, spliced, any_clean, any_donor;
     uint64_t alive = 0, word = 0;
     if constexpr (PACKED) {
-        chunk = rest / a.p_tiles;
+        // tiles that walk both forms of the span come first: begun late, they would end long after the others
+        const int heavy = a.p_heavy * a.n_p;
+        const bool first = rest < heavy;
+        const int of = first ? rest : rest - heavy, among = first ? a.p_heavy : a.p_tiles - a.p_heavy;
+        chunk = of / among;
         row0 = 0;
-        const int at = 32 * RW * (rest - chunk * a.p_tiles) + 32 * rw + r, n_rows = a.n_active * rows;
+        const int at = 32 * RW * (of - chunk * among + (first ? 0 : a.p_heavy)) + 32 * rw + r, n_rows = a.n_active * rows;
         const int ci = min(at, n_rows - 1) / rows;
         row = at - ci * rows;
         const uint32_t info = args.slots.info[ci];
