@@ -114,7 +114,7 @@ struct TreeTile {
     static constexpr int NL = TK * CPR / NT;                   // chunks a thread loads of a K (or V) tile
     static constexpr int NL8 = NL / 2;                         // ... of 8-bit rows
     static constexpr int NR = OWN ? NL : NL8;                  // ... by way of registers
-    static constexpr bool EARLY = !OWN && KB == 1 && D <= 128; // values are read before the softmax
+    static constexpr int EARLY = !OWN && D <= 128 ? 2 : 0;     // 16-key steps whose values are read before the softmax
     static constexpr int ND = D / 32;                          // 32-wide d blocks of the output
     static constexpr int PARTS = KW > 1 && KW * 32 * RW * D * 4 > TILES ? 2 : 1;   // in which the waves' results are joined
     static_assert(RW * KW == 4 && NL8 >= 1 && (KW == 1 || KW * 32 * RW * D * 4 <= TILES * PARTS), "");
@@ -580,9 +580,9 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
                     });
                 });
                 // with registers to spare the values are on their way while the softmax runs
-                u32x4_t vv[X::EARLY ? 2 * KB : 1][ND];
-                if constexpr (X::EARLY) {
-                    static_for<0, 2 * KB>([&](auto kk) { static_for<0, ND>([&](auto db) { vv[kk][db] = values(buf, db, kk); }); });
+                u32x4_t vv[X::EARLY > 0 ? X::EARLY : 1][ND];
+                if constexpr (X::EARLY > 0) {
+                    static_for<0, X::EARLY>([&](auto kk) { static_for<0, ND>([&](auto db) { vv[kk][db] = values(buf, db, kk); }); });
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 __builtin_amdgcn_s_setprio(0);
@@ -618,9 +618,9 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
                         pb[2 * kb + i / 8][i % 8] = (__bf16)p;
                     });
                 });
-                static_for<0, ND>([&](auto db) {
-                    static_for<0, 2 * KB>([&](auto kk) {
-                        if constexpr (X::EARLY) o[db] = product(vv[kk][db], pb[kk], o[db]);
+                static_for<0, 2 * KB>([&](auto kk) {
+                    static_for<0, ND>([&](auto db) {
+                        if constexpr (kk < X::EARLY) o[db] = product(vv[kk][db], pb[kk], o[db]);
                         else o[db] = product(values(buf, db, kk), pb[kk], o[db]);
                     });
                 });
