@@ -30,10 +30,13 @@ using namespace splice_dev;
 
 constexpr int kScoreThreads = 256;
 constexpr int kScoreWaves = kScoreThreads / 64;
-constexpr int kChunks = 4;            // 16-byte chunks a thread has in flight
+// 16-byte chunks a thread has in flight (us with 2 / 4 / 8: 1024 bf16 rows, k = 20, 83 / 80 / 98; 300 float32
+// rows, k = 8, 51 / 48 / 54, k = 0 34 / 37 / 39)
+constexpr int kChunks = 4;
 constexpr int kMaxParts = 64;
-constexpr int kPartBytes = 8 << 10;   // a part is at least this long
-constexpr int kPartsTarget = 1024;    // work groups that fill the GPU
+constexpr int kPartBytes = 8 << 10;   // a part is at least this long (7 rows of 600 KB: 15 us; 32 KB 19)
+// Work groups that fill the GPU (512 / 1024 / 2048: 300 float32 rows, k = 8, 56 / 48 / 51; 1024 bf16 rows, k = 20, 80 / 80 / 92)
+constexpr int kPartsTarget = 1024;
 constexpr int kWaveKeys = 256;        // a wave's list
 constexpr int kCutKeys = 128;         // one longer than this is cut to its first k
 constexpr int kCandidates = 1024;     // a work group's four lists; a row's parts have no more

@@ -31,8 +31,13 @@
 // rows of any cells walk chunks of it, and the cells' generated rows have work groups
 // of their own.  Chunks' results go to memory in 16 bits and tree_join_kernel joins them.
 //
-// What bounds it: the matrix products where many rows share keys, else bytes in
-// flight, and in small calls the chain of loads before the first tile.
+// What bounds it: where many rows share keys the tile loop, whose matrix products
+// (35% busy) and vector operations (40%) overlap in part only: 47 cells of 16 nodes, 32 heads of
+// 128 over 8k slots 135 us in the kernel (800 TFLOP/s); with small trees the generated
+// rows' bytes, 64 cells of 5 nodes, 4.3 TB/s of bf16 rows and 3.2 TB/s of 8-bit ones, 5.3 and 4.3
+// over longer lists (two 8-bit tiles in flight a wave measured the same as one: what is left is
+// the chain from codes through LDS to the products); in small calls
+// the chain of loads before the first tile (7.4 us with one tile).
 #pragma once
 
 #include <atomic>
@@ -789,7 +794,9 @@ __global__ __launch_bounds__(256, splice::tree_resident(D, F8)) void tree_packed
 // Joins the chunks of every row (blockIdx.x the active cell and node).  D / 8
 // lanes read a chunk's values.  MANY: a wave a row, whose lanes read a chunk's
 // record each, and 64 / (D / 8) chunks at once; otherwise, with at most D / 8
-// and at most 8 chunks, 64 / (D / 8) rows a wave.
+// and at most 8 chunks, 64 / (D / 8) rows a wave (64 cells of 16 nodes, 2 chunks:
+// a call of 131 us; with a wave a row 138).  Bound by the chunks' bytes: 10 us for
+// 48 cells of 16 nodes, 32 heads, 7 chunks (4.5 TB/s), else by launch and one round of loads, 4.5.
 template <int D, bool MANY>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
     constexpr int LPR = D / 8, SP = 64 / LPR, GROUP = MANY ? 64 : LPR;

@@ -67,7 +67,12 @@ void with_format(int D, int kv_format, F f) {
 // ---------------------------------------------------------------- attention
 
 // Waves of a work group that take different rows (32 each); the other of its
-// four waves take different keys of the same rows.
+// four waves take different keys of the same rows.  One up to 32 rows: waves of
+// bytes in flight that do not wait for each other (us, one / two row waves: 64
+// cells of 5 nodes, D = 128, 2k 8-bit rows each 82 / 96, bf16 rows 115 / 117; 3 cells of
+// 5 nodes, D = 64, 16 / 21; but one cell of one node over 8k slots 20 / 19).  Two up
+// to 64 rows, where two more would have none; four above, as a tile then serves
+// 128 rows (four / two: 8 cells of 32 nodes over 8k slots 58 / 64).
 constexpr int tree_row_waves(int D, int rows) { return rows <= 32 && D <= 128 ? 1 : (rows <= 64 ? 2 : 4); }
 // 32-key blocks a wave takes of a tile.
 constexpr int tree_key_blocks(int D, int row_waves) { return row_waves == 4 && D <= 128 ? 2 : 1; }
@@ -80,8 +85,12 @@ constexpr int tree_resident(int D, bool f8) { return D > 128 && f8 ? 1 : 2; }   
 // A cell's list of keys is cut into chunks of `per` tiles, one work group
 // each (per KV head and row tile); a slot is one chunk of one cell.
 constexpr int kTreeMaxSlots = 640;
-constexpr int kTreeRounds = 6;    // rounds of resident work groups a plan may take to balance its chunks
-constexpr int kTreeStart = 8;     // what a work group costs beside its tiles, in tiles
+// Rounds of resident work groups a plan may take to balance its chunks, and what a
+// work group costs beside its tiles, in tiles (us: 48 cells of 16 nodes over 8k
+// slots, 6 rounds 158, 1 round 216; 8 tiles 158, 2 168, 16 216; 64 cells of 16 nodes,
+// 2k bf16 rows each, 6 rounds 131, 1 round 126).
+constexpr int kTreeRounds = 6;
+constexpr int kTreeStart = 8;
 constexpr int kTreeMaxChunks = 64;
 
 struct TreePlan {
