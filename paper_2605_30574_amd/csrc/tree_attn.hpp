@@ -32,7 +32,7 @@
 // of their own.  Chunks' results go to memory in 16 bits and tree_join_kernel joins them.
 //
 // What bounds it: where many rows share keys the tile loop, whose matrix products
-// (35% busy) and vector operations (40%) overlap in part only: 47 cells of 16 nodes, 32 heads of
+// (40% busy) and vector operations (45%) overlap in part only: 47 cells of 16 nodes, 32 heads of
 // 128 over 8k slots 135 us in the kernel (800 TFLOP/s); with small trees the generated
 // rows' bytes, 64 cells of 5 nodes, 4.3 TB/s of bf16 rows and 3.2 TB/s of 8-bit ones, 5.3 and 4.3
 // over longer lists (two 8-bit tiles in flight a wave measured the same as one: what is left is
@@ -425,11 +425,13 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     }
 
     // What load() left in registers, into the tile.  8-bit rows: a lane has two
-    // neighbouring chunks, and every other lane begins with the second, so that
-    // a store of the wave meets every bank.
+    // neighbouring chunks.  A store of the wave meets every bank, of K by the
+    // swizzle, of V as every other eight lanes begin with the second.
     auto store = [&](char *buf, int seg) {
-        auto put = [&](int key, int chunk, u32x4_t k, u32x4_t v) {
+        auto put_k = [&](int key, int chunk, u32x4_t k) {
             *reinterpret_cast<u32x4_t *>(buf + key * X::ROW + ((chunk ^ tree_swz_k<D>(key)) << 4)) = k;
+        };
+        auto put_v = [&](int key, int chunk, u32x4_t v) {
             *reinterpret_cast<u32x4_t *>(buf + X::TILE + key * X::ROW + ((chunk ^ tree_swz_v<D>(key)) << 4)) = v;
         };
         if (F8 && seg == 4) {
@@ -438,14 +440,15 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
                 static_for<0, 2>([&](auto j) {
                     const bool second = (int)j != odd;
                     const u32x4_t k = kr[i], v = vr[i];
-                    put(key, ch + (second ? 1 : 0), e4m3_to_bf16(second ? make_uint2(k.z, k.w) : make_uint2(k.x, k.y), ke[i]),
-                        e4m3_to_bf16(second ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y), ve[i]));
+                    put_k(key, ch + j, e4m3_to_bf16(j ? make_uint2(k.z, k.w) : make_uint2(k.x, k.y), ke[i]));
+                    put_v(key, ch + (second ? 1 : 0), e4m3_to_bf16(second ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y), ve[i]));
                 });
             });
         } else if constexpr (X::OWN) {
             static_for<0, X::NL>([&](auto i) {
                 const int u = (int)i * X::NT + ltid;
-                put(u / X::CPR, u % X::CPR, kr[i], vr[i]);
+                put_k(u / X::CPR, u % X::CPR, kr[i]);
+                put_v(u / X::CPR, u % X::CPR, vr[i]);
             });
         }
     };
