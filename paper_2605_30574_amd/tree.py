@@ -167,6 +167,21 @@ def _stream(stream, dev) -> int:
     return S._stream_ptr(stream, dev[1])
 
 
+_INT32 = np.dtype(np.int32)
+
+
+def _host(x, rows: int, cols: int, name: str, what: str):
+    """Host int32 values [rows][cols] as what ctypes passes the address of: a copy, for an array of that many a quicker one
+    than asking for its address."""
+    if type(x) is np.ndarray and x.dtype == _INT32 and x.size == rows * cols:
+        return x.tobytes()
+    return S._host_i32(x, rows, cols, name, what)[0].tobytes()
+
+
+def _steps(cell_step, n_cells: int):
+    return _host(cell_step, n_cells, 1, "cell_step", "entries")
+
+
 def _caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp):
     n = shape.n_cells * shape.n_kv_heads * shape.gen_capacity
     if tree.kv_format != SPLICE_KV_E4M3:
@@ -182,12 +197,13 @@ def _caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp):
 
 def _rows(t, name: str, shape, T: int, heads: int, dev) -> Tuple[int, int]:
     """(address, values from one token to the next) of bf16 [C][T][heads][D], tokens evenly apart, each one's heads dense."""
-    D, dims = shape.head_dim, (shape.n_cells, T, heads, shape.head_dim)
-    if t is None or not t.is_cuda or t.get_device() != dev[0]:
+    D = shape.head_dim
+    dims = (shape.n_cells, T, heads, D)
+    if t is None or t.get_device() != dev[0]:
         raise ValueError(f"{name} must be a tensor on {dev[1]}")
     if t.dtype is not S._torch.bfloat16:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {S._torch.bfloat16}")
-    if tuple(t.shape) != dims:
+    if t.shape != dims:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {dims}")
     if t.is_contiguous():
         return t.data_ptr(), heads * D
@@ -219,7 +235,7 @@ def splice_tree_append(shape, tree, rope, freq, cell_step, depth, q, k, v, q_out
     dp = _ptr(depth, "depth", C * T, t.int32, dev)
     pp = None if pos is None else _ptr(pos, "pos", C * T, t.int64, dev)
     fp = None if rope.rotary_dim == 0 and freq is None else _ptr(freq, "freq", rope.rotary_dim // 2, t.float64, dev)
-    st, stp = S._steps(cell_step, C)
+    stp = _steps(cell_step, C)
     S._check(lib.splice_tree_append(ctypes.byref(shape), ctypes.byref(tree), ctypes.byref(rope), stp, dp, pp, fp, qp, qs, kp,
                                     ks, vp, vs, qo, *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp),
                                     _stream(stream, dev)), "splice_tree_append")
@@ -231,7 +247,7 @@ def splice_tree_read(shape, tree, cell_step, gen_k, gen_v, gen_k_exp, gen_v_exp,
     dev = _anchor(rows_k, "rows_k")
     n = shape.n_cells * shape.n_kv_heads * tree.n_nodes * shape.head_dim
     rk, rv = (_ptr(x, name, n, S._torch.bfloat16, dev) for x, name in ((rows_k, "rows_k"), (rows_v, "rows_v")))
-    st, stp = S._steps(cell_step, shape.n_cells)
+    stp = _steps(cell_step, shape.n_cells)
     S._check(lib.splice_tree_read(ctypes.byref(shape), ctypes.byref(tree), stp,
                                   *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp), rk, rv,
                                   _stream(stream, dev)), "splice_tree_read")
@@ -244,8 +260,13 @@ def splice_tree_attn_workspace_bytes(shape, call, tree) -> int:
 
 def _workspace(workspace, dev) -> Tuple[Optional[int], int]:
     """(address, bytes) of a workspace; None, or an empty tensor, where none is needed."""
-    if workspace is None or workspace.numel() == 0:
+    if workspace is None:
         return None, 0
+    n = workspace.numel()
+    if n == 0:
+        return None, 0
+    if workspace.dtype is S._torch.uint8 and workspace.get_device() == dev[0] and workspace.is_contiguous():
+        return workspace.data_ptr(), n
     return S._dev_ptr(workspace, "workspace", None, None, dev[1])[0], workspace.numel() * workspace.element_size()
 
 
@@ -272,8 +293,7 @@ def splice_tree_attn(shape, call, tree, cell_LW, cell_step, depth, visible, q, c
     vp = _ptr(visible, "visible", C * T, words, dev)
     op, lp = _ptr(out, "out", C * T * Hq * D, bf16, dev), _ptr(lse, "lse", C * T * Hq, t.float32, dev)
     wp, wbytes = _workspace(workspace, dev)
-    lw, lwp = S._cells(cell_LW, C)
-    st, stp = S._steps(cell_step, C)
+    lwp, stp = _host(cell_LW, C, 2, "cell_LW", "rows"), _steps(cell_step, C)
     S._check(lib.splice_tree_attn(ctypes.byref(shape), ctypes.byref(call), ctypes.byref(tree), lwp, stp, dp, vp, qp, ck, cv,
                                   dk, dv, *gen, op, lp, wp, wbytes, _stream(stream, dev)), "splice_tree_attn")
 
@@ -283,7 +303,7 @@ def splice_tree_keep(shape, tree, cell_step, keep, gen_k, gen_v, gen_k_exp=None,
     lib = _library()
     dev = _anchor(keep, "keep")
     kp = _ptr(keep, "keep", shape.n_cells * tree.n_nodes, S._torch.int32, dev)
-    st, stp = S._steps(cell_step, shape.n_cells)
+    stp = _steps(cell_step, shape.n_cells)
     S._check(lib.splice_tree_keep(ctypes.byref(shape), ctypes.byref(tree), stp, kp,
                                   *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp),
                                   _stream(stream, dev)), "splice_tree_keep")
