@@ -67,7 +67,7 @@ typedef struct {
 typedef struct {
     int32_t layout;      /* splice_rope_layout: pairs (i, i + R / 2), or (2 i, 2 i + 1)       */
     int32_t rotary_dim;  /* R: the first R values of a head turn; a multiple of 16 in 0..D  */
-    float mscale;        /* factor on cos and sin (1, or a long-context scaling's), finite  */
+    double mscale;       /* factor on cos and sin (1, or a long-context scaling's), finite  */
 } splice_rope;
 
 /*
@@ -76,7 +76,8 @@ typedef struct {
  *   q_out[c][t]  = the rotated q[c][t], bf16 [C][T][Hq][D]; q_out may be q
  *                  when q is dense;
  *   row s_c + t of gen_k, gen_v = the rotated k[c][t], and v[c][t], in
- *                  tree->kv_format (one rounding from the rotation in fp32).
+ *                  tree->kv_format (bf16: one rounding from the rotation in fp32;
+ *                  e4m3: codes and exponents of the rotation in 64 bits).
  * q, k, v: bf16, a token's heads dense ([heads][D]) and q_stride, k_stride,
  * v_stride values from one token to the next (multiples of 8, at least
  * heads * D), so they may be parts of one projection's rows.  pos: device

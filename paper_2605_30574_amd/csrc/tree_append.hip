@@ -34,7 +34,7 @@ struct AppendArgs {
     const double *freq;
     int64_t q_stride, k_stride, v_stride;
     int T, Hq, Hkv, cap, Tp, half_rotary, interleaved;
-    float mscale;
+    double mscale;
     TreeCells cells;
 };
 
@@ -62,11 +62,10 @@ __device__ __forceinline__ uint2 quantise(const f32x8v_t &x, uint32_t bits, uint
     return make_uint2((uint32_t)lo, (uint32_t)hi);
 }
 
-// (cos, sin) of so many turns, times a factor, each rounded once: an 8-bit code
-// next to a border falls on the side where the exact rotation lies.  To
-// the nearest quarter turn, then the series of sine and cosine on
-// [-pi / 4, pi / 4], whose first term left out is below 2^-33.
-__device__ __forceinline__ float2 turned(double turns, double factor) {
+// (cos, sin) of so many turns, times a factor.  To the nearest quarter turn,
+// then the series of sine and cosine on [-pi / 4, pi / 4], whose first term
+// left out is below 2^-33.
+__device__ __forceinline__ double2 turned(double turns, double factor) {
     turns -= rint(turns);
     const double n = rint(4. * turns);
     const double x = (turns - 0.25 * n) * 6.28318530717958647693, y = x * x;
@@ -83,7 +82,17 @@ __device__ __forceinline__ float2 turned(double turns, double factor) {
     cs = fma(cs, y, 1.);
     const int k = (int)n & 3;   // quarters
     const double c = k & 1 ? sn : cs, s = k & 1 ? cs : sn;
-    return make_float2((float)((k == 1 || k == 2 ? -c : c) * factor), (float)((k & 2 ? -s : s) * factor));
+    return make_double2((k == 1 || k == 2 ? -c : c) * factor, (k & 2 ? -s : s) * factor);
+}
+
+// x in 32 bits so that a further rounding, to an 8-bit code, is that of x
+// itself: of the two floats beside an inexact x the one with an odd last bit.
+__device__ __forceinline__ float odd_float(double x) {
+    const float f = (float)x;
+    const double rest = x - (double)f;
+    uint32_t b = __float_as_uint(f);
+    if ((rest > 0. || rest < 0.) && !(b & 1) && fabsf(f) < INFINITY) b += (rest > 0.) != (x < 0.) ? 1 : -1;
+    return __uint_as_float(b);
 }
 
 // A work group takes one node's heads kAppendThreads / LPR at a time (LPR = D / 8
@@ -91,11 +100,12 @@ __device__ __forceinline__ float2 turned(double turns, double factor) {
 // heads.  The angles of the node are computed once a work group and shared.  Launch and
 // two rounds of loads (the depth, the row) bound it at few nodes, 3.9 us for 32
 // tokens; the rows' bytes at many: 128 cells of 33 nodes, 32 + 2 x 8 heads of 128
-// to an 8-bit cache, 95 MB in 19.4 us (4.9 TB/s).
+// to an 8-bit cache, 95 MB in 21.0 us (4.5 TB/s; 19.2 with the keys rotated in 32 bits).
 template <int D, bool F8>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
     constexpr int LPR = D / 8, ROWS = kAppendThreads / LPR;
     __shared__ float2 s_cs[D / 2];
+    __shared__ double2 s_cs64[F8 ? D / 2 : 1];   // for the keys of an 8-bit cache
     const int ci = blockIdx.x / a.T, t = blockIdx.x % a.T, tid = threadIdx.x;
     const int c = (int)a.cells.cell[ci], step = a.cells.step[ci];
     const int64_t token = (int64_t)c * a.T + t;
@@ -103,7 +113,9 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
     if (depth < 0) return;   // padding
     if (tid < a.half_rotary) {
         const double p = a.pos ? (double)a.pos[token] : (double)(a.Tp + step) + (double)min(depth, a.T - 1);
-        s_cs[tid] = turned(p * (a.freq[tid] * 0.15915494309189533577), (double)a.mscale);   // 1 / (2 pi)
+        const double2 cs = turned(p * (a.freq[tid] * 0.15915494309189533577), a.mscale);   // 1 / (2 pi)
+        s_cs[tid] = make_float2((float)cs.x, (float)cs.y);
+        if constexpr (F8) s_cs64[tid] = cs;
     }
     __syncthreads();
     const int hd = blockIdx.y * ROWS + tid / LPR, l = tid % LPR;
@@ -114,25 +126,29 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
                         (int64_t)g * D;
     f32x8v_t x = __builtin_convertvector(*reinterpret_cast<const bf16x8v_t *>(src + 8 * l), f32x8v_t);
     const int d = 8 * l, half = a.half_rotary;
-    if (!is_v && d < 2 * half) {
+    // the lane's eight values, turned: turn(u, w, pair) is u cos + w sin of the pair's angle
+    auto rotate = [&](auto turn) {
         if (a.interleaved) {
             static_for<0, 4>([&](auto i) {
-                const float2 cs = s_cs[d / 2 + (int)i];
                 const float u = x[2 * (int)i], w = x[2 * (int)i + 1];
-                x[2 * (int)i] = fmaf(u, cs.x, -(w * cs.y));
-                x[2 * (int)i + 1] = fmaf(w, cs.x, u * cs.y);
+                x[2 * (int)i] = turn(u, -w, d / 2 + (int)i);
+                x[2 * (int)i + 1] = turn(w, u, d / 2 + (int)i);
             });
         } else {
             const bool low = d < half;
             const f32x8v_t o = __builtin_convertvector(
                 *reinterpret_cast<const bf16x8v_t *>(src + (low ? d + half : d - half)), f32x8v_t);
             const int f = low ? d : d - half;
-            static_for<0, 8>([&](auto i) {
-                const float2 cs = s_cs[f + (int)i];
-                const float u = x[(int)i], w = o[(int)i];
-                x[(int)i] = fmaf(u, cs.x, low ? -(w * cs.y) : w * cs.y);
-            });
+            static_for<0, 8>([&](auto i) { x[(int)i] = turn(x[(int)i], low ? -o[(int)i] : o[(int)i], f + (int)i); });
         }
+    };
+    if (!is_v && d < 2 * half) {
+        // in 64 bits where an 8-bit code comes of it: its borders leave fp32's roundings no room
+        if (F8 && !is_q) rotate([&](float u, float w, int pair) {
+            const double2 cs = s_cs64[F8 ? pair : 0];
+            return odd_float(fma((double)u, cs.x, (double)w * cs.y));
+        });
+        else rotate([&](float u, float w, int pair) { return fmaf(u, s_cs[pair].x, w * s_cs[pair].y); });
     }
     if (is_q) {
         *reinterpret_cast<bf16x8v_t *>(a.q_out + (token * a.Hq + g) * D + d) = __builtin_convertvector(x, bf16x8v_t);

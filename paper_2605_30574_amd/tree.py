@@ -33,7 +33,7 @@ class SpliceTree(ctypes.Structure):
 
 
 class SpliceRope(ctypes.Structure):
-    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("mscale", ctypes.c_float)]
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("mscale", ctypes.c_double)]
 
 
 _declared = None

@@ -249,3 +249,22 @@ def test_captured_append_attend_keep(kv):
             assert torch.equal(cap[name], eager[name]), name
         for x, y in zip(cap["gen"] + cap["e"], eager["gen"] + eager["e"]):
             assert x is None or torch.equal(x, y)
+
+
+@pytest.mark.parametrize("layout,D,R", [("half", 128, 128), ("interleaved", 128, 64), ("half", 64, 64), ("interleaved", 256, 256)])
+def test_codes_are_those_of_the_rotation_in_64_bits(layout, D, R):
+    """A million rotated values: every code and exponent, those next to a border too (a rotation in fp32 has some of them wrong).
+    The kernel's angles and its series are off by some 2^-33, which no border here is as near as."""
+    r = Rows(41 + D, C=4, T=64, Hq=16 * 128 // D, Hkv=16 * 128 // D, D=D, cap=80, Tp=50000, kv="e4m3", steps=[0, 16, 3, 7], fused=False)
+    freq = 1e6 ** (-np.arange(0, R, 2) / R) / 8
+    r.append(sp.make_rope(layout, R, 1.1), torch.from_numpy(freq).cuda())
+    y = f64(r.k)
+    pos = np.broadcast_to((r.Tp + r.steps[:, None].astype(np.int64) + r.depth)[..., None], y.shape[:3])
+    code, e = ref.quantised(ref.rotated(y, pos, freq, layout, R, 1.1))
+    got, exps, on = r.values()[0], f64(r.exps[0]), r.written()
+    wrong = 0
+    for c, t in np.argwhere(on):
+        row = r.steps[c] + t
+        assert np.array_equal(exps[c, :, row], e[c, t] + 127)
+        wrong += int((got[c, :, row] != np.ldexp(code[c, t], e[c, t][..., None])).sum())
+    assert wrong == 0
