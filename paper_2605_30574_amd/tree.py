@@ -56,7 +56,7 @@ def _library():
                 ("splice_token_scores_workspace_bytes", i64, [i64, i64, i32]),
                 ("splice_token_scores", i32, [vp, i32, i64, i64, i64, ctypes.c_float, vp, i32] + [vp] * 7 + [size, vp])):
             f = getattr(lib, name)
-            f.restype, f.argtypes = res, args
+            f.restype, f.argtypes = res, args   # (a structure passes by reference where its pointer is declared)
         _declared = lib
     return lib
 
@@ -236,9 +236,9 @@ def splice_tree_append(shape, tree, rope, freq, cell_step, depth, q, k, v, q_out
     pp = None if pos is None else _ptr(pos, "pos", C * T, t.int64, dev)
     fp = None if rope.rotary_dim == 0 and freq is None else _ptr(freq, "freq", rope.rotary_dim // 2, t.float64, dev)
     stp = _steps(cell_step, C)
-    S._check(lib.splice_tree_append(ctypes.byref(shape), ctypes.byref(tree), ctypes.byref(rope), stp, dp, pp, fp, qp, qs, kp,
-                                    ks, vp, vs, qo, *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp),
-                                    _stream(stream, dev)), "splice_tree_append")
+    S._check(lib.splice_tree_append(shape, tree, rope, stp, dp, pp, fp, qp, qs, kp, ks, vp, vs, qo,
+                                    *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp), _stream(stream, dev)),
+             "splice_tree_append")
 
 
 def splice_tree_read(shape, tree, cell_step, gen_k, gen_v, gen_k_exp, gen_v_exp, rows_k, rows_v, stream=None) -> None:
@@ -248,13 +248,13 @@ def splice_tree_read(shape, tree, cell_step, gen_k, gen_v, gen_k_exp, gen_v_exp,
     n = shape.n_cells * shape.n_kv_heads * tree.n_nodes * shape.head_dim
     rk, rv = (_ptr(x, name, n, S._torch.bfloat16, dev) for x, name in ((rows_k, "rows_k"), (rows_v, "rows_v")))
     stp = _steps(cell_step, shape.n_cells)
-    S._check(lib.splice_tree_read(ctypes.byref(shape), ctypes.byref(tree), stp,
+    S._check(lib.splice_tree_read(shape, tree, stp,
                                   *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp), rk, rv,
                                   _stream(stream, dev)), "splice_tree_read")
 
 
 def splice_tree_attn_workspace_bytes(shape, call, tree) -> int:
-    return S._check(_library().splice_tree_attn_workspace_bytes(ctypes.byref(shape), ctypes.byref(call), ctypes.byref(tree)),
+    return S._check(_library().splice_tree_attn_workspace_bytes(shape, call, tree),
                     "splice_tree_attn_workspace_bytes")
 
 
@@ -294,7 +294,7 @@ def splice_tree_attn(shape, call, tree, cell_LW, cell_step, depth, visible, q, c
     op, lp = _ptr(out, "out", C * T * Hq * D, bf16, dev), _ptr(lse, "lse", C * T * Hq, t.float32, dev)
     wp, wbytes = _workspace(workspace, dev)
     lwp, stp = _host(cell_LW, C, 2, "cell_LW", "rows"), _steps(cell_step, C)
-    S._check(lib.splice_tree_attn(ctypes.byref(shape), ctypes.byref(call), ctypes.byref(tree), lwp, stp, dp, vp, qp, ck, cv,
+    S._check(lib.splice_tree_attn(shape, call, tree, lwp, stp, dp, vp, qp, ck, cv,
                                   dk, dv, *gen, op, lp, wp, wbytes, _stream(stream, dev)), "splice_tree_attn")
 
 
@@ -304,7 +304,7 @@ def splice_tree_keep(shape, tree, cell_step, keep, gen_k, gen_v, gen_k_exp=None,
     dev = _anchor(keep, "keep")
     kp = _ptr(keep, "keep", shape.n_cells * tree.n_nodes, S._torch.int32, dev)
     stp = _steps(cell_step, shape.n_cells)
-    S._check(lib.splice_tree_keep(ctypes.byref(shape), ctypes.byref(tree), stp, kp,
+    S._check(lib.splice_tree_keep(shape, tree, stp, kp,
                                   *_caches(shape, tree, dev, gen_k, gen_v, gen_k_exp, gen_v_exp),
                                   _stream(stream, dev)), "splice_tree_keep")
 
