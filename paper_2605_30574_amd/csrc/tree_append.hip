@@ -24,6 +24,7 @@ constexpr int kMinExp = -100;   // smallest exponent of an 8-bit row
 typedef __bf16 bf16x8v_t __attribute__((ext_vector_type(8)));
 typedef float f32x8v_t __attribute__((ext_vector_type(8)));
 
+template <int CELLS>
 struct AppendArgs {
     const __bf16 *q, *k, *v;
     __bf16 *q_out;
@@ -35,7 +36,7 @@ struct AppendArgs {
     int64_t q_stride, k_stride, v_stride;
     int T, Hq, Hkv, cap, Tp, half_rotary, interleaved;
     double mscale;
-    TreeCells cells;
+    TreeCells<CELLS> cells;
 };
 
 // Eight values of a cache row to 8-bit codes: x 2^-e, to the nearest, ties to
@@ -101,8 +102,8 @@ __device__ __forceinline__ float odd_float(double x) {
 // two rounds of loads (the depth, the row) bound it at few nodes, 3.9 us for 32
 // tokens; the rows' bytes at many: 128 cells of 33 nodes, 32 + 2 x 8 heads of 128
 // to an 8-bit cache, 95 MB in 21.0 us (4.5 TB/s; 19.2 with the keys rotated in 32 bits).
-template <int D, bool F8>
-__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
+template <int D, bool F8, int CELLS>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs<CELLS> a) {
     constexpr int LPR = D / 8, ROWS = kAppendThreads / LPR;
     __shared__ float2 s_cs[D / 2];
     __shared__ double2 s_cs64[F8 ? D / 2 : 1];   // for the keys of an 8-bit cache
@@ -170,20 +171,21 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
     }
 }
 
+template <int CELLS>
 struct RowsArgs {
     char *gk, *gv;
     uint8_t *gke, *gve;
     __bf16 *rows_k, *rows_v;
     const int32_t *keep;
     int T, Hkv, cap;
-    TreeCells cells;
+    TreeCells<CELLS> cells;
 };
 
 // One thread reads eight values of one row: blockIdx.x (active cell, KV head),
 // blockIdx.y K or V.  Bound by its bytes: the rows of those 128 x 33 nodes,
 // 26 MB in 5.4 us.
-template <int D, bool F8>
-__global__ __launch_bounds__(kAppendThreads) void read_kernel(RowsArgs a) {
+template <int D, bool F8, int CELLS>
+__global__ __launch_bounds__(kAppendThreads) void read_kernel(RowsArgs<CELLS> a) {
     constexpr int LPR = D / 8;
     const int ci = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv;
     const int64_t pair = (int64_t)a.cells.cell[ci] * a.Hkv + g, row0 = pair * a.cap + a.cells.step[ci];
@@ -210,8 +212,8 @@ __global__ __launch_bounds__(kAppendThreads) void read_kernel(RowsArgs a) {
 // elsewhere.  A row's exponent moves with its first unit.  Launch and two
 // rounds of memory bound it: 128 cells of 8 heads, up to 64 rows of 128
 // bytes, 17 MB in 5.0 us.
-template <int ROW, bool F8>
-__global__ __launch_bounds__(kAppendThreads) void keep_kernel(RowsArgs a) {
+template <int ROW, bool F8, int CELLS>
+__global__ __launch_bounds__(kAppendThreads) void keep_kernel(RowsArgs<CELLS> a) {
     constexpr int LPR = ROW / 16, U = SPLICE_MAX_NODES * LPR / kAppendThreads;
     __shared__ int s_from[SPLICE_MAX_NODES];
     const int ci = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, tid = threadIdx.x, lane = tid & 63;
@@ -285,17 +287,19 @@ int32_t splice_tree_append(const splice_shape *shape, const splice_tree *tree, c
         k_stride % 8 || v_stride % 8)
         return SPLICE_ESHAPE;
     if (q == q_out && q_stride != (int64_t)sh.n_q_heads * D) return SPLICE_EINVAL;
-    AppendArgs a{(const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, (__bf16 *)q_out, (char *)gen_k, (char *)gen_v,
-                 gen_k_exp, gen_v_exp, depth, pos, freq, q_stride, k_stride, v_stride, tree->n_nodes, sh.n_q_heads,
-                 sh.n_kv_heads, sh.gen_capacity, sh.prompt_len, rope->rotary_dim / 2,
-                 rope->layout == SPLICE_ROPE_INTERLEAVED, rope->mscale, {}};
-    const int n = splice::active_cells(sh, cell_step, a.cells);
+    const int n = splice::active_cells(sh, cell_step);
     if (n == 0) return SPLICE_OK;
     const int rows = kAppendThreads / (D / 8);
     const dim3 grid((unsigned)(n * tree->n_nodes), (unsigned)splice::ceil_div(sh.n_q_heads + 2 * sh.n_kv_heads, rows));
-    splice::with_format(D, tree->kv_format, [&](auto d, auto f8) {
-        hipLaunchKernelGGL((append_kernel<decltype(d)::value, decltype(f8)::value>), grid, dim3(kAppendThreads), 0,
-                           (hipStream_t)stream, a);
+    splice::with_format(D, tree->kv_format, n, [&](auto d, auto f8, auto room) {
+        AppendArgs<decltype(room)::value> a{
+            (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, (__bf16 *)q_out, (char *)gen_k, (char *)gen_v,
+            gen_k_exp, gen_v_exp, depth, pos, freq, q_stride, k_stride, v_stride, tree->n_nodes, sh.n_q_heads,
+            sh.n_kv_heads, sh.gen_capacity, sh.prompt_len, rope->rotary_dim / 2,
+            rope->layout == SPLICE_ROPE_INTERLEAVED, rope->mscale, {}};
+        splice::list_cells(sh, cell_step, a.cells);
+        hipLaunchKernelGGL((append_kernel<decltype(d)::value, decltype(f8)::value, decltype(room)::value>), grid,
+                           dim3(kAppendThreads), 0, (hipStream_t)stream, a);
     });
     return launched();
 }
@@ -309,15 +313,17 @@ int32_t splice_tree_read(const splice_shape *shape, const splice_tree *tree, con
     if (!rows_k || !rows_v || !splice::aligned(rows_k, 16) || !splice::aligned(rows_v, 16) ||
         !caches_ok(*tree, gen_k, gen_v, gen_k_exp, gen_v_exp))
         return SPLICE_EINVAL;
-    RowsArgs a{(char *)const_cast<void *>(gen_k), (char *)const_cast<void *>(gen_v), const_cast<uint8_t *>(gen_k_exp),
-               const_cast<uint8_t *>(gen_v_exp), (__bf16 *)rows_k, (__bf16 *)rows_v, nullptr, tree->n_nodes,
-               shape->n_kv_heads, shape->gen_capacity, {}};
-    const int n = splice::active_cells(*shape, cell_step, a.cells);
+    const int n = splice::active_cells(*shape, cell_step);
     if (n == 0) return SPLICE_OK;
     const dim3 grid((unsigned)(n * shape->n_kv_heads), 2);
-    splice::with_format(shape->head_dim, tree->kv_format, [&](auto d, auto f8) {
-        hipLaunchKernelGGL((read_kernel<decltype(d)::value, decltype(f8)::value>), grid, dim3(kAppendThreads), 0,
-                           (hipStream_t)stream, a);
+    splice::with_format(shape->head_dim, tree->kv_format, n, [&](auto d, auto f8, auto room) {
+        RowsArgs<decltype(room)::value> a{
+            (char *)const_cast<void *>(gen_k), (char *)const_cast<void *>(gen_v), const_cast<uint8_t *>(gen_k_exp),
+            const_cast<uint8_t *>(gen_v_exp), (__bf16 *)rows_k, (__bf16 *)rows_v, nullptr, tree->n_nodes,
+            shape->n_kv_heads, shape->gen_capacity, {}};
+        splice::list_cells(*shape, cell_step, a.cells);
+        hipLaunchKernelGGL((read_kernel<decltype(d)::value, decltype(f8)::value, decltype(room)::value>), grid,
+                           dim3(kAppendThreads), 0, (hipStream_t)stream, a);
     });
     return launched();
 }
@@ -329,14 +335,16 @@ int32_t splice_tree_keep(const splice_shape *shape, const splice_tree *tree, con
     if (rc != SPLICE_OK) return rc;
     if (shape->n_cells == 0) return SPLICE_OK;
     if (!keep || !splice::aligned(keep, 4) || !caches_ok(*tree, gen_k, gen_v, gen_k_exp, gen_v_exp)) return SPLICE_EINVAL;
-    RowsArgs a{(char *)gen_k, (char *)gen_v, gen_k_exp, gen_v_exp, nullptr, nullptr, keep, tree->n_nodes,
-               shape->n_kv_heads, shape->gen_capacity, {}};
-    const int n = splice::active_cells(*shape, cell_step, a.cells);
+    const int n = splice::active_cells(*shape, cell_step);
     if (n == 0) return SPLICE_OK;
     const dim3 grid((unsigned)(n * shape->n_kv_heads), 2);
-    splice::with_format(shape->head_dim, tree->kv_format, [&](auto d, auto f8) {
+    splice::with_format(shape->head_dim, tree->kv_format, n, [&](auto d, auto f8, auto room) {
         constexpr int ROW = decltype(d)::value * (decltype(f8)::value ? 1 : 2);
-        hipLaunchKernelGGL((keep_kernel<ROW, decltype(f8)::value>), grid, dim3(kAppendThreads), 0, (hipStream_t)stream, a);
+        RowsArgs<decltype(room)::value> a{(char *)gen_k, (char *)gen_v, gen_k_exp, gen_v_exp, nullptr, nullptr, keep,
+                                          tree->n_nodes, shape->n_kv_heads, shape->gen_capacity, {}};
+        splice::list_cells(*shape, cell_step, a.cells);
+        hipLaunchKernelGGL((keep_kernel<ROW, decltype(f8)::value, decltype(room)::value>), grid, dim3(kAppendThreads), 0,
+                           (hipStream_t)stream, a);
     });
     return launched();
 }

@@ -11,23 +11,30 @@
 
 namespace splice {
 
-// The cells that are not finished, in order: their steps and indexes.  Words
+// Up to N cells that are not finished, in order: their steps and indexes.  Words
 // throughout, as kernels read these at a computed place: a byte array beside a
 // word array under one index has been compiled into a scalar load whose base
 // is no multiple of four, and the hardware drops those bits.
+template <int N>
 struct TreeCells {
-    int32_t step[SPLICE_MAX_CELLS];
-    uint32_t cell[SPLICE_MAX_CELLS];
+    int32_t step[N];
+    uint32_t cell[N];
 };
 
-inline int active_cells(const splice_shape &sh, const int32_t *cell_step, TreeCells &out) {
+inline int active_cells(const splice_shape &sh, const int32_t *cell_step) {
     int n = 0;
-    for (int c = 0; c < sh.n_cells; ++c)
+    for (int c = 0; c < sh.n_cells; ++c) n += cell_step[c] >= 0;
+    return n;
+}
+
+template <int N>
+void list_cells(const splice_shape &sh, const int32_t *cell_step, TreeCells<N> &out) {
+    int n = 0;
+    for (int c = 0; c < sh.n_cells && n < N; ++c)
         if (cell_step[c] >= 0) {
             out.step[n] = cell_step[c];
             out.cell[n++] = (uint32_t)c;
         }
-    return n;
 }
 
 inline int32_t validate_tree_shape(const splice_shape *shape, const splice_tree *tree) {
@@ -52,12 +59,19 @@ inline int32_t validate_tree(const splice_shape *shape, const splice_tree *tree,
     return SPLICE_OK;
 }
 
-// Calls f with (head_dim, 8-bit cache) as compile-time constants.
+// Calls f with (head_dim, 8-bit cache, room for the n active cells) as
+// compile-time constants.  Up to 32 cells have arguments of their own size: a launch copies them, and
+// 2 KB of cells more took 0.4 us of the host's 6.7 for a call that moves a few rows.
+constexpr int kTreeFewCells = 32;
 template <class F>
-void with_format(int D, int kv_format, F f) {
+void with_format(int D, int kv_format, int n, F f) {
+    auto room = [&](auto d, auto f8) {
+        if (n <= kTreeFewCells) f(d, f8, std::integral_constant<int, kTreeFewCells>{});
+        else f(d, f8, std::integral_constant<int, SPLICE_MAX_CELLS>{});
+    };
     auto pick = [&](auto d) {
-        if (kv_format == SPLICE_KV_E4M3) f(d, std::true_type{});
-        else f(d, std::false_type{});
+        if (kv_format == SPLICE_KV_E4M3) room(d, std::true_type{});
+        else room(d, std::false_type{});
     };
     if (D == 64) pick(std::integral_constant<int, 64>{});
     else if (D == 128) pick(std::integral_constant<int, 128>{});
@@ -114,7 +128,7 @@ struct TreeSlots {
     uint32_t order[kTreeMaxSlots / 2];     // active cell | chunk << 8, in 16 bits
 };
 
-inline void tree_slots(const TreeCells &cells, const uint8_t *onset, const int *tiles, int n, const TreePlan &p, TreeSlots &out) {
+inline void tree_slots(const TreeCells<SPLICE_MAX_CELLS> &cells, const uint8_t *onset, const int *tiles, int n, const TreePlan &p, TreeSlots &out) {
     uint32_t first = 0;
     int most = 0;
     for (int i = 0; i < n; ++i) {
@@ -260,9 +274,10 @@ inline TreePlan tree_prepare(const splice_shape &sh, const splice_call &call, co
                              const int32_t *cell_step, int n_cu, int &n, int32_t *step, TreeSlots &slots) {
     const int T = tree.n_nodes;
     const bool f8 = tree.kv_format == SPLICE_KV_E4M3;
-    TreeCells cells, sorted;
-    n = active_cells(sh, cell_step, cells);
+    TreeCells<SPLICE_MAX_CELLS> cells, sorted;
+    n = active_cells(sh, cell_step);
     if (n == 0) return TreePlan{};
+    list_cells(sh, cell_step, cells);
     uint8_t onset[SPLICE_MAX_CELLS], sorted_onset[SPLICE_MAX_CELLS], cls[SPLICE_MAX_CELLS];
     int n_of[3] = {0, 0, 0};
     for (int i = 0; i < n; ++i) {

@@ -268,3 +268,39 @@ def test_codes_are_those_of_the_rotation_in_64_bits(layout, D, R):
         assert np.array_equal(exps[c, :, row], e[c, t] + 127)
         wrong += int((got[c, :, row] != np.ldexp(code[c, t], e[c, t][..., None])).sum())
     assert wrong == 0
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("C,finished", [(32, 0), (33, 0), (40, 8), (41, 8), (256, 0), (256, 100)])
+def test_many_cells(C, finished, kv):
+    """Rows of up to as many cells as a call takes, some finished: appended unturned, read back, the second node kept as the first."""
+    rng = np.random.default_rng(C + finished)
+    steps = rng.integers(0, 9, C).astype(np.int32)
+    steps[rng.choice(C, finished, replace=False)] = -1
+    r = Rows(51, C=C, T=3, cap=11, kv=kv, steps=steps, fused=False)
+    r.depth[:] = np.arange(3)
+    r.depth_dev = torch.from_numpy(r.depth).cuda()
+    start = [x.clone() for x in r.gen]
+    r.append(sp.make_rope("half", 0), None)
+    rows = [torch.full((C, r.Hkv, 3, r.D), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    sp.splice_tree_read(r.shape, r.tree, r.steps, *r.gen, *r.exps, *rows)
+    torch.cuda.synchronize()
+    on = torch.from_numpy(steps >= 0).cuda()
+    for got, x, cache, before in zip(rows, (r.k, r.v), r.gen, start):
+        want = x.transpose(1, 2)
+        if kv == "bf16":
+            assert torch.equal(got[on], want[on])
+        else:
+            code, e = ref.quantised(f64(want))
+            assert np.array_equal(f64(got)[steps >= 0], np.ldexp(code, e[..., None])[steps >= 0])
+        assert (got[~on] == 5.0).all() and torch.equal(cache[~on], before[~on])
+    kept = [x.clone() for x in r.gen]
+    keep = torch.tensor([[1, 2, -1]] * C, dtype=torch.int32).cuda()
+    sp.splice_tree_keep(r.shape, r.tree, r.steps, keep, *r.gen, *r.exps)
+    torch.cuda.synchronize()
+    for x, y in zip(r.gen, kept):
+        for c in range(C):
+            s = steps[c]
+            if s >= 0:
+                y[c, :, s:s + 2] = y[c, :, s + 1:s + 3].clone()
+        assert torch.equal(x, y)
