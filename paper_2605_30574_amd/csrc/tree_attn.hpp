@@ -129,9 +129,9 @@ struct TreeTile {
 // that a quarter-wave reads of K, and the four rows that a 16-lane group reads
 // 32 bytes each of V, fall into different banks.
 template <int D>
-__device__ __forceinline__ int tree_swz_k(int r) { return D == 64 ? (r >> 1) & 7 : r & 15; }
+__device__ __forceinline__ constexpr int tree_swz_k(int r) { return D == 64 ? (r >> 1) & 7 : r & 15; }
 template <int D>
-__device__ __forceinline__ int tree_swz_v(int r) { return D == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; }
+__device__ __forceinline__ constexpr int tree_swz_v(int r) { return D == 64 ? ((r >> 1) & 1) * 5 : (r & 3) << 2 | (r & 1); }
 
 // Bits [b, e) of a word, for any b and e.
 __device__ __forceinline__ uint64_t bits(int b, int e) {
@@ -424,31 +424,33 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
         v_at = X::TILE + vrow * X::ROW + ((chunk_of ^ tree_swz_v<D>(vrow)) << 4) + 8 * (lane & 1);
     }
 
-    // What load() left in registers, into the tile.  8-bit rows: a lane has two
-    // neighbouring chunks.  A store of the wave meets every bank, of K by the
-    // swizzle, of V as every other eight lanes begin with the second.
+    // What load() left in registers, into the tile: 8-bit rows two neighbouring
+    // chunks a lane.  A lane's i-th key is i * step rows behind its first, whose
+    // swizzle differs by a constant: one address each of K and V, and constants.
     auto store = [&](char *buf, int seg) {
-        auto put_k = [&](int key, int chunk, u32x4_t k) {
-            *reinterpret_cast<u32x4_t *>(buf + key * X::ROW + ((chunk ^ tree_swz_k<D>(key)) << 4)) = k;
-        };
-        auto put_v = [&](int key, int chunk, u32x4_t v) {
-            *reinterpret_cast<u32x4_t *>(buf + X::TILE + key * X::ROW + ((chunk ^ tree_swz_v<D>(key)) << 4)) = v;
-        };
         if (F8 && seg == 4) {
+            constexpr int LPR = D / 16, STEP = X::NT / LPR;
+            const int key = ltid / LPR, ch = 2 * (ltid % LPR);
+            const int at_k = key * X::ROW + ((ch ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((ch ^ tree_swz_v<D>(key)) << 4);
             static_for<0, X::NL8>([&](auto i) {
-                const int u = (int)i * X::NT + ltid, key = u / (D / 16), ch = 2 * (u % (D / 16)), odd = (lane >> 3) & 1;
+                const u32x4_t k = kr[i], v = vr[i];
                 static_for<0, 2>([&](auto j) {
-                    const bool second = (int)j != odd;
-                    const u32x4_t k = kr[i], v = vr[i];
-                    put_k(key, ch + j, e4m3_to_bf16(j ? make_uint2(k.z, k.w) : make_uint2(k.x, k.y), ke[i]));
-                    put_v(key, ch + (second ? 1 : 0), e4m3_to_bf16(second ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y), ve[i]));
+                    constexpr int ck = (j ^ tree_swz_k<D>(i * STEP)) << 4, cv = (j ^ tree_swz_v<D>(i * STEP)) << 4;
+                    char *const to = buf + i * STEP * X::ROW;
+                    *reinterpret_cast<u32x4_t *>(to + (at_k ^ ck)) = e4m3_to_bf16(j ? make_uint2(k.z, k.w) : make_uint2(k.x, k.y), ke[i]);
+                    *reinterpret_cast<u32x4_t *>(to + X::TILE + (at_v ^ cv)) =
+                        e4m3_to_bf16(j ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y), ve[i]);
                 });
             });
         } else if constexpr (X::OWN) {
+            constexpr int STEP = X::NT / X::CPR;
+            const int key = ltid / X::CPR, ch = ltid % X::CPR;
+            const int at_k = key * X::ROW + ((ch ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((ch ^ tree_swz_v<D>(key)) << 4);
             static_for<0, X::NL>([&](auto i) {
-                const int u = (int)i * X::NT + ltid;
-                put_k(u / X::CPR, u % X::CPR, kr[i]);
-                put_v(u / X::CPR, u % X::CPR, vr[i]);
+                constexpr int ck = tree_swz_k<D>(i * STEP) << 4, cv = tree_swz_v<D>(i * STEP) << 4;
+                char *const to = buf + i * STEP * X::ROW;
+                *reinterpret_cast<u32x4_t *>(to + (at_k ^ ck)) = kr[i];
+                *reinterpret_cast<u32x4_t *>(to + X::TILE + (at_v ^ cv)) = vr[i];
             });
         }
     };
