@@ -17,8 +17,8 @@
 //                 which P lies in the lanes; P rounded to bf16 (weights of at
 //                 most 2^kSlack with relative errors of 2^-9 that average
 //                 out; their sum is not rounded).
-// RW = 1: every wave has a tile of its own, with the next one in registers, and
-// waits for no other; else a tile is for all waves, and bf16 rows go straight
+// RW = 1: every wave has a tile of its own, with the next one (of 8-bit rows the
+// next two) in registers, and waits for no other; else a tile is for all waves, and bf16 rows go straight
 // to one of two buffers in LDS while the other is computed.
 //
 // The list has up to five segments (prompt before, in and behind the span, each
@@ -34,9 +34,9 @@
 // What bounds it: where many rows share keys the tile loop, whose matrix products
 // (40% busy) and vector operations (45%) overlap in part only: 47 cells of 16 nodes, 32 heads of
 // 128 over 8k slots 135 us in the kernel (800 TFLOP/s); with small trees the generated
-// rows' bytes, 64 cells of 5 nodes, 4.3 TB/s of bf16 rows and 3.2 TB/s of 8-bit ones, 5.3 and 4.3
-// over longer lists (two 8-bit tiles in flight a wave measured the same as one: what is left is
-// the chain from codes through LDS to the products); in small calls
+// rows' bytes, 64 cells of 5 nodes, 4.4 TB/s of bf16 rows and 3.3 TB/s of 8-bit ones, 5.3 and 4.5
+// over longer lists (4.2 with one 8-bit tile in flight a wave; with half the bytes a key the
+// chain from codes through LDS to the products counts for more); in small calls
 // the chain of loads before the first tile (7.4 us with one tile).
 #pragma once
 
@@ -119,6 +119,8 @@ struct TreeTile {
     static constexpr int NL = TK * CPR / NT;                   // chunks a thread loads of a K (or V) tile
     static constexpr int NL8 = NL / 2;                         // ... of 8-bit rows
     static constexpr int NR = OWN ? NL : NL8;                  // ... by way of registers
+    static constexpr bool DEEP = OWN && F8;                    // two 8-bit tiles fit the registers of a bf16 one
+    static constexpr int NE = OWN ? 2 : NL8;                   // exponents a thread holds: of a key of each tile, or a chunk
     static constexpr int EARLY = !OWN && D <= 128 ? 2 : 0;     // 16-key steps whose values are read before the softmax
     static constexpr int ND = D / 32;                          // 32-wide d blocks of the output
     static constexpr int PARTS = KW > 1 && KW * 32 * RW * D * 4 > TILES ? 2 : 1;   // in which the waves' results are joined
@@ -345,18 +347,20 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
         w.rem = __builtin_amdgcn_readfirstlane(x.len - skip * TK);
     };
     // The tile under way: how many keys, which, and what has to be looked at.
-    auto tile_of = [&]() {
+    auto tile = [&](int seg, int key0, int rem) {
         TreeTileRef x;
-        x.seg = w.seg;
-        x.key0 = w.key0;
-        x.n = min(TK, w.rem);
-        x.other = any_clean && any_donor && (w.seg == 1 || w.seg == 2);
-        const bool gen = !PACKED && w.seg == 4;
-        x.dead = gen && w.key0 + TK > step && alive != bits(0, a.T);
-        x.differ = x.other || (gen ? a.Tp + w.key0 < low_max || w.key0 + TK > step : w.key0 < low_max);
-        x.edge = x.n < TK || (x.differ && !x.other) || (x.other && w.key0 < low_max);
+        x.seg = seg;
+        x.key0 = key0;
+        x.n = min(TK, rem);
+        x.other = any_clean && any_donor && (seg == 1 || seg == 2);
+        const bool gen = !PACKED && seg == 4;
+        x.dead = gen && key0 + TK > step && alive != bits(0, a.T);
+        x.differ = x.other || (gen ? a.Tp + key0 < low_max || key0 + TK > step : key0 < low_max);
+        x.edge = x.n < TK || (x.differ && !x.other) || (x.other && key0 < low_max);
         return x;
     };
+    auto tile_of = [&]() { return tile(w.seg, w.key0, w.rem); };
+    auto generated = [&](int key0) { return tile(4, key0, step + a.T - key0); };
     auto advance = [&]() {   // to the wave's next tile
         const int row_bytes = F8 && w.seg == 4 ? D : X::ROW;
         constexpr int N = X::OWN ? 4 : 1;
@@ -385,28 +389,45 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
         });
     }
     u32x4_t kr[X::NR], vr[X::NR];
-    uint32_t ke[X::NL8], ve[X::NL8];
-    auto load = [&](int b) {   // the walk's tile
-        const int n = min(TK, w.rem);
-        if (F8 && w.seg == 4) {
-            const int64_t ex = pair * a.cap + w.key0;
-            const __amdgpu_buffer_rsrc_t rk = rows_rsrc(w.k, n * D), rv = rows_rsrc(w.v, n * D);
-            const __amdgpu_buffer_rsrc_t re = rows_rsrc(uniform(reinterpret_cast<const char *>(a.gke + ex)), n);
-            const __amdgpu_buffer_rsrc_t rf = rows_rsrc(uniform(reinterpret_cast<const char *>(a.gve + ex)), n);
-            static_for<0, X::NL8>([&](auto i) {
-                const int u = (int)i * X::NT + ltid;
-                kr[i] = row_load<0>(rk, u * 16);
-                vr[i] = row_load<0>(rv, u * 16);
+    uint8_t ke[X::NE], ve[X::NE];   // bytes: made words where they are loaded, they would be waited for there
+    constexpr std::integral_constant<int, 0> kFirst{};
+    constexpr std::integral_constant<int, 1> kSecond{};
+    auto load8 = [&](auto set) {   // the walk's tile of 8-bit rows; nothing behind the list's end
+        const int n = __builtin_amdgcn_readfirstlane(X::DEEP ? max(min(TK, w.rem), 0) : min(TK, w.rem));
+        const int64_t ex = pair * a.cap + w.key0;
+        const __amdgpu_buffer_rsrc_t rk = rows_rsrc(uniform(w.k), n * D), rv = rows_rsrc(uniform(w.v), n * D);
+        const __amdgpu_buffer_rsrc_t re = rows_rsrc(uniform(reinterpret_cast<const char *>(a.gke + ex)), n);
+        const __amdgpu_buffer_rsrc_t rf = rows_rsrc(uniform(reinterpret_cast<const char *>(a.gve + ex)), n);
+        constexpr int at = decltype(set)::value * X::NL8;
+        static_for<0, X::NL8>([&](auto i) {
+            const int u = (int)i * X::NT + ltid;
+            kr[at + i] = row_load<0>(rk, u * 16);
+            vr[at + i] = row_load<0>(rv, u * 16);
+            if constexpr (!X::OWN) {
                 ke[i] = __builtin_amdgcn_raw_buffer_load_b8(re, u / (D / 16), 0, 0);
                 ve[i] = __builtin_amdgcn_raw_buffer_load_b8(rf, u / (D / 16), 0, 0);
-            });
+            }
+        });
+        if constexpr (X::OWN) {
+            ke[set] = __builtin_amdgcn_raw_buffer_load_b8(re, r, 0, 0);
+            ve[set] = __builtin_amdgcn_raw_buffer_load_b8(rf, r, 0, 0);
+        }
+    };
+    auto load16 = [&]() {   // ... of a wave's own
+        const int n = min(TK, w.rem);
+        const __amdgpu_buffer_rsrc_t rk = rows_rsrc(w.k, n * X::ROW), rv = rows_rsrc(w.v, n * X::ROW);
+        static_for<0, X::NL>([&](auto i) {
+            kr[i] = row_load<0>(rk, ((int)i * X::NT + ltid) * 16);
+            vr[i] = row_load<0>(rv, ((int)i * X::NT + ltid) * 16);
+        });
+    };
+    auto load = [&](int b) {   // the walk's tile
+        if (F8 && w.seg == 4) {
+            load8(kFirst);
         } else if constexpr (X::OWN) {
-            const __amdgpu_buffer_rsrc_t rk = rows_rsrc(w.k, n * X::ROW), rv = rows_rsrc(w.v, n * X::ROW);
-            static_for<0, X::NL>([&](auto i) {
-                kr[i] = row_load<0>(rk, ((int)i * X::NT + ltid) * 16);
-                vr[i] = row_load<0>(rv, ((int)i * X::NT + ltid) * 16);
-            });
+            load16();
         } else {
+            const int n = min(TK, w.rem);
             const u32x4_t rk = rows_desc(w.k, n * X::ROW), rv = rows_desc(w.v, n * X::ROW);
             const uint32_t base = lds0 + b * 2 * X::TILE;
             static_for<0, X::NL>([&](auto i) {
@@ -427,32 +448,44 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     // What load() left in registers, into the tile: 8-bit rows two neighbouring
     // chunks a lane.  A lane's i-th key is i * step rows behind its first, whose
     // swizzle differs by a constant: one address each of K and V, and constants.
-    auto store = [&](char *buf, int seg) {
-        if (F8 && seg == 4) {
-            constexpr int LPR = D / 16, STEP = X::NT / LPR;
-            const int key = ltid / LPR, ch = 2 * (ltid % LPR);
-            const int at_k = key * X::ROW + ((ch ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((ch ^ tree_swz_v<D>(key)) << 4);
-            static_for<0, X::NL8>([&](auto i) {
-                const u32x4_t k = kr[i], v = vr[i];
-                static_for<0, 2>([&](auto j) {
-                    constexpr int ck = (j ^ tree_swz_k<D>(i * STEP)) << 4, cv = (j ^ tree_swz_v<D>(i * STEP)) << 4;
-                    char *const to = buf + i * STEP * X::ROW;
-                    *reinterpret_cast<u32x4_t *>(to + (at_k ^ ck)) = e4m3_to_bf16(j ? make_uint2(k.z, k.w) : make_uint2(k.x, k.y), ke[i]);
-                    *reinterpret_cast<u32x4_t *>(to + X::TILE + (at_v ^ cv)) =
-                        e4m3_to_bf16(j ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y), ve[i]);
-                });
-            });
-        } else if constexpr (X::OWN) {
-            constexpr int STEP = X::NT / X::CPR;
-            const int key = ltid / X::CPR, ch = ltid % X::CPR;
-            const int at_k = key * X::ROW + ((ch ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((ch ^ tree_swz_v<D>(key)) << 4);
-            static_for<0, X::NL>([&](auto i) {
-                constexpr int ck = tree_swz_k<D>(i * STEP) << 4, cv = tree_swz_v<D>(i * STEP) << 4;
+    auto store8 = [&](char *buf, auto set) {
+        constexpr int LPR = D / 16, STEP = X::NT / LPR;
+        const int key = ltid / LPR, ch = 2 * (ltid % LPR);
+        const int at_k = key * X::ROW + ((ch ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((ch ^ tree_swz_v<D>(key)) << 4);
+        static_for<0, X::NL8>([&](auto i) {
+            constexpr int from = decltype(set)::value * X::NL8 + i;
+            const u32x4_t k = kr[from], v = vr[from];
+            uint32_t ek, ev;
+            if constexpr (X::OWN) {
+                ek = __shfl((int)ke[set], key + i * STEP);
+                ev = __shfl((int)ve[set], key + i * STEP);
+            } else {
+                ek = ke[i];
+                ev = ve[i];
+            }
+            static_for<0, 2>([&](auto j) {
+                constexpr int ck = (j ^ tree_swz_k<D>(i * STEP)) << 4, cv = (j ^ tree_swz_v<D>(i * STEP)) << 4;
                 char *const to = buf + i * STEP * X::ROW;
-                *reinterpret_cast<u32x4_t *>(to + (at_k ^ ck)) = kr[i];
-                *reinterpret_cast<u32x4_t *>(to + X::TILE + (at_v ^ cv)) = vr[i];
+                *reinterpret_cast<u32x4_t *>(to + (at_k ^ ck)) = e4m3_to_bf16(j ? make_uint2(k.z, k.w) : make_uint2(k.x, k.y), ek);
+                *reinterpret_cast<u32x4_t *>(to + X::TILE + (at_v ^ cv)) =
+                    e4m3_to_bf16(j ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y), ev);
             });
-        }
+        });
+    };
+    auto store16 = [&](char *buf) {
+        constexpr int STEP = X::NT / X::CPR;
+        const int key = ltid / X::CPR, ch = ltid % X::CPR;
+        const int at_k = key * X::ROW + ((ch ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((ch ^ tree_swz_v<D>(key)) << 4);
+        static_for<0, X::NL>([&](auto i) {
+            constexpr int ck = tree_swz_k<D>(i * STEP) << 4, cv = tree_swz_v<D>(i * STEP) << 4;
+            char *const to = buf + i * STEP * X::ROW;
+            *reinterpret_cast<u32x4_t *>(to + (at_k ^ ck)) = kr[i];
+            *reinterpret_cast<u32x4_t *>(to + X::TILE + (at_v ^ cv)) = vr[i];
+        });
+    };
+    auto store = [&](char *buf, int seg) {
+        if (F8 && seg == 4) store8(buf, kFirst);
+        else if constexpr (X::OWN) store16(buf);
     };
     // Values that are looked at: those of nodes that are not there become 0, and
     // so do infinities and NaN, which must not reach the rows that do not see
@@ -491,11 +524,23 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     const int t_first = X::OWN ? t0 + kw : t0;
     constexpr int t_step = X::OWN ? 4 : 1;
     TreeTileRef cur;
+    // Two tiles of 8-bit rows: always both, so that the number of loads in flight is known where the first is waited for.
+    auto two = [&]() {
+        load8(kFirst);
+        advance();
+        __builtin_amdgcn_sched_barrier(0);   // in this order
+        load8(kSecond);
+        advance();
+    };
     auto begin = [&]() {   // the wave's first tile
         enter(0, t_first);
         cur = tile_of();
-        if (t_first < t1) {
-            load(0);
+        if (t_first >= t1) return;
+        if (X::DEEP && cur.seg == 4) {
+            two();
+        } else {
+            if constexpr (X::DEEP) load16();
+            else load(0);
             advance();
         }
     };
@@ -541,33 +586,8 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
             }
         }
 
-        if constexpr (!X::OWN && X::NBUF == 2) {
-            wait_vmcnt<0>();   // this wave's part of the first tile
-            if (t_first < t1) store(own, cur.seg);
-        }
-        for (int t = t_first; t < t1; t += t_step) {
-            const int b = X::NBUF == 1 ? 0 : (t - t0) & 1;
-            char *const buf = own + b * 2 * X::TILE;
-            // addresses are worked out anew for every tile: kept, they would take the registers of the tile in flight
-            asm volatile("" : "+v"(ltid), "+v"(k_at), "+v"(v_at));
-            if constexpr (X::OWN) {
-                wave_fence();   // the wave has read the tile before
-                store(buf, cur.seg);
-                wave_fence();
-            } else if constexpr (X::NBUF == 1) {
-                wait_vmcnt<0>();
-                store(buf, cur.seg);
-                __syncthreads();
-            } else {
-                __syncthreads();   // every wave's part of tile t is in LDS, and tile t - 1 has been read
-            }
-            const TreeTileRef next = tile_of();
-            // the matrix products of one wave go before the softmax of another on its SIMD
-            __builtin_amdgcn_s_setprio(1);
-            if (t + t_step < t1 && (X::OWN || X::NBUF == 2)) {
-                load(b ^ 1);
-                advance();
-            }
+        // the tile cur, which is in buf
+        auto work = [&](char *buf) {
             if (careful ? cur.differ : cur.dead) {
                 look(cur, buf);
                 if constexpr (X::OWN) wave_fence();
@@ -635,6 +655,36 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
                     });
                 });
             }
+        };
+        if constexpr (!X::OWN && X::NBUF == 2) {
+            wait_vmcnt<0>();   // this wave's part of the first tile
+            if (t_first < t1) store(own, cur.seg);
+        }
+        int t = t_first;
+        for (; !X::DEEP && t < t1; t += t_step) {
+            const int b = X::NBUF == 1 ? 0 : (t - t0) & 1;
+            char *const buf = own + b * 2 * X::TILE;
+            // addresses are worked out anew for every tile: kept, they would take the registers of the tile in flight
+            asm volatile("" : "+v"(ltid), "+v"(k_at), "+v"(v_at));
+            if constexpr (X::OWN) {
+                wave_fence();   // the wave has read the tile before
+                store(buf, cur.seg);
+                wave_fence();
+            } else if constexpr (X::NBUF == 1) {
+                wait_vmcnt<0>();
+                store(buf, cur.seg);
+                __syncthreads();
+            } else {
+                __syncthreads();   // every wave's part of tile t is in LDS, and tile t - 1 has been read
+            }
+            const TreeTileRef next = tile_of();
+            // the matrix products of one wave go before the softmax of another on its SIMD
+            __builtin_amdgcn_s_setprio(1);
+            if (t + t_step < t1 && (X::OWN || X::NBUF == 2)) {
+                load(b ^ 1);
+                advance();
+            }
+            work(buf);
             cur = next;
             if constexpr (!X::OWN && X::NBUF == 1) {
                 __syncthreads();   // tile t has been read
@@ -647,6 +697,61 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
                 wait_vmcnt<0>();
                 if (t + 1 < t1) store(own + (b ^ 1) * 2 * X::TILE, cur.seg);
             }
+        }
+        if constexpr (X::DEEP) {
+            // the prompt's tiles
+            bool turn = false;
+            if (t < t1 && cur.seg != 4) {
+                TreeTileRef next;
+                for (;; t += t_step) {
+                    asm volatile("" : "+v"(ltid), "+v"(k_at), "+v"(v_at));
+                    wave_fence();
+                    store16(own);
+                    wave_fence();
+                    next = tile_of();
+                    __builtin_amdgcn_s_setprio(1);
+                    turn = t + t_step < t1 && next.seg == 4;
+                    if (turn) break;
+                    const bool more = t + t_step < t1;
+                    if (more) {
+                        load16();
+                        advance();
+                    }
+                    work(own);
+                    cur = next;
+                    if (!more) break;
+                }
+                if (turn) {
+                    two();
+                    work(own);
+                    cur = next;
+                } else {
+                    wait_vmcnt<0>();
+                }
+                t += t_step;
+            }
+            // the generated rows, to the list's end: two tiles are in registers, the third is asked for as the first goes to LDS
+            // (a pair of steps without a way out between them, on which loads in flight would be taken to be others)
+            auto step_of = [&](auto set) {
+                const bool on = decltype(set)::value == 0 || t < t1;
+                asm volatile("" : "+v"(ltid), "+v"(k_at), "+v"(v_at));
+                if (on) {
+                    wave_fence();
+                    store8(own, set);
+                    wave_fence();
+                }
+                __builtin_amdgcn_s_setprio(1);
+                load8(set);
+                advance();
+                if (on) work(own);
+                t += t_step;
+                cur = generated(cur.key0 + t_step * TK);
+            };
+            while (t < t1) {
+                step_of(kFirst);
+                step_of(kSecond);
+            }
+            wait_vmcnt<0>();   // what was asked for behind the end: else a walk that follows would seem to have it in flight
         }
         __syncthreads();
         if (careful) break;
