@@ -135,6 +135,10 @@ __device__ __forceinline__ constexpr int tree_swz_k(int r) { return D == 64 ? (r
 template <int D>
 __device__ __forceinline__ constexpr int tree_swz_v(int r) { return D == 64 ? ((r >> 1) & 1) * 5 : (r & 3) << 2 | (r & 1); }
 
+// ... and chunks 8 to 15 of every 16 in pairs the other way round, so that the
+// eight lanes that store every second chunk of an 8-bit row meet every bank.
+__device__ __forceinline__ constexpr int tree_pair(int chunk) { return chunk ^ ((chunk >> 3) & 1); }
+
 // Bits [b, e) of a word, for any b and e.
 __device__ __forceinline__ uint64_t bits(int b, int e) {
     b = max(b, 0);
@@ -384,8 +388,8 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     if constexpr (!X::OWN) {
         static_for<0, X::NL>([&](auto i) {
             const int u = (int)i * 256 + tid, key = u / X::CPR, slot_of = u % X::CPR;
-            k_src[i] = key * X::ROW + ((slot_of ^ tree_swz_k<D>(key)) << 4);
-            v_src[i] = key * X::ROW + ((slot_of ^ tree_swz_v<D>(key)) << 4);
+            k_src[i] = key * X::ROW + (tree_pair(slot_of ^ tree_swz_k<D>(key)) << 4);
+            v_src[i] = key * X::ROW + (tree_pair(slot_of ^ tree_swz_v<D>(key)) << 4);
         });
     }
     u32x4_t kr[X::NR], vr[X::NR];
@@ -437,7 +441,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
             });
         }
     };
-    // ---- addresses of the operands within a buffer: K at k_at ^ 32 st, V at v_at ^ 64 db
+    // ---- addresses of the operands within a buffer: K at k_at ^ 16 tree_pair(2 st), V at v_at ^ 16 tree_pair(4 db)
     int k_at = ((X::OWN ? 0 : kw * 32 * KB) + r) * X::ROW + ((h ^ tree_swz_k<D>(r)) << 4), v_at;
     {
         const int vrow = (X::OWN ? 0 : kw * 32 * KB) + 4 * h + ((lane & 15) >> 2);
@@ -451,7 +455,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     auto store8 = [&](char *buf, auto set) {
         constexpr int LPR = D / 16, STEP = X::NT / LPR;
         const int key = ltid / LPR, ch = 2 * (ltid % LPR);
-        const int at_k = key * X::ROW + ((ch ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((ch ^ tree_swz_v<D>(key)) << 4);
+        const int at_k = key * X::ROW + ((tree_pair(ch) ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((tree_pair(ch) ^ tree_swz_v<D>(key)) << 4);
         static_for<0, X::NL8>([&](auto i) {
             constexpr int from = decltype(set)::value * X::NL8 + i;
             const u32x4_t k = kr[from], v = vr[from];
@@ -475,7 +479,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     auto store16 = [&](char *buf) {
         constexpr int STEP = X::NT / X::CPR;
         const int key = ltid / X::CPR, ch = ltid % X::CPR;
-        const int at_k = key * X::ROW + ((ch ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((ch ^ tree_swz_v<D>(key)) << 4);
+        const int at_k = key * X::ROW + ((tree_pair(ch) ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((tree_pair(ch) ^ tree_swz_v<D>(key)) << 4);
         static_for<0, X::NL>([&](auto i) {
             constexpr int ck = tree_swz_k<D>(i * STEP) << 4, cv = tree_swz_v<D>(i * STEP) << 4;
             char *const to = buf + i * STEP * X::ROW;
@@ -512,7 +516,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
         return x.other && (x.seg == 2) != spliced ? 0 : bits(low - first, n);
     };
     auto values = [&](const char *buf, int db, int kk) {   // 32 d of 16 keys, in the lanes of the A operand
-        const char *at = buf + (v_at ^ 64 * db) + 16 * kk * X::ROW;
+        const char *at = buf + (v_at ^ (tree_pair(4 * db) << 4)) + 16 * kk * X::ROW;
         const u32x2_t lo = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)at));
         const u32x2_t hi = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(at + 8 * X::ROW)));
         return u32x4_t{lo.x, lo.y, hi.x, hi.y};
@@ -555,7 +559,7 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
             for (int ch = 2 * kw + h; ch < X::CPR; ch += 8) {
                 u32x4_t x = {0, 0, 0, 0};
                 if (valid) x = *reinterpret_cast<const u32x4_t *>(a.q + (q_row * D + 8 * ch) * 2);
-                *reinterpret_cast<u32x4_t *>(s_q + r * X::ROW + ((ch ^ tree_swz_k<D>(r)) << 4)) = x;
+                *reinterpret_cast<u32x4_t *>(s_q + r * X::ROW + ((tree_pair(ch) ^ tree_swz_k<D>(r)) << 4)) = x;
             }
             __syncthreads();
         } else {
@@ -599,12 +603,12 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
                 static_for<0, KB>([&](auto kb) {
                     u32x4_t ka[NST];
                     static_for<0, NST>([&](auto st) {
-                        ka[st] = *reinterpret_cast<const u32x4_t *>(buf + (k_at ^ 32 * (int)st) + (int)kb * 32 * X::ROW);
+                        ka[st] = *reinterpret_cast<const u32x4_t *>(buf + (k_at ^ (tree_pair(2 * (int)st) << 4)) + (int)kb * 32 * X::ROW);
                     });
                     static_for<0, 16>([&](auto i) { s[kb][(int)i] = 0.f; });
                     static_for<0, NST>([&](auto st) {
                         bf16x8_t q;
-                        if constexpr (X::OWN) q = *reinterpret_cast<const bf16x8_t *>(s_q + (k_at ^ 32 * (int)st));
+                        if constexpr (X::OWN) q = *reinterpret_cast<const bf16x8_t *>(s_q + (k_at ^ (tree_pair(2 * (int)st) << 4)));
                         else q = qb[st];
                         s[kb] = product(ka[st], q, s[kb]);
                     });
