@@ -106,6 +106,7 @@ int32_t splice_tree_attn(const splice_shape *shape, const splice_call *call, con
     a.per = p.per;
     a.n_p = p.n_p;
     a.p_tiles = p.p_tiles;
+    a.p_heavy0 = p.p_heavy0;
     a.p_heavy = p.p_heavy;
     a.split = p.split;
     a.qk_scale = call->scale * splice_dev::kLog2e;

@@ -69,7 +69,8 @@ struct TreeCall {
     _Float16 *part;
     float4 *record;
     int T, G, lgG, Hkv, Tp, cap, span_lo, span_hi, window, zero_donor, n_active, row_tiles, per;
-    int n_p, p_tiles, p_heavy;   // packed calls: chunks of the prompt, tiles of 128 rows, those that may walk the span twice; else 0
+    int n_p, p_tiles, p_heavy0, p_heavy;   // packed calls: chunks of the prompt, tiles of 128 rows, those that may walk
+                                           // the span twice (first, number); else 0
     bool split;
     float qk_scale;   // scale * log2(e)
 };
@@ -232,7 +233,10 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
         const int of = first ? rest : rest - heavy, among = first ? a.p_heavy : a.p_tiles - a.p_heavy;
         chunk = of / among;
         row0 = 0;
-        const int at = 32 * RW * (of - chunk * among + (first ? 0 : a.p_heavy)) + 32 * rw + r, n_rows = a.n_active * rows;
+        int rt = of - chunk * among;
+        if (first) rt += a.p_heavy0;
+        else if (rt >= a.p_heavy0) rt += a.p_heavy;
+        const int at = 32 * RW * rt + 32 * rw + r, n_rows = a.n_active * rows;
         const int ci = min(at, n_rows - 1) / rows;
         row = at - ci * rows;
         const uint32_t info = args.slots.info[ci];

@@ -110,7 +110,7 @@ constexpr int kTreeMaxChunks = 64;
 struct TreePlan {
     int row_waves, row_tiles, per;
     int n_p, p_tiles;      // packed: chunks of the prompt, tiles of 128 rows; else 0
-    int p_heavy;           // ... the first of them, with nodes on both sides of an onset
+    int p_heavy0, p_heavy; // ... of them, first and number, with unspliced and spliced nodes
     int n_slots, blocks;   // partial results a (node, q head) may have, over all cells; work groups a KV head
     int most_chunks;       // of a cell
     bool split;            // some cell has more than one chunk
@@ -121,8 +121,8 @@ struct TreePlan {
 // none) and its first slot (there is one more, for the end).  An item of the
 // grid: its active cell and chunk, two items a word; chunks of one number
 // stand together, so that work groups that run together read the same part of
-// the prompt, and the active cells are in the order of their class (on both
-// sides of the onset, unspliced, spliced), so that they read the same span.
+// the prompt, and the active cells are in the order of their class (unspliced,
+// on both sides of the onset, spliced), so that they read the same span.
 struct TreeSlots {
     uint32_t info[SPLICE_MAX_CELLS + 1];   // cell | onset << 8 | first slot << 16
     uint32_t order[kTreeMaxSlots / 2];     // active cell | chunk << 8, in 16 bits
@@ -200,13 +200,13 @@ inline bool tree_packed(const splice_shape &sh, const splice_call &call, int T, 
 // D = 256, 1024 keys in view: 16 chunks of two tiles 44 us, 8 of four, beside
 // which they fit, 32).  tiles: of the cells' lists, in a packed call without
 // the prompt, whose list is prompt_tiles long.
-inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, int n_mixed, int n_cu, bool f8,
+inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, const int *n_of, int n_cu, bool f8,
                           bool packed, int prompt_tiles) {
     TreePlan p;
     const int rows = T * group_of(sh);
     p.row_waves = tree_row_waves(sh.head_dim, rows);
     p.row_tiles = ceil_div(rows, 32 * p.row_waves);
-    p.n_p = p.p_tiles = p.p_heavy = 0;
+    p.n_p = p.p_tiles = p.p_heavy0 = p.p_heavy = 0;
     const int tile = tree_tile_keys(sh.head_dim, p.row_waves), step = p.row_waves == 1 ? 4 : 1;   // four waves, four tiles
     const int64_t items = (int64_t)sh.n_kv_heads * p.row_tiles, room = (int64_t)n_cu * tree_resident(sh.head_dim, f8);
     int64_t sum = 0;
@@ -244,7 +244,10 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
     p.split = p.n_slots > n;
     if (packed) {
         p.p_tiles = ceil_div((int64_t)n * rows, 128);
-        p.p_heavy = ceil_div((int64_t)n_mixed * rows, 128);
+        if (n_of[0] < n) {
+            p.p_heavy0 = (int)((int64_t)n_of[0] * rows / 128);
+            p.p_heavy = n_of[0] + n_of[1] > 0 ? ceil_div((int64_t)(n_of[0] + n_of[1]) * rows, 128) - p.p_heavy0 : 0;
+        }
         const int64_t row_items = (int64_t)sh.n_kv_heads * p.p_tiles;
         const int64_t gen_items = (int64_t)sh.n_kv_heads * p.blocks;
         int64_t best = INT64_MAX;
@@ -288,7 +291,7 @@ inline TreePlan tree_prepare(const splice_shape &sh, const splice_call &call, co
         cls[i] = never ? 0 : (ahead > 0 ? 1 : 2);
         ++n_of[cls[i]];
     }
-    int at[3] = {n_of[1], 0, n_of[1] + n_of[0]}, min_step = cells.step[0];
+    int at[3] = {0, n_of[0], n_of[0] + n_of[1]}, min_step = cells.step[0];
     for (int i = 0; i < n; ++i) {
         const int to = at[cls[i]]++;
         sorted.cell[to] = cells.cell[i];
@@ -306,10 +309,10 @@ inline TreePlan tree_prepare(const splice_shape &sh, const splice_call &call, co
     int tiles[SPLICE_MAX_CELLS];
     const int tile = tree_tile_keys(sh.head_dim, tree_row_waves(sh.head_dim, T * group_of(sh)));
     for (int i = 0; i < n; ++i) {
-        const bool mixed = i < n_of[1];
-        tiles[i] = tree_tiles(sh, call, T, tile, sorted.step[i], mixed || i >= n_of[1] + n_of[0], mixed, !packed, true);
+        const bool spliced = i >= n_of[0], mixed = spliced && i < n_of[0] + n_of[1];
+        tiles[i] = tree_tiles(sh, call, T, tile, sorted.step[i], spliced, mixed, !packed, true);
     }
-    const TreePlan p = tree_plan(sh, call, T, tiles, n, n_of[1], n_cu, f8, packed, prompt_tiles);
+    const TreePlan p = tree_plan(sh, call, T, tiles, n, n_of, n_cu, f8, packed, prompt_tiles);
     tree_slots(sorted, sorted_onset, tiles, n, p, slots);
     return p;
 }

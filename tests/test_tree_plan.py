@@ -16,7 +16,8 @@ SRC = r"""
 using namespace splice;
 extern "C" {
 int limits(int *r) { r[0] = kTreeMaxSlots; r[1] = kTreeMaxChunks; r[2] = kTreeMaxPrompt; return (int)sizeof(TreeSlots); }
-// info [257], order [640], step [256], plan: n, row_waves, row_tiles, per, n_p, p_tiles, n_slots, blocks, most_chunks, split
+// info [257], order [640], step [256], plan: n, row_waves, row_tiles, per, n_p, p_tiles, n_slots, blocks, most_chunks, split,
+// p_heavy0, p_heavy
 int64_t prepare(const splice_shape *sh, const splice_call *call, const splice_tree *tree, const int32_t *lw, const int32_t *steps,
                 int n_cu, uint32_t *info, uint32_t *order, int32_t *step, int64_t *plan, int64_t *most) {
     if (validate_tree(sh, tree, steps) != SPLICE_OK) return -1;
@@ -25,8 +26,8 @@ int64_t prepare(const splice_shape *sh, const splice_call *call, const splice_tr
     const TreePlan p = tree_prepare(*sh, *call, *tree, lw, steps, n_cu, n, step, s);
     for (int i = 0; i <= SPLICE_MAX_CELLS; ++i) info[i] = s.info[i];
     for (int i = 0; i < kTreeMaxSlots; ++i) order[i] = (s.order[i / 2] >> (16 * (i % 2))) & 0xffff;
-    const int64_t v[] = {n, p.row_waves, p.row_tiles, p.per, p.n_p, p.p_tiles, p.n_slots, p.blocks, p.most_chunks, p.split};
-    for (int i = 0; i < 10; ++i) plan[i] = v[i];
+    const int64_t v[] = {n, p.row_waves, p.row_tiles, p.per, p.n_p, p.p_tiles, p.n_slots, p.blocks, p.most_chunks, p.split, p.p_heavy0, p.p_heavy};
+    for (int i = 0; i < 12; ++i) plan[i] = v[i];
     *most = (int64_t)tree_most_bytes(*sh, *call, tree->n_nodes, n_cu);
     return (int64_t)p.bytes;
 }
@@ -71,11 +72,11 @@ def test_plans(plan):
         sh, call, tree, lw, steps = draw(rng)
         C, n_nodes = sh.n_cells, tree.n_nodes
         info, order, step = (ctypes.c_uint32 * 257)(), (ctypes.c_uint32 * slots_max)(), (ctypes.c_int32 * 256)()
-        v, most = (ctypes.c_int64 * 10)(), ctypes.c_int64()
+        v, most = (ctypes.c_int64 * 12)(), ctypes.c_int64()
         flat = (ctypes.c_int32 * (2 * C))(*[x for p in lw for x in p])
         n_bytes = plan.prepare(ctypes.byref(sh), ctypes.byref(call), ctypes.byref(tree), flat, (ctypes.c_int32 * C)(*steps),
                                rng.choice((256, 304, 64)), info, order, step, v, ctypes.byref(most))
-        n, row_waves, row_tiles, per, n_p, p_tiles, n_slots, blocks, most_chunks, is_split = v
+        n, row_waves, row_tiles, per, n_p, p_tiles, n_slots, blocks, most_chunks, is_split, heavy0, heavy = v
         active = [c for c in range(C) if steps[c] >= 0]
         assert n == len(active)
         if n == 0:
@@ -97,6 +98,12 @@ def test_plans(plan):
         items = n_slots - n * n_p
         assert items <= slots_max and n_p <= prompt_max and blocks == row_tiles * items + n_p * p_tiles <= 65535
         assert not n_p or (p_tiles * 128 >= n * rows > (p_tiles - 1) * 128 and rows <= 64)
+        if n_p:   # row tiles with unspliced and spliced nodes are among the heavy ones, which begin first
+            assert 0 <= heavy0 and 0 <= heavy and heavy0 + heavy <= p_tiles
+            for t in range(p_tiles):
+                cells = range(t * 128 // rows, min((t * 128 + 127) // rows + 1, n))
+                if any(onset[i] > 0 for i in cells) and any(onset[i] < 64 for i in cells):
+                    assert heavy0 <= t < heavy0 + heavy
         seen = {(order[i] & 255, order[i] >> 8) for i in range(items)}
         assert seen == {(i, k) for i in range(n) for k in range(first[i + 1] - first[i] - n_p)}
         assert is_split == (n_slots > n)
