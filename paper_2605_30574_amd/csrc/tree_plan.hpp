@@ -105,6 +105,10 @@ constexpr int kTreeMaxSlots = 640;
 // 2k bf16 rows each, 6 rounds 131, 1 round 126).
 constexpr int kTreeRounds = 6;
 constexpr int kTreeStart = 8;
+// What the join of chunks costs, in tiles: a launch and the partial results' way (two sets
+// of 79 shapes, geometric means in us, 0 tiles 23.1 and 24.6, 3 22.1 and 23.7, 6 21.8 and 22.1, 8 21.8 and 22.0,
+// where some lists of 100 tiles are no longer cut and take 19 rather than 15).
+constexpr int kTreeJoin = 6;
 constexpr int kTreeMaxChunks = 64;
 
 struct TreePlan {
@@ -195,7 +199,7 @@ inline bool tree_packed(const splice_shape &sh, const splice_call &call, int T, 
 
 // Chunks of equal length, so that the work groups of all cells fill k rounds
 // of what the GPU holds at once; k is the one that takes least by
-// k * (per + kTreeStart); of a packed call's prompt one more kTreeStart where the
+// k * (per + kTreeStart), and kTreeJoin where lists are cut; of a packed call's prompt one more kTreeStart where the
 // generated rows' items do not fit beside its last round (40 cells of 12 nodes,
 // D = 256, 1024 keys in view: 16 chunks of two tiles 44 us, 8 of four, beside
 // which they fit, 32).  tiles: of the cells' lists, in a packed call without
@@ -223,8 +227,8 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
         if (p.per < least) p.per = least;
         while (!fits(p.per, kTreeMaxSlots)) p.per *= 2;
     } else {
-        p.per = most;
-        int64_t best = INT64_MAX;
+        p.per = step * ceil_div(most, step);   // whole lists
+        int64_t best = packed ? INT64_MAX : ceil_div(n * items, room) * ((int64_t)p.per / step + kTreeStart);
         for (int k = 1; k <= (packed ? 1 : kTreeRounds); ++k) {   // the prompt's items fill the further rounds
             int64_t limit = k * room / items;
             limit = limit < kTreeMaxSlots ? limit : kTreeMaxSlots;
@@ -232,7 +236,8 @@ inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T
             int per = step * ceil_div(sum, limit * step);
             if (per < least) per = least;
             while (per < most && !fits(per, limit)) per += step * (1 + per / (16 * step));
-            const int64_t cost = k * ((int64_t)per / step + kTreeStart);
+            const bool cut = !packed && tree_chunks(tiles, n, per) > n;   // (packed results are joined anyhow)
+            const int64_t cost = k * ((int64_t)per / step + kTreeStart) + (cut ? kTreeJoin : 0);
             if (cost < best) {
                 best = cost;
                 p.per = per;
