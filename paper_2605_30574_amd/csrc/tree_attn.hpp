@@ -289,7 +289,8 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
         word = a.visible[node0 + node];
         d_node = min(d_node, a.T - 1);
         alive = __ballot(d_node >= 0);
-        const uint64_t mine = bits(row0 >> a.lgG, (min(row0 + 32 * RW - 1, rows - 1) >> a.lgG) + 1) & alive;   // the work group's nodes
+        // the work group's nodes
+        const uint64_t mine = bits(row0 >> a.lgG, (min(row0 + 32 * RW - 1, rows - 1) >> a.lgG) + 1) & alive;
         if (mine == 0) return;
         depth = __shfl(d_node, node);
         const int p0 = a.Tp + step;
@@ -382,8 +383,8 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     // ---- tiles into LDS.  A tile for all waves: bf16 rows go there straight
     // from memory (lds_dma16: a lane names 16 bytes for chunk slot 64 q + lane)
     // into the other of two buffers, 8-bit ones by way of registers, where they
-    // become bf16.  Tiles of a wave's own: the next one waits in registers, so
-    // that one buffer a wave is enough, two work groups fit a compute unit and
+    // become bf16.  Tiles of a wave's own: the next one or two wait in registers,
+    // so that one buffer a wave is enough, two work groups fit a compute unit and
     // no wave waits for another.
     int ltid = X::OWN ? lane : tid;
     char *const own = lds + (X::OWN ? wave * 2 * X::TILE : 0);
@@ -459,7 +460,8 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     auto store8 = [&](char *buf, auto set) {
         constexpr int LPR = D / 16, STEP = X::NT / LPR;
         const int key = ltid / LPR, ch = 2 * (ltid % LPR);
-        const int at_k = key * X::ROW + ((tree_pair(ch) ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((tree_pair(ch) ^ tree_swz_v<D>(key)) << 4);
+        const int at_k = key * X::ROW + ((tree_pair(ch) ^ tree_swz_k<D>(key)) << 4);
+        const int at_v = key * X::ROW + ((tree_pair(ch) ^ tree_swz_v<D>(key)) << 4);
         static_for<0, X::NL8>([&](auto i) {
             constexpr int from = decltype(set)::value * X::NL8 + i;
             const u32x4_t k = kr[from], v = vr[from];
@@ -483,7 +485,8 @@ __device__ __forceinline__ void tree_item(const TreeArgs &args, int rest) {
     auto store16 = [&](char *buf) {
         constexpr int STEP = X::NT / X::CPR;
         const int key = ltid / X::CPR, ch = ltid % X::CPR;
-        const int at_k = key * X::ROW + ((tree_pair(ch) ^ tree_swz_k<D>(key)) << 4), at_v = key * X::ROW + ((tree_pair(ch) ^ tree_swz_v<D>(key)) << 4);
+        const int at_k = key * X::ROW + ((tree_pair(ch) ^ tree_swz_k<D>(key)) << 4);
+        const int at_v = key * X::ROW + ((tree_pair(ch) ^ tree_swz_v<D>(key)) << 4);
         static_for<0, X::NL>([&](auto i) {
             constexpr int ck = tree_swz_k<D>(i * STEP) << 4, cv = tree_swz_v<D>(i * STEP) << 4;
             char *const to = buf + i * STEP * X::ROW;
@@ -959,7 +962,8 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs args) {
 
 template <int D, int RW, bool F8, bool PACKED>
 bool launch_tree_kernel(const TreeArgs &args, int blocks, hipStream_t stream) {
-    constexpr int LDS = PACKED && TreeTile<D, 4, false>::LDS > TreeTile<D, RW, F8>::LDS ? TreeTile<D, 4, false>::LDS : TreeTile<D, RW, F8>::LDS;
+    constexpr int OWN_LDS = TreeTile<D, RW, F8>::LDS, PROMPT_LDS = PACKED ? TreeTile<D, 4, false>::LDS : 0;
+    constexpr int LDS = PROMPT_LDS > OWN_LDS ? PROMPT_LDS : OWN_LDS;
     void (*kernel)(TreeArgs);
     if constexpr (PACKED) kernel = tree_packed_kernel<D, RW, F8>;
     else kernel = tree_kernel<D, RW, F8>;

@@ -204,8 +204,9 @@ inline bool tree_packed(const splice_shape &sh, const splice_call &call, int T, 
 // D = 256, 1024 keys in view: 16 chunks of two tiles 44 us, 8 of four, beside
 // which they fit, 32).  tiles: of the cells' lists, in a packed call without
 // the prompt, whose list is prompt_tiles long.
-inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, const int *n_of, int n_cu, bool f8,
-                          bool packed, int prompt_tiles) {
+// n_of: cells of each class.
+inline TreePlan tree_plan(const splice_shape &sh, const splice_call &call, int T, const int *tiles, int n, const int *n_of,
+                          int n_cu, bool f8, bool packed, int prompt_tiles) {
     TreePlan p;
     const int rows = T * group_of(sh);
     p.row_waves = tree_row_waves(sh.head_dim, rows);

@@ -127,3 +127,21 @@ def test_replayed_graph_and_same_bits():
         for a, b in zip(o, eager):
             assert torch.equal(a, b)
         check(x, t, 5, got=sp.TokenScores(*o))
+
+
+@pytest.mark.parametrize("k", [1, 7, 20, 64])
+@pytest.mark.parametrize("kind", ["rising", "falling", "constant", "steps", "late"])
+@pytest.mark.parametrize("rows", [1, 3, 1100])
+def test_candidates_in_any_order(rows, kind, k):
+    """Rows whose candidates fill a wave's list again and again, or come all at the end; as one part and as several."""
+    vocab = 33000 if rows < 100 else 9000
+    i = torch.arange(vocab, dtype=torch.float32)
+    x = {"rising": i / vocab, "falling": -i / vocab, "constant": i * 0, "steps": torch.floor(i / 97),
+         "late": torch.where(i < vocab - 300, i * 0 - 5, torch.sin(i))}[kind]
+    x = x.repeat(rows, 1).cuda()
+    t = torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(k)).cuda()
+    got = sp.token_scores(x, t, k)
+    check(x[:1], t[:1], k, got=sp.TokenScores(*(f[:1] for f in got)))
+    torch.cuda.synchronize()
+    for f in (got.lse, got.entropy, got.top, got.top_logp):   # the same row: the same bits
+        assert torch.equal(f, f[:1].expand_as(f))
