@@ -199,6 +199,11 @@ __device__ __forceinline__ void rank_first(Candidates &c, int n, int k) {
 // Where weights are 0 their z, which may be -inf, stops here: 0 times a finite number.
 constexpr float kLeastZ = -1e4f;
 
+// z = x scale2 - m scale2 in one operation where m scale2 is below this: its rounding, 2^-17 at most, is
+// then all that a weight is off by.  Beyond, where the rounding grows with m (logits of
+// 1e8 would have weights of 0 or infinity) and the product may be no float, x - m comes first.
+constexpr float kMostRef = 256.f;
+
 // Joins (m, s, t) of two parts of a row.
 __device__ __forceinline__ void join(float scale2, float &m, float &s, float &t, float m2, float s2, float t2) {
     const float mm = fmaxf(m, m2), ref = mm == -INFINITY ? 0.f : mm;
@@ -364,11 +369,11 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreArgs a) {
             if (j < c1) {
                 static_for<0, VE>([&](auto i) { top[u] = fmaxf(top[u], x[u][i]); });
                 raise(top[u]);
-                if (__any(m < -1e30f)) {   // m * scale2 may be no float
-                    const float ref = m == -INFINITY ? 0.f : m;
-                    static_for<0, VE>([&](auto i) { add((x[u][i] - ref) * a.scale2); });
+                const float ref = -m * a.scale2;
+                if (__any(!(fabsf(ref) < kMostRef))) {
+                    const float from = m == -INFINITY ? 0.f : m;
+                    static_for<0, VE>([&](auto i) { add((x[u][i] - from) * a.scale2); });
                 } else {
-                    const float ref = -m * a.scale2;
                     static_for<0, VE>([&](auto i) { add(fmaf(x[u][i], a.scale2, ref)); });
                 }
                 if (xt_nan) {

@@ -145,3 +145,71 @@ def test_candidates_in_any_order(rows, kind, k):
     torch.cuda.synchronize()
     for f in (got.lse, got.entropy, got.top, got.top_logp):   # the same row: the same bits
         assert torch.equal(f, f[:1].expand_as(f))
+
+
+def exact_in_distances(logits, tokens, k, scale=1.0):
+    """Like check, with tolerances that do not grow with the logits: log s is off by the sums' 2^-24 vocab / 256, 64 for v_exp_f32,
+    v_log_f32 and the joins, 96 for a reference of up to 256 rounded once (2^-17 ln 2 = 89 * 2^-24), and three roundings of each
+    distance, which the weights sum to less than ln vocab; a distance (x - m) scale by four roundings, lse by two."""
+    got = sp.token_scores(logits, tokens, k, scale)
+    torch.cuda.synchronize()
+    raw = f64(logits)
+    most, t = raw.max(-1), tokens.cpu().numpy()
+    # (in float64 too a log-sum of some 1e20 would lose the logarithm that log probabilities are made of, and distances from it the
+    # order of what is near 0)
+    logp, lse, entropy, _, _, top_logp = ref.scores((raw - most[:, None]) * scale, t, k)
+    _, _, _, rank, top, _ = ref.scores(raw, t, k)
+    lse = most * scale + lse
+    vocab = raw.shape[1]
+    tol = 2.0 ** -24 * (vocab / 256 + 64 + 96 + 3 * np.log(vocab))
+
+    def near(name, want, bound):
+        a = f64(getattr(got, name))
+        assert np.isfinite(a).all(), (name, a)
+        assert (np.abs(a - want) <= bound).all(), (name, a, want)
+    near("lse", lse, tol + 2.0 ** -23 * np.abs(lse))
+    near("logp", logp, tol + 2.0 ** -22 * np.abs(logp))
+    near("entropy", entropy, 2 * tol * (1 + np.log(vocab) + entropy))
+    assert np.array_equal(got.rank.cpu().numpy(), rank) and np.array_equal(got.top.cpu().numpy(), top)
+    near("top_logp", top_logp, tol + 2.0 ** -22 * np.abs(top_logp))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,pad", [(1001, 0), (1001, 3), (20003, 5)])
+def test_logits_near_the_largest_float(vocab, pad, dtype):
+    """A forced token: the largest number of the type at a row's first and last values, within it, twice, and beside the lowest."""
+    announce(f"largest logits {vocab} {pad} {dtype}")
+    big = torch.finfo(dtype).max
+    x, t = draw(vocab + pad, 12, vocab, dtype, pad=pad)
+    at = [0, 1, 2, 7, vocab // 2, vocab // 2 + 5, vocab - 1, vocab - 2, vocab - 6]
+    for r, i in enumerate(at):
+        x[r, i] = big
+        t[r] = i if r % 2 == 0 else (i + 9) % vocab
+    x[9, 5], x[9, vocab - 5] = big, big
+    t[9] = 5
+    x[10] = -big
+    x[10, 11] = big
+    t[10] = 11
+    x[11] = big
+    exact_in_distances(x, t, 1)   # (the others' log probabilities are beyond float's range where the lowest float is among them)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("size", [300.0, -300.0, 3.0e6, 1.0e10, -1.0e10, 1.0e20, 1.0e38, -1.0e38])
+def test_logits_far_from_zero(size, dtype):
+    """What a row's values have in common does not reach its probabilities."""
+    announce(f"logits about {size} {dtype}")
+    for vocab in (1001, 20003):
+        x, t = draw(int(abs(size)) % 9973, 4, vocab, torch.float32)
+        x = (x + size).to(dtype)
+        x[1] = size
+        exact_in_distances(x, t, 3)
+
+
+def test_scale_that_takes_the_largest_logit_near_the_largest_float():
+    """scale * logit is a float, and not so with the factor log2(e)."""
+    x = torch.full((3, 2000), -2.0e30, device="cuda")
+    x[0, 7] = x[0, 1500] = 1.0e30
+    x[1, ::3] = 1.0e30
+    x[2] = 1.0e30
+    exact_in_distances(x, torch.tensor([7, 3, 5], device="cuda"), 2, float(np.float32(3.0e8)))
