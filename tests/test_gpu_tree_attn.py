@@ -359,3 +359,19 @@ def test_two_calls_at_once():
     for (out, lse), h in zip(alone, held):
         for (o, l), _ in h:
             assert torch.equal(o, out) and torch.equal(l, lse)
+
+
+@pytest.mark.parametrize("split", [0, 64, 256])
+@pytest.mark.parametrize("span", [(0, 1400), (3, 1390)])
+@pytest.mark.parametrize("unspliced", [0, 1, 20, 39])
+def test_zero_donor_whose_span_is_the_prompt(unspliced, span, split):
+    """Cells that walk the whole prompt beside cells that walk nothing of it, or next to nothing."""
+    C, T = 40, 5
+    rng = np.random.default_rng(unspliced)
+    steps = rng.integers(0, 60, C)
+    steps[7] = -1
+    LW = [[9, 0] if c < unspliced else [0, 0] for c in range(C)]
+    if unspliced == 20:
+        LW[19] = [0, max(int(steps[19]), 0) + 2]   # one on both sides of its onset
+    s = Sweep(271, C=C, T=T, Tp=1400, span=span, cap=70, steps=steps, LW=LW, donor="zero", Hq=4, Hkv=1, D=128)
+    run(s, split, f"ZERO donor, {unspliced} unspliced, span {span}, split {split}")

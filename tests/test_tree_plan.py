@@ -117,3 +117,79 @@ def test_python_asks_the_library_for_the_bytes():
     assert sp.splice_tree_attn_workspace_bytes(sh, call, sp.make_tree(4)) > 0
     with pytest.raises(sp.SpliceError):
         sp.splice_tree_attn_workspace_bytes(sh, call, T.SpliceTree(4, 9))
+
+
+def plan_of(plan, sh, call, tree, lw, steps, n_cu=256):
+    """The plan's values by name, and the workspace's bytes."""
+    info, order, step = (ctypes.c_uint32 * 257)(), (ctypes.c_uint32 * 640)(), (ctypes.c_int32 * 256)()
+    v, most = (ctypes.c_int64 * 12)(), ctypes.c_int64()
+    flat = (ctypes.c_int32 * (2 * len(steps)))(*[x for p in lw for x in p])
+    n_bytes = plan.prepare(ctypes.byref(sh), ctypes.byref(call), ctypes.byref(tree), flat, (ctypes.c_int32 * len(steps))(*steps), n_cu,
+                           info, order, step, v, ctypes.byref(most))
+    assert 0 <= n_bytes <= most.value
+    names = ("n", "row_waves", "row_tiles", "per", "n_p", "p_tiles", "n_slots", "blocks", "most_chunks", "split", "heavy0", "heavy")
+    return dict(zip(names, v), bytes=n_bytes)
+
+
+NEVER, ALWAYS = (9, 0), (0, 0)
+
+
+@pytest.mark.parametrize("split", [0, 256, 1024])
+@pytest.mark.parametrize("C,T,heads,Tp,span,unspliced", [
+    (48, 16, (32, 8, 128), 8192, (128, 8128), 24), (48, 16, (32, 8, 128), 8192, (0, 8192), 24), (48, 16, (32, 8, 128), 8192, (0, 8192), 1),
+    (8, 4, (8, 2, 128), 32768, (0, 32768), 7), (8, 4, (8, 2, 128), 32768, (128, 32640), 7), (40, 12, (8, 4, 256), 4096, (0, 4096), 39)])
+def test_shared_prompt_of_the_zero_donor(plan, C, T, heads, Tp, span, unspliced, split):
+    """Spliced cells, which walk nothing of the span, do not take its chunks from the cells that walk all of it."""
+    def of(donor_zero, lw):
+        sh = sp.make_shape(C, 8, *heads, Tp, span, 1024, donor_zero, "bf16")
+        return plan_of(plan, sh, sp.make_call(3, 0, 0, 0.1, split), sp.make_tree(T), lw, [7 * c for c in range(C)])
+    alone = of(True, [NEVER] * C)
+    some = of(True, [NEVER if c < unspliced else ALWAYS for c in range(C)])
+    assert alone["n_p"] > 0 and some["n_p"] == alone["n_p"] and some["n_slots"] == alone["n_slots"]
+    # nodes on both sides of the onset: no fewer chunks than for the unspliced ones
+    inside = of(True, [(0, 7 * c + 1) if c < unspliced else ALWAYS for c in range(C)])
+    assert inside["n_p"] >= alone["n_p"]
+    # cells that are all spliced share what is left of the prompt, if anything
+    none = of(True, [ALWAYS] * C)
+    if span == (0, Tp):
+        bare = plan_of(plan, sp.make_shape(C, 8, *heads, 0, (0, 0), 1024, True, "bf16"), sp.make_call(3, 0, 0, 0.1, split),
+                       sp.make_tree(T), [ALWAYS] * C, [7 * c for c in range(C)])
+        assert none == bare and none["n_p"] == 0
+    else:
+        assert none["n_p"] > 0 if split else none["n_p"] <= alone["n_p"]
+    assert of(False, [NEVER] * C)["n_p"] == alone["n_p"]
+
+
+def test_zero_donor_shares_the_prompt_like_unspliced_cells(plan):
+    rng = random.Random(11)
+    packed = 0
+    for trial in range(2000):
+        sh, call, tree, _, steps = draw(rng)
+        sh.donor_kind = sp.SPLICE_DONOR_ZERO
+        if rng.random() < 0.3:
+            sh.span_lo, sh.span_hi = 0, sh.prompt_len
+        active = [c for c in range(sh.n_cells) if steps[c] >= 0]
+        # a spliced list, whose parts before and behind the span end in tiles of their own, is the shorter one from a span of a
+        # tile on: ceil(x) + ceil(y) <= ceil(x + y) + 1
+        low = sh.prompt_len + min((steps[c] for c in active), default=0) - call.window + 1 if call.window else 0
+        if not active or sh.span_hi - max(sh.span_lo, low) < 64:
+            continue
+        lw = [rng.choice((NEVER, ALWAYS)) for _ in steps]
+        lw[rng.choice(active)] = NEVER
+        alone = plan_of(plan, sh, call, tree, [NEVER] * len(steps), steps)
+        some = plan_of(plan, sh, call, tree, lw, steps)
+        assert some["n_p"] == alone["n_p"], trial
+        packed += alone["n_p"] > 0
+    assert packed > 100
+
+
+def test_shared_prompts_have_chunks(plan):
+    """A call that leaves the prompt to shared items has some: else each cell's prompt would hang behind its last chunk."""
+    rng = random.Random(13)
+    for trial in range(2000):
+        sh, call, tree, lw, steps = draw(rng)
+        if rng.random() < 0.5:
+            sh.donor_kind, sh.span_lo, sh.span_hi = sp.SPLICE_DONOR_ZERO, 0, sh.prompt_len
+        p = plan_of(plan, sh, call, tree, lw, steps)
+        if p["n"]:
+            assert bool(p["split"]) == (p["n_slots"] > p["n"]), trial
