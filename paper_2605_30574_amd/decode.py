@@ -333,9 +333,9 @@ class SweepDecoder:
 
     @torch.no_grad()
     def tree_logits(self, tokens: torch.Tensor, tree: DecoderTree, steps: np.ndarray) -> torch.Tensor:
-        """Logits [C * T][V] of one pass over the trees' nodes: node t of cell c is the token tokens[c][t] (int64) at
-        decode step steps[c] + its depth, behind the steps[c] rows of the cell's generated caches and its ancestors.
-        Its K/V become row steps[c] + t, so steps[c] + T must not pass the caches' rows; cells with a
+        """Logits [C * T][V] of one pass over the trees' nodes (bfloat16 where the head's product is, else float32): node t
+        of cell c is the token tokens[c][t] (int64) at decode step steps[c] + its depth, behind the steps[c] rows of the
+        cell's generated caches and its ancestors.  Its K/V become row steps[c] + t, so steps[c] + T must not pass the caches' rows; cells with a
         negative step are skipped.  Rows of padding and of skipped cells hold no meaning (their tokens are any of the
         vocabulary).  No gradients."""
         w, m, wt = self.w, self.m, self.wt
@@ -372,7 +372,8 @@ class SweepDecoder:
                 x = x + (attend(l, h @ p["w_q"], h @ p["w_k"], h @ p["w_v"]).to(cdt) @ p["w_o"]).float()
                 h = rms_norm(x, p["norm_2"], m.rms_eps).to(cdt)
                 x = x + ((torch.nn.functional.silu((h @ p["w_gate"]).float()).to(cdt) * (h @ p["w_up"])) @ p["w_down"]).float()
-            return rms_norm(x, wt["norm_f"], m.rms_eps).to(cdt) @ wt["lm_head"]
+            logits = rms_norm(x, wt["norm_f"], m.rms_eps).to(cdt) @ wt["lm_head"]
+            return logits if logits.dtype in (bf16, torch.float32) else logits.float()   # (what splice_token_scores takes)
 
         lib, ok, stream, d = _library(), S._check, S._stream_ptr(None, dev), x.shape[1]
         res, h = torch.empty((rows, d), dtype=torch.float32, device=dev), torch.empty((rows, d), dtype=bf16, device=dev)
