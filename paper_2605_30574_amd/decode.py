@@ -118,6 +118,12 @@ def rope(x: torch.Tensor, pos: torch.Tensor, theta: float) -> torch.Tensor:
     inv = theta ** (-torch.arange(0, half, device=x.device, dtype=torch.float64) * 2.0 / D)
     ang = (pos.to(torch.float64)[:, None] * inv[None, :]).to(torch.float32)   # [C][D/2]
     cos, sin = torch.cos(ang)[:, None, :], torch.sin(ang)[:, None, :]
+    return _rotated(x, cos, sin)
+
+
+def _rotated(x: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor) -> torch.Tensor:
+    """x [..][D]: pairs (i, i + D/2) turned by the angles of cos, sin [..][D/2]."""
+    half = x.shape[-1] // 2
     x1, x2 = x[..., :half], x[..., half:]
     return torch.cat([x1 * cos - x2 * sin, x2 * cos + x1 * sin], dim=-1)
 
@@ -331,6 +337,21 @@ class SweepDecoder:
                            torch.from_numpy(T.rope_frequencies(self.w.head_dim, float(self.m.rope_theta))[0]).to(self.device),
                            parents.astype(np.int64))
 
+    def _turns(self, tree: DecoderTree, steps: np.ndarray, pos: Optional[torch.Tensor]):
+        """(cos, sin) float32 [C][T][1][D / 2] of the nodes' positions: pos [C][T], or T_p + step + depth, whose T_p + step
+        is the cells' (from the steps by value, so that a pass can be captured), the depth's angle added to it."""
+        C, D, (_, dev) = self.C, self.w.head_dim, T._anchor(tree.depth, "tree.depth")
+        ang = (tree.depth if pos is None else pos).to(torch.float64)[:, :, None, None] * tree.freq
+        cos, sin = torch.cos(ang).float(), torch.sin(ang).float()
+        if pos is not None or C == 0:
+            return cos, sin
+        tab = torch.empty((C, 1, 1, D // 2, 2), dtype=torch.float32, device=dev)
+        S._check(_library().splice_decoder_rope_table(tab.data_ptr(), None, S._steps(steps, C)[1], C, D, self.w.prompt_len,
+                                                      float(self.m.rope_theta), S._stream_ptr(None, dev)),
+                 "splice_decoder_rope_table")
+        c, s = tab[..., 0], tab[..., 1]
+        return c * cos - s * sin, s * cos + c * sin
+
     @torch.no_grad()
     def tree_logits(self, tokens: torch.Tensor, tree: DecoderTree, steps: np.ndarray) -> torch.Tensor:
         """Logits [C * T][V] of one pass over the trees' nodes (bfloat16 where the head's product is, else float32): node t
@@ -348,18 +369,25 @@ class SweepDecoder:
             pos = (self.positions(st).to(torch.int64)[:, None] + tree.depth).contiguous()
         x = wt["embed"][tokens.reshape(-1)]
         cdt, dev, rows = x.dtype, x.device, C * n
-        rope_of, bf16 = T.make_rope("half", D), torch.bfloat16
+        rope_of, unturned, bf16 = T.make_rope("half", D), T.make_rope("half", 0), torch.bfloat16
         out = torch.zeros((C, n, Hq, D), dtype=bf16, device=dev)
         lse = torch.empty((C, n, Hq), dtype=torch.float32, device=dev)
         exps = ("gen_k_exp", "gen_v_exp") if tree.spec.kv_format == T.SPLICE_KV_E4M3 else ()
         fused = self._fused(x, None, rows) and x.shape[1] <= 8192   # SPLICE_ADD_NORM_MAX_D
 
+        turns = None   # (cos, sin) of the nodes' positions, where products of other types need them
+
         def attend(l, q, k, v):
+            nonlocal turns
             c = self.caches[l]
             e = [c[name] for name in exps] or [None, None]
-            q, k, v = q.to(bf16).view(C, n, Hq, D), k.to(bf16).view(C, n, Hkv, D), v.to(bf16).view(C, n, Hkv, D)
-            T.splice_tree_append(self.shape, tree.spec, rope_of, tree.freq, st, tree.depth, q, k, v, q, c["gen_k"], c["gen_v"], *e,
-                                 pos=pos)
+            q, k, v = q.view(C, n, Hq, D), k.view(C, n, Hkv, D), v.to(bf16).view(C, n, Hkv, D)
+            rotary, freq = rope_of, tree.freq
+            if q.dtype != bf16 or k.dtype != bf16:   # of more bits: rotated before they are rounded, as in forward
+                turns = turns or self._turns(tree, st, pos)
+                q, k = (_rotated(y.float(), *turns).to(bf16) for y in (q, k))
+                rotary, freq = unturned, None
+            T.splice_tree_append(self.shape, tree.spec, rotary, freq, st, tree.depth, q, k, v, q, c["gen_k"], c["gen_v"], *e, pos=pos)
             T.splice_tree_attn(self.shape, self.calls[l], tree.spec, self.lw, st, tree.depth, tree.visible, q, c["clean_k"],
                                c["clean_v"], c["donor_k"], c["donor_v"], c["gen_k"], c["gen_v"], *e, out, lse, tree.workspace)
             return out.view(rows, Hq * D)

@@ -5,6 +5,8 @@ import torch
 
 import decode_bar
 import gpu_common as gc
+import paper_2605_30574_amd as sp
+import tree_reference
 import workloads
 from paper_2605_30574_amd import decode
 from test_gpu_tree_pass import TREE_REL, chain
@@ -46,3 +48,58 @@ def test_weights_of_other_types_are_scored(dtype, cast):
     for t in range(T):   # each side is off by its own bar from the float64 decoder
         err = (logits.view(C, T, -1)[:, t].double() - want[t].double()).abs().max()
         assert err <= 2 * TREE_REL * max(1.0, float(want[t].abs().max())), t
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("own_positions", [False, True])
+def test_keys_of_the_first_layer_are_rounded_once(dtype, own_positions):
+    """Where the products have more bits than bfloat16, keys are rotated before they are rounded, as a decode step's are."""
+    w = decode_bar.case("blank-sink")
+    lw, _, gpu, _, caches = setup(w, dtype)
+    C, T, D, Hkv = lw.shape[0], 6, w.head_dim, w.n_kv_heads
+    ahead = 1000 if own_positions else 0
+    if own_positions:
+        plain = gpu.positions
+        gpu.positions = lambda steps: plain(steps) + ahead
+    rng = np.random.default_rng(8)
+    parents = np.array([[-1] + [int(rng.integers(0, t)) for t in range(1, T)] for _ in range(C)])
+    tokens = torch.from_numpy(rng.integers(0, MODEL.vocab, (C, T))).cuda()
+    steps = rng.integers(0, w.n_steps - T + 1, C).astype(np.int32)
+    gc.announce(f"keys of layer 0, {dtype}, own positions {own_positions}")
+    gpu.tree_logits(tokens, gpu.make_tree(parents), steps)
+    p = gpu.wt["layers"][0]
+    h = decode.rms_norm(gpu.wt["embed"][tokens.reshape(-1)].float(), p["norm_1"], MODEL.rms_eps).to(dtype)
+    k = (h @ p["w_k"]).double().cpu().numpy().reshape(C, T, Hkv, D)   # the product whose rotation the rows hold
+    depth, _ = sp.tree_layout(parents)
+    pos = np.broadcast_to((w.prompt_len + ahead + steps[:, None] + depth)[..., None], k.shape[:3])
+    want = tree_reference.rotated(k, pos, MODEL.rope_theta ** (-np.arange(0, D, 2) / D), "half", D, 1.0)
+    # half a step of the result; of the pair's values, the angle's half step in float32 and the rotation's roundings
+    pair = np.abs(k) + np.abs(np.roll(k, D // 2, -1))
+    tol = 2.0 ** -8 * np.abs(want) + (pos[..., None] * 2.0 ** -24 + 2.0 ** -20) * pair
+    got = caches[0]["gen_k"].double().cpu().numpy()
+    for c in range(C):
+        off = np.abs(got[c, :, steps[c]:steps[c] + T].transpose(1, 0, 2) - want[c]) - tol[c]
+        assert (off <= 0).all(), f"cell {c}: off by {off.max():.3e} more than it may be"
+
+
+def test_captured_pass_with_float32_weights():
+    """A captured pass of the written-out form, replayed on other tokens between eager ones: the eager bits."""
+    w = decode_bar.case("blank-sink")
+    lw, _, gpu, _, caches = setup(w)
+    C, T = lw.shape[0], 5
+    tree, steps = gpu.make_tree(chain(C, T)), np.arange(C).astype(np.int32)
+    tokens = torch.zeros((C, T), dtype=torch.int64, device="cuda")
+    gpu.tree_logits(tokens, tree, steps)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        logits = gpu.tree_logits(tokens, tree, steps)
+    for n in range(3):
+        gc.announce(f"captured float32 tree pass, replay {n}")
+        tokens.copy_(torch.randint(0, MODEL.vocab, (C, T), generator=torch.Generator().manual_seed(n)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got, rows = logits.clone(), [c["gen_k"].clone() for c in caches]
+        assert torch.equal(got, gpu.tree_logits(tokens, tree, steps))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c["gen_k"]) for a, c in zip(rows, caches))
