@@ -1,4 +1,4 @@
-"""SweepDecoder's tree passes with weights of every type that the plain decode loop takes."""
+"""SweepDecoder's tree passes: what a branch sees, and weights of every type that the plain decode loop takes."""
 import numpy as np
 import pytest
 import torch
@@ -8,6 +8,7 @@ import gpu_common as gc
 import paper_2605_30574_amd as sp
 import tree_reference
 import workloads
+from oracle import decoder as ref
 from paper_2605_30574_amd import decode
 from test_gpu_tree_pass import TREE_REL, chain
 from workloads.model import make_weights
@@ -15,6 +16,11 @@ from workloads.model import make_weights
 pytestmark = pytest.mark.gpu
 
 MODEL = decode_bar.MODEL
+
+
+def short_prompt():
+    """A prompt of 8 slots, beside which a few nodes weigh much."""
+    return decode_bar.case("blank-sink").with_(prompt_len=8, span=(2, 6))
 
 
 def setup(w, dtype=torch.float32):
@@ -26,6 +32,61 @@ def setup(w, dtype=torch.float32):
     caches = [gc.gpu_layer(w, l, n_cells=lw.shape[0]) for l in range(w.n_layers)]
     prompts = [{k: v for k, v in gc.host(c).items() if k in ("clean_k", "clean_v", "donor_k", "donor_v")} for c in caches]
     return lw, wt, decode.SweepDecoder(w, MODEL, gpu_wt, caches, lw), prompts, caches
+
+
+def test_branches_see_their_own_path():
+    """The logits of every node are the float64 decoder's behind the node's path; behind a path with another parent that
+    decoder's own are further off than four times the bar, so that a wrong branch fails here."""
+    w = short_prompt()
+    lw, wt, gpu, prompts, _ = setup(w)
+    C, T = lw.shape[0], 7
+    parents = np.tile([-1, 0, 0, 1, 2, -1, 5], (C, 1))
+    depth, words = sp.tree_layout(parents)
+    rng = np.random.default_rng(5)
+    tokens, before = rng.integers(0, MODEL.vocab, (C, T)), rng.integers(0, MODEL.vocab, (C, 2))
+    weights = decode_bar.f64_weights(wt)
+
+    def along(path):
+        cpu, steps = ref.ReferenceDecoder(w, MODEL, weights, prompts, lw), np.zeros(C, np.int32)
+        for t in (*before.T, *tokens[:, path].T):
+            logits = cpu.forward(t, steps)
+            steps = steps + 1
+        return logits
+
+    gpu.tree_logits(torch.from_numpy(before).cuda(), gpu.make_tree(chain(C, 2)), np.zeros(C, np.int32))
+    gc.announce("branches of a tree")
+    steps = np.full(C, 2, np.int32)
+    got = gpu.tree_logits(torch.from_numpy(tokens).cuda(), gpu.make_tree(parents), steps).double().cpu().numpy().reshape(C, T, -1)
+    for t in range(T):
+        path = [u for u in range(T) if (int(words[0, t]) >> u) & 1]
+        want = along(path)
+        size = max(1.0, np.abs(want).max())
+        assert np.abs(got[:, t] - want).max() <= TREE_REL * size, f"node {t}"
+        for i in range(len(path) - 1):
+            for other in set(range(T)) - set(path):
+                wrong = path[:i] + [other] + path[i + 1:]
+                assert np.abs(along(wrong) - want).max() > 4 * TREE_REL * size, (t, wrong)
+
+
+def test_ranks_and_alternatives_of_every_node():
+    """score_tree's fields are those of tree_logits' rows, in float64."""
+    w = short_prompt()
+    lw, _, gpu, _, _ = setup(w)
+    C, T, k = lw.shape[0], 7, 4
+    parents = np.tile([-1, 0, 0, 1, 2, -1, 5], (C, 1))
+    parents[1, 5:] = -2
+    rng = np.random.default_rng(6)
+    tokens, targets = (torch.from_numpy(rng.integers(0, MODEL.vocab, (C, T))).cuda() for _ in range(2))
+    steps = np.arange(C).astype(np.int32)
+    tree = gpu.make_tree(parents)
+    got = gpu.score_tree(tokens, tree, steps, targets, top=k)
+    x = gpu.tree_logits(tokens, tree, steps).double().cpu().numpy()
+    logp, lse, entropy, rank, top, top_logp = tree_reference.scores(x, targets.reshape(-1).cpu().numpy(), k)
+    on = (parents >= -1).reshape(-1)
+    assert np.array_equal(got.rank.reshape(-1).cpu().numpy()[on], rank[on])
+    assert np.array_equal(got.top.reshape(-1, k).cpu().numpy()[on], top[on])
+    for name, want in (("logp", logp), ("lse", lse), ("entropy", entropy), ("top_logp", top_logp)):
+        assert np.abs(getattr(got, name).double().cpu().numpy().reshape(want.shape) - want)[on].max() < 1e-4, name
 
 
 @pytest.mark.parametrize("dtype,cast", [(torch.float16, False), (torch.float64, False), (torch.bfloat16, True), (torch.float32, True)])
