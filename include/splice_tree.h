@@ -141,8 +141,11 @@ SPLICE_API int32_t splice_tree_keep(const splice_shape *shape, const splice_tree
  *             probabilities; 0 <= k <= min(vocab, SPLICE_MAX_TOP), both may be
  *             NULL when k is 0.
  * Logits of -inf have probability 0 (a row of nothing else: lse -inf,
- * entropy and logp NaN).  NaN logits make the row's lse, entropy and log
- * probabilities NaN and come first in its order; ranks count them as above every number.
+ * entropy and logp NaN).  Logits of NaN or +inf make the row's lse, entropy and log
+ * probabilities NaN (with +inf the softmax is inf / inf); NaN ones come first in its
+ * order, and ranks count them as above every number.  Finite logits may be
+ * as large as a float: what a row's have in common does not reach its
+ * probabilities.  What passes a float (lse, logp, a distance between two logits) is infinite.
  * Sums are fp32; rows < 2^24, vocab <= 2^28.  logp, lse, entropy fp32 [rows]; rank, tokens, top int64.
  * workspace: 16-byte aligned, splice_token_scores_workspace_bytes bytes, no
  * initialisation.
