@@ -111,8 +111,10 @@ def rope_frequencies(rotary_dim: int, theta: float, scaling: Optional[str] = Non
       "banded"   f / factor where the wavelength 2 pi / f is over original_len / low_freq_factor, f where it is under
                  original_len / high_freq_factor, and in between (1 - s) f / factor + s f with s linear in
                  original_len / wavelength;
-      "yarn"     f / factor for pairs of under beta_slow turns in original_len, f for over beta_fast, a linear ramp over
-                 the pair index between, and mscale = 0.1 ln(factor) + 1 (YaRN, arXiv 2309.00071, equations 17 to 22)."""
+      "yarn"     f / factor for pairs of under beta_slow turns in original_len, f for over beta_fast, and between, with
+                 i(n) = R ln(original_len / (2 pi n)) / (2 ln theta) the index whose pair makes n turns, a ramp that is linear
+                 in the index from floor i(beta_fast) to ceil i(beta_slow), both within 0..R - 1, as models are trained
+                 with it (YaRN, arXiv 2309.00071, has it linear in the turns); mscale = 0.1 ln(factor) + 1, its equation 22."""
     if rotary_dim < 0 or rotary_dim % 2:
         raise ValueError("rotary_dim is an even number")
     if not factor >= 1.0 or not theta > 1.0:
