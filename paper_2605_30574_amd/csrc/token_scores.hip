@@ -12,8 +12,8 @@
 // chunk.  The bound comes from all four waves (each tells one that k / 4 of its
 // keys are not below), so that together they list k (1 + ln(row / first trip))
 // keys rather than four times as many; after the first trip they do not wait for each other.
-// 1024 rows of 128256 bf16 logits: 57 us without alternatives (4.6 TB/s), 75 with
-// 20 (92 with a bound a wave), 96 with 64 (162).
+// 1024 rows of 128256 bf16 logits: 54 us without alternatives (4.8 TB/s), 76 with
+// 20 (92 with a bound a wave), 97 with 64 (162).
 // A row is cut into parts when there are too few rows for the GPU, and a
 // second kernel joins the parts' sums and lists.
 
@@ -30,12 +30,12 @@ using namespace splice_dev;
 
 constexpr int kScoreThreads = 256;
 constexpr int kScoreWaves = kScoreThreads / 64;
-// 16-byte chunks a thread has in flight (us with 2 / 4 / 8: 1024 bf16 rows, k = 20, 83 / 80 / 98; 300 float32
-// rows, k = 8, 51 / 48 / 54, k = 0 34 / 37 / 39)
+// 16-byte chunks a thread has in flight (us with 2 / 4 / 8: 1024 bf16 rows, k = 20, 79 / 76 / 98; 300 float32
+// rows, k = 8, 51 / 48 / 56, k = 0 38 / 41 / 42)
 constexpr int kChunks = 4;
 constexpr int kMaxParts = 64;
-constexpr int kPartBytes = 8 << 10;   // a part is at least this long (7 rows of 600 KB: 15 us; 32 KB 19)
-// Work groups that fill the GPU (512 / 1024 / 2048: 300 float32 rows, k = 8, 56 / 48 / 51; 1024 bf16 rows, k = 20, 80 / 80 / 92)
+constexpr int kPartBytes = 8 << 10;   // a part is at least this long (7 rows of 600 KB: 12 us; 32 KB 19)
+// Work groups that fill the GPU (512 / 1024 / 2048: 300 float32 rows, k = 8, 56 / 48 / 52; 1024 bf16 rows, k = 20, 76 / 76 / 89)
 constexpr int kPartsTarget = 1024;
 constexpr int kWaveKeys = 256;        // a wave's list
 constexpr int kCutKeys = 128;         // one longer than this is cut to its first k

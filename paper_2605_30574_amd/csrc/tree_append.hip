@@ -99,9 +99,10 @@ __device__ __forceinline__ float odd_float(double x) {
 // A work group takes one node's heads kAppendThreads / LPR at a time (LPR = D / 8
 // lanes a head row, eight values a lane): blockIdx.x the node, blockIdx.y the
 // heads.  The angles of the node are computed once a work group and shared.  Launch and
-// two rounds of loads (the depth, the row) bound it at few nodes, 3.9 us for 32
+// two rounds of loads (the depth, the row) bound it at few nodes, 3.6 us for 32
 // tokens; the rows' bytes at many: 128 cells of 33 nodes, 32 + 2 x 8 heads of 128
-// to an 8-bit cache, 95 MB in 21.0 us (4.5 TB/s; 19.2 with the keys rotated in 32 bits).
+// to an 8-bit cache, 95 MB in 26.8 us (3.5 TB/s; on the same inputs again, partly still
+// cached, 21.6, and 19.2 with the keys rotated in 32 bits).
 template <int D, bool F8, int CELLS>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs<CELLS> a) {
     constexpr int LPR = D / 8, ROWS = kAppendThreads / LPR;
@@ -183,7 +184,7 @@ struct RowsArgs {
 
 // One thread reads eight values of one row: blockIdx.x (active cell, KV head),
 // blockIdx.y K or V.  Bound by its bytes: the rows of those 128 x 33 nodes,
-// 26 MB in 5.4 us.
+// 26 MB in 6.6 us (5.2 where they are still cached).
 template <int D, bool F8, int CELLS>
 __global__ __launch_bounds__(kAppendThreads) void read_kernel(RowsArgs<CELLS> a) {
     constexpr int LPR = D / 8;
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(kAppendThreads) void read_kernel(RowsArgs<CELLS> a)
 // has come back, then stores, so that rows may overlap without a copy
 // elsewhere.  A row's exponent moves with its first unit.  Launch and two
 // rounds of memory bound it: 128 cells of 8 heads, up to 64 rows of 128
-// bytes, 17 MB in 5.0 us.
+// bytes, 17 MB in 5.1 us (3.3 TB/s, 1.5 times a copy's time).
 template <int ROW, bool F8, int CELLS>
 __global__ __launch_bounds__(kAppendThreads) void keep_kernel(RowsArgs<CELLS> a) {
     constexpr int LPR = ROW / 16, U = SPLICE_MAX_NODES * LPR / kAppendThreads;

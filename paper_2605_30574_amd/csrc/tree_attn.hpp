@@ -14,9 +14,11 @@
 //                 that only where its maximum rises by more than kSlack;
 //   softmax       sums in fp32;
 //   O^T += V^T P  A = V^T by transposing LDS reads, in the order of keys in
-//                 which P lies in the lanes; P rounded to bf16 (weights of at
-//                 most 2^kSlack with relative errors of 2^-9 that average
-//                 out; their sum is not rounded).
+//                 which P lies in the lanes; P rounded to bf16, the type of V: a
+//                 weight is off by 2^-8 of itself at most, a result by 2^-8
+//                 sum p |v| (12 nodes a cell, window 1024, D = 256, against 64
+//                 bits: 2.3e-3 of the results' size, of which rounding the
+//                 result alone makes 1.7e-3).  The weights' sum is not rounded.
 // RW = 1: every wave has a tile of its own, with the next one (of 8-bit rows the
 // next two) in registers, and waits for no other; else a tile is for all waves, and bf16 rows go straight
 // to one of two buffers in LDS while the other is computed.
@@ -33,11 +35,11 @@
 //
 // What bounds it: where many rows share keys the tile loop, whose matrix products
 // (40% busy) and vector operations (45%) overlap in part only: 47 cells of 16 nodes, 32 heads of
-// 128 over 8k slots 135 us in the kernel (800 TFLOP/s); with small trees the generated
+// 128 over 8k slots 137 us in the kernel (780 TFLOP/s); with small trees the generated
 // rows' bytes, 64 cells of 5 nodes, 4.4 TB/s of bf16 rows and 3.3 TB/s of 8-bit ones, 5.3 and 4.5
 // over longer lists (4.2 with one 8-bit tile in flight a wave; with half the bytes a key the
 // chain from codes through LDS to the products counts for more); in small calls
-// the chain of loads before the first tile (7.4 us with one tile).
+// the chain of loads before the first tile (7.1 us with one tile).
 #pragma once
 
 #include <atomic>
@@ -63,8 +65,8 @@ struct TreeCall {
     float *lse;
     // Partial results, [slot][node][q head]: o / l (a convex combination of
     // value rows) in fp16, times a power of two sc that brings a row's
-    // largest value to 2^14 .. 2^15, and m, l, 1 / sc.  A rounding of 2^-12 of
-    // it is small beside the bf16 result's, and 32 bits would be 1.9 times the
+    // largest value to 2^14 .. 2^15, and m, l, 1 / sc.  A rounding of 2^-11 of
+    // a value is small beside the bf16 result's 2^-8, and 32 bits would be 1.9 times the
     // bytes that a call of many chunks writes and reads again.
     _Float16 *part;
     float4 *record;

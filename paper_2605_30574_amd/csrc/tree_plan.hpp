@@ -101,8 +101,9 @@ constexpr int tree_resident(int D, bool f8) { return D > 128 && f8 ? 1 : 2; }   
 constexpr int kTreeMaxSlots = 640;
 // Rounds of resident work groups a plan may take to balance its chunks, and what a
 // work group costs beside its tiles, in tiles (us: 48 cells of 16 nodes over 8k
-// slots, 6 rounds 158, 1 round 216; 8 tiles 158, 2 168, 16 216; 64 cells of 16 nodes,
-// 2k bf16 rows each, 6 rounds 131, 1 round 126).
+// slots, some on both sides of their onset, 6 rounds 152, 1 round 198, and 8 tiles 152, 2 165, 16 198;
+// half of the cells spliced and none so, 148, 140, and 148, 166, 136; 64 cells of 16
+// nodes, 2k bf16 rows each, 118, 119, and 118 with any).
 constexpr int kTreeRounds = 6;
 constexpr int kTreeStart = 8;
 // What the join of chunks costs, in tiles: a launch and the partial results' way (two sets
@@ -181,10 +182,11 @@ inline int64_t tree_chunks(const int *tiles, int n, int per) {
 // prompt's tiles, and each cell's generated rows have items of their own.
 // That takes another partial result a row, and pays where the cells together
 // walk much prompt: n cells times its keys times head_dim from 5 * 2^20 on
-// (us, apart / packed: 64 cells of 5 nodes, D = 128, 512 keys 24 / 33, 1024
-// 45 / 37, 2048 60 / 42; 40 cells of 12 nodes 512 keys 34 / 38, 2048 58 / 48; 8 cells
-// of 5 nodes 2048 keys 19 / 22; D = 256, 64 cells of one node 256 keys 21 / 25,
-// 1024 44 / 26; D = 64, 64 cells of 5 nodes 1024 keys 29 / 24). A call that sets
+// (us, apart / packed, half of the cells spliced: 64 cells of 5 nodes, D = 128, 512 keys
+// 20 / 30, 1024 27 / 34, 2048 40 / 38; 40 cells of 12 nodes 512 keys 24 / 33, 2048 46 / 44;
+// 8 cells of 5 nodes 2048 keys 21 / 21; 48 cells of 16 nodes 8192 keys 171 / 148; D = 256, 64
+// cells of one node 256 keys 27 / 22, 1024 38 / 26; D = 64, 64 cells of 5 nodes 1024 keys
+// 16 / 17; the border itself is coarse: near it either side may be the faster one). A call that sets
 // split_keys packs whenever it can.
 constexpr int kTreeMaxPrompt = 16;                 // chunks of the prompt
 constexpr int kTreePackedRows = 64;                // rows of a cell (more fill the waves of a work group by themselves)
