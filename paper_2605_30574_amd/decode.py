@@ -337,6 +337,16 @@ class SweepDecoder:
                            torch.from_numpy(T.rope_frequencies(self.w.head_dim, float(self.m.rope_theta))[0]).to(self.device),
                            parents.astype(np.int64))
 
+    def _node_positions(self, tree: DecoderTree, steps: np.ndarray) -> Optional[torch.Tensor]:
+        """Positions [C][T] of the nodes where they are not T_p + step + depth (None): what a decoder's own positions() says of
+        each node's step, asked depth by depth, as passes of one token would."""
+        if getattr(self.positions, "__func__", None) is SweepDecoder.positions:
+            return None
+        most = max(int(T.tree_layout(tree.parents)[0].max(initial=0)), 0)
+        pos = [self.positions(np.where(steps >= 0, steps + d, steps)) for d in range(most + 1)]
+        pos = torch.stack(pos, 1).gather(1, tree.depth.clamp(min=0).to(torch.int64))
+        return pos.to(torch.float64 if pos.is_floating_point() else torch.int64)
+
     def _turns(self, tree: DecoderTree, steps: np.ndarray, pos: Optional[torch.Tensor]):
         """(cos, sin) float32 [C][T][1][D / 2] of the nodes' positions: pos [C][T], or T_p + step + depth, whose T_p + step
         is the cells' (from the steps by value, so that a pass can be captured), the depth's angle added to it."""
@@ -355,18 +365,17 @@ class SweepDecoder:
     @torch.no_grad()
     def tree_logits(self, tokens: torch.Tensor, tree: DecoderTree, steps: np.ndarray) -> torch.Tensor:
         """Logits [C * T][V] of one pass over the trees' nodes (bfloat16 where the head's product is, else float32): node t
-        of cell c is the token tokens[c][t] (int64) at decode step steps[c] + its depth, behind the steps[c] rows of the
-        cell's generated caches and its ancestors.  Its K/V become row steps[c] + t, so steps[c] + T must not pass the caches' rows; cells with a
-        negative step are skipped.  Rows of padding and of skipped cells hold no meaning (their tokens are any of the
-        vocabulary).  No gradients."""
+        of cell c is the token tokens[c][t] (int64) at decode step steps[c] + its depth (at the position that positions()
+        gives for that step), behind the steps[c] rows of the cell's generated caches and its ancestors.  Its K/V become row
+        steps[c] + t, so steps[c] + T must not pass the caches' rows; cells with a negative step are skipped.  Rows of
+        padding and of skipped cells hold no meaning (their tokens are any of the vocabulary).  No gradients."""
         w, m, wt = self.w, self.m, self.wt
         C, Hq, Hkv, D, n = self.C, w.n_q_heads, w.n_kv_heads, w.head_dim, tree.spec.n_nodes
         if tuple(tokens.shape) != (C, n):
             raise ValueError(f"tokens has shape {tuple(tokens.shape)}, expected ({C}, {n})")
         st, _ = S._steps(steps, C)
-        pos = None
-        if getattr(self.positions, "__func__", None) is not SweepDecoder.positions:   # not T_p + s
-            pos = (self.positions(st).to(torch.int64)[:, None] + tree.depth).contiguous()
+        pos = self._node_positions(tree, st)
+        whole = pos is None or not pos.is_floating_point()
         x = wt["embed"][tokens.reshape(-1)]
         cdt, dev, rows = x.dtype, x.device, C * n
         rope_of, unturned, bf16 = T.make_rope("half", D), T.make_rope("half", 0), torch.bfloat16
@@ -382,12 +391,13 @@ class SweepDecoder:
             c = self.caches[l]
             e = [c[name] for name in exps] or [None, None]
             q, k, v = q.view(C, n, Hq, D), k.view(C, n, Hkv, D), v.to(bf16).view(C, n, Hkv, D)
-            rotary, freq = rope_of, tree.freq
-            if q.dtype != bf16 or k.dtype != bf16:   # of more bits: rotated before they are rounded, as in forward
+            rotary, freq, at = rope_of, tree.freq, pos
+            # of more bits: rotated before they are rounded, as in forward; and the kernel's positions are whole numbers
+            if q.dtype != bf16 or k.dtype != bf16 or not whole:
                 turns = turns or self._turns(tree, st, pos)
                 q, k = (_rotated(y.float(), *turns).to(bf16) for y in (q, k))
-                rotary, freq = unturned, None
-            T.splice_tree_append(self.shape, tree.spec, rotary, freq, st, tree.depth, q, k, v, q, c["gen_k"], c["gen_v"], *e, pos=pos)
+                rotary, freq, at = unturned, None, None
+            T.splice_tree_append(self.shape, tree.spec, rotary, freq, st, tree.depth, q, k, v, q, c["gen_k"], c["gen_v"], *e, pos=at)
             T.splice_tree_attn(self.shape, self.calls[l], tree.spec, self.lw, st, tree.depth, tree.visible, q, c["clean_k"],
                                c["clean_v"], c["donor_k"], c["donor_v"], c["gen_k"], c["gen_v"], *e, out, lse, tree.workspace)
             return out.view(rows, Hq * D)

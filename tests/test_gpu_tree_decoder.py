@@ -164,3 +164,60 @@ def test_captured_pass_with_float32_weights():
         assert torch.equal(got, gpu.tree_logits(tokens, tree, steps))
         torch.cuda.synchronize()
         assert all(torch.equal(a, c["gen_k"]) for a, c in zip(rows, caches))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind", ["stretched", "between", "by cell"])
+def test_positions_of_the_decoders_own(kind, dtype):
+    """A node's position is what positions() says of its step, whatever that is: the keys and logits of a chain are those of
+    decode steps."""
+    w = decode_bar.case("blank-sink")
+    lw, _, gpu, _, caches = setup(w, dtype)
+    *_, plain, _, plain_caches = setup(w, dtype)
+    C, T, D = lw.shape[0], 5, w.head_dim
+    cell = np.arange(C)
+    own = {"stretched": lambda s: w.prompt_len + 3 * np.maximum(s, 0), "between": lambda s: (w.prompt_len + np.maximum(s, 0)) / 4,
+           "by cell": lambda s: w.prompt_len + cell + (1 + cell % 2) * np.maximum(s, 0)}[kind]
+    for d in (gpu, plain):
+        d.positions = lambda s: torch.as_tensor(own(s)).cuda()
+    tokens = torch.randint(0, MODEL.vocab, (C, T), generator=torch.Generator().manual_seed(2)).cuda()
+    steps = np.arange(C).astype(np.int32)
+    gc.announce(f"positions {kind}, {dtype}")
+    got = gpu.tree_logits(tokens, gpu.make_tree(chain(C, T)), steps).view(C, T, -1).double()
+    for t in range(T):
+        want = plain.forward(tokens[:, t], steps + t).double()
+        assert (got[:, t] - want).abs().max() <= 2 * TREE_REL * max(1.0, float(want.abs().max())), t
+    # two roundings to bf16 of a rotation, whose pairs keep their length, and their products' own
+    a, b = (x[0]["gen_k"].double().cpu().numpy() for x in (caches, plain_caches))
+    length = np.hypot(b, np.roll(b, D // 2, -1))
+    assert (length > 0).any() and (np.abs(a - b) <= 2.0 ** -6 * length).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_captured_pass_with_positions_on_the_device(dtype):
+    """positions() that makes no copy from the host is asked within a captured pass; cells that are finished and padding too."""
+    w = decode_bar.case("blank-sink")
+    lw, _, gpu, _, _ = setup(w, dtype)
+    C = lw.shape[0]
+    table = (torch.arange(w.n_steps * C, device="cuda").view(w.n_steps, C) * 5) % 97   # [step][cell]
+    steps = np.full(C, 3, np.int32)
+    steps[1] = -1
+    gpu.positions = lambda s: table[int(s.max())]
+    parents = np.tile([-1, 0, 0, 2, -1], (C, 1))
+    parents[2, 3:] = -2
+    tree, tokens = gpu.make_tree(parents), torch.zeros((C, 5), dtype=torch.int64, device="cuda")
+    gpu.tree_logits(tokens, tree, steps)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        logits = gpu.tree_logits(tokens, tree, steps)
+    on = torch.from_numpy(((parents >= -1) & (steps >= 0)[:, None]).reshape(-1)).cuda()
+    for n in range(3):
+        gc.announce(f"captured tree pass, positions on the device, {dtype}, replay {n}")
+        tokens.copy_(torch.randint(0, MODEL.vocab, tokens.shape, generator=torch.Generator().manual_seed(n)))
+        table.add_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = logits.clone()
+        assert torch.equal(got[on], gpu.tree_logits(tokens, tree, steps)[on])
+        torch.cuda.synchronize()
