@@ -199,9 +199,10 @@ __device__ __forceinline__ void rank_first(Candidates &c, int n, int k) {
 // Where weights are 0 their z, which may be -inf, stops here: 0 times a finite number.
 constexpr float kLeastZ = -1e4f;
 
-// z = x scale2 - m scale2 in one operation where m scale2 is below this: its rounding, 2^-17 at most, is
-// then all that a weight is off by.  Beyond, where the rounding grows with m (logits of
-// 1e8 would have weights of 0 or infinity) and the product may be no float, x - m comes first.
+// z = x scale2 - m scale2 in one operation where |m scale2| is below this: the
+// product's rounding, 2^-17 at most, is then what a weight's exponent is off by.
+// Beyond, where it grows with m (2^9 for logits of 1e10, weights of 0 or infinity)
+// and the product may be no float, x - m comes first.
 constexpr float kMostRef = 256.f;
 
 // Joins (m, s, t) of two parts of a row.
