@@ -6,7 +6,11 @@ prompt cache whose span slots are read, per sweep cell (L, W), from a donor
 cache.  The work runs in hand-written HIP kernels behind the C ABI declared
 in include/splice_attn.h; ``splice`` is its ctypes binding.  ``tree`` binds
 include/splice_tree.h: several candidate tokens per cell judged in one pass.
+``pages`` binds include/splice_pages.h: caches in 4 bits, in pages that cells share.
 """
+from .pages import (SPLICE_MAX_PAGE_TOKENS, SPLICE_PAGE_ROWS, SplicePages, make_pages, splice_page_append,
+                    splice_page_attn, splice_page_attn_workspace_bytes, splice_page_bytes, splice_page_compact,
+                    splice_page_fork, splice_page_read)
 from .splice import (EXPORTS, LIB_PATH, SPLICE_BF16, SPLICE_DONOR_BUFFER, SPLICE_DONOR_ZERO,
                      SPLICE_EHIP, SPLICE_EINVAL, SPLICE_ESHAPE, SPLICE_EUNSUPPORTED,
                      SPLICE_EWORKSPACE, SPLICE_F32, SPLICE_MAX_CELLS, SPLICE_OK, SPLICE_SRC_CLEAN,

@@ -1,0 +1,187 @@
+"""Python binding of include/splice_pages.h: K and V in 4 bits, in pages of 64 tokens that cells share.
+
+A layer's pool is a uint8 tensor [n_pages][splice_page_bytes(shape)]; a cell's rows lie in the pages that its row of a table
+(int32 [C][table_len] on the device) names.  ``splice_page_append`` writes new tokens, ``splice_page_attn`` attends,
+``splice_page_fork`` says who holds which pages next, ``splice_page_compact`` moves the rows that stay together, and
+``splice_page_read`` reads rows back.  ``PageCache`` keeps the pools, tables and counts of a sweep, and
+``decode.SweepDecoder.page_logits`` runs a pass over them.
+
+As in ``splice``, functions have the C names, marshal arguments only and check every tensor's device, dtype, layout and size
+before calling into C; a negative status raises ``SpliceError``.  The kernels run on the current device: tensors of another one
+are refused.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Tuple
+
+import numpy as np
+
+from . import splice as S
+from . import tree as T
+
+SPLICE_PAGE_ROWS, SPLICE_MAX_PAGE_TOKENS = 64, 32768
+
+EXPORTS = ("splice_page_bytes", "splice_page_append", "splice_page_read", "splice_page_attn_workspace_bytes",
+           "splice_page_attn", "splice_page_fork", "splice_page_compact")
+
+
+class SplicePages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("table_len", ctypes.c_int32), ("n_tokens", ctypes.c_int32)]
+
+
+_declared = None
+
+
+def _library():
+    """The library with the prototypes of include/splice_pages.h."""
+    global _declared
+    lib = S.load_library()
+    if _declared is not lib:
+        vp, i32, i64, size = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        shp, cal = ctypes.POINTER(S.SpliceShape), ctypes.POINTER(S.SpliceCall)
+        pgs, rop = ctypes.POINTER(SplicePages), ctypes.POINTER(T.SpliceRope)
+        for name, res, args in (
+                ("splice_page_bytes", i64, [shp]),
+                ("splice_page_append", i32, [shp, pgs, rop] + [vp] * 5 + [vp, i64] * 3 + [vp] * 3),
+                ("splice_page_read", i32, [shp, pgs] + [vp] * 7),
+                ("splice_page_attn_workspace_bytes", i64, [shp, cal, pgs]),
+                ("splice_page_attn", i32, [shp, cal, pgs] + [vp] * 11 + [size, vp]),
+                ("splice_page_fork", i32, [shp, pgs] + [vp] * 10 + [i64, vp]),
+                ("splice_page_compact", i32, [shp, pgs] + [vp] * 4 + [i64, vp])):
+            f = getattr(lib, name)
+            f.restype, f.argtypes = res, args   # (a structure passes by reference where its pointer is declared)
+        _declared = lib
+    return lib
+
+
+# ------------------------------------------------------------------ structs, checks
+
+def make_pages(n_pages: int, table_len: int, n_tokens: int = 1) -> SplicePages:
+    """Pools of ``n_pages`` pages, tables of ``table_len`` entries a cell, and T = ``n_tokens`` tokens a cell in a call."""
+    return SplicePages(n_pages, table_len, n_tokens)
+
+
+def splice_page_bytes(shape) -> int:
+    """Bytes of one page of one layer."""
+    return S._check(_library().splice_page_bytes(shape), "splice_page_bytes")
+
+
+def _cells(shape, pages, cell_step, cell_new) -> Tuple[bytes, Optional[bytes]]:
+    steps = T._steps(cell_step, shape.n_cells)
+    return steps, None if cell_new is None else T._host(cell_new, shape.n_cells, 1, "cell_new", "entries")
+
+
+def _tables(t, name: str, shape, pages, dev) -> int:
+    return T._ptr(t, name, shape.n_cells * pages.table_len, S._torch.int32, dev)
+
+
+def _pool(t, shape, pages, dev) -> int:
+    return T._ptr(t, "pool", pages.n_pages * splice_page_bytes(shape), S._torch.uint8, dev)
+
+
+def _pools(t, shape, pages, dev) -> Tuple[int, int]:
+    """(address, bytes from one layer to the next) of uint8 [n_layers][n_pages][page_bytes], each layer dense."""
+    dims = (shape.n_layers, pages.n_pages, splice_page_bytes(shape))
+    if t is None or t.get_device() != dev[0]:
+        raise ValueError(f"pools must be a tensor on {dev[1]}")
+    if t.dtype is not S._torch.uint8:
+        raise ValueError(f"pools has dtype {t.dtype}, expected {S._torch.uint8}")
+    if t.shape != dims:
+        raise ValueError(f"pools has shape {tuple(t.shape)}, expected {dims}")
+    layer = dims[1] * dims[2]
+    if not t[0].is_contiguous() or (dims[0] > 1 and t.stride(0) < layer):
+        raise ValueError("pools: every layer must be dense and the layers apart")
+    return t.data_ptr(), t.stride(0) if dims[0] > 1 else layer
+
+
+# ------------------------------------------------------------------ C entry points
+
+def splice_page_append(shape, pages, rope, freq, cell_step, cell_new, tables, q, k, v, q_out, pool, pos=None,
+                       stream=None) -> None:
+    """Rotate the tokens' ``q`` [C][T][Hq][D] into ``q_out`` and write their rotated ``k`` and their ``v``
+    ([C][T][Hkv][D]) as rows s_c .. of the cells, in 4 bits (``cell_new``: how many of each cell, None for all T)."""
+    lib = _library()
+    dev = T._anchor(q_out, "q_out")
+    n, C, t = pages.n_tokens, shape.n_cells, S._torch
+    qo = T._ptr(q_out, "q_out", C * n * shape.n_q_heads * shape.head_dim, t.bfloat16, dev)
+    qp, qs = T._rows(q, "q", shape, n, shape.n_q_heads, dev)
+    kp, ks = T._rows(k, "k", shape, n, shape.n_kv_heads, dev)
+    vp, vs = T._rows(v, "v", shape, n, shape.n_kv_heads, dev)
+    tp, pl = _tables(tables, "tables", shape, pages, dev), _pool(pool, shape, pages, dev)
+    pp = None if pos is None else T._ptr(pos, "pos", C * n, t.int64, dev)
+    fp = None if rope.rotary_dim == 0 and freq is None else T._ptr(freq, "freq", rope.rotary_dim // 2, t.float64, dev)
+    steps, new = _cells(shape, pages, cell_step, cell_new)
+    S._check(lib.splice_page_append(shape, pages, rope, steps, new, tp, pp, fp, qp, qs, kp, ks, vp, vs, qo, pl,
+                                    T._stream(stream, dev)), "splice_page_append")
+
+
+def splice_page_read(shape, pages, cell_step, cell_new, tables, pool, rows_k, rows_v, stream=None) -> None:
+    """``rows_k``, ``rows_v`` (bf16 [C][Hkv][T][D]): rows cell_step[c] + i of the cells, i < cell_new[c]."""
+    lib = _library()
+    dev = T._anchor(rows_k, "rows_k")
+    n = shape.n_cells * shape.n_kv_heads * pages.n_tokens * shape.head_dim
+    rk, rv = (T._ptr(x, name, n, S._torch.bfloat16, dev) for x, name in ((rows_k, "rows_k"), (rows_v, "rows_v")))
+    tp, pl = _tables(tables, "tables", shape, pages, dev), _pool(pool, shape, pages, dev)
+    steps, new = _cells(shape, pages, cell_step, cell_new)
+    S._check(lib.splice_page_read(shape, pages, steps, new, tp, pl, rk, rv, T._stream(stream, dev)), "splice_page_read")
+
+
+def splice_page_attn_workspace_bytes(shape, call, pages) -> int:
+    return S._check(_library().splice_page_attn_workspace_bytes(shape, call, pages), "splice_page_attn_workspace_bytes")
+
+
+def splice_page_attn(shape, call, pages, cell_LW, cell_step, cell_new, tables, clean_table, donor_table, q, pool, out, lse,
+                     workspace, stream=None) -> None:
+    """Spliced attention of every cell's tokens: ``out`` bf16 [C][T][Hq][D], ``lse`` float32 [C][T][Hq].
+
+    ``clean_table``, ``donor_table``: int32 [ceil(T_p / 64)] pages of the prompt's slots (donor None for ZERO)."""
+    lib = _library()
+    dev = T._anchor(q, "q")
+    t, C, n, Hq, D = S._torch, shape.n_cells, pages.n_tokens, shape.n_q_heads, shape.head_dim
+    qp = T._ptr(q, "q", C * n * Hq * D, t.bfloat16, dev)
+    tp, pl = _tables(tables, "tables", shape, pages, dev), _pool(pool, shape, pages, dev)
+    n_prompt = -(-shape.prompt_len // SPLICE_PAGE_ROWS)
+    cp = None if n_prompt == 0 and clean_table is None else T._ptr(clean_table, "clean_table", n_prompt, t.int32, dev)
+    if shape.donor_kind == S.SPLICE_DONOR_ZERO:
+        if donor_table is not None:
+            raise ValueError("the ZERO donor takes no table")
+        dp = None
+    else:
+        dp = None if n_prompt == 0 and donor_table is None else T._ptr(donor_table, "donor_table", n_prompt, t.int32, dev)
+    op, lp = T._ptr(out, "out", C * n * Hq * D, t.bfloat16, dev), T._ptr(lse, "lse", C * n * Hq, t.float32, dev)
+    wp, wbytes = T._workspace(workspace, dev)
+    lwp = T._host(cell_LW, C, 2, "cell_LW", "rows")
+    steps, new = _cells(shape, pages, cell_step, cell_new)
+    S._check(lib.splice_page_attn(shape, call, pages, lwp, steps, new, tp, cp, dp, qp, pl, op, lp, wp, wbytes,
+                                  T._stream(stream, dev)), "splice_page_attn")
+
+
+def splice_page_fork(shape, pages, parent, rows, want, tables, refs, new_tables, new_refs, missing, copied, pools,
+                     stream=None) -> None:
+    """Cell c becomes the first ``rows[c]`` rows of cell ``parent[c]`` (-1: empty), with pages for ``want[c]`` rows: see
+    include/splice_pages.h.  ``tables`` int32 [C][table_len] and ``refs`` int32 [n_pages] as they are, ``new_tables`` and
+    ``new_refs`` as they become; ``missing`` int32 [1], ``copied`` int32 [C][2]; ``pools`` uint8
+    [n_layers][n_pages][page_bytes]."""
+    lib = _library()
+    dev = T._anchor(tables, "tables")
+    i32, C = S._torch.int32, shape.n_cells
+    tp, np_ = _tables(tables, "tables", shape, pages, dev), _tables(new_tables, "new_tables", shape, pages, dev)
+    rp, nr = T._ptr(refs, "refs", pages.n_pages, i32, dev), T._ptr(new_refs, "new_refs", pages.n_pages, i32, dev)
+    mp, cp = T._ptr(missing, "missing", 1, i32, dev), T._ptr(copied, "copied", 2 * C, i32, dev)
+    pl, stride = _pools(pools, shape, pages, dev)
+    host = [T._host(x, C, 1, name, "entries") for x, name in ((parent, "parent"), (rows, "rows"), (want, "want"))]
+    S._check(lib.splice_page_fork(shape, pages, *host, tp, rp, np_, nr, mp, cp, pl, stride, T._stream(stream, dev)),
+             "splice_page_fork")
+
+
+def splice_page_compact(shape, pages, cell_step, keep, tables, pools, stream=None) -> None:
+    """Row cell_step[c] + i = row cell_step[c] + keep[c][i] in every layer of ``pools`` (``keep`` int32 [C][T], ascending, ended
+    by -1)."""
+    lib = _library()
+    dev = T._anchor(keep, "keep")
+    kp = T._ptr(keep, "keep", shape.n_cells * pages.n_tokens, S._torch.int32, dev)
+    tp = _tables(tables, "tables", shape, pages, dev)
+    pl, stride = _pools(pools, shape, pages, dev)
+    S._check(lib.splice_page_compact(shape, pages, T._steps(cell_step, shape.n_cells), kp, tp, pl, stride,
+                                     T._stream(stream, dev)), "splice_page_compact")
