@@ -33,6 +33,7 @@ using splice::kPageRows;
 using splice::PageLayout;
 
 constexpr float kLowest = -3.0e38f;   // a running maximum before the first key
+constexpr float kMostWeight = 256.f;  // 2^kSlack
 
 struct PageCall {
     const char *q;
@@ -70,16 +71,44 @@ struct PageTile {
     int pos, lo, hi; // position of its first row, which of its positions count
 };
 
-__device__ __forceinline__ PageTile tile_of(const PageWalk &w, int i) {
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Page `at` of the walk; behind `end` none.  A table's entry is read on every path (one of a
+// walk with pages), so that waits for loads can be counted.  Everything is taken from the walk before
+// anything is chosen, and the choice is the same for a whole wave: it stays in scalar registers.
+__device__ __forceinline__ PageTile tile_of(const PageWalk &w, int at, int end) {
+    const int32_t *t0 = w.table[0], *t1 = w.table[1], *t2 = w.table[2], *t3 = w.table[3];
+    const int f1 = w.first[1], f2 = w.first[2], f3 = w.first[3], p0 = w.page0[0], p1 = w.page0[1], p2 = w.page0[2], p3 = w.page0[3];
+    const int l0 = w.lo[0], l1 = w.lo[1], l2 = w.lo[2], l3 = w.lo[3], h0 = w.hi[0], h1 = w.hi[1], h2 = w.hi[2], h3 = w.hi[3];
+    const int i = uniform(min(at, end - 1));
     PageTile t;
-    const int s = i < w.first[1] ? 0 : (i < w.first[2] ? 1 : (i < w.first[3] ? 2 : 3));
-    const int32_t *table = s == 0 ? w.table[0] : (s == 1 ? w.table[1] : (s == 2 ? w.table[2] : w.table[3]));
-    const int first = s == 0 ? w.first[0] : (s == 1 ? w.first[1] : (s == 2 ? w.first[2] : w.first[3]));
-    const int page = (s == 0 ? w.page0[0] : (s == 1 ? w.page0[1] : (s == 2 ? w.page0[2] : w.page0[3]))) + i - first;
-    t.lo = s == 0 ? w.lo[0] : (s == 1 ? w.lo[1] : (s == 2 ? w.lo[2] : w.lo[3]));
-    t.hi = s == 0 ? w.hi[0] : (s == 1 ? w.hi[1] : (s == 2 ? w.hi[2] : w.hi[3]));
-    t.pos = page * kPageRows + (s == 3 ? w.shift : 0);
-    t.id = table[page];
+    int page = p0 + i;
+    const int32_t *table = t0;
+    t.lo = l0;
+    t.hi = h0;
+    if (i >= f1) {
+        page = p1 + i - f1;
+        table = t1;
+        t.lo = l1;
+        t.hi = h1;
+    }
+    if (i >= f2) {
+        page = p2 + i - f2;
+        table = t2;
+        t.lo = l2;
+        t.hi = h2;
+    }
+    t.pos = page * kPageRows;
+    if (i >= f3) {
+        page = p3 + i - f3;
+        table = t3;
+        t.pos = page * kPageRows + w.shift;
+        t.lo = l3;
+        t.hi = h3;
+    }
+    // nobody writes tables meanwhile: a scalar load, which no wait for pages' bytes waits for
+    t.id = ((const __attribute__((address_space(4))) int32_t *)(uintptr_t)table)[page];
+    if (at >= end) t.id = -1;
     return t;
 }
 
@@ -109,17 +138,29 @@ __device__ __forceinline__ void load_query(const char *row, int quad, QueryRow<D
     });
 }
 
+// A lane's places in the bytes of a page's head, unsigned words: added to a base in scalar registers by the loads.
+template <int D>
+struct LanePlaces {
+    uint32_t key, key_exp, value, value_exp;   // of tile 0, piece 0
+    __device__ __forceinline__ explicit LanePlaces(int lane) {
+        const uint32_t col = lane & 15, quad = lane >> 4;
+        key = col * (D / 2) + (D == 64 ? 8 * quad : 16 * quad);
+        key_exp = PageLayout<D>::kKScale + (col * PageLayout<D>::kChunkBlocks + (D == 64 ? quad >> 1 : quad)) * 4;
+        value = PageLayout<D>::kV + lane * 16;
+        value_exp = PageLayout<D>::kVScale + (quad * 2 + (col >> 3)) * (D / 8);
+    }
+};
+
 // The lane's codes of 16 keys (tile t of a page).
 template <int D>
-__device__ __forceinline__ void load_codes(const uint8_t *head, int t, int col, int quad, uint32_t (&w)[KeyShare<D>::N]) {
-    const uint8_t *p = head + (16 * t + col) * (D / 2) + KeyShare<D>::first(quad) / 2;
+__device__ __forceinline__ void load_codes(const uint8_t *head, uint32_t at, uint32_t (&w)[KeyShare<D>::N]) {
     if constexpr (D == 64) {
-        const uint2 x = *reinterpret_cast<const uint2 *>(p);
+        const uint2 x = *reinterpret_cast<const uint2 *>(head + at);
         w[0] = x.x;
         w[1] = x.y;
     } else {
         static_for<0, KeyShare<D>::CH>([&](auto c) {
-            const u32x4_t x = *reinterpret_cast<const u32x4_t *>(p + c * 64);
+            const u32x4_t x = *reinterpret_cast<const u32x4_t *>(head + at + c * 64);
             static_for<0, 4>([&](auto j) { w[4 * c + j] = x[(int)j]; });
         });
     }
@@ -127,9 +168,8 @@ __device__ __forceinline__ void load_codes(const uint8_t *head, int t, int col, 
 
 // The lane's exponent bytes of each piece, a byte a tile of the page.
 template <int D>
-__device__ __forceinline__ void load_exponents(const uint8_t *head, int col, int quad, uint32_t (&s)[KeyShare<D>::CH]) {
-    const uint8_t *p = head + PageLayout<D>::kKScale + (col * PageLayout<D>::kChunkBlocks + (D == 64 ? quad >> 1 : quad)) * 4;
-    static_for<0, KeyShare<D>::CH>([&](auto c) { s[c] = *reinterpret_cast<const uint32_t *>(p + c * 256); });
+__device__ __forceinline__ void load_exponents(const uint8_t *head, uint32_t at, uint32_t (&s)[KeyShare<D>::CH]) {
+    static_for<0, KeyShare<D>::CH>([&](auto c) { s[c] = *reinterpret_cast<const uint32_t *>(head + at + c * 256); });
 }
 
 // Byte n of a word as the power of two that it stands for; 255: infinity, which makes what it scales NaN or infinite.
@@ -232,41 +272,70 @@ __device__ __forceinline__ void start(PageState<D, R> &st, const PageRowsOf<R> &
     });
 }
 
-// Scores of a page to weights, as operands of the second product (two of 32 keys).  from, to: the
-// lane's visible keys, counted from its first one of the page; nan: keys that are NaN.
-template <int D, int R, int RI>
-__device__ __forceinline__ void softmax(PageState<D, R> &st, f32x4_t (&s)[4], bool masked, int from, int to, uint64_t nan, int quad,
-                                        float qk, bf16x8_t (&p)[2]) {
+// What a page's scores are worth to some rows: from, to: the lane's visible keys, counted from its first one of the
+// page; nan: keys that are NaN.
+__device__ __forceinline__ void mark(f32x4_t (&s)[4], int from, int to, uint64_t nan, int quad) {
     if (nan) static_for<0, 4>([&](auto t) {
         static_for<0, 4>([&](auto r) {
             if ((nan >> (16 * t + r)) >> (4 * quad) & 1) s[t][(int)r] = __uint_as_float(0x7fc00000u);
         });
     });
-    if (masked) static_for<0, 4>([&](auto t) {
+    static_for<0, 4>([&](auto t) {
         static_for<0, 4>([&](auto r) { s[t][(int)r] = 16 * t + r >= from && 16 * t + r < to ? s[t][(int)r] : -INFINITY; });
     });
-    float top = s[0][0];
-    static_for<1, 16>([&](auto i) { top = fmaxf(top, s[i / 4][i % 4]); });
-    top *= qk;
-    if (__any(top > st.m[RI] + kSlack)) {
+}
+
+// The running maxima raised to what the page's scores ask for.
+template <int D, int R>
+__device__ __forceinline__ void raise(PageState<D, R> &st, const f32x4_t (&s)[R][4], float qk) {
+    static_for<0, R>([&](auto r) {
+        float top = s[r][0][0];
+        static_for<1, 16>([&](auto i) { top = fmaxf(top, s[r][i / 4][i % 4]); });
+        top *= qk;
         top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float now = fmaxf(top, st.m[RI]), f = fast_exp2(st.m[RI] - now);
-        st.m[RI] = now;
-        st.l[RI] *= f;
-        static_for<0, D / 64>([&](auto b) { static_for<0, 4>([&](auto m) { st.o[RI][b][m] *= f; }); });
-    }
-    typedef float f32x8_t __attribute__((ext_vector_type(8)));
-    float sum = 0.f;
-    static_for<0, 2>([&](auto a) {
-        f32x8_t w;
-        static_for<0, 8>([&](auto i) {
-            w[(int)i] = fast_exp2(fmaf(s[2 * a + i / 4][i % 4], qk, -st.m[RI]));
-            sum += w[(int)i];
-        });
-        p[a] = __builtin_convertvector(w, bf16x8_t);
+        const float now = fmaxf(fmaxf(top, __shfl_xor(top, 32)), st.m[r]), f = fast_exp2(st.m[r] - now);
+        st.m[r] = now;
+        st.l[r] *= f;
+        static_for<0, D / 64>([&](auto b) { static_for<0, 4>([&](auto m) { st.o[r][b][m] *= f; }); });
     });
-    st.l[RI] += sum;
+}
+
+// Weights of a page as the second product's operands (two of 32 keys); their sums to the rows'.  The scores'
+// maximum is looked for only where a lane's weights sum to more than 2^8 (or to NaN): one of them may then.
+template <int D, int R>
+__device__ __forceinline__ void weights(PageState<D, R> &st, const f32x4_t (&s)[R][4], float qk, bf16x8_t (&p)[R][2]) {
+    typedef float f32x8_t __attribute__((ext_vector_type(8)));
+    float sum[R];
+    auto all = [&]() {
+        static_for<0, R>([&](auto r) {
+            static_for<0, 2>([&](auto h) {
+                f32x8_t w;
+                static_for<0, 8>([&](auto i) { w[(int)i] = fast_exp2(fmaf(s[r][2 * h + i / 4][i % 4], qk, -st.m[r])); });
+                const float x = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+                sum[r] = h ? sum[r] + x : x;
+                p[r][h] = __builtin_convertvector(w, bf16x8_t);
+            });
+        });
+    };
+    all();
+    bool up = false;
+    static_for<0, R>([&](auto r) { up |= !(sum[r] <= kMostWeight); });
+    if (__any(up)) {
+        raise<D, R>(st, s, qk);
+        all();
+    }
+    static_for<0, R>([&](auto r) { st.l[r] += sum[r]; });
+}
+
+// A row's values are there before what follows: a wait in a loop would take later loads with it.
+template <int D, int R>
+__device__ __forceinline__ void settle(const QueryRow<D> (&q)[R]) {
+    static_for<0, R>([&](auto r) {
+        static_for<0, KeyShare<D>::N>([&](auto n) {
+            const u32x4_t w = __builtin_bit_cast(u32x4_t, q[r].v[n]);
+            asm volatile("" ::"v"(w));
+        });
+    });
 }
 
 // Least and largest over the wave's rows.
@@ -319,14 +388,20 @@ struct NarrowShared {
     int64_t at[16 * R];
 };
 
+// Pages that a wave has in registers or on their way there.  Two hide the memory's latency behind the other's
+// products (64 cells of 8k rows, D = 128: one 178 us, two PF2TIME); what they take of registers beside two sets
+// of rows, or rows of 256, leaves room for one.
+constexpr int narrow_pages(int D, int R) { return D == 64 || (D == 128 && R == 1) ? 2 : 1; }
+
 // Pages [i0, i1) of the walk for R x 16 rows, the waves a page each in turn.
 template <int D, int R>
 __device__ __forceinline__ void narrow(const PageCall &a, const PageWalk &walk, int i0, int i1, int h, const PageRowsOf<R> &rows,
                                        bool first, int part, NarrowShared<D, R> &sh) {
-    constexpr int B = D / 64;
+    constexpr int B = D / 64, PF = narrow_pages(D, R), STEP = 4 * PF;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
     const int64_t page_bytes = (int64_t)a.Hkv * PageLayout<D>::kBytes;
     const uint8_t *pool = a.pool + (int64_t)h * PageLayout<D>::kBytes;
+    const LanePlaces<D> at(lane);
     QueryRow<D> q[R];
     int lo_most = rows.lo[0], hi_least = rows.hi[0];
     static_for<0, R>([&](auto r) {
@@ -338,63 +413,60 @@ __device__ __forceinline__ void narrow(const PageCall &a, const PageWalk &walk, 
     hi_least = wave_min(hi_least);
     PageState<D, R> st;
     start<D, R>(st, rows, first && wave == 0, quad);
-    uint32_t kc[4][KeyShare<D>::N], ke[KeyShare<D>::CH];
-    u32x4_t vc[2][B];
-    uint32_t vs[2][B][2];
-    auto load_keys = [&](const uint8_t *head) {
-        static_for<0, 4>([&](auto t) { load_codes<D>(head, t, col, quad, kc[t]); });
-        load_exponents<D>(head, col, quad, ke);
+    struct Slot {
+        PageTile now, next;   // the page in the registers, and the one that follows it there
+        uint32_t kc[4][KeyShare<D>::N], ke[KeyShare<D>::CH];
+        u32x4_t vc[2][B];
+        uint32_t vs[2][B][2];
     };
     auto there = [&](const PageTile &t) { return t.id >= 0 && t.id < a.n_pages; };
-    auto head_of = [&](const PageTile &t) { return pool + (int64_t)(there(t) ? t.id : 0) * page_bytes; };
-    auto load_values = [&](const uint8_t *head) {
+    auto head_of = [&](const PageTile &t) { return pool + (uint64_t)(uint32_t)(there(t) ? t.id : 0) * (uint64_t)page_bytes; };
+    auto load_keys = [&](Slot &p, const uint8_t *head) {
+        static_for<0, 4>([&](auto t) { load_codes<D>(head, at.key + t * (8 * D), p.kc[t]); });
+        load_exponents<D>(head, at.key_exp, p.ke);
+    };
+    auto load_values = [&](Slot &p, const uint8_t *head) {
         static_for<0, 2>([&](auto t) {
             static_for<0, B>([&](auto b) {
-                vc[t][b] = *reinterpret_cast<const u32x4_t *>(head + PageLayout<D>::kV + (t * B + b) * 1024 + lane * 16);
-                const uint2 s = *reinterpret_cast<const uint2 *>(head + PageLayout<D>::kVScale + (((t * 4 + quad) * 2 + (col >> 3)) * B + b) * 8);
-                vs[t][b][0] = s.x;
-                vs[t][b][1] = s.y;
+                p.vc[t][b] = *reinterpret_cast<const u32x4_t *>(head + at.value + (t * B + b) * 1024);
+                const uint2 s = *reinterpret_cast<const uint2 *>(head + at.value_exp + t * D + b * 8);
+                p.vs[t][b][0] = s.x;
+                p.vs[t][b][1] = s.y;
             });
         });
     };
-    int i = i0 + wave;
-    PageTile now{-1, 0, 0, 0}, next{-1, 0, 0, 0};
-    if (i < i1) {
-        now = tile_of(walk, i);
-        load_keys(head_of(now));
-        load_values(head_of(now));
-        if (i + 4 < i1) next = tile_of(walk, i + 4);
-    }
-    for (; i < i1; i += 4) {
-        const bool more = i + 4 < i1, use = there(now);
+    // The page of a slot, number i of the walk; the bytes of page i + STEP take its place.
+    auto page = [&](Slot &slot, int i) {
+        const PageTile now = slot.now;
         f32x4_t s[R][4];
-        static_for<0, 4>([&](auto t) { scores<D, decltype(t)::value, R>(kc[t], ke, q, s); });
-        const uint64_t nan = nan_keys(ke[0]);
-        const uint8_t *head = head_of(next);
-        if (more) load_keys(head);
-        PageTile after{-1, 0, 0, 0};
-        if (i + 8 < i1) after = tile_of(walk, i + 8);
-        if (use) {
+        static_for<0, 4>([&](auto t) { scores<D, decltype(t)::value, R>(slot.kc[t], slot.ke, q, s); });
+        const uint64_t nan = nan_keys(slot.ke[0]);
+        const uint8_t *head = head_of(slot.next);
+        load_keys(slot, head);
+        slot.now = slot.next;
+        slot.next = tile_of(walk, i + 2 * STEP, i1);
+        if (there(now)) {
             const bool edge = now.pos < now.lo || now.pos + kPageRows > now.hi;
-            const bool masked = edge || now.pos < lo_most || now.pos + kPageRows > hi_least;
-            if (edge || nan) static_for<0, 2>([&](auto t) {
-                static_for<0, B>([&](auto b) {
-                    static_for<0, 2>([&](auto e) {
-                        vs[t][b][e] = finite_scales(vs[t][b][e], now.pos + 32 * t + 16 * e + 4 * quad, now.lo, now.hi);
+            if (edge || nan || now.pos < lo_most || now.pos + kPageRows > hi_least) {
+                if (edge || nan) static_for<0, 2>([&](auto t) {
+                    static_for<0, B>([&](auto b) {
+                        static_for<0, 2>([&](auto e) {
+                            slot.vs[t][b][e] = finite_scales(slot.vs[t][b][e], now.pos + 32 * t + 16 * e + 4 * quad, now.lo, now.hi);
+                        });
                     });
                 });
-            });
-            bf16x8_t p[R][2];
-            static_for<0, R>([&](auto r) {
                 const int base = now.pos + 4 * quad;
-                softmax<D, R, decltype(r)::value>(st, s[r], masked, max(now.lo, rows.lo[r]) - base, min(now.hi, rows.hi[r]) - base,
-                                                  nan, quad, a.qk_scale, p[r]);
-            });
+                static_for<0, R>([&](auto r) {
+                    mark(s[r], max(now.lo, rows.lo[r]) - base, min(now.hi, rows.hi[r]) - base, nan, quad);
+                });
+            }
+            bf16x8_t p[R][2];
+            weights<D, R>(st, s, a.qk_scale, p);
             static_for<0, 2>([&](auto t) {
                 static_for<0, B>([&](auto b) {
-                    const uint32_t code[4] = {vc[t][b][0], vc[t][b][1], vc[t][b][2], vc[t][b][3]};
+                    const uint32_t code[4] = {slot.vc[t][b][0], slot.vc[t][b][1], slot.vc[t][b][2], slot.vc[t][b][3]};
                     uint32_t op[4][4];
-                    value_operands<4>(code, vs[t][b], op);
+                    value_operands<4>(code, slot.vs[t][b], op);
                     static_for<0, 4>([&](auto m) {
                         static_for<0, R>([&](auto r) {
                             st.o[r][b][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_operand(op[m]), p[r][t], st.o[r][b][m], 0, 0, 0);
@@ -403,9 +475,22 @@ __device__ __forceinline__ void narrow(const PageCall &a, const PageWalk &walk, 
                 });
             });
         }
-        if (more) load_values(head);
-        now = next;
-        next = after;
+        load_values(slot, head);
+    };
+    Slot slot[PF];
+    int i = i0 + wave;
+    if (i < i1) {
+        static_for<0, PF>([&](auto n) {
+            slot[n].now = tile_of(walk, i + 4 * n, i1);
+            slot[n].next = tile_of(walk, i + 4 * n + STEP, i1);
+        });
+        static_for<0, PF>([&](auto n) {
+            load_keys(slot[n], head_of(slot[n].now));
+            load_values(slot[n], head_of(slot[n].now));
+            __builtin_amdgcn_sched_barrier(0);   // in the loop's order, so that its waits count as few of them
+        });
+        settle<D, R>(q);   // asked for before the pages
+        for (; i < i1; i += STEP) static_for<0, PF>([&](auto n) { page(slot[n], i + 4 * n); });
     }
     // the four waves' results are one
     static_for<0, R>([&](auto r) {
@@ -468,9 +553,10 @@ __device__ __forceinline__ void wide(const PageCall &a, const PageWalk &walk, in
     constexpr int B = D / 64, UNITS = D >= 128 ? D / 128 : 1;   // pieces of V a wave expands
     constexpr int DW = D == 64 ? 2 : 4;                         // ... dwords of codes a lane has of each
     constexpr int N = KeyShare<D>::N, CH = KeyShare<D>::CH, KT = WideShared<D>::kKeys ? 1 : 4;   // 16-key tiles of K a wave expands
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
     const int64_t page_bytes = (int64_t)a.Hkv * PageLayout<D>::kBytes;
     const uint8_t *pool = a.pool + (int64_t)h * PageLayout<D>::kBytes;
+    const LanePlaces<D> place(lane);
     QueryRow<D> q[R];
     int lo_most = rows.lo[0], hi_least = rows.hi[0], lo_least = rows.lo[0], hi_most = rows.hi[0];
     static_for<0, R>([&](auto r) {
@@ -489,45 +575,50 @@ __device__ __forceinline__ void wide(const PageCall &a, const PageWalk &walk, in
     uint32_t kc[KT][N], ke[CH], vc[UNITS][DW], vs[UNITS][DW / 2];
     uint32_t kn = 0;   // with K's bytes loaded a page later than V's: exponents that tell of NaN
     auto there = [&](const PageTile &t) { return t.id >= 0 && t.id < a.n_pages; };
-    auto head_of = [&](const PageTile &t) { return pool + (int64_t)(there(t) ? t.id : 0) * page_bytes; };
-    const int lane_word = (col * PageLayout<D>::kChunkBlocks + quad) * 4;
+    auto head_of = [&](const PageTile &t) { return pool + (uint64_t)(uint32_t)(there(t) ? t.id : 0) * (uint64_t)page_bytes; };
     auto load_keys = [&](const uint8_t *head) {
-        static_for<0, KT>([&](auto t) { load_codes<D>(head, KT == 1 ? wave : (int)t, col, quad, kc[t]); });
-        load_exponents<D>(head, col, quad, ke);
+        static_for<0, KT>([&](auto t) { load_codes<D>(head, place.key + (KT == 1 ? wave * (8 * D) : t * (8 * D)), kc[t]); });
+        load_exponents<D>(head, place.key_exp, ke);
     };
     // piece u of wave w: D = 64 (32-key tile w / 2, half w % 2 of its keys), else (tile, 64 values) w * UNITS + u
     auto load_values = [&](const uint8_t *head) {
-        if constexpr (KT == 4) kn = *reinterpret_cast<const uint32_t *>(head + PageLayout<D>::kKScale + lane_word);
+        if constexpr (KT == 4) kn = *reinterpret_cast<const uint32_t *>(head + place.key_exp);
         if constexpr (D == 64) {
             const int t = wave >> 1, e = wave & 1;
-            const uint2 c = *reinterpret_cast<const uint2 *>(head + PageLayout<D>::kV + t * 1024 + lane * 16 + e * 8);
+            const uint2 c = *reinterpret_cast<const uint2 *>(head + (place.value + t * 1024 + e * 8));
             vc[0][0] = c.x;
             vc[0][1] = c.y;
-            vs[0][0] = *reinterpret_cast<const uint32_t *>(head + PageLayout<D>::kVScale + ((t * 4 + quad) * 2 + (col >> 3)) * 8 + e * 4);
+            vs[0][0] = *reinterpret_cast<const uint32_t *>(head + (place.value_exp + t * D + e * 4));
         } else {
             static_for<0, UNITS>([&](auto u) {
                 const int n = wave * UNITS + u, t = n / B, b = n % B;
-                const u32x4_t c = *reinterpret_cast<const u32x4_t *>(head + PageLayout<D>::kV + n * 1024 + lane * 16);
-                const uint2 s = *reinterpret_cast<const uint2 *>(head + PageLayout<D>::kVScale + (((t * 4 + quad) * 2 + (col >> 3)) * B + b) * 8);
+                const u32x4_t c = *reinterpret_cast<const u32x4_t *>(head + (place.value + n * 1024));
+                const uint2 s = *reinterpret_cast<const uint2 *>(head + (place.value_exp + t * D + b * 8));
                 static_for<0, 4>([&](auto j) { vc[u][j] = c[(int)j]; });
                 vs[u][0] = s.x;
                 vs[u][1] = s.y;
             });
         }
     };
+    // What of the values' exponents stands for nothing, out of the way.
+    auto clean = [&](const PageTile &t) {
+        static_for<0, UNITS>([&](auto u) {
+            const int n = D == 64 ? wave >> 1 : wave * UNITS + u;
+            static_for<0, DW / 2>([&](auto e) {
+                const int half = D == 64 ? wave & 1 : (int)e;
+                vs[u][e] = finite_scales(vs[u][e], t.pos + 32 * (n / B) + 16 * half + 4 * quad, t.lo, t.hi);
+            });
+        });
+    };
+    auto at_edge = [&](const PageTile &t) { return t.pos < t.lo || t.pos + kPageRows > t.hi; };
     // The wave's share of a page to LDS.
-    auto hand_over = [&](const PageTile &t, uint64_t nan, int at) {
+    auto hand_over = [&](int at) {
         if constexpr (WideShared<D>::kKeys) static_for<0, N>([&](auto n) {
             const float f = __uint_as_float((ke[n / KeyShare<D>::W] >> (8 * wave) & 255u) << 23);
             sh.k[at][wave * N + n][lane] = __builtin_bit_cast(u32x4_t, expand(kc[0][n], f));
         });
-        const bool edge = t.pos < t.lo || t.pos + kPageRows > t.hi;
         static_for<0, UNITS>([&](auto u) {
             const int n = D == 64 ? wave >> 1 : wave * UNITS + u;
-            if (edge || nan) static_for<0, DW / 2>([&](auto e) {
-                const int half = D == 64 ? wave & 1 : (int)e;
-                vs[u][e] = finite_scales(vs[u][e], t.pos + 32 * (n / B) + 16 * half + 4 * quad, t.lo, t.hi);
-            });
             uint32_t op[4][DW];
             value_operands<DW>(vc[u], vs[u], op);
             static_for<0, 4>([&](auto m) {
@@ -542,54 +633,58 @@ __device__ __forceinline__ void wide(const PageCall &a, const PageWalk &walk, in
     PageTile now{-1, 0, 0, 0}, next{-1, 0, 0, 0}, after{-1, 0, 0, 0};
     uint64_t nan = 0;
     if (i0 < i1) {
-        now = tile_of(walk, i0);
+        now = tile_of(walk, i0, i1);
+        next = tile_of(walk, i0 + 1, i1);
+        after = tile_of(walk, i0 + 2, i1);
         load_keys(head_of(now));
         load_values(head_of(now));
-        if (i0 + 1 < i1) next = tile_of(walk, i0 + 1);
         nan = nan_keys(KT == 4 ? kn : ke[0]);
-        hand_over(now, nan, 0);
-        if (i0 + 1 < i1) {
-            if (KT == 1) load_keys(head_of(next));
-            load_values(head_of(next));
-        }
-        if (i0 + 2 < i1) after = tile_of(walk, i0 + 2);
+        if (at_edge(now) || nan) clean(now);
+        hand_over(0);
+        if (KT == 1) load_keys(head_of(next));
+        load_values(head_of(next));
+        settle<D, R>(q);
     }
     for (int i = i0; i < i1; ++i) {
         const int at = (i - i0) & 1;
-        const bool edge = now.pos < now.lo || now.pos + kPageRows > now.hi;
         const bool seen = there(now) && now.pos < hi_most && now.pos + kPageRows > lo_least;   // by some row of the wave
-        f32x4_t s[R][4];
-        uint64_t nan_next = 0;
+        const bool masked = at_edge(now) || now.pos < lo_most || now.pos + kPageRows > hi_least;
+        const uint64_t nan_next = nan_keys(KT == 4 ? kn : ke[0]);
+        if (at_edge(next) || nan_next) clean(next);
         __syncthreads();   // page i is in LDS, and of page i - 1 nothing is read any more
-        if constexpr (KT == 4) {
-            // K is the wave's own: this page's, then the next one's bytes
-            if (seen) static_for<0, 4>([&](auto t) { scores<D, decltype(t)::value, R>(kc[KT == 4 ? (int)t : 0], ke, q, s); });
-            if (i + 1 < i1) load_keys(head_of(next));
+        // the next page is handed over (behind the last one some page, which nobody reads), the one behind it asked for
+        auto go_on = [&]() {
+            hand_over(at ^ 1);
+            if (KT == 1) load_keys(head_of(after));
+            load_values(head_of(after));
+        };
+        if (!seen) {
+            if constexpr (KT == 4) load_keys(head_of(next));
+            go_on();
         } else {
-            if (seen) static_for<0, 4>([&](auto t) {
-                static_for<0, R>([&](auto r) { s[r][t] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
-                static_for<0, N>([&](auto n) {
-                    const bf16x8_t k = __builtin_bit_cast(bf16x8_t, sh.k[at][t * N + n][lane]);
-                    static_for<0, R>([&](auto r) { s[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[r].v[n], s[r][t], 0, 0, 0); });
+            f32x4_t s[R][4];
+            if constexpr (KT == 4) {
+                // K is the wave's own: this page's, then the next one's bytes
+                static_for<0, 4>([&](auto t) { scores<D, decltype(t)::value, R>(kc[KT == 4 ? (int)t : 0], ke, q, s); });
+                load_keys(head_of(next));
+            } else {
+                static_for<0, 4>([&](auto t) {
+                    static_for<0, R>([&](auto r) { s[r][t] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
+                    static_for<0, N>([&](auto n) {
+                        const bf16x8_t k = __builtin_bit_cast(bf16x8_t, sh.k[at][t * N + n][lane]);
+                        static_for<0, R>([&](auto r) { s[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[r].v[n], s[r][t], 0, 0, 0); });
+                    });
                 });
-            });
-        }
-        if (i + 1 < i1) {
-            nan_next = nan_keys(KT == 4 ? kn : ke[0]);
-            hand_over(next, nan_next, at ^ 1);
-            if (i + 2 < i1) {
-                if (KT == 1) load_keys(head_of(after));
-                load_values(head_of(after));
             }
-        }
-        if (seen) {
-            bf16x8_t p[R][2];
-            static_for<0, R>([&](auto r) {
-                const bool masked = edge || now.pos < lo_most || now.pos + kPageRows > hi_least;
+            go_on();
+            if (masked || nan) {
                 const int base = now.pos + 4 * quad;
-                softmax<D, R, decltype(r)::value>(st, s[r], masked, max(now.lo, rows.lo[r]) - base, min(now.hi, rows.hi[r]) - base,
-                                                  nan, quad, a.qk_scale, p[r]);
-            });
+                static_for<0, R>([&](auto r) {
+                    mark(s[r], max(now.lo, rows.lo[r]) - base, min(now.hi, rows.hi[r]) - base, nan, quad);
+                });
+            }
+            bf16x8_t p[R][2];
+            weights<D, R>(st, s, a.qk_scale, p);
             static_for<0, 2>([&](auto t) {
                 static_for<0, B>([&](auto b) {
                     static_for<0, 4>([&](auto m) {
@@ -603,8 +698,7 @@ __device__ __forceinline__ void wide(const PageCall &a, const PageWalk &walk, in
         }
         now = next;
         next = after;
-        after = PageTile{-1, 0, 0, 0};
-        if (i + 3 < i1) after = tile_of(walk, i + 3);
+        after = tile_of(walk, i + 3, i1);
         nan = nan_next;
     }
     static_for<0, R>([&](auto r) {
@@ -767,13 +861,15 @@ __global__ __launch_bounds__(kThreads, 2) void page_attn_kernel(PageArgs args) {
     }
 }
 
-// Joins a row's partial results, a wave a row: blockIdx.y the cell.
-template <int D>
+// Joins rows' partial results, W waves a row: blockIdx.y the cell.  A lane has four values of a row, so that a
+// load of a wave takes 256 / D parts, and up to eight loads are on their way.
+template <int D, int W>
 __global__ __launch_bounds__(kThreads) void page_join_kernel(PageArgs args) {
+    constexpr int L = D / 4, PP = 64 / L, AHEAD = 8;
+    __shared__ f32x4_t s_sum[W == 1 ? 1 : kWaves][L];
     const PageCall &a = args.call;
-    constexpr int V = D / 64;
-    const int ci = blockIdx.y, lane = threadIdx.x & 63, Hq = a.Hkv * a.G;
-    const int row = blockIdx.x * kWaves + (threadIdx.x >> 6);
+    const int ci = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, Hq = a.Hkv * a.G, sub = lane / L, d = lane % L;
+    const int row = W == 1 ? blockIdx.x * kWaves + wave : blockIdx.x, w0 = W == 1 ? 0 : wave;
     if (row >= (int)(args.count_split[ci] & 0xffffu) * Hq) return;
     const int64_t at = (int64_t)(args.cell_tile[ci] >> 24) * a.T * Hq + row;
     const int64_t records = (int64_t)a.C * a.T * Hq * D;
@@ -790,21 +886,32 @@ __global__ __launch_bounds__(kThreads) void page_join_kernel(PageArgs args) {
     float sum = l * w;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    uint64_t some = __ballot(w != 0.f);
-    float o[V] = {};
-    typedef float vec_t __attribute__((ext_vector_type(V)));
-    for (; some; some &= some - 1) {
-        const int p = __builtin_ctzll(some);
-        const float f = __shfl(w, p);
-        if constexpr (V == 1) o[0] += f * (a.part + p * a.part_stride + at * D)[lane];
-        else {
-            const vec_t y = reinterpret_cast<const vec_t *>(a.part + p * a.part_stride + at * D)[lane];
-            static_for<0, V>([&](auto i) { o[i] += f * y[(int)i]; });
-        }
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = w0 * PP + sub; p0 < a.parts; p0 += AHEAD * W * PP) {
+        f32x4_t y[AHEAD];
+        static_for<0, AHEAD>([&](auto k) {
+            const int p = min(p0 + k * (W * PP), a.parts - 1);
+            y[k] = reinterpret_cast<const f32x4_t *>(a.part + p * a.part_stride + at * D)[d];
+        });
+        static_for<0, AHEAD>([&](auto k) {
+            const int p = p0 + k * (W * PP);
+            const float f = __shfl(w, p & 63);
+            if (p < a.parts && f != 0.f) o += f * y[k];   // a part that saw nothing has no values
+        });
     }
+    static_for<0, 4>([&](auto i) {
+#pragma unroll
+        for (int x = L; x < 64; x <<= 1) o[(int)i] += __shfl_xor(o[(int)i], x);
+    });
+    if constexpr (W > 1) {
+        if (lane < L) s_sum[wave][d] = o;
+        __syncthreads();
+        o = s_sum[0][d] + s_sum[1][d] + s_sum[2][d] + s_sum[3][d];
+    }
+    if (w0 > 0 || lane >= L) return;
     const float by = inverse(sum);
-    __bf16 *out = a.out + at * D + lane * V;
-    static_for<0, V>([&](auto i) { out[i] = (__bf16)(o[i] * by); });
+    typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4_t *>(a.out + at * D + 4 * d) = __builtin_convertvector(o * by, bf16x4_t);
     if (lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
@@ -823,8 +930,12 @@ bool launch_page_attn(const PageArgs &args, const splice::PagePlan &p, int most_
     else pick(std::integral_constant<int, 1>{});
     if (hipGetLastError() != hipSuccess) return false;
     if (p.parts == 1) return true;
-    const dim3 join((unsigned)splice::ceil_div((int64_t)most_count * args.call.Hkv * args.call.G, kWaves), (unsigned)args.call.n_active);
-    hipLaunchKernelGGL((page_join_kernel<D>), join, block, 0, stream, args);
+    // four waves a row where the rows alone do not fill the GPU (32 rows of 64 parts: one wave each, one load at a time 19.6 us)
+    const int64_t rows = (int64_t)most_count * args.call.Hkv * args.call.G;
+    const bool few = rows * args.call.n_active <= 1024;
+    const dim3 join((unsigned)(few ? rows : (rows + kWaves - 1) / kWaves), (unsigned)args.call.n_active);
+    if (few) hipLaunchKernelGGL((page_join_kernel<D, kWaves>), join, block, 0, stream, args);
+    else hipLaunchKernelGGL((page_join_kernel<D, 1>), join, block, 0, stream, args);
     return hipGetLastError() == hipSuccess;
 }
 

@@ -65,69 +65,112 @@ inline int own_list(const splice_shape &sh, int window, const PageCell &c, int t
     return sh.donor_kind == SPLICE_DONOR_ZERO ? n : n + page_pages(std::max(v0, sh.span_lo), sh.span_hi);
 }
 
-inline PagePlan page_plan(const splice_shape &sh, const splice_call &call, const splice_pages &pg, const PageCell *cells, int n,
-                          int units) {
-    PagePlan p{};
-    const int G = group_of(sh), D = sh.head_dim, Hkv = sh.n_kv_heads;
-    int most_rows = 0;
-    for (int i = 0; i < n; ++i) most_rows = std::max(most_rows, cells[i].count * G);
-    const int seen = call.window > 0 ? std::min(sh.prompt_len, call.window) : sh.prompt_len;
-    p.own = most_rows <= 16 ? 1 : (most_rows <= 64 ? (D <= 128 ? 2 : 1) : 0);
-    p.own_rows = p.own ? page_narrow_rows(D, p.own) : page_wide_rows(D);
-    // tiles of several cells' rows save walks over the prompt only where a cell's own rows do not fill them
-    p.shared = n > 1 && most_rows <= 64 && (int64_t)(n - 1) * seen * D >= (int64_t)5 << 18;
-    // own tiles, their number and pages
-    int64_t pages = 0;
-    int longest = 0;
-    p.own_each = -1;
+// What a walk is taken to cost, in us, fitted to sweeps of the part lengths of ten shapes (D = 128; pages of other
+// heads by their bytes): a page takes a work group `alone` where the GPU has room for all of them, and all of
+// them take `rate` pages a us where it has not.  A narrow work group's four waves take a page each, a wide one's all the
+// same page for eight times the rows.
+struct PageCost {
+    double alone, rate;
+};
+inline PageCost page_cost(int D, int own) {
+    const double size = D / 128.0;
+    if (own == 1) return {D == 256 ? 0.45 : 0.24 * size, 588 / size};
+    if (own == 2) return {0.35 * size, 400 / size};
+    return {1.55 * size, 216 / size};
+}
+constexpr double kPageStart = 4;       // a launch and a work group's first bytes
+constexpr double kPageNext = 2;        // what a work group costs that follows another
+constexpr double kPageJoin = 4;        // a second launch, and the partial results' way there and back:
+constexpr double kPageJoinRate = 4e6;  // bytes a us
+
+struct PageWork {
+    int tiles, each, longest;
+    int64_t pages;   // of all tiles of a KV head
+};
+
+inline PageWork own_work(const splice_shape &sh, const splice_call &call, const PageCell *cells, int n, int own_rows, bool shared) {
+    PageWork w{0, -1, 0, 0};
+    const int G = group_of(sh), per_tile = own_rows / G;
     for (int i = 0; i < n; ++i) {
         const PageCell &c = cells[i];
         int tiles = 0;
         auto add = [&](int t0, int t1, bool spliced) {
-            const int rows = (t1 - t0) * G, of = ceil_div(rows, p.own_rows), per_tile = p.own_rows / G;
+            const int of = ceil_div((int64_t)(t1 - t0) * G, own_rows);
             tiles += of;
-            // the last and the first tile's lists bound the others'
-            const int hi = own_list(sh, call.window, c, std::max(t0, t1 - per_tile), t1, spliced, p.shared);
-            const int lo = own_list(sh, call.window, c, t0, std::min(t1, t0 + per_tile), spliced, p.shared);
-            longest = std::max(longest, std::max(lo, hi));
-            pages += (int64_t)of * (lo + hi) / 2;
+            const int hi = own_list(sh, call.window, c, std::max(t0, t1 - per_tile), t1, spliced, shared);
+            const int lo = of == 1 ? hi : own_list(sh, call.window, c, t0, std::min(t1, t0 + per_tile), spliced, shared);
+            w.longest = std::max(w.longest, std::max(lo, hi));
+            w.pages += (int64_t)of * (lo + hi) / 2;
         };
-        if (p.shared) add(0, c.count, false);
-        else {
-            if (c.split > 0) add(0, c.split, false);
-            if (c.split < c.count) add(c.split, c.count, true);
-        }
-        p.own_each = p.own_each == -1 || p.own_each == tiles ? tiles : 0;
-        p.own_tiles += tiles;
+        const int split = shared ? c.count : c.split;
+        if (split > 0) add(0, split, false);
+        if (split < c.count) add(split, c.count, true);
+        w.each = w.each == -1 || w.each == tiles ? tiles : 0;
+        w.tiles += tiles;
     }
-    int cap = page_most_parts(sh, pg);
-    // the prompt's tiles
-    if (p.shared) {
-        for (int i = 0; i < n; ++i) {
-            p.rows_u += cells[i].split * G;
-            p.rows_s += (cells[i].count - cells[i].split) * G;
-        }
-        const int RT = page_wide_rows(D), list = page_pages(0, seen) + 2;
-        p.tiles_u = ceil_div(p.rows_u, RT);
-        p.tiles_s = ceil_div(p.rows_s, RT);
-        const int64_t tiles = (int64_t)(p.tiles_u + p.tiles_s) * Hkv;
-        int parts = (int)std::min<int64_t>(std::max(1, cap / 2), std::max<int64_t>(1, 2 * units / tiles));
-        p.prompt_per = call.split_keys ? call.split_keys / kPageRows : std::max(4, ceil_div(list, parts));
-        p.prompt_parts = std::min(ceil_div(list, p.prompt_per), std::max(1, cap - 1));
-        p.prompt_per = ceil_div(list, p.prompt_parts);
-        cap = std::max(1, cap - p.prompt_parts);
+    return w;
+}
+
+inline PagePlan page_plan(const splice_shape &sh, const splice_call &call, const splice_pages &pg, const PageCell *cells, int n,
+                          int units) {
+    static const int counts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
+    const int G = group_of(sh), D = sh.head_dim, Hkv = sh.n_kv_heads, cap = page_most_parts(sh, pg);
+    int most_rows = 0, rows_u = 0, rows_s = 0;
+    for (int i = 0; i < n; ++i) {
+        most_rows = std::max(most_rows, cells[i].count * G);
+        rows_u += cells[i].split * G;
+        rows_s += (cells[i].count - cells[i].split) * G;
     }
-    const int64_t target = (int64_t)units * (p.own ? 3 : 2);
-    const int64_t blocks = (int64_t)p.own_tiles * Hkv;
-    int per = (int)std::max<int64_t>(p.own ? 4 : 8, (pages * Hkv + target - 1) / target);
-    if (blocks >= 2 * target) per = std::max(1, longest);   // enough work groups without a cut
-    if (call.split_keys) per = call.split_keys / kPageRows;
-    p.own_parts = std::min(std::max(1, ceil_div(longest, per)), cap);
-    p.own_per = std::max(1, ceil_div(longest, p.own_parts));
-    p.parts = p.own_parts + p.prompt_parts;
-    p.blocks = blocks * p.own_parts + (int64_t)(p.tiles_u + p.tiles_s) * Hkv * p.prompt_parts;
-    p.bytes = p.parts > 1 ? p.parts * page_part_bytes(sh, pg) : 0;
-    return p;
+    const int own = most_rows <= 16 ? 1 : (most_rows <= 64 ? (D <= 128 ? 2 : 1) : 0);
+    const int own_rows = own ? page_narrow_rows(D, own) : page_wide_rows(D);
+    const PageCost cost = page_cost(D, own), wide = page_cost(D, 0);
+    const double slots = 2.0 * units, result = (double)(rows_u + rows_s) * Hkv * D * 4 * 2 / kPageJoinRate;
+    const int seen = call.window > 0 ? std::min(sh.prompt_len, call.window) : sh.prompt_len, list = page_pages(0, seen) + 2;
+    const int tiles_u = ceil_div(rows_u, page_wide_rows(D)), tiles_s = ceil_div(rows_s, page_wide_rows(D));
+    const int forced = call.split_keys / kPageRows;
+    PagePlan best{};
+    double least = 0;
+    bool any = false;
+    // tiles of several cells' rows save walks over the prompt where a cell's own rows do not fill them
+    for (int shared = 0; shared <= (n > 1 && own && seen > 0 ? 1 : 0); ++shared) {
+        const PageWork w = own_work(sh, call, cells, n, own_rows, shared != 0);
+        const double own_pages = (double)w.pages * Hkv, prompt_tiles = shared ? (double)(tiles_u + tiles_s) * Hkv : 0;
+        int last_prompt = 0;
+        for (int pc : counts) {
+            int per_prompt = shared ? (forced ? forced : ceil_div(list, pc)) : 0;
+            const int prompt_parts = shared ? std::min(ceil_div(list, per_prompt), cap - 1) : 0;
+            if (shared) per_prompt = ceil_div(list, prompt_parts);
+            if (pc > 1 && prompt_parts == last_prompt) break;   // as before: no more parts than pages, or than there is room for
+            last_prompt = prompt_parts;
+            int last_own = 0;
+            for (int oc : counts) {
+                int per = forced ? forced : std::max(1, ceil_div(w.longest, oc));
+                const int parts = std::min(std::max(1, ceil_div(w.longest, per)), cap - prompt_parts);
+                per = std::max(1, ceil_div(w.longest, parts));
+                if (oc > 1 && parts == last_own) break;
+                last_own = parts;
+                // work groups with pages: every tile's list is cut after `per`
+                const double groups = std::max((double)w.tiles * Hkv, std::min((double)w.tiles * Hkv * parts, own_pages / per + 0.5 * w.tiles * Hkv));
+                const double prompts = prompt_tiles * prompt_parts, all = groups + prompts;
+                double t = own_pages / std::min(groups / cost.alone, cost.rate) + 0.5 * per * cost.alone;
+                if (shared) {
+                    t += prompt_tiles * list / std::min(prompts / wide.alone, wide.rate);
+                    t = std::max(t, per_prompt * wide.alone * 1.3);
+                }
+                t += kPageStart + kPageNext * std::max(0.0, all - slots) / slots;
+                if (parts + prompt_parts > 1) t += kPageJoin + result * (parts + prompt_parts);
+                if (!any || t < least) {
+                    any = true;
+                    least = t;
+                    best = PagePlan{own, shared != 0, own_rows, w.tiles, w.each, per, parts, shared ? rows_u : 0, shared ? rows_s : 0,
+                                    shared ? tiles_u : 0, shared ? tiles_s : 0, per_prompt, prompt_parts, parts + prompt_parts, 0, 0};
+                }
+            }
+        }
+    }
+    best.blocks = (int64_t)best.own_tiles * Hkv * best.own_parts + (int64_t)(best.tiles_u + best.tiles_s) * Hkv * best.prompt_parts;
+    best.bytes = best.parts > 1 ? best.parts * page_part_bytes(sh, pg) : 0;
+    return best;
 }
 
 }  // namespace splice
