@@ -389,8 +389,8 @@ struct NarrowShared {
 };
 
 // Pages that a wave has in registers or on their way there.  Two hide the memory's latency behind the other's
-// products (64 cells of 8k rows, D = 128: one 178 us, two PF2TIME); what they take of registers beside two sets
-// of rows, or rows of 256, leaves room for one.
+// products (64 cells of 8k rows, D = 128: 181 us with one, 126 with two); what they take of registers beside two
+// sets of rows, or rows of 256, leaves room for one.
 constexpr int narrow_pages(int D, int R) { return D == 64 || (D == 128 && R == 1) ? 2 : 1; }
 
 // Pages [i0, i1) of the walk for R x 16 rows, the waves a page each in turn.

@@ -77,12 +77,12 @@ def _tables(t, name: str, shape, pages, dev) -> int:
 
 
 def _pool(t, shape, pages, dev) -> int:
-    return T._ptr(t, "pool", pages.n_pages * splice_page_bytes(shape), S._torch.uint8, dev)
+    return T._ptr(t, "pool", pages.n_pages * (68 * shape.n_kv_heads * shape.head_dim), S._torch.uint8, dev)
 
 
 def _pools(t, shape, pages, dev) -> Tuple[int, int]:
     """(address, bytes from one layer to the next) of uint8 [n_layers][n_pages][page_bytes], each layer dense."""
-    dims = (shape.n_layers, pages.n_pages, splice_page_bytes(shape))
+    dims = (shape.n_layers, pages.n_pages, 68 * shape.n_kv_heads * shape.head_dim)
     if t is None or t.get_device() != dev[0]:
         raise ValueError(f"pools must be a tensor on {dev[1]}")
     if t.dtype is not S._torch.uint8:
