@@ -67,9 +67,16 @@ struct PageWalk {
 };
 
 struct PageTile {
-    int id;          // page, -1: none
-    int pos, lo, hi; // position of its first row, which of its positions count
+    int id;               // page, -1: none
+    int pos, lo, hi;      // position of its first row, which of its positions count
+    const int32_t *entry; // in its table
+    int end;              // the walk's number of the page behind its run
 };
+
+// Nobody writes tables meanwhile: scalar loads, which no wait for pages' bytes waits for.
+__device__ __forceinline__ int entry_of(const int32_t *table) {
+    return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)table;
+}
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -86,17 +93,20 @@ __device__ __forceinline__ PageTile tile_of(const PageWalk &w, int at, int end) 
     const int32_t *table = t0;
     t.lo = l0;
     t.hi = h0;
+    t.end = f1;
     if (i >= f1) {
         page = p1 + i - f1;
         table = t1;
         t.lo = l1;
         t.hi = h1;
+        t.end = f2;
     }
     if (i >= f2) {
         page = p2 + i - f2;
         table = t2;
         t.lo = l2;
         t.hi = h2;
+        t.end = f3;
     }
     t.pos = page * kPageRows;
     if (i >= f3) {
@@ -105,11 +115,23 @@ __device__ __forceinline__ PageTile tile_of(const PageWalk &w, int at, int end) 
         t.pos = page * kPageRows + w.shift;
         t.lo = l3;
         t.hi = h3;
+        t.end = w.n;
     }
-    // nobody writes tables meanwhile: a scalar load, which no wait for pages' bytes waits for
-    t.id = ((const __attribute__((address_space(4))) int32_t *)(uintptr_t)table)[page];
+    t.entry = table + page;
+    t.id = entry_of(t.entry);
     if (at >= end) t.id = -1;
     return t;
+}
+
+// Page `at`, STEP pages behind t (pages of one run lie evenly apart: the usual case).
+template <int STEP>
+__device__ __forceinline__ PageTile tile_after(const PageWalk &w, const PageTile &t, int at, int end) {
+    if (at >= min(t.end, end)) return tile_of(w, at, end);
+    PageTile n = t;
+    n.pos += STEP * kPageRows;
+    n.entry += STEP;
+    n.id = entry_of(n.entry);
+    return n;
 }
 
 // ---------------------------------------------------------------- operands
@@ -444,7 +466,7 @@ __device__ __forceinline__ void narrow(const PageCall &a, const PageWalk &walk, 
         const uint8_t *head = head_of(slot.next);
         load_keys(slot, head);
         slot.now = slot.next;
-        slot.next = tile_of(walk, i + 2 * STEP, i1);
+        slot.next = tile_after<STEP>(walk, slot.now, i + 2 * STEP, i1);
         if (there(now)) {
             const bool edge = now.pos < now.lo || now.pos + kPageRows > now.hi;
             if (edge || nan || now.pos < lo_most || now.pos + kPageRows > hi_least) {
@@ -482,7 +504,7 @@ __device__ __forceinline__ void narrow(const PageCall &a, const PageWalk &walk, 
     if (i < i1) {
         static_for<0, PF>([&](auto n) {
             slot[n].now = tile_of(walk, i + 4 * n, i1);
-            slot[n].next = tile_of(walk, i + 4 * n + STEP, i1);
+            slot[n].next = tile_after<STEP>(walk, slot[n].now, i + 4 * n + STEP, i1);
         });
         static_for<0, PF>([&](auto n) {
             load_keys(slot[n], head_of(slot[n].now));
@@ -630,7 +652,7 @@ __device__ __forceinline__ void wide(const PageCall &a, const PageWalk &walk, in
             });
         });
     };
-    PageTile now{-1, 0, 0, 0}, next{-1, 0, 0, 0}, after{-1, 0, 0, 0};
+    PageTile now{}, next{}, after{};
     uint64_t nan = 0;
     if (i0 < i1) {
         now = tile_of(walk, i0, i1);
@@ -698,7 +720,7 @@ __device__ __forceinline__ void wide(const PageCall &a, const PageWalk &walk, in
         }
         now = next;
         next = after;
-        after = tile_of(walk, i + 3, i1);
+        after = tile_after<1>(walk, next, i + 3, i1);
         nan = nan_next;
     }
     static_for<0, R>([&](auto r) {
