@@ -79,7 +79,8 @@ SPLICE_API int64_t splice_page_bytes(const splice_shape *shape);
  *                  rounding); q_out may be q when q is dense;
  *   row s_c + t  = the rotated k[c][t] and v[c][t] in 4 bits (rotated in 64 bits).
  * q, k, v, their strides, pos (device int64 [C][T], or NULL) and freq: as
- * splice_tree_append takes them, with T = pages->n_tokens.  A page that is written
+ * splice_tree_append takes them, with T = pages->n_tokens; q and q_out may both be NULL
+ * (then only rows are written).  A page that is written
  * to is in one cell's table only (splice_page_fork sees to that).
  */
 SPLICE_API int32_t splice_page_append(const splice_shape *shape, const splice_pages *pages, const splice_rope *rope,

@@ -8,7 +8,7 @@ in include/splice_attn.h; ``splice`` is its ctypes binding.  ``tree`` binds
 include/splice_tree.h: several candidate tokens per cell judged in one pass.
 ``pages`` binds include/splice_pages.h: caches in 4 bits, in pages that cells share.
 """
-from .pages import (SPLICE_MAX_PAGE_TOKENS, SPLICE_PAGE_ROWS, SplicePages, make_pages, splice_page_append,
+from .pages import (SPLICE_MAX_PAGE_TOKENS, SPLICE_PAGE_ROWS, PageCache, SplicePages, make_pages, splice_page_append,
                     splice_page_attn, splice_page_attn_workspace_bytes, splice_page_bytes, splice_page_compact,
                     splice_page_fork, splice_page_read)
 from .splice import (EXPORTS, LIB_PATH, SPLICE_BF16, SPLICE_DONOR_BUFFER, SPLICE_DONOR_ZERO,

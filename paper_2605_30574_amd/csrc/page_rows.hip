@@ -207,25 +207,26 @@ int32_t splice_page_append(const splice_shape *shape, const splice_pages *pages,
         return SPLICE_EINVAL;
     if (rope->rotary_dim < 0 || rope->rotary_dim > D || rope->rotary_dim % 16) return SPLICE_ESHAPE;
     if (sh.n_cells == 0) return SPLICE_OK;
-    if (!tables || !q || !k || !v || !q_out || !pool || (rope->rotary_dim > 0 && !freq)) return SPLICE_EINVAL;
+    const int Hq = q || q_out ? sh.n_q_heads : 0;   // none: only rows are written
+    if (!tables || !k || !v || !pool || (Hq > 0 && (!q || !q_out)) || (rope->rotary_dim > 0 && !freq)) return SPLICE_EINVAL;
     if (!splice::aligned(tables, 4) || !splice::aligned(pos, 8) || !splice::aligned(freq, 8)) return SPLICE_EINVAL;
     const void *ptrs[] = {q, k, v, q_out, pool};
     for (const void *p : ptrs)
         if (!splice::aligned(p, 16)) return SPLICE_EINVAL;
     const int64_t most = (int64_t)1 << 32;
-    if (q_stride < (int64_t)sh.n_q_heads * D || k_stride < (int64_t)sh.n_kv_heads * D ||
+    if (q_stride < (int64_t)Hq * D || k_stride < (int64_t)sh.n_kv_heads * D ||
         v_stride < (int64_t)sh.n_kv_heads * D || q_stride > most || k_stride > most || v_stride > most || q_stride % 8 ||
         k_stride % 8 || v_stride % 8)
         return SPLICE_ESHAPE;
-    if (q == q_out && q_stride != (int64_t)sh.n_q_heads * D) return SPLICE_EINVAL;
+    if (Hq > 0 && q == q_out && q_stride != (int64_t)Hq * D) return SPLICE_EINVAL;
     const int n = splice::cells_with_tokens(sh, *pages, cell_step, cell_new);
     if (n == 0) return SPLICE_OK;
     const dim3 grid((unsigned)(n * pages->n_tokens),
-                    (unsigned)splice::ceil_div(sh.n_q_heads + sh.n_kv_heads, kRowThreads / (D / 8)));
+                    (unsigned)splice::ceil_div(Hq + sh.n_kv_heads, kRowThreads / (D / 8)));
     splice::with_head_dim(D, n, [&](auto d, auto room) {
         PageAppendArgs<decltype(room)::value> a{
             (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, (__bf16 *)q_out, (uint8_t *)pool, tables, pos, freq,
-            q_stride, k_stride, v_stride, pages->n_tokens, sh.n_q_heads, sh.n_kv_heads, sh.prompt_len, rope->rotary_dim / 2,
+            q_stride, k_stride, v_stride, pages->n_tokens, Hq, sh.n_kv_heads, sh.prompt_len, rope->rotary_dim / 2,
             rope->layout == SPLICE_ROPE_INTERLEAVED, pages->n_pages, pages->table_len, rope->mscale, {}};
         splice::list_page_cells(sh, *pages, cell_step, cell_new, a.cells);
         hipLaunchKernelGGL((page_append_kernel<decltype(d)::value, decltype(room)::value>), grid, dim3(kRowThreads), 0,

@@ -14,6 +14,8 @@ tiles for are this library's kernels too (``include/splice_decoder.h``); the
 other products, and passes with other weights, are PyTorch operations.
 ``SweepDecoder.score_tree`` is a pass over a tree of candidate tokens per cell
 (``tree``): what the model says about each of them, without a pass per token.
+``SweepDecoder.page_logits`` is a pass over caches in 4 bits, in pages that the
+cells share (``pages``).
 
 Readings of what the paper leaves to the model (the same on the CPU
 reference in ``oracle.decoder``):
@@ -34,6 +36,7 @@ import torch
 from torch.autograd import forward_ad
 from torch.utils._device import DeviceContext
 
+from . import pages as P
 from . import splice as S
 from . import tree as T
 
@@ -136,6 +139,15 @@ class DecoderTree(NamedTuple):
     workspace: torch.Tensor   # of one pass at a time
     freq: torch.Tensor        # float64 [D / 2], of the rotary positions
     parents: np.ndarray       # int64 [C][T]
+
+
+class DecoderPages(NamedTuple):
+    """A cache in 4-bit pages on the decoder's device, and what passes of n tokens a cell over it need (SweepDecoder.make_pages)."""
+    cache: P.PageCache
+    spec: P.SplicePages
+    depth: torch.Tensor       # int32 [C][n]: 0, 1, ...
+    workspace: torch.Tensor   # of one pass at a time
+    freq: torch.Tensor        # float64 [D / 2], of the rotary positions
 
 
 def accept(parents: np.ndarray, tokens: np.ndarray, first: np.ndarray, best: np.ndarray):
@@ -347,10 +359,10 @@ class SweepDecoder:
         pos = torch.stack(pos, 1).gather(1, tree.depth.clamp(min=0).to(torch.int64))
         return pos.to(torch.float64 if pos.is_floating_point() else torch.int64)
 
-    def _turns(self, tree: DecoderTree, steps: np.ndarray, pos: Optional[torch.Tensor]):
-        """(cos, sin) float32 [C][T][1][D / 2] of the nodes' positions: pos [C][T], or T_p + step + depth, whose T_p + step
-        is the cells' (from the steps by value, so that a pass can be captured), the depth's angle added to it."""
-        C, D, (_, dev) = self.C, self.w.head_dim, T._anchor(tree.depth, "tree.depth")
+    def _turns(self, tree, steps: np.ndarray, pos: Optional[torch.Tensor]):
+        """(cos, sin) float32 [C][T][1][D / 2] of the nodes' (or tokens') positions: pos [C][T], or T_p + step + depth, whose
+        T_p + step is the cells' (from the steps by value, so that a pass can be captured), the depth's angle added to it."""
+        C, D, (_, dev) = self.C, self.w.head_dim, T._anchor(tree.depth, "depth")
         ang = (tree.depth if pos is None else pos).to(torch.float64)[:, :, None, None] * tree.freq
         cos, sin = torch.cos(ang).float(), torch.sin(ang).float()
         if pos is not None or C == 0:
@@ -369,38 +381,51 @@ class SweepDecoder:
         gives for that step), behind the steps[c] rows of the cell's generated caches and its ancestors.  Its K/V become row
         steps[c] + t, so steps[c] + T must not pass the caches' rows; cells with a negative step are skipped.  Rows of
         padding and of skipped cells hold no meaning (their tokens are any of the vocabulary).  No gradients."""
-        w, m, wt = self.w, self.m, self.wt
+        w = self.w
         C, Hq, Hkv, D, n = self.C, w.n_q_heads, w.n_kv_heads, w.head_dim, tree.spec.n_nodes
         if tuple(tokens.shape) != (C, n):
             raise ValueError(f"tokens has shape {tuple(tokens.shape)}, expected ({C}, {n})")
         st, _ = S._steps(steps, C)
         pos = self._node_positions(tree, st)
-        whole = pos is None or not pos.is_floating_point()
-        x = wt["embed"][tokens.reshape(-1)]
-        cdt, dev, rows = x.dtype, x.device, C * n
-        rope_of, unturned, bf16 = T.make_rope("half", D), T.make_rope("half", 0), torch.bfloat16
+        x = self.wt["embed"][tokens.reshape(-1)]
+        dev, bf16 = x.device, torch.bfloat16
         out = torch.zeros((C, n, Hq, D), dtype=bf16, device=dev)
         lse = torch.empty((C, n, Hq), dtype=torch.float32, device=dev)
         exps = ("gen_k_exp", "gen_v_exp") if tree.spec.kv_format == T.SPLICE_KV_E4M3 else ()
-        fused = self._fused(x, None, rows) and x.shape[1] <= 8192   # SPLICE_ADD_NORM_MAX_D
-
-        turns = None   # (cos, sin) of the nodes' positions, where products of other types need them
+        turned = self._turner(tree, st, pos)
 
         def attend(l, q, k, v):
-            nonlocal turns
             c = self.caches[l]
             e = [c[name] for name in exps] or [None, None]
             q, k, v = q.view(C, n, Hq, D), k.view(C, n, Hkv, D), v.to(bf16).view(C, n, Hkv, D)
-            rotary, freq, at = rope_of, tree.freq, pos
-            # of more bits: rotated before they are rounded, as in forward; and the kernel's positions are whole numbers
-            if q.dtype != bf16 or k.dtype != bf16 or not whole:
-                turns = turns or self._turns(tree, st, pos)
-                q, k = (_rotated(y.float(), *turns).to(bf16) for y in (q, k))
-                rotary, freq, at = unturned, None, None
+            q, k, rotary, freq, at = turned(q, k)
             T.splice_tree_append(self.shape, tree.spec, rotary, freq, st, tree.depth, q, k, v, q, c["gen_k"], c["gen_v"], *e, pos=at)
             T.splice_tree_attn(self.shape, self.calls[l], tree.spec, self.lw, st, tree.depth, tree.visible, q, c["clean_k"],
                                c["clean_v"], c["donor_k"], c["donor_v"], c["gen_k"], c["gen_v"], *e, out, lse, tree.workspace)
-            return out.view(rows, Hq * D)
+            return out.view(C * n, Hq * D)
+
+        return self._pass(x, attend)
+
+    def _turner(self, tree, st: np.ndarray, pos: Optional[torch.Tensor]):
+        """What a pass's entries take of q and k [C][n][..][D]: (q, k, rope, freq, pos)."""
+        D, bf16 = self.w.head_dim, torch.bfloat16
+        rope_of, unturned, whole = T.make_rope("half", D), T.make_rope("half", 0), pos is None or not pos.is_floating_point()
+        turns = None   # (cos, sin) of the positions, where products of other types need them
+
+        def turned(q, k):
+            nonlocal turns
+            # of more bits: rotated before they are rounded, as in forward; and the kernel's positions are whole numbers
+            if q.dtype != bf16 or k.dtype != bf16 or not whole:
+                turns = turns or self._turns(tree, st, pos)
+                return *(_rotated(y.float(), *turns).to(bf16) for y in (q, k)), unturned, None, None
+            return q, k, rope_of, tree.freq, pos
+        return turned
+
+    def _pass(self, x: torch.Tensor, attend) -> torch.Tensor:
+        """Logits [rows][V] of embedded tokens x [rows][d]; attend(l, q, k, v): the layer's attention over them."""
+        m, wt = self.m, self.wt
+        cdt, dev, rows, bf16 = x.dtype, x.device, x.shape[0], torch.bfloat16
+        fused = self._fused(x, None, rows) and x.shape[1] <= 8192   # SPLICE_ADD_NORM_MAX_D
 
         if not fused:
             x = x.float()
@@ -453,6 +478,60 @@ class SweepDecoder:
         for c in self.caches:
             e = [c[name] for name in ("gen_k_exp", "gen_v_exp")] if tree.spec.kv_format == T.SPLICE_KV_E4M3 else []
             T.splice_tree_keep(self.shape, tree.spec, steps, keep, c["gen_k"], c["gen_v"], *e)
+
+    # ------------------------------------------------------------- caches in 4-bit pages
+
+    def make_pages(self, n_tokens: int = 1, n_pages: Optional[int] = None, cache: Optional[P.PageCache] = None) -> DecoderPages:
+        """A cache in 4-bit pages for passes of ``n_tokens`` tokens a cell (``page_logits``), the prompts of ``caches`` in it,
+        or passes of another number of tokens over the cache of an earlier one.  ``n_pages``: pages of each layer, by default
+        as many as all cells can fill.  Passes over one object share its workspace: order them on one stream."""
+        w, dev = self.w, self.device
+        if cache is None:
+            prompt, rows = -(-w.prompt_len // P.SPLICE_PAGE_ROWS), -(-w.n_steps // P.SPLICE_PAGE_ROWS)
+            cache = P.PageCache(self.C, self.N, w.n_q_heads, w.n_kv_heads, w.head_dim, w.prompt_len, w.span, w.n_steps,
+                                2 * prompt + self.C * rows if n_pages is None else n_pages, w.donor == "zero", dev)
+            for l, c in enumerate(self.caches):
+                cache.load_prompt(l, c["clean_k"], c["clean_v"])
+                if w.donor != "zero":
+                    cache.load_prompt(l, c["donor_k"], c["donor_v"], donor=True)
+        spec = cache.pages(n_tokens)
+        need = max((P.splice_page_attn_workspace_bytes(cache.shape, call, spec) for call in self.calls), default=0)
+        depth = torch.arange(n_tokens, dtype=torch.int32, device=dev).repeat(self.C, 1)
+        return DecoderPages(cache, spec, depth, torch.empty(need, dtype=torch.uint8, device=dev),
+                            torch.from_numpy(T.rope_frequencies(w.head_dim, float(self.m.rope_theta))[0]).to(dev))
+
+    @torch.no_grad()
+    def page_logits(self, tokens: torch.Tensor, pages: DecoderPages, steps: np.ndarray, new=None) -> torch.Tensor:
+        """Logits [C * n][V] (bfloat16 where the head's product is, else float32) of one pass over n tokens a cell: token t of
+        cell c is tokens[c][t] (int64) at decode step steps[c] + t, behind the cell's steps[c] rows and the tokens before it;
+        its K/V become row steps[c] + t, for which the cell has its pages (``pages.cache.reserve``, ``fork``: rows without
+        one are dropped).  ``new``: how many tokens each cell has (host int32 [C]; all n without); cells with a negative
+        step are skipped.  Logits of skipped cells and of tokens behind new[c] hold no meaning.  No gradients."""
+        w, cache = self.w, pages.cache
+        C, Hq, Hkv, D, n = self.C, w.n_q_heads, w.n_kv_heads, w.head_dim, pages.spec.n_tokens
+        if tuple(tokens.shape) != (C, n):
+            raise ValueError(f"tokens has shape {tuple(tokens.shape)}, expected ({C}, {n})")
+        st, _ = S._steps(steps, C)
+        pos = None
+        if getattr(self.positions, "__func__", None) is not SweepDecoder.positions:   # a decoder's own, asked step by step
+            pos = torch.stack([self.positions(np.where(st >= 0, st + t, st)) for t in range(n)], 1)
+            pos = pos.to(torch.float64 if pos.is_floating_point() else torch.int64)
+        x = self.wt["embed"][tokens.reshape(-1)]
+        bf16 = torch.bfloat16
+        out = torch.zeros((C, n, Hq, D), dtype=bf16, device=x.device)
+        lse = torch.empty((C, n, Hq), dtype=torch.float32, device=x.device)
+        turned = self._turner(pages, st, pos)
+
+        def attend(l, q, k, v):
+            q, k, v = q.view(C, n, Hq, D), k.view(C, n, Hkv, D), v.to(bf16).view(C, n, Hkv, D)
+            q, k, rotary, freq, at = turned(q, k)
+            pool = cache.pools[l]
+            P.splice_page_append(cache.shape, pages.spec, rotary, freq, st, new, cache.tables, q, k, v, q, pool, pos=at)
+            P.splice_page_attn(cache.shape, self.calls[l], pages.spec, self.lw, st, new, cache.tables, cache.clean_table,
+                               cache.donor_table, q, pool, out, lse, pages.workspace)
+            return out.view(C * n, Hq * D)
+
+        return self._pass(x, attend)
 
     def step(self, tokens: torch.Tensor, steps: np.ndarray, pos: Optional[torch.Tensor] = None):
         """One decode pass: (next tokens [C] int64, logits [C][V]); of equal

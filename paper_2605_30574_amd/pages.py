@@ -100,12 +100,15 @@ def _pools(t, shape, pages, dev) -> Tuple[int, int]:
 def splice_page_append(shape, pages, rope, freq, cell_step, cell_new, tables, q, k, v, q_out, pool, pos=None,
                        stream=None) -> None:
     """Rotate the tokens' ``q`` [C][T][Hq][D] into ``q_out`` and write their rotated ``k`` and their ``v``
-    ([C][T][Hkv][D]) as rows s_c .. of the cells, in 4 bits (``cell_new``: how many of each cell, None for all T)."""
+    ([C][T][Hkv][D]) as rows s_c .. of the cells, in 4 bits (``cell_new``: how many of each cell, None for all T).
+    ``q`` and ``q_out`` may both be None: then only rows are written."""
     lib = _library()
-    dev = T._anchor(q_out, "q_out")
+    dev = T._anchor(pool, "pool")
     n, C, t = pages.n_tokens, shape.n_cells, S._torch
-    qo = T._ptr(q_out, "q_out", C * n * shape.n_q_heads * shape.head_dim, t.bfloat16, dev)
-    qp, qs = T._rows(q, "q", shape, n, shape.n_q_heads, dev)
+    qo, qp, qs = None, None, 0
+    if q is not None or q_out is not None:
+        qo = T._ptr(q_out, "q_out", C * n * shape.n_q_heads * shape.head_dim, t.bfloat16, dev)
+        qp, qs = T._rows(q, "q", shape, n, shape.n_q_heads, dev)
     kp, ks = T._rows(k, "k", shape, n, shape.n_kv_heads, dev)
     vp, vs = T._rows(v, "v", shape, n, shape.n_kv_heads, dev)
     tp, pl = _tables(tables, "tables", shape, pages, dev), _pool(pool, shape, pages, dev)
@@ -185,3 +188,102 @@ def splice_page_compact(shape, pages, cell_step, keep, tables, pools, stream=Non
     pl, stride = _pools(pools, shape, pages, dev)
     S._check(lib.splice_page_compact(shape, pages, T._steps(cell_step, shape.n_cells), kp, tp, pl, stride,
                                      T._stream(stream, dev)), "splice_page_compact")
+
+
+# ------------------------------------------------------------------ a sweep's cache
+
+class PageCache:
+    """The pages of C sweep cells and of the prompts that they share, for all layers: ``pools`` (uint8
+    [n_layers][n_pages][page_bytes]), ``tables`` (int32, a row a cell), ``refs`` (int32 [n_pages]: who holds a page).
+
+    A cell has pages for as many rows as ``fork`` or ``reserve`` last gave it; the clean prompt's pages and the donor's are
+    two rows more of the table, filled by ``load_prompt``.  The tensors stay where they are, so that captured calls keep
+    working.  Calls go to the current stream."""
+
+    def __init__(self, n_cells: int, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, prompt_len: int, span,
+                 capacity: int, n_pages: int, donor_zero: bool = False, device="cuda"):
+        S.load_library()
+        t = S._torch
+        if n_cells + 2 > S.SPLICE_MAX_CELLS:
+            raise ValueError(f"a cache has {S.SPLICE_MAX_CELLS - 2} cells at most, and its prompts")
+        self.n_cells, self.capacity, self.prompt_len = n_cells, capacity, prompt_len
+        self.table_len = max(-(-capacity // SPLICE_PAGE_ROWS), -(-prompt_len // SPLICE_PAGE_ROWS), 1)
+        shape = lambda cells, layers, rows: S.make_shape(cells, layers, n_q_heads, n_kv_heads, head_dim, prompt_len, span,  # noqa: E731
+                                                         rows, donor_zero, "bf16")
+        self.shape = shape(n_cells, n_layers, capacity)                # of the cells
+        self._every = shape(n_cells + 2, n_layers, self.table_len * SPLICE_PAGE_ROWS)
+        self._row = shape(1, n_layers, self.table_len * SPLICE_PAGE_ROWS)
+        with t.device(device):
+            # (bytes that no row has filled are never looked at: clear them all the same, a pool is handed on)
+            self.pools = t.zeros((n_layers, n_pages, splice_page_bytes(self.shape)), dtype=t.uint8, device=device)
+            self._tables = t.full((n_cells + 2, self.table_len), -1, dtype=t.int32, device=device)
+            self.refs = t.zeros(n_pages, dtype=t.int32, device=device)
+            self._next = t.empty_like(self._tables), t.empty_like(self.refs)
+            self.missing = t.zeros(1, dtype=t.int32, device=device)
+            self.copied = t.zeros((n_cells + 2, 2), dtype=t.int32, device=device)
+        self._prompts = [prompt_len, 0 if donor_zero else prompt_len]
+        self._held = [0, 0]                                            # rows of the prompts that have pages
+        self.rows = np.zeros(n_cells, np.int32)                        # rows of the cells that have pages
+        self.fork(np.full(n_cells, -1), self.rows, self.rows)
+
+    @property
+    def tables(self):
+        """The cells' tables (int32 [C][table_len])."""
+        return self._tables[:self.n_cells]
+
+    @property
+    def clean_table(self):
+        return self._tables[self.n_cells, :-(-self.prompt_len // SPLICE_PAGE_ROWS)]
+
+    @property
+    def donor_table(self):
+        """The donor's pages; None for ZERO."""
+        if self.shape.donor_kind == S.SPLICE_DONOR_ZERO:
+            return None
+        return self._tables[self.n_cells + 1, :-(-self.prompt_len // SPLICE_PAGE_ROWS)]
+
+    def pages(self, n_tokens: int) -> SplicePages:
+        return make_pages(self.pools.shape[1], self.table_len, n_tokens)
+
+    def fork(self, parent, rows, want=None) -> None:
+        """Cell c goes on from the first ``rows[c]`` rows of cell ``parent[c]`` (-1: from none), with pages for ``want[c]`` rows
+        (``rows`` without): ``splice_page_fork``.  ``missing`` says how many pages there were too few, ``copied`` which were."""
+        want = rows if want is None else want
+        C = self.n_cells
+        cells = [np.asarray(x, dtype=np.int32).reshape(-1) for x in (parent, rows, want)]
+        if any(len(x) != C for x in cells):
+            raise ValueError(f"parent, rows and want have an entry for each of the {C} cells")
+        if C and cells[2].max() > self.capacity:
+            raise ValueError(f"a cell has {self.capacity} rows at most")
+        if (cells[1] > self.rows[np.maximum(cells[0], 0)])[cells[0] >= 0].any():
+            raise ValueError("a cell cannot take over more rows than its parent has pages for")
+        more = [C, C + 1], self._held, self._prompts
+        host = [np.concatenate([x, np.asarray(y, dtype=np.int32)]) for x, y in zip(cells, more)]
+        splice_page_fork(self._every, self.pages(1), *host, self._tables, self.refs, *self._next, self.missing, self.copied,
+                         self.pools)
+        self._tables.copy_(self._next[0])
+        self.refs.copy_(self._next[1])
+        self._held, self.rows = list(self._prompts), cells[2].copy()
+
+    def reserve(self, want) -> None:
+        """Pages for ``want[c]`` rows of every cell; rows that it has stay."""
+        want = np.asarray(want, dtype=np.int32).reshape(-1)
+        self.fork(np.arange(self.n_cells), np.minimum(want, self.rows), want)
+
+    def load_prompt(self, layer: int, k, v, donor: bool = False) -> None:
+        """Rows of the clean prompt's (or the donor's) pages of a layer from bf16 [Hkv][T_p][D]."""
+        t, sh = S._torch, self.shape
+        dims = (sh.n_kv_heads, self.prompt_len, sh.head_dim)
+        if tuple(k.shape) != dims or tuple(v.shape) != dims:
+            raise ValueError(f"a prompt's k and v have shape {dims}")
+        table = self._tables[self.n_cells + bool(donor)]
+        rope = T.make_rope("half", 0)
+        for a in range(0, self.prompt_len, SPLICE_MAX_PAGE_TOKENS):
+            n = min(SPLICE_MAX_PAGE_TOKENS, self.prompt_len - a)
+            part = [x[:, a:a + n].transpose(0, 1).contiguous()[None] for x in (k, v)]
+            splice_page_append(self._row, self.pages(n), rope, None, [a], None, table, None, *part, None, self.pools[layer])
+
+    def compact(self, cell_step, keep) -> None:
+        """Row cell_step[c] + i of the cells = row cell_step[c] + keep[c][i] (``keep`` int32 [C][T] on the device): the tokens
+        that were accepted, or that an eviction leaves."""
+        splice_page_compact(self.shape, self.pages(keep.shape[1]), cell_step, keep, self.tables, self.pools)

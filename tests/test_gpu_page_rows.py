@@ -181,6 +181,17 @@ def test_in_place_query_and_another_stream():
     assert torch.equal(out, q)
 
 
+def test_rows_without_queries():
+    announce("page append rows only")
+    s = Rows(13, C=3, T=70)
+    out, *want = s.run()
+    full = s.mem.clone()
+    s.mem.copy_(torch.from_numpy(s.pool.reshape(s.n_pages, -1)))
+    freq = torch.from_numpy(s.freq).cuda()
+    sp.splice_page_append(s.shape, s.pages, sp.make_rope("half", s.D), freq, s.steps, None, s.tab, None, s.k.cuda(), s.v.cuda(), None, s.mem)
+    assert torch.equal(s.mem, full)
+
+
 def test_replayed_graph():
     """A captured append and read keeps its steps, and takes what its tensors hold at each replay."""
     announce("page append graph")
@@ -221,7 +232,7 @@ def test_refused_tensors():
                                                         tables=s.tab, q=q, k=k, v=v, q_out=out, pool=s.mem), **kw})
     for bad in (dict(q=s.q), dict(k=k.float()), dict(v=v[:, :, :1]), dict(tables=s.tab.long()), dict(tables=s.tab[:, :2]),
                 dict(pool=s.mem[:-1]), dict(pool=s.mem.cpu()), dict(q_out=out.transpose(1, 2)), dict(freq=None), dict(cell_new=[1, 2]),
-                dict(cell_step=s.steps[:2]), dict(q_out=None)):
+                dict(cell_step=s.steps[:2]), dict(q_out=None), dict(q=None)):
         with pytest.raises(ValueError):
             call(**bad)
     with pytest.raises(sp.SpliceError):

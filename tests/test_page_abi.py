@@ -209,3 +209,10 @@ def test_reference_quantisation():
     k, v = ref.rows_of(ref.page_of(rng.standard_normal((64, 128)), rng.standard_normal((64, 128))), 128)
     k2, v2 = ref.rows_of(ref.page_of(k, v), 128)
     assert (k == k2).all() and (v == v2).all()
+
+
+def test_rows_alone():
+    """Without q and q_out nothing is rotated; one of them alone is an error."""
+    assert append(q=None) == append(q_out=None) == sp.SPLICE_EINVAL
+    assert append(q=None, q_out=None, qs=0, k=None) == sp.SPLICE_EINVAL
+    assert append(q=None, q_out=None, qs=0, new=ints(0, 0, 0)) == sp.SPLICE_OK
