@@ -105,6 +105,7 @@ SPLICE_API int32_t splice_page_read(const splice_shape *shape, const splice_page
  * takes (0: planned).  Scores are fp32; one that is NaN or +inf makes the query's
  * results NaN, one of -inf has weight 0.  Weights enter the second product as bf16, and weighted values are
  * summed in fp32 before the division by the weights' sum (a weight may be 2^8).
+ * Calls of 2^24 work groups and more are SPLICE_EUNSUPPORTED (2^26 rows, tokens x q heads, of one cell).
  * workspace: 256-byte aligned, splice_page_attn_workspace_bytes(shape, call,
  * pages) bytes (enough for any steps; it may be 0), no initialisation.  Calls that
  * share a workspace must be ordered on one stream.

@@ -81,7 +81,9 @@ int32_t splice_page_attn(const splice_shape *shape, const splice_call *call, con
     }
     if (n == 0) return SPLICE_OK;
     const splice::PagePlan p = splice::page_plan(sh, *call, *pages, cells, n, compute_units());
-    if (p.blocks >= (int64_t)1 << 24 || p.own_tiles >= 1 << 24) return SPLICE_EUNSUPPORTED;
+    // a launch has fewer than 2^32 threads along x, the join a wave a row
+    if (p.blocks >= (int64_t)1 << 24 || p.own_tiles >= 1 << 24 || (p.parts > 1 && (int64_t)most_count * sh.n_q_heads >= (int64_t)1 << 26))
+        return SPLICE_EUNSUPPORTED;
     if (p.bytes > 0 && (!workspace || !splice::aligned(workspace, 256) || workspace_bytes < (size_t)p.bytes)) return SPLICE_EWORKSPACE;
     PageArgs args;
     int tile = 0;

@@ -592,6 +592,9 @@ __device__ __forceinline__ void wide(const PageCall &a, const PageWalk &walk, in
     lo_least = wave_min(lo_least);
     hi_least = wave_min(hi_least);
     hi_most = wave_max(hi_most);
+    bool some = false;   // a wave without rows hands over its share of the pages, and computes nothing
+    static_for<0, R>([&](auto r) { some |= rows.at[r] >= 0; });
+    if (!__any(some)) hi_most = -1;
     PageState<D, R> st;
     start<D, R>(st, rows, first, quad);
     uint32_t kc[KT][N], ke[CH], vc[UNITS][DW], vs[UNITS][DW / 2];

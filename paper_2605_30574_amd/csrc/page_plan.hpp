@@ -81,7 +81,9 @@ inline PageCost page_cost(int D, int own) {
 constexpr double kPageStart = 4;       // a launch and a work group's first bytes
 constexpr double kPageNext = 2;        // what a work group costs that follows another
 constexpr double kPageJoin = 4;        // a second launch, and the partial results' way there and back:
+constexpr double kPageJoinPart = 0.2;  // each
 constexpr double kPageJoinRate = 4e6;  // bytes a us
+constexpr double kPageAgain = 1000;    // pages (D = 128) a us that several cells' narrow tiles take of one prompt, from the caches
 
 struct PageWork {
     int tiles, each, longest;
@@ -123,17 +125,23 @@ inline PagePlan page_plan(const splice_shape &sh, const splice_call &call, const
     }
     const int own = most_rows <= 16 ? 1 : (most_rows <= 64 ? (D <= 128 ? 2 : 1) : 0);
     const int own_rows = own ? page_narrow_rows(D, own) : page_wide_rows(D);
-    const PageCost cost = page_cost(D, own), wide = page_cost(D, 0);
+    const PageCost cost = page_cost(D, own);
+    PageCost wide = page_cost(D, 0);
     const double slots = 2.0 * units, result = (double)(rows_u + rows_s) * Hkv * D * 4 * 2 / kPageJoinRate;
     const int seen = call.window > 0 ? std::min(sh.prompt_len, call.window) : sh.prompt_len, list = page_pages(0, seen) + 2;
     const int tiles_u = ceil_div(rows_u, page_wide_rows(D)), tiles_s = ceil_div(rows_s, page_wide_rows(D));
+    if (tiles_u + tiles_s > 0)   // waves without rows leave the others room
+        wide.alone *= 0.4 + 0.6 * (rows_u + rows_s) / ((tiles_u + tiles_s) * page_wide_rows(D));
     const int forced = call.split_keys / kPageRows;
     PagePlan best{};
     double least = 0;
     bool any = false;
     // tiles of several cells' rows save walks over the prompt where a cell's own rows do not fill them
+    double again = 0;   // pages of the prompt walked by tiles of their own
     for (int shared = 0; shared <= (n > 1 && own && seen > 0 ? 1 : 0); ++shared) {
         const PageWork w = own_work(sh, call, cells, n, own_rows, shared != 0);
+        if (shared == 0 && n > 1 && own == 1 && seen > 0)
+            again = std::max<int64_t>(0, w.pages - own_work(sh, call, cells, n, own_rows, true).pages) * (double)Hkv;
         const double own_pages = (double)w.pages * Hkv, prompt_tiles = shared ? (double)(tiles_u + tiles_s) * Hkv : 0;
         int last_prompt = 0;
         for (int pc : counts) {
@@ -147,18 +155,21 @@ inline PagePlan page_plan(const splice_shape &sh, const splice_call &call, const
                 int per = forced ? forced : std::max(1, ceil_div(w.longest, oc));
                 const int parts = std::min(std::max(1, ceil_div(w.longest, per)), cap - prompt_parts);
                 per = std::max(1, ceil_div(w.longest, parts));
+                if (own && per > 8) per = (per + 7) / 8 * 8;   // the four waves' two pages each
                 if (oc > 1 && parts == last_own) break;
                 last_own = parts;
                 // work groups with pages: every tile's list is cut after `per`
                 const double groups = std::max((double)w.tiles * Hkv, std::min((double)w.tiles * Hkv * parts, own_pages / per + 0.5 * w.tiles * Hkv));
                 const double prompts = prompt_tiles * prompt_parts, all = groups + prompts;
-                double t = own_pages / std::min(groups / cost.alone, cost.rate) + 0.5 * per * cost.alone;
+                const double most = groups / cost.alone;
+                double t = (shared ? own_pages : own_pages - again) / std::min(most, cost.rate) + 0.5 * per * cost.alone;
+                if (!shared) t += again / std::min(most, kPageAgain * 128 / D);
                 if (shared) {
                     t += prompt_tiles * list / std::min(prompts / wide.alone, wide.rate);
                     t = std::max(t, per_prompt * wide.alone * 1.3);
                 }
                 t += kPageStart + kPageNext * std::max(0.0, all - slots) / slots;
-                if (parts + prompt_parts > 1) t += kPageJoin + result * (parts + prompt_parts);
+                if (parts + prompt_parts > 1) t += kPageJoin + (kPageJoinPart + result) * (parts + prompt_parts);
                 if (!any || t < least) {
                     any = true;
                     least = t;

@@ -11,6 +11,25 @@ BF16 = 2.0 ** -8          # half a step of bfloat16
 FILL = 776.0              # exact in bfloat16
 
 
+# (donor, window): (D, (Hq, Hkv), T, C, T_p) whose prompts are walked by tiles of several cells' rows
+SHARED = {
+    ("diff", 0): [(64, (16, 8), 1, 16, 3000), (64, (16, 4), 5, 16, 3000), (128, (16, 8), 1, 16, 3000), (128, (16, 4), 5, 16, 3000),
+                  (256, (16, 8), 1, 16, 3000), (128, (8, 2), 1, 160, 3000)],
+    ("diff", 2000): [(64, (16, 8), 1, 80, 1500), (64, (8, 2), 5, 160, 1500), (128, (16, 8), 1, 16, 3000), (128, (8, 2), 5, 120, 1500),
+                     (256, (16, 8), 1, 16, 3000)],
+    ("zero", 0): [(64, (16, 8), 2, 16, 5000), (64, (16, 4), 5, 16, 5000), (128, (16, 8), 1, 16, 5000), (128, (16, 4), 5, 16, 5000),
+                  (256, (16, 8), 1, 40, 1500)],
+    ("zero", 2000): [(64, (16, 8), 1, 120, 1500), (128, (16, 8), 1, 16, 5000), (128, (8, 2), 5, 80, 3000), (256, (16, 8), 1, 40, 1500)],
+}
+
+
+def shared_case(D, heads, T, C, Tp):
+    """Arguments of Sweep: cells at two steps, not spliced, spliced, or from the middle of their tokens on."""
+    steps = [60 if c % 2 else 5 for c in range(C)]
+    return dict(C=C, T=T, Hq=heads[0], Hkv=heads[1], D=D, Tp=Tp, span=(70, Tp // 2), cap=80, steps=steps,
+                LW=[([9, 0], [0, 0], [1, steps[c] + T // 2])[c % 3] for c in range(C)])
+
+
 class Sweep:
     """One call's tensors on the GPU and their float64 values."""
 

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import page_reference as ref
-from page_common import FILL, P, Sweep, announce, sp
+from page_common import SHARED, P, Sweep, announce, shared_case, sp
 
 pytestmark = pytest.mark.gpu
 
@@ -66,6 +66,20 @@ def test_a_prompt_shared_by_many_cells(T, D, donor, window):
     LW = [[0, 0] if c % 3 == 0 else ([9, 0] if c % 3 == 1 else [1, int(steps[c]) + 1]) for c in range(C)]
     s = Sweep(23, C=C, T=T, Hq=8, Hkv=2, D=D, Tp=1500, span=(70, 1300), donor=donor, window=window, cap=80, steps=steps, LW=LW)
     run(s, what=f"shared T={T} D={D} {donor} {window}")
+
+
+@pytest.mark.parametrize("kind,case", [(kind, case) for kind in SHARED for case in SHARED[kind]])
+def test_tiles_of_several_cells(kind, case):
+    """test_page_plan.py holds that the plan takes them for these shapes."""
+    s = Sweep(97, donor=kind[0], window=kind[1], **shared_case(*case))
+    s.tables[3, 0] = -1
+    run(s, what=f"several cells {kind} {case}")
+
+
+def test_tiles_of_several_cells_in_other_parts():
+    s = Sweep(98, **shared_case(*SHARED["diff", 0][2]))
+    for split in (64, 512, 65536):
+        run(s, split, f"several cells, parts of {split}")
 
 
 def test_ragged_tokens():

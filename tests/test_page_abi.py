@@ -131,6 +131,15 @@ def test_attention_refusals():
         sp.splice_page_attn_workspace_bytes(shape(dtype="f32"), sp.make_call(1, 0, 0, 0.125), sp.make_pages(9, 2, 4))
 
 
+def test_more_rows_than_a_launch_takes():
+    sh = shape(n_cells=1, n_q_heads=65528, n_kv_heads=8191, head_dim=256, prompt_len=1 << 27, gen_capacity=1 << 20, span=(0, 0))
+    pages = sp.make_pages(9, 1 << 14, 32768)
+    assert attn(sh=sh, pages=pages, steps=ints(5), new=ints(32768), bytes=1 << 62) == sp.SPLICE_EUNSUPPORTED
+    sh = shape(n_cells=256, n_q_heads=65528, n_kv_heads=8191, gen_capacity=1 << 20)
+    many = (ctypes.c_int32 * 256)(*([5] * 256))
+    assert attn(sh=sh, pages=pages, steps=many, new=None, LW=(ctypes.c_int32 * 512)(), bytes=1 << 62) == sp.SPLICE_EUNSUPPORTED
+
+
 def test_append_refusals():
     for name in ("q", "k", "v", "q_out"):
         assert append(**{name: None}) == sp.SPLICE_EINVAL

@@ -118,3 +118,19 @@ def test_what_the_plan_is_for(plan):
     prompt = plan(sp.make_shape(1, 4, 32, 8, 128, 0, (0, 0), 4096, False, "bf16"), sp.make_call(1, 0, 0, 0.1), sp.make_pages(9, 64, 4096),
                   [(0, 0, 4096, 0)])
     assert prompt["own"] == 0 and prompt["parts"] == 1
+
+
+def test_shapes_of_the_gpu_tests_share_their_prompts(plan):
+    from page_common import SHARED, shared_case
+    for (donor, window), cases in SHARED.items():
+        own = set()
+        for case in cases:
+            c = shared_case(*case)
+            T = c["T"]
+            cells = [(i, s, T, T if L > 1 else min(T, max(0, W - s))) for i, (s, (L, W)) in enumerate(zip(c["steps"], c["LW"]))]
+            sh = sp.make_shape(c["C"], 4, c["Hq"], c["Hkv"], c["D"], c["Tp"], c["span"], c["cap"], donor == "zero", "bf16")
+            p = plan(sh, sp.make_call(1, 0, window, 0.1), sp.make_pages(999, 2, T), cells)
+            assert p["shared"] and p["prompt_parts"] > 1 and p["rows_u"] and p["rows_s"], (donor, window, case)
+            own.add((c["D"], p["own"]))
+        # every kernel that has such tiles
+        assert own >= {(64, 1), (128, 1), (128, 2), (256, 1)} and (window or (64, 2) in own), own
