@@ -249,3 +249,26 @@ def test_refused_tensors():
             sp.splice_page_attn(**{**good, **bad})
     sp.splice_page_attn(**good)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("D,parts", [(64, 33), (64, 34), (64, 35), (128, 17), (128, 33), (128, 49)])
+def test_numbers_of_parts_that_end_within_a_load(D, parts):
+    """A wave of the join loads 256 / D parts at a time: the last load has fewer."""
+    s = Sweep(43, C=1, T=300, Hq=4, Hkv=2, D=D, Tp=0, span=(0, 0), cap=parts * 64, steps=[parts * 64 - 300], LW=[[0, 0]])
+    run(s, 64, f"D={D} {parts} parts")
+
+
+@pytest.mark.parametrize("T,D", [(1, 64), (3, 128), (40, 128), (2, 256)])
+def test_a_query_does_not_move_its_neighbours(T, D):
+    """Queries of one tile do not share a running maximum: the others' bits stay where one of them is 100 times as large, or NaN."""
+    s = Sweep(47, C=2, T=T, Hq=8, Hkv=2, D=D, Tp=150, span=(20, 140), cap=T + 300, steps=[200, 299])
+    announce(f"neighbours T={T} D={D}")
+    want, mine = s.attend(), s.q.clone()
+    for other in (100.0, float("nan")):
+        s.q = mine.clone()
+        s.q[:, 0, 1] = s.q[:, 0, 1] * other
+        got = s.attend()
+        for x, y in zip(want, got):
+            a, b = x.clone(), y.clone()
+            a[:, 0, 1] = b[:, 0, 1] = 0
+            assert torch.equal(a, b)
