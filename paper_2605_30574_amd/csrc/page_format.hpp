@@ -4,9 +4,10 @@
 // The order of a page's bytes is that in which the attention's matrix
 // instructions take their operands, so that a lane's share of a tile is one
 // 16-byte load and nothing is transposed on the way:
-//   K: v_mfma_scale_f32_16x16x128_f8f6f4 takes 16 tokens x 128 values of codes, lane
-//      (token r mod 16, block of 32 values) 16 bytes; its scale operand is a
-//      dword a lane, of which the instruction picks a byte: that of tiles 0..3;
+//   K: v_mfma_f32_16x16x32_bf16 takes 16 tokens x 32 values, lane (token r mod 16, c) eight
+//      values.  q's and k's values may stand in any order that is the same for both: a
+//      lane's 16 bytes are its token's block c of 32 values, eight for each of four products,
+//      under one scale byte, of which a dword has those of tiles 0..3;
 //   V: v_mfma_f32_16x16x32_bf16 takes 16 values x 32 tokens, lane (value,
 //      c) the tokens whose scores lane (query, c) holds, 4 c + f of either 16-token tile e:
 //      16 bytes are 8 tokens of 4 values each.

@@ -514,7 +514,9 @@ class SweepDecoder:
         st, _ = S._steps(steps, C)
         pos = None
         if getattr(self.positions, "__func__", None) is not SweepDecoder.positions:   # a decoder's own, asked step by step
-            pos = torch.stack([self.positions(np.where(st >= 0, st + t, st)) for t in range(n)], 1)
+            # (none is asked for behind a cell's last token)
+            last = n - 1 if new is None else np.maximum(np.asarray(new).reshape(-1), 1) - 1
+            pos = torch.stack([self.positions(np.where(st >= 0, st + np.minimum(t, last), st).astype(np.int32)) for t in range(n)], 1)
             pos = pos.to(torch.float64 if pos.is_floating_point() else torch.int64)
         x = self.wt["embed"][tokens.reshape(-1)]
         bf16 = torch.bfloat16

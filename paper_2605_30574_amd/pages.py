@@ -206,6 +206,9 @@ class PageCache:
         t = S._torch
         if n_cells + 2 > S.SPLICE_MAX_CELLS:
             raise ValueError(f"a cache has {S.SPLICE_MAX_CELLS - 2} cells at most, and its prompts")
+        prompt = -(-prompt_len // SPLICE_PAGE_ROWS) * (1 if donor_zero else 2)
+        if n_pages < prompt:
+            raise ValueError(f"the prompts alone take {prompt} pages of {n_pages}")
         self.n_cells, self.capacity, self.prompt_len = n_cells, capacity, prompt_len
         self.table_len = max(-(-capacity // SPLICE_PAGE_ROWS), -(-prompt_len // SPLICE_PAGE_ROWS), 1)
         shape = lambda cells, layers, rows: S.make_shape(cells, layers, n_q_heads, n_kv_heads, head_dim, prompt_len, span,  # noqa: E731
@@ -253,6 +256,8 @@ class PageCache:
         cells = [np.asarray(x, dtype=np.int32).reshape(-1) for x in (parent, rows, want)]
         if any(len(x) != C for x in cells):
             raise ValueError(f"parent, rows and want have an entry for each of the {C} cells")
+        if (cells[0] >= C).any():
+            raise ValueError(f"a parent is one of the {C} cells, or negative")
         if C and cells[2].max() > self.capacity:
             raise ValueError(f"a cell has {self.capacity} rows at most")
         if (cells[1] > self.rows[np.maximum(cells[0], 0)])[cells[0] >= 0].any():
@@ -276,6 +281,8 @@ class PageCache:
         dims = (sh.n_kv_heads, self.prompt_len, sh.head_dim)
         if tuple(k.shape) != dims or tuple(v.shape) != dims:
             raise ValueError(f"a prompt's k and v have shape {dims}")
+        if donor and sh.donor_kind == S.SPLICE_DONOR_ZERO:
+            raise ValueError("the ZERO donor has no rows")
         table = self._tables[self.n_cells + bool(donor)]
         rope = T.make_rope("half", 0)
         for a in range(0, self.prompt_len, SPLICE_MAX_PAGE_TOKENS):

@@ -181,6 +181,13 @@ def test_cache_refusals():
                 lambda: sp.PageCache(255, 1, 4, 2, 64, 0, (0, 0), 64, 4)):
         with pytest.raises(ValueError):
             bad()
+    zero = sp.PageCache(2, 1, 4, 2, 64, 64, (0, 64), 64, 4, donor_zero=True)
+    rows = torch.zeros(2, 64, 64, dtype=torch.bfloat16, device="cuda")
+    for bad in (lambda: cache.fork([C] + [-1] * (C - 1), [0] * C),                     # a prompt is no cell
+                lambda: sp.PageCache(2, 1, 4, 2, 64, 65, (0, 64), 64, 3),              # too few pages for the prompts
+                lambda: zero.load_prompt(0, rows, rows, donor=True)):
+        with pytest.raises(ValueError):
+            bad()
     small = gpu.make_pages(1, n_pages=2 * (-(-w.prompt_len // 64)) + 1)
     small.cache.reserve([64] * C)
     assert int(small.cache.missing) == C - 1
