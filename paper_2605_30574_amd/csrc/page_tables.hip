@@ -119,7 +119,6 @@ __global__ __launch_bounds__(kTableThreads) void fork_kernel(ForkArgs a) {
         s_start[tid] = at;
         if (tid == a.C - 1) s_start[a.C] = at + asks;
     }
-    if (a.C == 0 && tid == 0) s_start[0] = 0;
     counts.phase();
     const int total = s_start[a.C];
     int found = 0;
@@ -170,8 +169,6 @@ __global__ __launch_bounds__(kTableThreads) void fork_kernel(ForkArgs a) {
 
 // Pages copied: blockIdx.x the cell, y a part of the page, z the layer.  None is
 // both read and written: a page that is read has a holder, one that is written was free.
-// Bound by the bytes written: one page of 8 heads of 128 to 127 cells in 36 layers, 318 MB, 72 us
-// (4.4 TB/s; the page that is read stays in the caches).
 __global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(const int32_t *copied, uint8_t *pool, int64_t layer_stride,
                                                                   int64_t page_bytes) {
     const int from = copied[2 * blockIdx.x], to = copied[2 * blockIdx.x + 1];
@@ -346,7 +343,8 @@ int32_t splice_page_fork(const splice_shape *shape, const splice_pages *pages, c
     if (rc != SPLICE_OK) return rc;
     const splice_shape &sh = *shape;
     const int C = sh.n_cells;
-    if (C > 0 && (!parent || !rows || !want)) return SPLICE_EINVAL;
+    if (C == 0) return SPLICE_OK;
+    if (!parent || !rows || !want) return SPLICE_EINVAL;
     bool parts = false;
     for (int c = 0; c < C; ++c) {
         if (parent[c] >= C || rows[c] < 0 || want[c] < rows[c] || want[c] > (int64_t)pages->table_len * kPageRows ||
@@ -355,10 +353,10 @@ int32_t splice_page_fork(const splice_shape *shape, const splice_pages *pages, c
         parts |= rows[c] % kPageRows != 0;
     }
     if ((int64_t)C * pages->table_len > 1 << 30) return SPLICE_EUNSUPPORTED;
-    const int32_t *const ints[] = {refs, new_refs, missing, tables, new_tables, copied};
-    for (int i = 0; i < (C > 0 ? 6 : 3); ++i)   // without cells the counts alone go on
-        if (!ints[i] || !splice::aligned(ints[i], 4)) return SPLICE_EINVAL;
-    if ((C > 0 && new_tables == tables) || new_refs == refs) return SPLICE_EINVAL;
+    int32_t *const ints[] = {const_cast<int32_t *>(tables), const_cast<int32_t *>(refs), new_tables, new_refs, missing, copied};
+    for (const int32_t *p : ints)
+        if (!p || !splice::aligned(p, 4)) return SPLICE_EINVAL;
+    if (new_tables == tables || new_refs == refs) return SPLICE_EINVAL;
     if (!pool_ok(sh, *pages, pool, layer_stride)) return SPLICE_EINVAL;
     ForkArgs a{tables, refs, new_tables, new_refs, missing, copied, C, pages->table_len, pages->n_pages, {}, {}, {}};
     for (int c = 0; c < C; ++c) {

@@ -239,14 +239,3 @@ def test_many_cells_and_another_stream():
     rng = np.random.default_rng(4)
     s = Held(27, [128] * 200, L=2, layers=1, Hkv=1)
     compact(s, rng.integers(-1, 120, 200).tolist(), [np.flatnonzero(rng.random(8) < 0.5) for _ in range(200)], T=8, stream=torch.cuda.Stream())
-
-
-def test_fork_of_no_cells():
-    """The counts that others hold are the counts after the call too."""
-    announce("fork of no cells")
-    sh = sp.make_shape(0, 1, 2, 2, 64, 0, (0, 0), 64, False, "bf16")
-    refs, new = up([3, 0, 1]), up([9, 9, 9])
-    none, missing = up(np.zeros((0, 1))), up([9])
-    pools = torch.zeros((1, 3, 2 * 64 * 68), dtype=torch.uint8, device="cuda")
-    sp.splice_page_fork(sh, sp.make_pages(3, 1), [], [], [], none, refs, none.clone(), new, missing, up(np.zeros((0, 2))), pools)
-    assert new.tolist() == [3, 0, 1] and missing.tolist() == [0]
