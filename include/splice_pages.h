@@ -135,7 +135,8 @@ SPLICE_API int32_t splice_page_attn(const splice_shape *shape, const splice_call
  *   - New pages are the free ones from the lowest on, in the order of cells and of a cell's rows.
  *     *missing (device int32): how many there were too few; their entries are -1.
  * rows[c], want[c] <= 64 * table_len; shape: n_cells, the heads and D; pool: the first
- * layer's, n_layers = shape->n_layers of them.  pages->n_tokens is ignored.
+ * layer's, n_layers = shape->n_layers of them.  pages->n_tokens is ignored.  As everywhere, a call
+ * without cells does nothing: new_refs too is then left as it was.
  */
 SPLICE_API int32_t splice_page_fork(const splice_shape *shape, const splice_pages *pages, const int32_t *parent,
                                     const int32_t *rows, const int32_t *want, const int32_t *tables,

@@ -19,7 +19,7 @@
 //           through LDS, in operand order.
 // Measured (32 q heads, 8 KV heads of 128, with the join where there is one): narrow, 64 cells of up to
 // 16384 rows, 0.56 GB of pages, 120 us, 4.7 TB/s: bound by the bytes; wide, 4096 tokens of one cell over
-// themselves, 137 GFLOP, 131 us, 1050 TFLOP/s: bound by the matrix products and the softmax beside them.
+// themselves, 137 GFLOP, 133 us, 1030 TFLOP/s: bound by the matrix products and the softmax beside them.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -316,15 +316,14 @@ __device__ __forceinline__ void mark(f32x4_t (&s)[4], int from, int to, uint64_t
 template <int D, int R>
 __device__ __forceinline__ void raise(PageState<D, R> &st, const f32x4_t (&s)[R][4], const float (&sum)[R], float qk) {
     static_for<0, R>([&](auto r) {
-        int asks = !(sum[r] <= kMostWeight);
-        asks |= __shfl_xor(asks, 16);
-        asks |= __shfl_xor(asks, 32);
         float top = s[r][0][0];
         static_for<1, 16>([&](auto i) { top = fmaxf(top, s[r][i / 4][i % 4]); });
         top *= qk;
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float now = asks ? fmaxf(top, st.m[r]) : st.m[r], f = asks ? fast_exp2(st.m[r] - now) : 1.f;
+        const uint64_t lanes = __ballot(!(sum[r] <= kMostWeight));   // a row's are 16 apart
+        const uint32_t half = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+        const float now = (half | half >> 16) >> (threadIdx.x & 15) & 1 ? fmaxf(top, st.m[r]) : st.m[r], f = fast_exp2(st.m[r] - now);
         st.m[r] = now;
         st.l[r] *= f;
         static_for<0, D / 64>([&](auto b) { static_for<0, 4>([&](auto m) { st.o[r][b][m] *= f; }); });
@@ -420,7 +419,7 @@ struct NarrowShared {
 };
 
 // Pages that a wave has in registers or on their way there.  Two hide the memory's latency behind the other's
-// products (64 cells of 8k rows, D = 128: 181 us with one, 126 with two); what they take of registers beside two
+// products (64 cells of 8k rows, D = 128, a part a cell: 181 us with one, 126 with two; 120 with the plan of now); what they take of registers beside two
 // sets of rows, or rows of 256, leaves room for one.
 constexpr int narrow_pages(int D, int R) { return D == 64 || (D == 128 && R == 1) ? 2 : 1; }
 

@@ -169,6 +169,8 @@ __global__ __launch_bounds__(kTableThreads) void fork_kernel(ForkArgs a) {
 
 // Pages copied: blockIdx.x the cell, y a part of the page, z the layer.  None is
 // both read and written: a page that is read has a holder, one that is written was free.
+// Bound by the bytes written: one page of 8 heads of 128 to 127 cells in 36 layers, 318 MB, 72 us
+// (4.4 TB/s; the page that is read stays in the caches).
 __global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(const int32_t *copied, uint8_t *pool, int64_t layer_stride,
                                                                   int64_t page_bytes) {
     const int from = copied[2 * blockIdx.x], to = copied[2 * blockIdx.x + 1];
