@@ -133,7 +133,9 @@ SPLICE_API int32_t splice_page_attn(const splice_shape *shape, const splice_call
  *     first of them keeps it.  copied[c] (device int32 [C][2]) is (from, to),
  *     or (-1, -1).
  *   - New pages are the free ones from the lowest on, in the order of cells and of a cell's rows.
- *     *missing (device int32): how many there were too few; their entries are -1.
+ *     *missing (device int32): how many there were too few; their entries are -1.  A cell's are then
+ *     its last ones.  Entries below rows[c] rows that were absent stay so, and are not asked for: a later call
+ *     that is to fill them names fewer rows.
  * rows[c], want[c] <= 64 * table_len; shape: n_cells, the heads and D; pool: the first
  * layer's, n_layers = shape->n_layers of them.  pages->n_tokens is ignored.  As everywhere, a call
  * without cells does nothing: new_refs too is then left as it was.

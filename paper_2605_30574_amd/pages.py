@@ -196,9 +196,9 @@ class PageCache:
     """The pages of C sweep cells and of the prompts that they share, for all layers: ``pools`` (uint8
     [n_layers][n_pages][page_bytes]), ``tables`` (int32, a row a cell), ``refs`` (int32 [n_pages]: who holds a page).
 
-    A cell has pages for as many rows as ``fork`` or ``reserve`` last gave it; the clean prompt's pages and the donor's are
-    two rows more of the table, filled by ``load_prompt``.  The tensors stay where they are, so that captured calls keep
-    working.  Calls go to the current stream."""
+    A cell has pages for as many rows as ``fork`` or ``reserve`` last gave it (``rows``, on the host); the clean prompt's pages
+    and the donor's are two rows more of the table, filled by ``load_prompt``.  The tensors stay where they are, so that
+    captured calls keep working.  Calls go to the current stream."""
 
     def __init__(self, n_cells: int, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, prompt_len: int, span,
                  capacity: int, n_pages: int, donor_zero: bool = False, device="cuda"):
@@ -227,6 +227,7 @@ class PageCache:
         self._prompts = [prompt_len, 0 if donor_zero else prompt_len]
         self._held = [0, 0]                                            # rows of the prompts that have pages
         self.rows = np.zeros(n_cells, np.int32)                        # rows of the cells that have pages
+        self._lost = np.zeros(n_cells, bool)                           # cells without some of the rows that they took over
         self.fork(np.full(n_cells, -1), self.rows, self.rows)
 
     @property
@@ -250,7 +251,12 @@ class PageCache:
 
     def fork(self, parent, rows, want=None) -> None:
         """Cell c goes on from the first ``rows[c]`` rows of cell ``parent[c]`` (-1: from none), with pages for ``want[c]`` rows
-        (``rows`` without): ``splice_page_fork``.  ``missing`` says how many pages there were too few, ``copied`` which were."""
+        (``rows`` without): ``splice_page_fork``.  ``missing`` says how many pages there were too few, ``copied`` which were.
+
+        Where pages were too few a cell has those up to its first absent one, and ``rows`` says so: ask again when others have
+        given theirs back.  A cell for which the copy of a page in use was among them has lost that page's rows
+        (``rows`` is below what it was to take over).  To know this the host waits for a call that asks for pages, but
+        for a captured one, which is taken to find them all."""
         want = rows if want is None else want
         C = self.n_cells
         cells = [np.asarray(x, dtype=np.int32).reshape(-1) for x in (parent, rows, want)]
@@ -269,11 +275,25 @@ class PageCache:
         self._tables.copy_(self._next[0])
         self.refs.copy_(self._next[1])
         self._held, self.rows = list(self._prompts), cells[2].copy()
+        self._lost[:] = False
+        # a page is asked for behind the rows that a cell takes over, or for the copy of their last one
+        asks = (-(-cells[2] // SPLICE_PAGE_ROWS) > cells[1] // SPLICE_PAGE_ROWS).any()
+        if asks and not (self._tables.is_cuda and S._torch.cuda.is_current_stream_capturing()) and int(self.missing) > 0:
+            # a cell's pages are given from the first on, so what it has ends at the first absent one
+            tables = self.tables.cpu().numpy()
+            there = np.cumprod((tables >= 0) & (tables < self.pools.shape[1]), axis=1).sum(axis=1)
+            self.rows = np.minimum(self.rows, there * SPLICE_PAGE_ROWS).astype(np.int32)
+            self._lost = self.rows < cells[1]
 
     def reserve(self, want) -> None:
-        """Pages for ``want[c]`` rows of every cell; rows that it has stay."""
+        """Pages for ``want[c]`` rows of every cell; rows that it has stay.  A cell that has lost rows is given none behind
+        those that it has: fork it, from these or from others."""
         want = np.asarray(want, dtype=np.int32).reshape(-1)
+        if len(want) == self.n_cells and (self._lost & (want > self.rows)).any():
+            raise ValueError(f"cells {np.flatnonzero(self._lost & (want > self.rows)).tolist()} have lost rows: fork them anew")
+        lost = self._lost.copy()
         self.fork(np.arange(self.n_cells), np.minimum(want, self.rows), want)
+        self._lost |= lost
 
     def load_prompt(self, layer: int, k, v, donor: bool = False) -> None:
         """Rows of the clean prompt's (or the donor's) pages of a layer from bf16 [Hkv][T_p][D]."""

@@ -1,0 +1,65 @@
+"""PageCache over the kernels: pools that run short, pages that cells share, passes that ask for rows without pages."""
+import numpy as np
+import pytest
+import torch
+
+import gpu_common as gc
+from test_gpu_page_decoder import run, setup
+
+pytestmark = pytest.mark.gpu
+
+
+def test_shortage_freeing_retry_and_a_pass():
+    """A cell that found no page gets one when another's come free, and its tokens are then seen."""
+    w, m, lw, gpu, cpu = setup("blank-sink")
+    C = lw.shape[0]
+    rng = np.random.default_rng(5)
+    gc.announce("pages, short")
+    pages = gpu.make_pages(3, n_pages=2 * (-(-w.prompt_len // 64)) + C - 1)
+    cache = pages.cache
+    cache.reserve([64] * C)
+    assert int(cache.missing) == 1 and cache.rows.tolist() == [64] * (C - 1) + [0]
+    cache.fork([-1] + list(range(1, C)), [0] + [64] * (C - 2) + [0])
+    cache.reserve([0] + [64] * (C - 1))
+    assert int(cache.missing) == 0 and cache.rows.tolist() == [0] + [64] * (C - 1)
+    tables = cache.tables.cpu().numpy()
+    assert (tables[1:, 0] >= 0).all() and len(set(tables[1:, 0])) == C - 1 and (tables[0] == -1).all()
+    steps = np.array([-1] + [0] * (C - 1), np.int32)
+    run(gpu, cpu, pages, rng.integers(0, m.vocab, (C, 3)), steps, None, "after a shortage")
+    run(gpu, cpu, pages, rng.integers(0, m.vocab, (C, 3)), np.where(steps >= 0, 3, -1).astype(np.int32), None, "after a shortage, on")
+
+
+def test_a_copy_that_found_no_page():
+    w, m, lw, gpu, _ = setup("blank-sink")
+    C = lw.shape[0]
+    gc.announce("pages, no copy")
+    pages = gpu.make_pages(70, n_pages=2 * (-(-w.prompt_len // 64)) + 2)
+    cache = pages.cache
+    cache.reserve([70] + [0] * (C - 1))
+    gpu.page_logits(torch.zeros(C, 70, dtype=torch.int64, device="cuda"), pages, np.array([0] + [-1] * (C - 1), np.int32))
+    cache.fork([0] * C, [70] * C)
+    assert int(cache.missing) == C - 1 and cache.rows.tolist() == [70] + [64] * (C - 1)
+    with pytest.raises(ValueError):
+        cache.reserve([70] * C)
+    cache.fork([-1] + [1] * (C - 1), [0] + [64] * (C - 1), [0, 65] + [64] * (C - 2))
+    assert int(cache.missing) == 0 and cache.rows.tolist() == [0, 65] + [64] * (C - 2)
+
+
+def test_captured_fork():
+    """A fork in a graph asks nothing of the device: each replay forks what the tables then hold."""
+    w, m, lw, gpu, _ = setup("blank-sink")
+    C = lw.shape[0]
+    gc.announce("pages, captured fork")
+    cache = gpu.make_pages(1).cache
+    cache.reserve([70] * C)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.fork([0] * C, [70] * C, [130] * C)
+    assert cache.rows.tolist() == [130] * C
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        tables, refs = cache.tables.cpu().numpy(), cache.refs.cpu().numpy()
+        assert int(cache.missing) == 0 and len(set(tables[:, 0])) == 1 and len(set(tables[:, 1:].ravel())) == 2 * C
+        held = cache._tables.cpu().numpy()
+        assert (refs == np.bincount(held[held >= 0], minlength=len(refs))).all()

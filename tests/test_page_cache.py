@@ -1,0 +1,116 @@
+"""PageCache on the CPU: what it keeps of its cells' pages, with tests/page_reference.py's fork in the place of the kernel."""
+import numpy as np
+import pytest
+import torch
+
+import page_reference as ref
+import paper_2605_30574_amd as sp
+from paper_2605_30574_amd import pages as PG
+
+P = 64
+
+
+def fork(shape, pages, parent, rows, want, tables, refs, new_tables, new_refs, missing, copied, pools, stream=None):
+    got = ref.fork(*(np.asarray(x) for x in (parent, rows, want)), tables.numpy(), refs.numpy(), pages.n_pages)
+    for out, x in zip((new_tables, new_refs, missing, copied), got):
+        out.copy_(torch.from_numpy(np.asarray(x, dtype=np.int32).reshape(out.shape)))
+    for frm, to in got[3]:
+        if frm >= 0:
+            pools[:, to] = pools[:, frm]
+
+
+@pytest.fixture
+def cache(monkeypatch):
+    monkeypatch.setattr(PG, "splice_page_fork", fork)
+    return lambda C, n_pages, capacity=320, Tp=0: sp.PageCache(C, 1, 2, 1, 64, Tp, (0, 0), capacity, n_pages, device="cpu")
+
+
+def held(c):
+    """Rows of every cell up to its first absent page."""
+    there = np.cumprod(c.tables.numpy() >= 0, axis=1).sum(1)
+    return (there * P).tolist()
+
+
+def test_a_shortage_is_made_good_when_pages_come_free(cache):
+    c = cache(2, 1)
+    c.reserve([64, 64])
+    assert int(c.missing) == 1 and c.rows.tolist() == [64, 0]
+    c.reserve([64, 64])
+    assert int(c.missing) == 1 and c.rows.tolist() == [64, 0]      # and is told again
+    c.fork([-1, 1], [0, 0], [0, 0])
+    c.reserve([0, 64])
+    assert int(c.missing) == 0 and c.rows.tolist() == [0, 64] == held(c)
+
+
+def test_no_hole_is_left_below_rows_that_are_given_later(cache):
+    c = cache(2, 2)
+    c.reserve([128, 64])
+    assert int(c.missing) == 1 and c.rows.tolist() == [128, 0]
+    c.fork([0, 1], [64, 0], [64, 128])
+    assert int(c.missing) == 1 and c.rows.tolist() == [64, 64] == held(c)
+    c.fork([-1, 1], [0, 64], [0, 128])
+    assert int(c.missing) == 0 and c.rows.tolist() == [0, 128] == held(c)
+
+
+def test_a_part_of_what_is_wanted(cache):
+    c = cache(2, 4)
+    c.reserve([130, 130])
+    assert int(c.missing) == 2 and c.rows.tolist() == [130, 64] and held(c) == [192, 64]
+    with pytest.raises(ValueError):
+        c.fork([1, 1], [65, 64])                                   # cell 1 has no such row
+
+
+def test_rows_lost_with_the_page_that_was_to_be_copied(cache):
+    """A fork in the middle of a page, and no page for the copy: the cell has its whole pages, and is given none behind
+    them in the place of the rows that it lost until a fork says what it goes on from."""
+    c = cache(2, 3)
+    c.reserve([70, 0])
+    c.refs[2] += 1                                                 # the third page is somebody else's
+    c.fork([0, 0], [70, 70], [80, 80])
+    assert int(c.missing) == 1 and c.rows.tolist() == [80, 64]
+    c.refs[2] -= 1
+    with pytest.raises(ValueError):
+        c.reserve([80, 80])
+    c.reserve([80, 64])                                            # as it is
+    with pytest.raises(ValueError):
+        c.reserve([80, 128])
+    c.fork([0, 0], [70, 70], [80, 80])                             # from the same rows once more
+    assert int(c.missing) == 0 and c.rows.tolist() == [80, 80]
+    c.reserve([100, 100])
+    c.fork([0, 0], [70, 70], [80, 80])
+    assert c.rows.tolist() == [80, 80]
+
+
+def test_a_cell_that_lost_rows_may_go_on_from_those_it_has(cache):
+    c = cache(2, 2)
+    c.reserve([70, 0])
+    c.fork([0, 0], [70, 70])
+    assert int(c.missing) == 1 and c.rows.tolist() == [70, 64]
+    c.fork([-1, 1], [0, 64], [0, 70])
+    assert int(c.missing) == 0 and c.rows.tolist() == [0, 70]
+    c.reserve([0, 128])
+    assert int(c.missing) == 0 and c.rows.tolist() == [0, 128]
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_rows_are_those_that_have_pages(cache, seed):
+    rng = np.random.default_rng(seed)
+    C = int(rng.choice([1, 3, 9]))
+    c = cache(C, 4 + int(rng.integers(1, 3 * C + 3)), Tp=70)           # four of them the prompts'
+    for _ in range(30):
+        if rng.random() < 0.5:
+            want = rng.integers(0, 321, C)
+            try:
+                c.reserve(want)
+            except ValueError:
+                c.fork(np.arange(C), c.rows, c.rows)
+                continue
+        else:
+            parent = rng.integers(-1, C, C)
+            rows = np.array([0 if p < 0 else rng.integers(0, c.rows[p] + 1) for p in parent])
+            want = np.minimum(320, rows + rng.integers(0, 130, C))
+            c.fork(parent, rows, want)
+        assert (c.rows <= want).all() and (c.rows <= held(c)).all()
+        short = c.rows < want
+        assert short.any() == (int(c.missing) > 0) and (c.rows[short] == np.array(held(c))[short]).all()
+        assert (c.tables.numpy()[np.arange(c.table_len) >= -(-c.rows[:, None] // P)] == -1).all()
