@@ -504,14 +504,15 @@ class SweepDecoder:
     def page_logits(self, tokens: torch.Tensor, pages: DecoderPages, steps: np.ndarray, new=None) -> torch.Tensor:
         """Logits [C * n][V] (bfloat16 where the head's product is, else float32) of one pass over n tokens a cell: token t of
         cell c is tokens[c][t] (int64) at decode step steps[c] + t, behind the cell's steps[c] rows and the tokens before it;
-        its K/V become row steps[c] + t, for which the cell has its pages (``pages.cache.reserve``, ``fork``: rows without
-        one are dropped).  ``new``: how many tokens each cell has (host int32 [C]; all n without); cells with a negative
-        step are skipped.  Logits of skipped cells and of tokens behind new[c] hold no meaning.  No gradients."""
+        its K/V become row steps[c] + t, for which the cell has its pages (``pages.cache.reserve``, ``fork``: tokens behind
+        ``pages.cache.rows`` are refused).  ``new``: how many tokens each cell has (host int32 [C]; all n without); cells with a
+        negative step are skipped.  Logits of skipped cells and of tokens behind new[c] hold no meaning.  No gradients."""
         w, cache = self.w, pages.cache
         C, Hq, Hkv, D, n = self.C, w.n_q_heads, w.n_kv_heads, w.head_dim, pages.spec.n_tokens
         if tuple(tokens.shape) != (C, n):
             raise ValueError(f"tokens has shape {tuple(tokens.shape)}, expected ({C}, {n})")
         st, _ = S._steps(steps, C)
+        cache._check_rows(st, np.int32(n) if new is None else S._host_i32(new, C, 1, "new", "entries")[0])
         pos = None
         if getattr(self.positions, "__func__", None) is not SweepDecoder.positions:   # a decoder's own, asked step by step
             # (none is asked for behind a cell's last token)

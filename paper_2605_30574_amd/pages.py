@@ -295,6 +295,14 @@ class PageCache:
         self.fork(np.arange(self.n_cells), np.minimum(want, self.rows), want)
         self._lost |= lost
 
+    def _check_rows(self, steps, count) -> None:
+        """That every cell may write rows steps[c] .. steps[c] + count[c] - 1 (host arrays; none where either is not positive)."""
+        end = steps + np.asarray(count, dtype=np.int64)
+        bad = (steps >= 0) & (end > steps) & (end > self.rows)
+        if bad.any():
+            c = int(np.flatnonzero(bad)[0])
+            raise ValueError(f"cell {c} has pages for {self.rows[c]} rows, its tokens end at row {end[c]}: reserve them first")
+
     def load_prompt(self, layer: int, k, v, donor: bool = False) -> None:
         """Rows of the clean prompt's (or the donor's) pages of a layer from bf16 [Hkv][T_p][D]."""
         t, sh = S._torch, self.shape

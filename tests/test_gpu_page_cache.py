@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import gpu_common as gc
+import paper_2605_30574_amd as sp
 from test_gpu_page_decoder import run, setup
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +64,21 @@ def test_captured_fork():
         assert int(cache.missing) == 0 and len(set(tables[:, 0])) == 1 and len(set(tables[:, 1:].ravel())) == 2 * C
         held = cache._tables.cpu().numpy()
         assert (refs == np.bincount(held[held >= 0], minlength=len(refs))).all()
+
+
+def test_a_pass_without_pages_is_refused():
+    w, m, lw, gpu, _ = setup("blank-sink")
+    C = lw.shape[0]
+    gc.announce("pages, not reserved")
+    pages = gpu.make_pages(2)
+    tokens = torch.zeros(C, 2, dtype=torch.int64, device="cuda")
+    with pytest.raises(ValueError):
+        gpu.page_logits(tokens, pages, np.zeros(C, np.int32))
+    pages.cache.reserve([2] * (C - 1) + [1])
+    with pytest.raises(ValueError):
+        gpu.page_logits(tokens, pages, np.zeros(C, np.int32))
+    gpu.page_logits(tokens, pages, np.zeros(C, np.int32), [2] * (C - 1) + [1])
+    for new in ([3] + [1] * (C - 1), [-1] + [1] * (C - 1)):
+        with pytest.raises((ValueError, sp.SpliceError)):
+            gpu.page_logits(tokens, pages, np.zeros(C, np.int32), new)
+    torch.cuda.synchronize()

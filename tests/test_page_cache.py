@@ -1,4 +1,6 @@
 """PageCache on the CPU: what it keeps of its cells' pages, with tests/page_reference.py's fork in the place of the kernel."""
+from types import MethodType, SimpleNamespace
+
 import numpy as np
 import pytest
 import torch
@@ -6,6 +8,7 @@ import torch
 import page_reference as ref
 import paper_2605_30574_amd as sp
 from paper_2605_30574_amd import pages as PG
+from paper_2605_30574_amd.decode import SweepDecoder
 
 P = 64
 
@@ -114,3 +117,29 @@ def test_rows_are_those_that_have_pages(cache, seed):
         short = c.rows < want
         assert short.any() == (int(c.missing) > 0) and (c.rows[short] == np.array(held(c))[short]).all()
         assert (c.tables.numpy()[np.arange(c.table_len) >= -(-c.rows[:, None] // P)] == -1).all()
+
+
+def ask(c, n, steps, new=None):
+    """page_logits up to where the host has looked the call over: it stops at the weights, of which there are none."""
+    d = SimpleNamespace(C=c.n_cells, w=SimpleNamespace(n_q_heads=2, n_kv_heads=1, head_dim=64), wt={})
+    d.positions = MethodType(SweepDecoder.positions, d)
+    pages = SimpleNamespace(cache=c, spec=c.pages(n))
+    with pytest.raises(KeyError, match="embed"):
+        SweepDecoder.page_logits(d, torch.zeros(c.n_cells, n, dtype=torch.int64), pages, np.asarray(steps, np.int32), new)
+
+
+def test_a_pass_over_rows_without_pages_is_refused(cache):
+    c = cache(3, 9)
+    c.reserve([64, 10, 0])
+    ask(c, 4, [60, 6, -1])
+    ask(c, 4, [60, 6, 0], [4, 4, 0])
+    ask(c, 4, [64, 8, -5], [0, 2, 4])
+    for steps, new in (([61, 6, -1], None), ([60, 7, -1], None), ([60, 6, 0], None), ([60, 8, -1], [4, 3, 0]), ([0, 0, 0], [0, 0, 1]),
+                       ([2**31 - 1, 0, -1], None), ([0, 0, -1], [1, 1])):
+        with pytest.raises(ValueError):
+            ask(c, 4, steps, new)
+    short = cache(2, 1)
+    short.reserve([64, 64])
+    ask(short, 1, [63, -1])
+    with pytest.raises(ValueError):
+        ask(short, 1, [0, 0])
