@@ -228,6 +228,8 @@ class PageCache:
         self._held = [0, 0]                                            # rows of the prompts that have pages
         self.rows = np.zeros(n_cells, np.int32)                        # rows of the cells that have pages
         self._lost = np.zeros(n_cells, bool)                           # cells without some of the rows that they took over
+        self._common = np.zeros((n_cells, n_cells), np.int32)          # pages that two cells share: the first ones of both
+        self._shared = np.zeros(n_cells, np.int32)                     # rows of the pages that a cell shares
         self.fork(np.full(n_cells, -1), self.rows, self.rows)
 
     @property
@@ -256,7 +258,7 @@ class PageCache:
         Where pages were too few a cell has those up to its first absent one, and ``rows`` says so: ask again when others have
         given theirs back.  A cell for which the copy of a page in use was among them has lost that page's rows
         (``rows`` is below what it was to take over).  To know this the host waits for a call that asks for pages, but
-        for a captured one, which is taken to find them all."""
+        for a captured one, which is taken to find them all.  (What the host keeps of a captured call is that of its capture.)"""
         want = rows if want is None else want
         C = self.n_cells
         cells = [np.asarray(x, dtype=np.int32).reshape(-1) for x in (parent, rows, want)]
@@ -276,14 +278,25 @@ class PageCache:
         self.refs.copy_(self._next[1])
         self._held, self.rows = list(self._prompts), cells[2].copy()
         self._lost[:] = False
-        # a page is asked for behind the rows that a cell takes over, or for the copy of their last one
-        asks = (-(-cells[2] // SPLICE_PAGE_ROWS) > cells[1] // SPLICE_PAGE_ROWS).any()
+        # a page is asked for behind the rows that a cell takes over, or for the copy of their last one, if it is not its own
+        took = cells[1] > 0
+        alone = (~took | (cells[0] == np.arange(C))).all() and (~took | (cells[1] >= self._shared)).all()
+        held = cells[1] // SPLICE_PAGE_ROWS if not alone else -(-cells[1] // SPLICE_PAGE_ROWS)
+        asks = (-(-cells[2] // SPLICE_PAGE_ROWS) > held).any()
+        self._share(cells[0], cells[1] // SPLICE_PAGE_ROWS)
         if asks and not (self._tables.is_cuda and S._torch.cuda.is_current_stream_capturing()) and int(self.missing) > 0:
             # a cell's pages are given from the first on, so what it has ends at the first absent one
             tables = self.tables.cpu().numpy()
             there = np.cumprod((tables >= 0) & (tables < self.pools.shape[1]), axis=1).sum(axis=1)
             self.rows = np.minimum(self.rows, there * SPLICE_PAGE_ROWS).astype(np.int32)
             self._lost = self.rows < cells[1]
+
+    def _share(self, parent, whole) -> None:
+        """Cells have taken over ``whole[c]`` full pages of cell ``parent[c]``; all others of a cell are its own."""
+        of = np.maximum(parent, 0)
+        common = np.minimum(np.where(of[:, None] == of, np.iinfo(np.int32).max, self._common[np.ix_(of, of)]), np.minimum.outer(whole, whole))
+        np.fill_diagonal(common, 0)
+        self._common, self._shared = common, common.max(axis=1, initial=0) * np.int32(SPLICE_PAGE_ROWS)
 
     def reserve(self, want) -> None:
         """Pages for ``want[c]`` rows of every cell; rows that it has stay.  A cell that has lost rows is given none behind
@@ -296,12 +309,21 @@ class PageCache:
         self._lost |= lost
 
     def _check_rows(self, steps, count) -> None:
-        """That every cell may write rows steps[c] .. steps[c] + count[c] - 1 (host arrays; none where either is not positive)."""
+        """That every cell may write rows steps[c] .. steps[c] + count[c] - 1 (host arrays; none where the step is negative or the
+        count 0): they have pages, and no other cell has them too."""
         end = steps + np.asarray(count, dtype=np.int64)
         bad = (steps >= 0) & (end > steps) & (end > self.rows)
         if bad.any():
             c = int(np.flatnonzero(bad)[0])
             raise ValueError(f"cell {c} has pages for {self.rows[c]} rows, its tokens end at row {end[c]}: reserve them first")
+        self._check_own(steps, end > steps)
+
+    def _check_own(self, steps, writes) -> None:
+        bad = (steps >= 0) & (steps < self._shared) & writes
+        if bad.any():
+            c = int(np.flatnonzero(bad)[0])
+            raise ValueError(f"cell {c} shares its rows below {self._shared[c]} with other cells, so row {steps[c]} is not written: fork "
+                             "the cell from the rows before it")
 
     def load_prompt(self, layer: int, k, v, donor: bool = False) -> None:
         """Rows of the clean prompt's (or the donor's) pages of a layer from bf16 [Hkv][T_p][D]."""
@@ -320,5 +342,7 @@ class PageCache:
 
     def compact(self, cell_step, keep) -> None:
         """Row cell_step[c] + i of the cells = row cell_step[c] + keep[c][i] (``keep`` int32 [C][T] on the device): the tokens
-        that were accepted, or that an eviction leaves."""
+        that were accepted, or that an eviction leaves.  A cell_step[c] in a page that other cells have too is refused (a fork
+        shares the full pages of the rows that it takes over): ``fork`` the cell from its first cell_step[c] rows, or give -1."""
+        self._check_own(S._steps(cell_step, self.n_cells)[0], True)
         splice_page_compact(self.shape, self.pages(keep.shape[1]), cell_step, keep, self.tables, self.pools)

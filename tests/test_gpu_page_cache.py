@@ -82,3 +82,32 @@ def test_a_pass_without_pages_is_refused():
         with pytest.raises((ValueError, sp.SpliceError)):
             gpu.page_logits(tokens, pages, np.zeros(C, np.int32), new)
     torch.cuda.synchronize()
+
+
+def test_rows_that_cells_share_are_not_written():
+    """A step back into a shared page is refused; behind a fork to that row the pass writes the cells' own copies."""
+    w, m, lw, gpu, cpu = setup("diff-G8")
+    C = lw.shape[0]
+    rng = np.random.default_rng(6)
+    draw = lambda n: rng.integers(0, m.vocab, (C, n))  # noqa: E731
+    gc.announce("pages, shared rows")
+    pages = gpu.make_pages(130)
+    cache = pages.cache
+    cache.reserve([130] + [0] * (C - 1))
+    trunk = np.array([0] + [-1] * (C - 1), np.int32)
+    run(gpu, cpu, pages, draw(130), trunk, None, "trunk")
+    cache.fork([0] * C, [130] * C)
+    for x in (*cpu.gen_k, *cpu.gen_v):
+        x[1:] = x[0]
+    one, at = gpu.make_pages(1, cache=cache), np.array([127] + [-1] * (C - 1), np.int32)
+    keep = torch.zeros(C, 1, dtype=torch.int32, device="cuda")
+    for bad in (lambda: gpu.page_logits(torch.from_numpy(draw(1)).cuda(), one, at), lambda: cache.compact(at, keep),
+                lambda: cache.compact(np.full(C, 100), keep)):
+        with pytest.raises(ValueError):
+            bad()
+    run(gpu, cpu, one, draw(1), np.full(C, 129, np.int32), None, "the last row again")   # in the cells' own pages
+    cache.fork(list(range(C)), [100] + [130] * (C - 1))
+    cache.reserve([103] + [130] * (C - 1))
+    cache.compact(np.where(np.arange(C) == 0, 100, -1), keep)
+    steps = np.where(np.arange(C) == 0, 100, 129).astype(np.int32)
+    run(gpu, cpu, gpu.make_pages(3, cache=cache), draw(3), steps, np.where(steps == 100, 3, 1).astype(np.int32), "back")

@@ -143,3 +143,96 @@ def test_a_pass_over_rows_without_pages_is_refused(cache):
     ask(short, 1, [63, -1])
     with pytest.raises(ValueError):
         ask(short, 1, [0, 0])
+
+
+def shared_rows(c):
+    """Of every cell, the rows up to the last page that another cell's table names too."""
+    t = c.tables.numpy()
+    pages, number = np.unique(t[t >= 0], return_counts=True)
+    return [max([(j + 1) * P for j, p in enumerate(row) if p in pages[number > 1]], default=0) for row in t]
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_rows_of_pages_that_other_cells_have_are_not_written(cache, monkeypatch, seed):
+    """compact and a pass from a row on that lies in another cell's page too are refused, all others are not."""
+    calls = []
+    monkeypatch.setattr(PG, "splice_page_compact", lambda *a: calls.append(a))
+    rng = np.random.default_rng(100 + seed)
+    C = int(rng.choice([1, 2, 5, 12]))
+    c = cache(C, int(rng.choice([2 * C + 1, 5 * C])))
+    refused = 0
+    for _ in range(25):
+        if rng.random() < 0.4:
+            want = np.minimum(rng.integers(0, 321, C), np.where(c._lost, c.rows, 320))
+            c.reserve(want)
+        else:
+            parent = np.where(rng.random(C) < 0.3, np.arange(C), rng.integers(-1, C, C))
+            rows = np.array([0 if p < 0 else (c.rows[p] if rng.random() < 0.4 else rng.integers(0, c.rows[p] + 1)) for p in parent])
+            rows = np.where(rng.random(C) < 0.4, rows // P * P, rows)
+            c.fork(parent, rows, np.minimum(320, rows + rng.integers(0, 130, C)))
+        shared = shared_rows(c)
+        for cell in range(C):
+            for step in {0, 1, 63, 64, max(shared[cell] - 1, 0), shared[cell], int(c.rows[cell])}:
+                steps = np.full(C, -1)
+                steps[cell] = step
+                keep = torch.zeros(C, 4, dtype=torch.int32)
+                if step < shared[cell]:
+                    refused += 1
+                    with pytest.raises(ValueError):
+                        c.compact(steps, keep)
+                else:
+                    c.compact(steps, keep)
+                    assert calls.pop()[2] is steps and not calls
+                if step < c.rows[cell]:
+                    if step < shared[cell]:
+                        with pytest.raises(ValueError):
+                            ask(c, 1, steps)
+                    else:
+                        ask(c, 1, steps)
+    assert refused or C == 1
+
+
+def test_pages_become_a_cells_own_again(cache):
+    c = cache(2, 8)
+    c.reserve([130, 0])
+    c.fork([0, 0], [130, 128], [130, 140])
+    with pytest.raises(ValueError):
+        ask(c, 1, [127, -1])
+    ask(c, 1, [128, 128])
+    with pytest.raises(ValueError):
+        c.compact([-1, 100], torch.zeros(2, 4, dtype=torch.int32))
+    c.fork([0, 1], [130, 100], [130, 101])            # cell 1 drops rows 100 ..: the page of the others is copied
+    ask(c, 1, [128, 100])
+    ask(c, 1, [64, 64])
+    with pytest.raises(ValueError):
+        ask(c, 1, [63, -1])
+    c.fork([0, -1], [130, 0], [130, 0])               # cell 1 gives its pages back
+    ask(c, 1, [0, -1])
+
+
+def test_a_step_that_needs_no_page_does_not_wait(cache, monkeypatch):
+    """reserve within a cell's own last page reads nothing back; a copy that it may need is read."""
+    c = cache(2, 8)
+    c.reserve([65, 65])
+    read = []
+    monkeypatch.setattr(torch.Tensor, "__int__", lambda t: read.append(t) or 0)
+    for n in (66, 67, 128):
+        c.reserve([n, n])
+    assert not read
+    c.reserve([129, 128])
+    assert len(read) == 1
+    c.fork([0, 0], [128, 128])                        # whole pages alone
+    assert len(read) == 1
+    c.reserve([100, 128])                             # the end of a page that cell 1 has too
+    assert len(read) == 2
+    c.fork([0, 0], [70, 0])                           # of a page that is cell 0's alone
+    assert len(read) == 2
+    c.fork([0, 0], [70, 70])
+    assert len(read) == 3
+
+
+def test_no_cells(cache):
+    c = cache(0, 2, Tp=60)
+    c.fork([], [], [])
+    c.reserve([])
+    assert int(c.missing) == 0 and c.rows.size == 0 and c.refs.tolist() == [1, 1]
