@@ -484,12 +484,12 @@ class SweepDecoder:
     def make_pages(self, n_tokens: int = 1, n_pages: Optional[int] = None, cache: Optional[P.PageCache] = None) -> DecoderPages:
         """A cache in 4-bit pages for passes of ``n_tokens`` tokens a cell (``page_logits``), the prompts of ``caches`` in it,
         or passes of another number of tokens over the cache of an earlier one.  ``n_pages``: pages of each layer, by default
-        as many as all cells can fill.  Passes over one object share its workspace: order them on one stream."""
+        as many as they and all cells can fill.  Passes over one object share its workspace: order them on one stream."""
         w, dev = self.w, self.device
         if cache is None:
-            prompt, rows = -(-w.prompt_len // P.SPLICE_PAGE_ROWS), -(-w.n_steps // P.SPLICE_PAGE_ROWS)
+            prompt, rows = -(-w.prompt_len // P.SPLICE_PAGE_ROWS) * (1 if w.donor == "zero" else 2), -(-w.n_steps // P.SPLICE_PAGE_ROWS)
             cache = P.PageCache(self.C, self.N, w.n_q_heads, w.n_kv_heads, w.head_dim, w.prompt_len, w.span, w.n_steps,
-                                2 * prompt + self.C * rows if n_pages is None else n_pages, w.donor == "zero", dev)
+                                prompt + self.C * rows if n_pages is None else n_pages, w.donor == "zero", dev)
             for l, c in enumerate(self.caches):
                 cache.load_prompt(l, c["clean_k"], c["clean_v"])
                 if w.donor != "zero":

@@ -111,3 +111,18 @@ def test_rows_that_cells_share_are_not_written():
     cache.compact(np.where(np.arange(C) == 0, 100, -1), keep)
     steps = np.where(np.arange(C) == 0, 100, 129).astype(np.int32)
     run(gpu, cpu, gpu.make_pages(3, cache=cache), draw(3), steps, np.where(steps == 100, 3, 1).astype(np.int32), "back")
+
+
+@pytest.mark.parametrize("name,prompts", [("zero-window5", 1), ("diff-G8", 2)])
+def test_pages_by_default(name, prompts):
+    """As many as the prompts and all cells can fill: a ZERO donor has none."""
+    w, m, lw, gpu, _ = setup(name)
+    C = lw.shape[0]
+    gc.announce(f"pages by default {name}")
+    cache = gpu.make_pages(1).cache
+    assert cache.pools.shape[1] == prompts * -(-w.prompt_len // 64) + C * 3
+    cache.reserve([140] * C)
+    assert int(cache.missing) == 0 and int((cache.refs == 0).sum()) == 0
+    cache.fork([1] * C, [100] * C, [140] * C)
+    cache.fork(list(range(C)), [140] * C)
+    assert int(cache.missing) == 0 and cache.rows.tolist() == [140] * C
