@@ -26,10 +26,10 @@
  * 3/2, 2, 3, 4, 6 (OCP e2m1 under e8m0 scales, "MXFP4").  e - 127 is the smallest with
  * max |x| <= 6 * 2^(e - 127), at least -100 (blocks whose largest value is below
  * 2^-98 lose digits); codes are to the nearest, ties to the even code, and above
- * 3 * 2^126 they stop there.  Every stored value is exact in bf16.  Where k or v
- * of a token has an infinity or NaN in some head, every byte e of that head's k and v
- * row is 255: the rows read back as NaN, and out and lse of a query that sees
- * them are NaN.
+ * 3 * 2^126 they stop there (a rotated k beyond fp32's range, too).  Every stored value is
+ * exact in bf16.  Where k or v of a token has an infinity or NaN in some head, every
+ * byte e of that head's k and v row is 255: the rows read back as NaN, and out and lse
+ * of a query that sees them are NaN.
  *
  * Bytes of a page: Hkv heads of 68 D bytes, each, with r a token of the page:
  *   K codes   [64][D / 2]: values 2 i (low half) and 2 i + 1 of token r at [r][i];
@@ -77,7 +77,8 @@ SPLICE_API int64_t splice_page_bytes(const splice_shape *shape);
  * For token t of active cell c, with the angles of splice_tree_append:
  *   q_out[c][t]  = the rotated q[c][t], bf16 [C][T][Hq][D] (rotated in fp32, one
  *                  rounding); q_out may be q when q is dense;
- *   row s_c + t  = the rotated k[c][t] and v[c][t] in 4 bits (rotated in 64 bits).
+ *   row s_c + t  = the rotated k[c][t] and v[c][t] in 4 bits (rotated in 64 bits, by a sine
+ *                  and cosine that are off by 2^-33 and 2^-51 of the angle at most).
  * q, k, v, their strides, pos (device int64 [C][T], or NULL) and freq: as
  * splice_tree_append takes them, with T = pages->n_tokens; q and q_out may both be NULL
  * (then only rows are written).  A page that is written

@@ -1,6 +1,7 @@
 // page_rows.hip -- rows of a cache in 4-bit pages (splice_pages.h): rotated,
 // quantised and written (splice_page_append), read back (splice_page_read).
 
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -108,10 +109,13 @@ __global__ __launch_bounds__(kRowThreads) void page_append_kernel(PageAppendArgs
         }
     };
     if (d < 2 * half) {
-        // keys in 64 bits: the borders of their codes leave fp32's roundings no room
+        // keys in 64 bits: the borders of their codes leave fp32's roundings no room.  What lies beyond fp32's range stays finite:
+        // its code stops at 3 * 2^126 either way, and it is no infinity
         if (is_q) rotate([&](float u, float w, int pair) { return fmaf(u, (float)s_cs[pair].x, w * (float)s_cs[pair].y); });
         else rotate([&](float u, float w, int pair) {
-            return odd_float(fma((double)u, s_cs[pair].x, (double)w * s_cs[pair].y));
+            const double y = fma((double)u, s_cs[pair].x, (double)w * s_cs[pair].y);
+            const float f = odd_float(y);
+            return fabsf(f) == INFINITY && fabs(y) < INFINITY ? copysignf(FLT_MAX, f) : f;
         });
     }
     if (is_q) {

@@ -239,3 +239,19 @@ def test_refused_tensors():
         call(cell_new=[5, 0, 0])
     call()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("D,mscale", [(64, 1.0), (128, 1.05), (256, 1.0)])
+def test_rotated_keys_beyond_float32(D, mscale, layout):
+    """Finite keys whose rotation passes the largest float stop at their largest code, as all above 3 * 2^126 do."""
+    announce(f"page append far keys {D} {layout}")
+    s = Rows(14, C=2, T=6, Hq=4, Hkv=2, D=D)
+    top = float(torch.finfo(torch.bfloat16).max)
+    sign = torch.sign(torch.randn(s.k.shape, generator=torch.Generator().manual_seed(D))).to(torch.bfloat16)
+    s.k[0] = sign[0] * top
+    s.k[1, 0, :, ::3] = sign[1, 0, :, ::3] * top
+    s.k[0, 3, 0, 7], s.v[0, 4, 1, 5] = float("inf"), float("nan")
+    out, q, k, v = s.run(layout, mscale=mscale)
+    assert (np.abs(k[np.isfinite(k)]) > torch.finfo(torch.float32).max).any()
+    s.check_read(s.check(out, q, k, v))
