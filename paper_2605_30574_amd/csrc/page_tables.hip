@@ -49,8 +49,9 @@ struct Counts {
 // call, then every cell decides on its last page, then the pages are
 // walked from the lowest on and the free ones handed out by their ordinal.
 // Whole numbers are added in any order, so the result is one.  Its chain of memory round trips and
-// barriers bounds it: 128 cells of 16 entries, 4098 pages, 11.6 us with the counts in LDS, 26 with
-// them in memory and a page a thread and round.
+// barriers bounds it: 128 cells of 16 entries forked in the middle of a page, 4098 pages, 11.6 us.  Forked behind
+// full pages, in a replayed graph, they take 7.0 us with 4098 pages and 8.0 with 12288, whose counts are in
+// LDS; with the counts in memory 25 with 12289 pages and 40 with 131072.
 template <bool LDS>
 __global__ __launch_bounds__(kTableThreads) void fork_kernel(ForkArgs a) {
     extern __shared__ int32_t s_refs[];

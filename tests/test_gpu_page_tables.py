@@ -134,6 +134,71 @@ def test_many_pages():
     s.fork(list(range(40)), [320 - 7 * c for c in range(40)], [320] * 40)
 
 
+def around(free, layers=1):
+    """Three cells in a pool of so many pages more than they hold."""
+    return Held(28, [150, 320, 70], free=free, layers=layers, Hkv=1)
+
+
+@pytest.mark.parametrize("n_pages", [12287, 12288, 12289, 16384, 30011])
+def test_pools_with_more_pages_than_counts_fit_in_lds(n_pages):
+    """Counts in LDS up to 12288 pages, in memory above: trunk, beams, cells that give back, few free pages and those far behind."""
+    announce(f"fork of {n_pages} pages")
+    s = around(n_pages - 10)
+    assert s.n_pages == n_pages
+    m, cp = s.fork([0, 0, 0], [150, 140, 128], [200, 320, 130])
+    assert m == 0 and (cp[0] == -1).all() and (cp[1] >= 0).all()
+    s.fork([1, 2, 1], [300, 65, 70], [300, 100, 71])
+    s.fork([-1, 1, 2], [0, 60, 64], [320, 60, 64])
+    s.fork([0, 1, 0], [320, 60, 256], [320, 320, 256])
+    # none free but the last three
+    s.fork([0, -1, -1], [64, 0, 0], [64, 0, 0])
+    taken = np.flatnonzero(s.refs == 0)[:-3]
+    s.refs[taken] += 1
+    m, cp = s.fork([0, 0, 0], [64, 64, 40], [128, 320, 40])
+    assert m == 3 and (cp == -1).all() and s.refs.min() > 0      # the copy of the last cell's page among them
+    # and those far behind the first ones that are not
+    s.refs[taken[-200:]] -= 1
+    m, cp = s.fork([0, 0, 0], [128, 100, 40], [320, 320, 320])
+    assert m == 0 and (cp[1:] >= 0).all()
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_random_forks_with_counts_in_memory(seed):
+    announce(f"fork random, many pages {seed}")
+    rng = np.random.default_rng(seed)
+    C = int(rng.choice([3, 130, 256]))
+    s = Held(seed, rng.integers(0, 321, C), free=13000, layers=2, Hkv=1)
+    s.refs[np.flatnonzero(s.refs == 0)[:-int(rng.choice([1, C]))]] += 1
+    for _ in range(3):
+        parent = np.where(rng.random(C) < 0.2, np.arange(C), rng.integers(-1, C, C))
+        rows = np.array([0 if p < 0 else rng.integers(0, s.rows[p] + 1) for p in parent])
+        rows = np.where(rng.random(C) < 0.3, rows // P * P, rows)
+        s.fork(parent.tolist(), rows.tolist(), np.minimum(320, rows + rng.integers(0, 200, C)).tolist())
+
+
+def test_replayed_fork_with_counts_in_memory():
+    announce("fork graph, many pages")
+    s = around(13000)
+    bufs = [up(s.tables), up(s.refs)]
+    outs = [torch.zeros_like(bufs[0]), torch.zeros_like(bufs[1]), torch.zeros(1, dtype=torch.int32, device="cuda"),
+            torch.zeros(3, 2, dtype=torch.int32, device="cuda")]
+    args = [0, 0, 2], [150, 140, 70], [150, 200, 130]
+    call = lambda: sp.splice_page_fork(s.shape, sp.make_pages(s.n_pages, s.L), *args, *bufs, *outs, s.pools)  # noqa: E731
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        refs = s.refs.copy()
+        refs[np.flatnonzero(refs == 0)[:50 * i]] += 1         # other pages are free
+        bufs[1].copy_(up(refs))
+        for x in outs:
+            x.fill_(-5)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(outs, ref.fork(*(np.asarray(x) for x in args), s.tables, refs, s.n_pages)):
+            assert (x.cpu().numpy().reshape(np.shape(y)) == y).all(), i
+
+
 def test_fork_graph_and_stream():
     announce("fork graph")
     s = Held(10, [150, 0, 70], free=9)
