@@ -30,6 +30,19 @@ def shared_case(D, heads, T, C, Tp):
                 LW=[([9, 0], [0, 0], [1, steps[c] + T // 2])[c % 3] for c in range(C)])
 
 
+# ... with finished cells, cells without tokens and others with fewer than T among them: (donor, window, D, (Hq, Hkv), T, C, T_p)
+RAGGED = [("diff", 0, 64, (16, 8), 2, 60, 3000), ("diff", 0, 128, (16, 8), 1, 40, 3000), ("zero", 0, 128, (16, 4), 6, 40, 5000),
+          ("diff", 2000, 128, (8, 2), 5, 120, 3000), ("diff", 0, 256, (16, 8), 2, 40, 3000), ("zero", 2000, 256, (16, 8), 2, 80, 3000)]
+
+
+def ragged_case(donor, window, D, heads, T, C, Tp):
+    """Arguments of Sweep: every cell at a step of its own, every fifth finished, 0 to T tokens."""
+    steps = np.array([-1 if c % 5 == 3 else 7 * c % 73 for c in range(C)])
+    return dict(donor=donor, window=window, C=C, T=T, Hq=heads[0], Hkv=heads[1], D=D, Tp=Tp, span=(70, Tp // 2), cap=80, steps=steps,
+                new=np.array([T - c % 4 * T // 3 if c % 7 else 0 for c in range(C)]),
+                LW=[([9, 0], [0, 0], [1, max(int(steps[c]), 0) + T // 2])[c % 3] for c in range(C)])
+
+
 class Sweep:
     """One call's tensors on the GPU and their float64 values."""
 

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import page_reference as ref
-from page_common import SHARED, P, Sweep, announce, shared_case, sp
+from page_common import RAGGED, SHARED, P, Sweep, announce, ragged_case, shared_case, sp
 
 pytestmark = pytest.mark.gpu
 
@@ -272,3 +272,44 @@ def test_a_query_does_not_move_its_neighbours(T, D):
             a, b = x.clone(), y.clone()
             a[:, 0, 1] = b[:, 0, 1] = 0
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("case", RAGGED)
+def test_tiles_of_several_cells_some_of_them_finished(case):
+    """test_page_plan.py holds that the plan takes them for these shapes: a cell's number is not its place among those with tokens."""
+    s = Sweep(101, **ragged_case(*case))
+    s.tables[2, 0] = -1
+    run(s, what=f"several cells, ragged {case}")
+
+
+@pytest.mark.parametrize("split", [0, 256])
+@pytest.mark.parametrize("T", [1, 3, 9, 40, 90])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_nan_rows_inside_of_runs(D, T, split):
+    """Rows that are NaN in full pages of the prompt, the donor and a cell's rows, for each kind of work group and part."""
+    s = Sweep(103, C=3, T=T, Hq=8, Hkv=2, D=D, Tp=700, span=(130, 600), cap=T + 500, steps=[499, 300, 20], LW=[[0, 0], [9, 0], [0, 20 + T // 2]])
+
+    def spoil(page, r, h):
+        _, _, ks, vs = ref.places(r, np.arange(s.D), s.D)
+        s.pool[page, h, ks], s.pool[page, h, vs] = 255, 255
+    spoil(s.clean[5], 17, 0)                                  # of the span: seen by unspliced tokens only
+    spoil(s.donor[4], 63, 1)                                  # ... by spliced ones
+    spoil(s.tables[0, 3], 0, 1)
+    r = 300 + T // 2                                          # a new token in the middle
+    spoil(s.tables[1, r // P], r % P, 1)
+    announce(f"page attn nan inside D={D} T={T} split={split}")
+    out, lse = s.attend(split)
+    s.check(out, lse)
+    assert torch.isnan(lse).any() and not torch.isnan(lse).all()
+
+
+@pytest.mark.parametrize("case", [RAGGED[0], RAGGED[1], RAGGED[4]])
+def test_nan_rows_in_a_shared_prompt(case):
+    s = Sweep(107, **ragged_case(*case))
+    for page, r, h in ((s.clean[9], 40, 0), (s.donor[7], 1, 1)):
+        _, _, ks, vs = ref.places(r, np.arange(s.D), s.D)
+        s.pool[page, h, ks], s.pool[page, h, vs] = 255, 255
+    announce(f"page attn nan shared {case}")
+    out, lse = s.attend()
+    s.check(out, lse)
+    assert torch.isnan(lse).any() and not torch.isnan(lse).all()

@@ -134,3 +134,15 @@ def test_shapes_of_the_gpu_tests_share_their_prompts(plan):
             own.add((c["D"], p["own"]))
         # every kernel that has such tiles
         assert own >= {(64, 1), (128, 1), (128, 2), (256, 1)} and (window or (64, 2) in own), own
+
+
+def test_ragged_shapes_of_the_gpu_tests_share_their_prompts(plan):
+    from page_common import RAGGED, ragged_case
+    for case in RAGGED:
+        c = ragged_case(*case)
+        cells = [(i, int(s), int(n), int(n) if L > 1 else min(int(n), max(0, W - int(s))))
+                 for i, (s, n, (L, W)) in enumerate(zip(c["steps"], c["new"], c["LW"])) if s >= 0 and n > 0]
+        assert len(cells) < c["C"] and (c["T"] == 1 or len({n for _, _, n, _ in cells}) > 1)
+        sh = sp.make_shape(c["C"], 4, c["Hq"], c["Hkv"], c["D"], c["Tp"], c["span"], c["cap"], c["donor"] == "zero", "bf16")
+        p = plan(sh, sp.make_call(1, 0, c["window"], 0.1), sp.make_pages(999, 2, c["T"]), cells)
+        assert p["shared"] and p["prompt_parts"] > 1 and p["rows_u"] and p["rows_s"], (case, p)
