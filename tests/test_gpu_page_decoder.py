@@ -191,3 +191,52 @@ def test_cache_refusals():
     small = gpu.make_pages(1, n_pages=2 * (-(-w.prompt_len // 64)) + 1)
     small.cache.reserve([64] * C)
     assert int(small.cache.missing) == C - 1
+
+
+def rounded(x):
+    return ref.from_bf16_bits(ref.to_bf16_bits(x))
+
+
+class RoundedOverPages(OverPages):
+    """... whose products take and give bfloat16, as those of bfloat16 weights do; sums, norms and residuals stay float64."""
+
+    def forward(self, tokens, steps):
+        w, m, wt, C = self.w, self.m, self.wt, self.C
+        heads = lambda x, n: x.reshape(C, n, w.head_dim)  # noqa: E731
+        pos = w.prompt_len + np.maximum(steps, 0)
+        x = wt["embed"][tokens]
+        for l in range(self.N):
+            p = wt["layers"][l]
+            h = rounded(ref._rms_norm(x, p["norm_1"], m.rms_eps))
+            q, k, v = (heads(rounded(h @ p[n]), e) for n, e in (("w_q", w.n_q_heads), ("w_k", w.n_kv_heads), ("w_v", w.n_kv_heads)))
+            q, k, v = (ref.to_bf16_bits(y) for y in (ref._rope(q, pos, m.rope_theta), ref._rope(k, pos, m.rope_theta), v))
+            o = np.zeros((C, w.n_q_heads, w.head_dim))
+            for c in np.flatnonzero(steps >= 0):
+                s = int(steps[c])
+                self.gen_k[l][c, :, s], self.gen_v[l][c, :, s] = k[c], v[c]
+                o[c] = rounded(self.attend(l, c, s, q[c]))
+            x = x + rounded(o.reshape(C, -1) @ p["w_o"])
+            h = rounded(ref._rms_norm(x, p["norm_2"], m.rms_eps))
+            x = x + rounded(rounded(rounded(ref._silu(rounded(h @ p["w_gate"]))) * rounded(h @ p["w_up"])) @ p["w_down"])
+        return rounded(rounded(ref._rms_norm(x, wt["norm_f"], m.rms_eps)) @ wt["lm_head"])
+
+
+@pytest.mark.parametrize("name", decode_bar.CASES)
+def test_bf16_weights_against_the_reference(name):
+    """Passes of one and of many tokens around bfloat16 weights: off by the attention's own bar (TREE_REL less a rounding), and a
+    logit by one step of bfloat16, 2^-7 at most, where the two sides round to its neighbours."""
+    w, m, lw, gpu, cpu = setup(name, torch.bfloat16)
+    cpu.__class__ = RoundedOverPages
+    C, rng = lw.shape[0], np.random.default_rng(21)
+    pages = gpu.make_pages(70)
+    pages.cache.reserve([76] * C)
+    for n, at in ((70, 0), (1, 70), (5, 71)):
+        tokens = rng.integers(0, m.vocab, (C, n))
+        gc.announce(f"{name} bf16 weights, {n} at {at}")
+        p = gpu.make_pages(n, cache=pages.cache)
+        got = gpu.page_logits(torch.from_numpy(tokens).cuda(), p, np.full(C, at, np.int32)).double().cpu().numpy().reshape(C, n, -1)
+        cpu.rows = held_rows(pages.cache, np.full(C, at + n, np.int32))
+        for t in range(n):
+            want = cpu.forward(tokens[:, t], np.full(C, at + t, np.int32))
+            err = np.abs(got[:, t] - want).max() / max(1.0, np.abs(want).max())
+            assert err <= TREE_REL + 2.0 ** -8, f"{name} token {at + t}: logits off by {err:.2e}"
