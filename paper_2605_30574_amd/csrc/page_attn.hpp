@@ -330,7 +330,9 @@ __device__ __forceinline__ void raise(PageState<D, R> &st, const f32x4_t (&s)[R]
     });
 }
 
-// Weights of a page as the second product's operands (two of 32 keys); their sums to the rows'.  The scores'
+// Weights of a page as the second product's operands (two of 32 keys); their sums to the rows'.  The operands are
+// bf16, off by 2^-8 of a weight at most: a second term each would double the second product's instructions.  That is what sets the
+// results' errors, up to 1.41 times those with weights of 32 bits; the sums are of the unrounded weights, as lse is of 32 bits.  The scores'
 // maximum is looked for only where a lane's weights sum to more than 2^8 (or to NaN): one of them may then.
 template <int D, int R>
 __device__ __forceinline__ void weights(PageState<D, R> &st, const f32x4_t (&s)[R][4], float qk, bf16x8_t (&p)[R][2]) {
