@@ -228,7 +228,8 @@ class PageCache:
         self._held = [0, 0]                                            # rows of the prompts that have pages
         self.rows = np.zeros(n_cells, np.int32)                        # rows of the cells that have pages
         self._lost = np.zeros(n_cells, bool)                           # cells without some of the rows that they took over
-        self._common = np.zeros((n_cells, n_cells), np.int32)          # pages that two cells share: the first ones of both
+        self._all = np.iinfo(np.int32).max
+        self._common = np.diag(np.full(n_cells, self._all, np.int32))  # pages that two cells share: the first ones of both
         self._shared = np.zeros(n_cells, np.int32)                     # rows of the pages that a cell shares
         self.fork(np.full(n_cells, -1), self.rows, self.rows)
 
@@ -279,11 +280,10 @@ class PageCache:
         self._held, self.rows = list(self._prompts), cells[2].copy()
         self._lost[:] = False
         # a page is asked for behind the rows that a cell takes over, or for the copy of their last one, if it is not its own
-        took = cells[1] > 0
-        alone = (~took | (cells[0] == np.arange(C))).all() and (~took | (cells[1] >= self._shared)).all()
-        held = cells[1] // SPLICE_PAGE_ROWS if not alone else -(-cells[1] // SPLICE_PAGE_ROWS)
-        asks = (-(-cells[2] // SPLICE_PAGE_ROWS) > held).any()
-        self._share(cells[0], cells[1] // SPLICE_PAGE_ROWS)
+        parent, whole, part = cells[0], cells[1] // SPLICE_PAGE_ROWS, cells[1] % SPLICE_PAGE_ROWS > 0
+        own = ((cells[1] == 0) | (parent == np.arange(C)) & (cells[1] >= self._shared)).all()
+        asks = (-(-cells[2] // SPLICE_PAGE_ROWS) > (whole + part if own else whole)).any()
+        self._share(parent, whole)
         if asks and not (self._tables.is_cuda and S._torch.cuda.is_current_stream_capturing()) and int(self.missing) > 0:
             # a cell's pages are given from the first on, so what it has ends at the first absent one
             tables = self.tables.cpu().numpy()
@@ -293,10 +293,16 @@ class PageCache:
 
     def _share(self, parent, whole) -> None:
         """Cells have taken over ``whole[c]`` full pages of cell ``parent[c]``; all others of a cell are its own."""
+        if not self._shared.any() and np.bincount(parent[whole > 0], minlength=1).max() <= 1:
+            return   # none are shared, and no two cells took over those of one
         of = np.maximum(parent, 0)
-        common = np.minimum(np.where(of[:, None] == of, np.iinfo(np.int32).max, self._common[np.ix_(of, of)]), np.minimum.outer(whole, whole))
+        common = self._common.take(of, axis=0).take(of, axis=1)   # (of a cell with itself: all)
+        np.minimum(common, whole, out=common)
+        np.minimum(common, whole[:, None], out=common)
         np.fill_diagonal(common, 0)
-        self._common, self._shared = common, common.max(axis=1, initial=0) * np.int32(SPLICE_PAGE_ROWS)
+        self._shared = common.max(axis=1, initial=0) * np.int32(SPLICE_PAGE_ROWS)
+        np.fill_diagonal(common, self._all)
+        self._common = common
 
     def reserve(self, want) -> None:
         """Pages for ``want[c]`` rows of every cell; rows that it has stay.  A cell that has lost rows is given none behind
