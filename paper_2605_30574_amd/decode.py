@@ -505,8 +505,9 @@ class SweepDecoder:
         """Logits [C * n][V] (bfloat16 where the head's product is, else float32) of one pass over n tokens a cell: token t of
         cell c is tokens[c][t] (int64) at decode step steps[c] + t, behind the cell's steps[c] rows and the tokens before it;
         its K/V become row steps[c] + t, for which the cell has its pages (``pages.cache.reserve``, ``fork``: tokens behind
-        ``pages.cache.rows`` are refused, and a steps[c] in a page that other cells have too).  ``new``: how many tokens each cell has (host int32 [C]; all n without); cells with a
-        negative step are skipped.  Logits of skipped cells and of tokens behind new[c] hold no meaning.  No gradients."""
+        ``pages.cache.rows`` are refused, and a steps[c] in a page that other cells have too).  ``new``: how many tokens each cell
+        has (host int32 [C]; all n without); cells with a negative step are skipped.  Logits of skipped cells and of tokens behind
+        new[c] hold no meaning.  No gradients."""
         w, cache = self.w, pages.cache
         C, Hq, Hkv, D, n = self.C, w.n_q_heads, w.n_kv_heads, w.head_dim, pages.spec.n_tokens
         if tuple(tokens.shape) != (C, n):

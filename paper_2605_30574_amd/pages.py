@@ -223,6 +223,7 @@ class PageCache:
             self.refs = t.zeros(n_pages, dtype=t.int32, device=device)
             self._next = t.empty_like(self._tables), t.empty_like(self.refs)
             self.missing = t.zeros(1, dtype=t.int32, device=device)
+            self._unseen = t.zeros_like(self.missing)                  # pages missing since the host last waited
             self.copied = t.zeros((n_cells + 2, 2), dtype=t.int32, device=device)
         self._prompts = [prompt_len, 0 if donor_zero else prompt_len]
         self._held = [0, 0]                                            # rows of the prompts that have pages
@@ -258,8 +259,9 @@ class PageCache:
 
         Where pages were too few a cell has those up to its first absent one, and ``rows`` says so: ask again when others have
         given theirs back.  A cell for which the copy of a page in use was among them has lost that page's rows
-        (``rows`` is below what it was to take over).  To know this the host waits for a call that asks for pages, but
-        for a captured one, which is taken to find them all.  (What the host keeps of a captured call is that of its capture.)"""
+        (``rows`` is below what it was to take over).  To know this the host waits for a call that asks for pages.  It does not
+        for a captured one: that is taken to find them all, and what its replays missed is noticed behind the next call that is
+        waited for (as is the copy of a page that ``refs`` was raised for by hand)."""
         want = rows if want is None else want
         C = self.n_cells
         cells = [np.asarray(x, dtype=np.int32).reshape(-1) for x in (parent, rows, want)]
@@ -277,6 +279,7 @@ class PageCache:
                          self.pools)
         self._tables.copy_(self._next[0])
         self.refs.copy_(self._next[1])
+        self._unseen += self.missing
         self._held, self.rows = list(self._prompts), cells[2].copy()
         self._lost[:] = False
         # a page is asked for behind the rows that a cell takes over, or for the copy of their last one, if it is not its own
@@ -284,7 +287,8 @@ class PageCache:
         own = ((cells[1] == 0) | (parent == np.arange(C)) & (cells[1] >= self._shared)).all()
         asks = (-(-cells[2] // SPLICE_PAGE_ROWS) > (whole + part if own else whole)).any()
         self._share(parent, whole)
-        if asks and not (self._tables.is_cuda and S._torch.cuda.is_current_stream_capturing()) and int(self.missing) > 0:
+        if asks and not (self._tables.is_cuda and S._torch.cuda.is_current_stream_capturing()) and int(self._unseen) > 0:
+            self._unseen.zero_()
             # a cell's pages are given from the first on, so what it has ends at the first absent one
             tables = self.tables.cpu().numpy()
             there = np.cumprod((tables >= 0) & (tables < self.pools.shape[1]), axis=1).sum(axis=1)

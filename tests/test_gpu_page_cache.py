@@ -126,3 +126,22 @@ def test_pages_by_default(name, prompts):
     cache.fork([1] * C, [100] * C, [140] * C)
     cache.fork(list(range(C)), [140] * C)
     assert int(cache.missing) == 0 and cache.rows.tolist() == [140] * C
+
+
+def test_what_a_captured_fork_missed_is_noticed():
+    w, m, lw, gpu, _ = setup("blank-sink")
+    C = lw.shape[0]
+    gc.announce("pages, captured shortage")
+    cache = gpu.make_pages(1, n_pages=2 * (-(-w.prompt_len // 64)) + C).cache
+    cache.reserve([64] + [0] * (C - 1))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.reserve([128] * C)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(cache.missing) == C
+    cache.fork([0] * C, [0] * C, [64] * C)
+    assert int(cache.missing) == 0 and cache.rows.tolist() == [64] * C
+    cache.reserve([64] * (C - 1) + [128])
+    assert int(cache.missing) == 1 and cache.rows.tolist() == [64] * C

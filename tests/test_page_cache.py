@@ -231,6 +231,24 @@ def test_a_step_that_needs_no_page_does_not_wait(cache, monkeypatch):
     assert len(read) == 3
 
 
+def test_a_shortage_that_was_not_waited_for_is_noticed_behind_the_next_wait(cache):
+    """A page that somebody holds by its count is copied by a call that the host does not wait for."""
+    c = cache(2, 3)
+    c.reserve([70, 10])
+    c.refs += 1                                       # all pages
+    c.reserve([80, 10])
+    assert int(c.missing) == 2 and c.rows.tolist() == [80, 10]
+    c.refs -= 1
+    c.reserve([140, 10])                              # asks for a page and is waited for
+    assert c.rows.tolist() == [64, 0]
+    with pytest.raises(ValueError):
+        c.reserve([140, 0])
+    with pytest.raises(ValueError):
+        c.reserve([64, 10])
+    c.fork([0, -1], [64, 0], [140, 10])
+    assert int(c.missing) == 1 and c.rows.tolist() == [140, 0]
+
+
 def test_no_cells(cache):
     c = cache(0, 2, Tp=60)
     c.fork([], [], [])
